@@ -342,6 +342,161 @@ int lacache_profile_read(lacache_t h, double *stage1_ms, int64_t *lookups);
  */
 int lacache_replay_fallbacks(lacache_t h, int64_t *count);
 
+/*
+ * The decode step's own operators.  After a miss or a rejected lookahead the
+ * draft model g decodes k tokens (Section 4.3) and the target model f verifies
+ * them in one forward pass; both keep the keys and values of earlier tokens.
+ * The four calls below are that cache: rotary positions, writing new tokens
+ * into pages (in bfloat16 or 8 bits), reading them back, and the attention of
+ * a sequence's newest tokens over all of its cached ones.  They need no cache
+ * handle, run on the calling thread's current device, allocate nothing and
+ * only enqueue kernels, so they can be captured into a HIP graph.  What a
+ * captured call keeps is its arguments; lengths and page tables are read on
+ * the device at every replay.
+ */
+
+/* How a pool stores a number: 8-bit codes have one float scale a token and head (value = code * scale). */
+typedef enum { LACACHE_KV_BF16 = 1, LACACHE_KV_FP8 = 2 /* e4m3 */, LACACHE_KV_INT8 = 3 } lacache_kv_type;
+
+/*
+ * A paged key-value cache: memory of the caller, described on the host.
+ * n_pages pages of `page` tokens (32, 64, 128 or 256) for `heads` heads of d
+ * columns (a multiple of 8, 8 .. 256).  Columns are padded to D = 64, 96, 128,
+ * 192 or 256, the padding is stored as zeros.  k and v are
+ * [n_pages][heads][page / 32] tiles of 32 tokens x D columns, 16-byte aligned.
+ * With t = 16 b + r = 16 s + 4 g + i a token of the tile and
+ * c = 32 x + 8 u + e = 32 x + 16 y + m a column (b, s, y < 2; r, m < 16;
+ * g, i, u < 4; e < 8), the elements of a tile are ordered, last index fastest,
+ *     k, bfloat16  [x][b][u][r][e]        k, 8 bits  [x][u][r][b][e]
+ *     v, bfloat16  [x][y][g][m][s][i]     v, 8 bits  [x][g][m][y][s][i]
+ * which are the operands of the matrix instructions of lacache_kv_attend, 16
+ * bytes a lane.  k_scale and v_scale are [n_pages][heads][page] floats, NULL
+ * for LACACHE_KV_BF16.  Whatever memory holds where no token has been written
+ * (NaN too) has no effect on any result.
+ */
+typedef struct {
+    void *k, *v;
+    float *k_scale, *v_scale;
+    int64_t n_pages;
+    int32_t page, heads, d;
+    lacache_kv_type type;
+} lacache_kv;
+
+/*
+ * The sequences of a call (device arrays).  Rows start[b] .. start[b+1]-1 of
+ * the call's packed row arrays are the newest tokens of sequence b
+ * (0 <= start[0], start non-decreasing; at most 2^31 - 1 rows); lens[b] is the
+ * number of tokens that it has with them, so row start[b] + i is position
+ * lens[b] - (start[b+1] - start[b]) + i.  Position p lies at place p % page of
+ * page pages[b][p / page].  Rows of negative positions are positions that do
+ * not exist.  A page number outside 0 .. n_pages-1 is a page that is not there
+ * (given back by a sliding window, for example), and so is a position beyond
+ * max_pages pages: nothing is written there, reads give zeros, and attention
+ * does not see it.
+ */
+typedef struct {
+    const int32_t *start;  /* [n_seq + 1] */
+    const int32_t *lens;   /* [n_seq] */
+    const int32_t *pages;  /* [n_seq][max_pages] */
+    int32_t n_seq, max_pages;
+} lacache_seqs;
+
+/*
+ * Rotary positions.  The pairs of a head's first `rot` columns (even, 2 .. d)
+ * are turned: (a, b) -> (a c - b s, b c + a s) with the (c, s) of the position
+ * and pair in table [n_pos][rot / 2][2]; products and sums are rounded to
+ * float32 one by one.  Pair i is columns (i, i + rot / 2) (LACACHE_ROPE_HALF) or
+ * (2 i, 2 i + 1) (LACACHE_ROPE_PAIRS).  Positions outside the table take its
+ * nearest row.
+ */
+typedef enum { LACACHE_ROPE_HALF = 0, LACACHE_ROPE_PAIRS = 1 } lacache_rope_style;
+typedef struct {
+    const float *table;
+    int64_t n_pos;
+    int32_t rot;
+    lacache_rope_style style;
+} lacache_rotary;
+
+/*
+ * Fill rows first .. first+n-1 of a table (`table` points at row first):
+ * f_i = base^(-2 i / rot), table = magnitude * (cos, sin)(position * f_i'), in
+ * double, rounded once.  Scaling for long contexts, by parts: with
+ * r = original * f_i / (2 pi) turns over the original length,
+ * g = clamp((r - low) / (high - low), 0, 1), f_i' = (1 - g) f_i / factor + g f_i.
+ * factor = 1 leaves the frequencies as they are; original = 0 divides all of
+ * them by factor (linear interpolation of positions).
+ *   n >= 0, first >= 0, rot even, 2 .. 256, base > 1, factor >= 1,
+ *   original >= 0, 0 <= low < high, magnitude finite; EINVAL otherwise.
+ */
+int lacache_rope_table(float *table, int64_t first, int64_t n, int32_t rot, double base, double factor,
+                       double original, double low, double high, double magnitude, void *stream);
+
+/*
+ * y = x turned by the positions of its rows; columns from rot on are copied.
+ *   x, y   rows of H heads of d columns (dtype), row t at x + t * x_row, head h
+ *          at + h * x_head elements (y likewise); y may be x itself, and must
+ *          not overlap it otherwise
+ *   pos    [rows] int32
+ *   backward != 0: the transposed rotation, so that with dy in x the result is
+ *          dx: the gradient with respect to the input
+ *   1 <= H, 1 <= d <= 4096.  rows == 0 is a no-op.
+ */
+int lacache_rope(const void *x, void *y, lacache_dtype dtype, int64_t rows, int32_t H, int32_t d, int64_t x_row,
+                 int64_t x_head, int64_t y_row, int64_t y_head, const int32_t *pos, const lacache_rotary *rope,
+                 int32_t backward, void *stream);
+
+/*
+ * Store the newest tokens of every sequence: k is turned by its position (if
+ * rope is given) and v is taken as it is, in float32; both are rounded once, to
+ * nearest-even, to bfloat16, or to 8-bit codes x * (top / m), m the largest
+ * magnitude of the token's head, top = 448 (fp8) or 127 (int8), with the scale
+ * m / top (m below 2^-100 stores zeros).
+ *   k, v   [rows][heads][d] (dtype), rows k_row and v_row elements apart
+ *   q      [rows][q_heads][d], rows q_row elements apart: turned by its
+ *          position and written to q_out [rows][q_heads][d], contiguous; q_out
+ *          may be q if that is contiguous.  Both NULL, or neither (then rope is
+ *          needed).
+ *   max_new  a bound on the new tokens of a sequence (for the launch shape
+ *          alone; 0: not known)
+ * Positions that do not exist are not stored.  Rows before start[0] or from
+ * start[n_seq] on are not read, and their q_out is not written.
+ */
+int lacache_kv_append(const lacache_kv *kv, const lacache_seqs *seqs, const void *k, const void *v,
+                      lacache_dtype dtype, int64_t rows, int64_t k_row, int64_t v_row, const void *q, void *q_out,
+                      int32_t q_heads, int64_t q_row, const lacache_rotary *rope, int32_t max_new, void *stream);
+
+/*
+ * Read the newest tokens of every sequence back as the values they stand for,
+ * rounded once to dtype: k_out and v_out [rows][heads][d], contiguous; either
+ * may be NULL.  (With start the running sum of lens, that is all tokens.)
+ */
+int lacache_kv_read(const lacache_kv *kv, const lacache_seqs *seqs, void *k_out, void *v_out, lacache_dtype dtype,
+                    int64_t rows, int32_t max_new, void *stream);
+
+/*
+ * Attention of the newest tokens of every sequence over its cached ones.
+ *   q     [rows][q_heads][d] (dtype), rows q_row elements apart, already
+ *         turned; q_heads a multiple of heads, query head h reads head
+ *         h / (q_heads / heads)
+ *   The row of position p sees the positions j <= p that exist, with
+ *   p - j < window if window > 0:
+ *   out   [rows][q_heads][d] (dtype) = sum_j w_j v_j, w = softmax(scale q.k_j)
+ *   lse   [rows][q_heads] float = log sum_j exp(scale q.k_j); NULL: not wanted.
+ *         A row that sees nothing has out = 0 and lse = -infinity.
+ * Products are exact and sums are in float32; with bfloat16 rows the weights
+ * are rounded to bfloat16 before they multiply the values.
+ *   max_new    a bound on the new tokens of a sequence (for the launch shape
+ *              alone; 0: not known)
+ *   workspace  lacache_kv_attend_workspace bytes of device memory, 16-byte
+ *              aligned, for this call alone while it runs
+ * EINVAL too if workspace_bytes is less.
+ */
+int64_t lacache_kv_attend_workspace(const lacache_kv *kv, lacache_dtype dtype, int32_t n_seq, int32_t q_heads,
+                                    int32_t max_new);
+int lacache_kv_attend(const lacache_kv *kv, const lacache_seqs *seqs, const void *q, lacache_dtype dtype,
+                      int64_t rows, int32_t q_heads, int64_t q_row, int32_t max_new, float scale, int32_t window,
+                      void *out, float *lse, void *workspace, int64_t workspace_bytes, void *stream);
+
 /* Static text for a return code. */
 const char *lacache_strerror(int code);
 

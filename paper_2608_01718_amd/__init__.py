@@ -8,6 +8,7 @@ fallback: importing this module fails if ``liblacache.so`` has not been built
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -20,6 +21,8 @@ MISS, REJECT, HIT, HIT_EXACT = 0, 1, 2, 3
 OK, EINVAL, EFULL, ENOMEM, EHIP = 0, -1, -2, -3, -4
 F32, BF16 = 0, 1
 MAX_MODELS = 8
+KV_BF16, KV_FP8, KV_INT8 = 1, 2, 3
+ROPE_HALF, ROPE_PAIRS = 0, 1
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is missing: build it with `python paper_2608_01718_amd/build.py` "
@@ -52,6 +55,29 @@ _lib.lacache_set_small_batch.argtypes = [_P, _i32]
 _lib.lacache_profile.argtypes = [_P, _i32]
 _lib.lacache_profile_read.argtypes = [_P, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(_i64)]
 _lib.lacache_replay_fallbacks.argtypes = [_P, ctypes.POINTER(_i64)]
+
+
+class _KV(ctypes.Structure):
+    _fields_ = [("k", _P), ("v", _P), ("k_scale", _P), ("v_scale", _P), ("n_pages", _i64), ("page", _i32),
+                ("heads", _i32), ("d", _i32), ("type", ctypes.c_int)]
+
+
+class _Seqs(ctypes.Structure):
+    _fields_ = [("start", _P), ("lens", _P), ("pages", _P), ("n_seq", _i32), ("max_pages", _i32)]
+
+
+class _Rotary(ctypes.Structure):
+    _fields_ = [("table", _P), ("n_pos", _i64), ("rot", _i32), ("style", ctypes.c_int)]
+
+
+_f64 = ctypes.c_double
+_lib.lacache_rope_table.argtypes = [_P, _i64, _i64, _i32, _f64, _f64, _f64, _f64, _f64, _f64, _P]
+_lib.lacache_rope.argtypes = [_P, _P, ctypes.c_int, _i64, _i32, _i32, _i64, _i64, _i64, _i64, _P, _P, _i32, _P]
+_lib.lacache_kv_append.argtypes = [_P, _P, _P, _P, ctypes.c_int, _i64, _i64, _i64, _P, _P, _i32, _i64, _P, _i32, _P]
+_lib.lacache_kv_read.argtypes = [_P, _P, _P, _P, ctypes.c_int, _i64, _i32, _P]
+_lib.lacache_kv_attend_workspace.argtypes = [_P, ctypes.c_int, _i32, _i32, _i32]
+_lib.lacache_kv_attend_workspace.restype = _i64
+_lib.lacache_kv_attend.argtypes = [_P, _P, _P, ctypes.c_int, _i64, _i32, _i64, _i32, _f32, _i32, _P, _P, _P, _i64, _P]
 _lib.lacache_strerror.argtypes = [ctypes.c_int]
 _lib.lacache_strerror.restype = ctypes.c_char_p
 
@@ -61,7 +87,9 @@ EXPORTED = ("lacache_create", "lacache_create_ensemble", "lacache_models", "laca
             "lacache_accept_length",
             "lacache_enable_lsh", "lacache_lookup_lsh", "lacache_export_signatures",
             "lacache_set_small_batch",
-            "lacache_profile", "lacache_profile_read", "lacache_replay_fallbacks", "lacache_strerror")
+            "lacache_profile", "lacache_profile_read", "lacache_replay_fallbacks", "lacache_strerror",
+            "lacache_rope_table", "lacache_rope", "lacache_kv_append", "lacache_kv_read",
+            "lacache_kv_attend_workspace", "lacache_kv_attend")
 
 
 class LaCacheError(RuntimeError):
@@ -441,6 +469,246 @@ def lacache_replay_fallbacks(c: LaCache) -> int:
     n = _i64(0)
     _check(_lib.lacache_replay_fallbacks(c.handle, ctypes.byref(n)), "lacache_replay_fallbacks")
     return n.value
+
+
+_KV_DTYPES = {KV_BF16: torch.bfloat16, KV_FP8: torch.float8_e4m3fn, KV_INT8: torch.int8}
+_KV_TYPES = {t: k for k, t in _KV_DTYPES.items()}
+_ROW_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _current(dev: torch.device):
+    """A context in which `dev` is the calling thread's current device."""
+    return contextlib.nullcontext() if torch.cuda.current_device() == dev.index else torch.cuda.device(dev)
+
+
+def _rows(t: torch.Tensor, heads: int, d: int, dev: torch.device, dtype, name: str) -> int:
+    """The row stride of [rows, heads, d] activations whose rows are each contiguous."""
+    if t.dtype != dtype or t.device != dev:
+        raise ValueError(f"{name}: expected a {dtype} tensor on {dev}, got {t.dtype} on {t.device}")
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d or (
+            t.shape[0] and ((d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d))):
+        raise ValueError(f"{name}: expected [rows, {heads}, {d}] with contiguous rows, got {tuple(t.shape)} with strides "
+                         f"{t.stride()}")
+    return t.stride(0)
+
+
+def _made(shape, dtype, dev, stream):
+    """An empty tensor that belongs to the stream the call runs on."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+        stream = torch.cuda.ExternalStream(handle, device=dev) if handle else torch.cuda.default_stream(dev)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=dev)
+
+
+def _given(t: torch.Tensor, shape, dtype, dev, name: str) -> torch.Tensor:
+    if t.dtype != dtype or t.device != dev or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {list(shape)} {dtype} tensor on {dev}")
+    return t
+
+
+class Rope:
+    """A rotary table [positions, rot / 2, 2] (cos, sin; float32, for example from lacache_rope_table) and the layout of
+    the pairs."""
+
+    def __init__(self, table: torch.Tensor, style: int = ROPE_HALF):
+        if table.dtype != torch.float32 or table.device.type != "cuda" or table.dim() != 3 or table.shape[2] != 2 or \
+                not table.is_contiguous():
+            raise ValueError("table: expected a contiguous float32 [positions, rot / 2, 2] tensor on a GPU")
+        self.table, self.style, self.rot = table, style, 2 * table.shape[1]
+        self._c = _Rotary(table.data_ptr(), table.shape[0], self.rot, style)
+        self._ref = ctypes.addressof(self._c)
+
+
+class Sequences:
+    """The sequences of a call: start [n + 1] (their rows in the packed row tensors), lens [n] (their tokens, the new
+    ones included), pages [n, max_pages]; int32 on one GPU."""
+
+    def __init__(self, start: torch.Tensor, lens: torch.Tensor, pages: torch.Tensor):
+        n, dev = lens.shape[0], lens.device
+        if dev.type != "cuda" or pages.dim() != 2:
+            raise ValueError("sequences: expected tensors on a GPU, pages as [sequences, max_pages]")
+        _ints(start, (n + 1,), dev.index, "start")
+        _ints(lens, (n,), dev.index, "lens")
+        _ints(pages, (n, pages.shape[1]), dev.index, "pages")
+        self.start, self.lens, self.pages, self.device = start, lens, pages, dev
+        self._c = _Seqs(start.data_ptr(), lens.data_ptr(), pages.data_ptr(), n, pages.shape[1])
+        self._ref = ctypes.addressof(self._c)
+
+    def __len__(self) -> int:
+        return self._c.n_seq
+
+
+class KVCache:
+    """A paged key-value cache: the pools of lacache_kv in torch tensors, and the scratch of its attention.  Without
+    `pools` they are allocated here (zeros): k and v [n_pages, heads, page / 32, 32 D] (D: d padded to 64, 96, 128, 192 or
+    256) bfloat16, float8_e4m3fn or int8, and for the last two k_scale and v_scale [n_pages, heads, page] float32.  With
+    pools = (k, v, k_scale, v_scale) these tensors are used.  Calls on one cache are ordered on one stream (or by events):
+    they share the pools and the scratch."""
+
+    def __init__(self, n_pages: int = 0, heads: int = 0, d: int = 0, page: int = 64, type: int = KV_BF16, device: int = 0,
+                 pools=None):
+        if pools is None:
+            if type not in _KV_DTYPES or page not in (32, 64, 128, 256) or d < 1 or d > 256:
+                raise ValueError("KVCache: expected a KV_ type, a page of 32, 64, 128 or 256 tokens and 1 <= d <= 256")
+            dev = torch.device("cuda", device)
+            shape = (n_pages, heads, page // 32, 32 * _padded(d))
+            # (zeros of a one-byte type: fp8 has no fill everywhere, its zero is the byte 0)
+            k, v = (torch.zeros(shape, dtype=torch.bfloat16 if type == KV_BF16 else torch.int8, device=dev)
+                    .view(_KV_DTYPES[type]) for _ in range(2))
+            ks, vs = (None if type == KV_BF16 else torch.zeros((n_pages, heads, page), device=dev) for _ in range(2))
+        else:
+            k, v, ks, vs = pools
+            if k.dim() != 4 or k.dtype not in _KV_TYPES or k.device.type != "cuda":
+                raise ValueError("pools: expected [n_pages, heads, page / 32, 32 D] tensors on a GPU")
+            dev, type = k.device, _KV_TYPES[k.dtype]
+            n_pages, heads, page = k.shape[0], k.shape[1], 32 * k.shape[2]
+            if not 1 <= d <= 256 or k.shape[3] != 32 * _padded(d):
+                raise ValueError(f"pools: tiles of {k.shape[3]} elements do not fit d = {d}")
+            _given(k, k.shape, k.dtype, dev, "k")
+            _given(v, k.shape, k.dtype, dev, "v")
+            for t, name in ((ks, "k_scale"), (vs, "v_scale")):
+                if type != KV_BF16:
+                    _given(t, (n_pages, heads, page), torch.float32, dev, name)
+                elif t is not None:
+                    raise ValueError(f"{name}: a bfloat16 cache has no scales")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, ks, vs
+        self.n_pages, self.heads, self.d, self.page, self.type, self.device = n_pages, heads, d, page, type, dev
+        self._c = _KV(k.data_ptr(), v.data_ptr(), *(0 if t is None else t.data_ptr() for t in (ks, vs)), n_pages, page,
+                      heads, d, type)
+        self._ref = ctypes.addressof(self._c)
+        self._need, self._space = {}, None
+
+    def append(self, k, v, seqs, q=None, rope=None, q_out=None, max_new=0, stream=None):
+        return lacache_kv_append(self, k, v, seqs, q, rope, q_out, max_new, stream)
+
+    def read(self, seqs, rows, dtype=torch.bfloat16, out=None, max_new=0, stream=None):
+        return lacache_kv_read(self, seqs, rows, dtype, out, max_new, stream)
+
+    def attend(self, q, seqs, scale=None, window=0, max_new=0, out=None, stream=None):
+        return lacache_kv_attend(self, q, seqs, scale, window, max_new, out, stream)
+
+
+def _padded(d: int) -> int:
+    return next(D for D in (64, 96, 128, 192, 256) if d <= D)
+
+
+def lacache_rope_table(n: int, rot: int, base: float = 10000.0, factor: float = 1.0, original: float = 0.0,
+                       low: float = 1.0, high: float = 32.0, magnitude: float = 1.0, first: int = 0, device: int = 0,
+                       out=None, stream=None):
+    """(cos, sin) of positions first .. first+n-1 for rot / 2 pairs, [n, rot / 2, 2] float32, scaled by parts for long
+    contexts if factor > 1."""
+    dev = torch.device("cuda", device)
+    shape = (n, rot // 2, 2)
+    out = _made(shape, torch.float32, dev, stream) if out is None else _given(out, shape, torch.float32, dev, "out")
+    with _current(dev):
+        _check(_lib.lacache_rope_table(out.data_ptr(), first, n, rot, base, factor, original, low, high, magnitude,
+                                       _stream(dev.index, stream)), "lacache_rope_table")
+    return out
+
+
+def lacache_rope(x, pos, rope: Rope, backward: bool = False, out=None, stream=None):
+    """x [rows, H, d] float32 or bfloat16 (any strides, the last one 1), pos [rows] int32.  Returns the turned rows
+    (`out`, which may be x; otherwise a new contiguous tensor); with backward=True the gradient of the input from that of
+    the output."""
+    dev = x.device
+    if x.dim() != 3 or x.dtype not in _ROW_DTYPES or dev.type != "cuda" or (x.shape[2] > 1 and x.stride(2) != 1):
+        raise ValueError("x: expected a float32 or bfloat16 [rows, H, d] tensor on a GPU, its last stride 1")
+    rows, H, d = x.shape
+    if out is None:
+        out = _made(x.shape, x.dtype, dev, stream)
+    elif out.shape != x.shape or out.dtype != x.dtype or out.device != dev or (d > 1 and out.stride(2) != 1):
+        raise ValueError(f"out: expected {tuple(x.shape)} {x.dtype} on {dev}, its last stride 1")
+    if rope.table.device != dev:
+        raise ValueError(f"rope: expected a table on {dev}")
+    with _current(dev):
+        _check(_lib.lacache_rope(x.data_ptr(), out.data_ptr(), _ROW_DTYPES[x.dtype], rows, H, d, x.stride(0), x.stride(1),
+                                 out.stride(0), out.stride(1), _ints(pos, (rows,), dev.index, "pos"), rope._ref,
+                                 int(backward), _stream(dev.index, stream)), "lacache_rope")
+    return out
+
+
+def lacache_kv_append(c: KVCache, k, v, seqs: Sequences, q=None, rope=None, q_out=None, max_new: int = 0, stream=None):
+    """Store the new tokens k, v [rows, heads, d] (float32 or bfloat16, for example parts of one projection's output) of
+    every sequence; k and q [rows, q_heads, d] are turned by `rope`.  Returns the turned q (None without q)."""
+    dev, dtype = c.device, k.dtype
+    if dtype not in _ROW_DTYPES:
+        raise ValueError(f"k: unsupported dtype {dtype}")
+    rows = k.shape[0]
+    k_row, v_row = _rows(k, c.heads, c.d, dev, dtype, "k"), _rows(v, c.heads, c.d, dev, dtype, "v")
+    if v.shape[0] != rows or seqs.device != dev or (rope is not None and rope.table.device != dev):
+        raise ValueError(f"expected {rows} rows of v, and sequences and table on {dev}")
+    q_ptr = o_ptr = None
+    q_row = q_heads = 0
+    if q is not None:
+        q_heads = q.shape[1]
+        q_row = _rows(q, q_heads, c.d, dev, dtype, "q")
+        if q.shape[0] != rows:
+            raise ValueError(f"q: expected {rows} rows")
+        q_out = _made(q.shape, dtype, dev, stream) if q_out is None else _given(q_out, q.shape, dtype, dev, "q_out")
+        q_ptr, o_ptr = q.data_ptr(), q_out.data_ptr()
+    with _current(dev):
+        _check(_lib.lacache_kv_append(c._ref, seqs._ref, k.data_ptr(), v.data_ptr(), _ROW_DTYPES[dtype], rows, k_row,
+                                      v_row, q_ptr, o_ptr, q_heads, q_row, None if rope is None else rope._ref, max_new,
+                                      _stream(dev.index, stream)), "lacache_kv_append")
+    return q_out if q is not None else None
+
+
+def lacache_kv_read(c: KVCache, seqs: Sequences, rows: int, dtype=torch.bfloat16, out=None, max_new: int = 0,
+                    stream=None):
+    """The newest tokens of every sequence as (k, v), each [rows, heads, d] of dtype; rows is start[-1]."""
+    dev = c.device
+    if dtype not in _ROW_DTYPES or seqs.device != dev:
+        raise ValueError(f"expected float32 or bfloat16, and sequences on {dev}")
+    shape = (rows, c.heads, c.d)
+    if out is None:
+        out = (_made(shape, dtype, dev, stream), _made(shape, dtype, dev, stream))
+    for t, name in zip(out, ("k", "v")):
+        _given(t, shape, dtype, dev, name)
+    with _current(dev):
+        _check(_lib.lacache_kv_read(c._ref, seqs._ref, out[0].data_ptr(), out[1].data_ptr(), _ROW_DTYPES[dtype], rows,
+                                    max_new, _stream(dev.index, stream)), "lacache_kv_read")
+    return out
+
+
+def lacache_kv_attend_workspace(c: KVCache, dtype: int, n_seq: int, q_heads: int, max_new: int = 0) -> int:
+    """Bytes of scratch that lacache_kv_attend needs (dtype: F32 or BF16)."""
+    with _current(c.device):
+        n = int(_lib.lacache_kv_attend_workspace(c._ref, dtype, n_seq, q_heads, max_new))
+    if n < 0:
+        raise LaCacheError(n, "lacache_kv_attend_workspace")
+    return n
+
+
+def lacache_kv_attend(c: KVCache, q, seqs: Sequences, scale=None, window: int = 0, max_new: int = 0, out=None,
+                      stream=None):
+    """Attention of the new rows q [rows, q_heads, d] (already turned) over the cached tokens.  scale defaults to
+    1 / sqrt(d).  Returns (out [rows, q_heads, d] of q's dtype, lse [rows, q_heads] float32)."""
+    dev, dtype = c.device, q.dtype
+    if dtype not in _ROW_DTYPES or q.dim() != 3 or seqs.device != dev:
+        raise ValueError(f"q: expected float32 or bfloat16 [rows, q_heads, d], and sequences on {dev}")
+    rows, q_heads = q.shape[0], q.shape[1]
+    q_row = _rows(q, q_heads, c.d, dev, dtype, "q")
+    if out is None:
+        out = (_made(q.shape, dtype, dev, stream), _made((rows, q_heads), torch.float32, dev, stream))
+    else:
+        _given(out[0], q.shape, dtype, dev, "out")
+        _given(out[1], (rows, q_heads), torch.float32, dev, "lse")
+    o, lse = out
+    key = (dtype, len(seqs), q_heads, max_new)
+    need = c._need.get(key)
+    if need is None:
+        need = c._need[key] = lacache_kv_attend_workspace(c, _ROW_DTYPES[dtype], len(seqs), q_heads, max_new)
+    if c._space is None or c._space.numel() < need:
+        c._space = _made((need,), torch.uint8, dev, stream)
+    with _current(dev):
+        _check(_lib.lacache_kv_attend(c._ref, seqs._ref, q.data_ptr(), _ROW_DTYPES[dtype], rows, q_heads, q_row, max_new,
+                                      c.d ** -0.5 if scale is None else scale, window, o.data_ptr(), lse.data_ptr(),
+                                      c._space.data_ptr(), c._space.numel(), _stream(dev.index, stream)),
+               "lacache_kv_attend")
+    return out
 
 
 def raw_library() -> ctypes.CDLL:
