@@ -484,7 +484,7 @@ int lacache_kv_read(const lacache_kv *kv, const lacache_seqs *seqs, void *k_out,
  *   lse   [rows][q_heads] float = log sum_j exp(scale q.k_j); NULL: not wanted.
  *         A row that sees nothing has out = 0 and lse = -infinity.
  * Products are exact and sums are in float32; with bfloat16 rows the weights
- * are rounded to bfloat16 before they multiply the values.
+ * are rounded to 16 bits before they multiply the values.
  *   max_new    a bound on the new tokens of a sequence (for the launch shape
  *              alone; 0: not known)
  *   workspace  lacache_kv_attend_workspace bytes of device memory, 16-byte

@@ -17,7 +17,7 @@ bool is_dtype(lacache_dtype t) { return t == LACACHE_F32 || t == LACACHE_BF16; }
 
 // `data`: the pools' memory is looked at too.
 bool to_pool(const lacache_kv* kv, bool data, KvPool* p) {
-    if (!kv || kv->n_pages < 0 || kv->n_pages > INT32_MAX || kv->heads < 1 || kv->heads > 65536 || kv->d < 8 ||
+    if (!kv || kv->n_pages < 0 || kv->n_pages > INT32_MAX || kv->heads < 1 || kv->heads > 65535 || kv->d < 8 ||
         kv->d > 256 || kv->d % 8 != 0 || kv->type < LACACHE_KV_BF16 || kv->type > LACACHE_KV_INT8)
         return false;
     const int shift = kv->page == 32 ? 5 : kv->page == 64 ? 6 : kv->page == 128 ? 7 : kv->page == 256 ? 8 : 0;
@@ -80,7 +80,7 @@ int lacache_rope(const void* x, void* y, lacache_dtype dtype, int64_t rows, int3
                  int64_t x_head, int64_t y_row, int64_t y_head, const int32_t* pos, const lacache_rotary* rope,
                  int32_t backward, void* stream) {
     RopeArgs r;
-    if (!is_dtype(dtype) || rows < 0 || rows > INT32_MAX || H < 1 || H > 65536 || d < 1 || d > 4096 || x_row < 0 ||
+    if (!is_dtype(dtype) || rows < 0 || rows > INT32_MAX || H < 1 || H > 65535 || d < 1 || d > 4096 || x_row < 0 ||
         x_head < 0 || y_row < 0 || y_head < 0 || !rope || !to_rope(rope, d, &r))
         return LACACHE_EINVAL;
     if (rows == 0) return LACACHE_OK;
@@ -98,7 +98,7 @@ int lacache_kv_append(const lacache_kv* kv, const lacache_seqs* seqs, const void
         q_row < 0 || max_new < 0 || !to_rope(rope, kv->d, &a.rope))
         return LACACHE_EINVAL;
     const bool with_q = q || q_out;
-    if (with_q && (q_heads < 1 || q_heads > 65536 || !rope)) return LACACHE_EINVAL;
+    if (with_q && (q_heads < 1 || q_heads > 65535 || !rope)) return LACACHE_EINVAL;
     if (rows == 0 || seqs->n_seq == 0) return LACACHE_OK;
     const uintptr_t esz = dtype == LACACHE_F32 ? 4 : 2;
     if (!k || !v || !aligned(k, esz) || !aligned(v, esz) || (with_q && (!q || !q_out || !aligned(q, esz) || !aligned(q_out, esz))))
@@ -124,7 +124,7 @@ int lacache_kv_read(const lacache_kv* kv, const lacache_seqs* seqs, void* k_out,
 int64_t lacache_kv_attend_workspace(const lacache_kv* kv, lacache_dtype dtype, int32_t n_seq, int32_t q_heads,
                                     int32_t max_new) {
     KvPool p;
-    if (!to_pool(kv, false, &p) || !is_dtype(dtype) || n_seq < 0 || q_heads < 1 || q_heads > 65536 ||
+    if (!to_pool(kv, false, &p) || !is_dtype(dtype) || n_seq < 0 || q_heads < 1 || q_heads > 65535 ||
         q_heads % kv->heads != 0 || max_new < 0)
         return LACACHE_EINVAL;
     const int cu = compute_units();
@@ -136,8 +136,8 @@ int lacache_kv_attend(const lacache_kv* kv, const lacache_seqs* seqs, const void
                       float* lse, void* workspace, int64_t workspace_bytes, void* stream) {
     AttendArgs a{};
     if (!to_pool(kv, true, &a.pool) || !to_seqs(seqs, rows, &a.seqs) || !is_dtype(dtype) || q_heads < 1 ||
-        q_heads > 65536 || q_heads % kv->heads != 0 || q_row < 0 || max_new < 0 || !std::isfinite(scale) ||
-        window < 0 || workspace_bytes < 0)
+        q_heads > 65535 || q_heads % kv->heads != 0 || q_row < 0 || max_new < 0 || !std::isfinite(scale) ||
+        rows * (q_heads / kv->heads) > INT32_MAX || window < 0 || workspace_bytes < 0)
         return LACACHE_EINVAL;
     if (rows == 0 || seqs->n_seq == 0) return LACACHE_OK;
     const uintptr_t esz = dtype == LACACHE_F32 ? 4 : 2;

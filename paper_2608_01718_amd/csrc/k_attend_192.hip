@@ -1,0 +1,6 @@
+// k_attend_192.hip -- the attention kernels of heads padded to 192 columns.
+#include "attend.hpp"
+
+namespace lacache {
+template hipError_t launch_attend<192>(const AttendArgs&, const AttendPlan&, int, hipStream_t);
+}  // namespace lacache

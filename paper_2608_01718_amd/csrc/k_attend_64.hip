@@ -1,0 +1,6 @@
+// k_attend_64.hip -- the attention kernels of heads padded to 64 columns.
+#include "attend.hpp"
+
+namespace lacache {
+template hipError_t launch_attend<64>(const AttendArgs&, const AttendPlan&, int, hipStream_t);
+}  // namespace lacache
