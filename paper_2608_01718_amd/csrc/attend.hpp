@@ -26,59 +26,123 @@ constexpr float kLn2 = 0.69314718055994530942f;
 // and weights, and what goes around them.  (A wave of four has a SIMD's 512 registers to itself.)
 constexpr int attend_occupancy(int dp, bool bytes, int R, bool f32) {
     const int terms = f32 ? 3 : 1;
-    const int regs = R * dp / 4 + R * dp / 8 * terms + (bytes ? dp / 4 : dp / 2) + 12 * R + 4 * R * (f32 ? 3 : 2) + 4 * R +
+    const int regs = R * dp / 4 + R * dp / 8 * terms + (bytes ? dp / 4 + 16 : dp / 2) + 12 * R + 4 * R * (f32 ? 3 : 2) + 4 * R +
                      8 * (terms - 1) + 56;
-    return regs <= 170 ? 3 : regs <= 256 ? 2 : 1;
+    return regs <= 136 ? 4 : regs <= 170 ? 3 : regs <= 256 ? 2 : 1;
 }
 
-// What a launch works with besides the arguments: the shape of a row group, the grid, the workspace.
+// What a launch works with besides the arguments: the shape of a row group, its workers, the workspace.
 struct AttendPlan {
-    int row_waves;   // the row group's rows are split over this many waves (1, 2 or 4), its tiles over the others
-    int group_rows;  // rows of a row group: 16 R row_waves
-    int workgroups;
-    int64_t* base;   // [n_seq + 1] first item of each sequence; then the range of a workgroup
-    float* part_o;   // [2 workgroups][group_rows][dp] partial sums of values
-    float2* part_ml; // [2 workgroups][group_rows] their maxima and sums of weights
+    int group_shift;   // rows of a row group, as a shift
+    int workers;       // workgroups of the launch
+    int chunk_shift;   // the work is dealt out in chunks of this many tiles (a shift), so that counts fit in 32 bits
+    uint32_t group_magic, group_bits;  // row / group = row * magic >> bits
+    struct AttendSplit* split;  // [workers]: the row group whose last part a worker had
+    float* part_o;     // [2 workers][group rows][dp] partial sums of values
+    float2* part_ml;   // [2 workers][group rows] their maxima and sums of weights
+};
+
+// A row group of which several workers had a part, the last of them the one whose entry this is.
+struct alignas(16) AttendSplit {
+    int seq_row0, head0;   // the sequence's first row, the first query head
+    int row, n_rows;       // rows row .. row + n_rows - 1 of the sequence's (0: there is no such row group)
+    int worker0;           // the first of its workers
+    int unused[3];
 };
 
 // What the work of a sequence is: its rows and their groups, its tiles.
 struct AttendSpan {
-    KvSpan span;
+    int row0, n, len;    // first row, new tokens, tokens with them
     int rows, groups;    // new tokens x group; row groups
     int first, tiles;    // the first tile that any row sees, the number of tiles
     int cap;             // positions that exist
+    int chunks;          // the tiles in chunks
+    __device__ int64_t pos0() const { return (int64_t)len - n; }  // of the first row
+    __device__ int items(const AttendArgs& a) const { return groups * a.pool.heads * chunks; }
 };
 __device__ inline AttendSpan attend_span(const AttendArgs& a, const AttendPlan& p, int b) {
     AttendSpan r;
-    r.span = span_of(a.seqs, b);
-    r.rows = r.span.n * a.group;
-    r.groups = (r.rows + p.group_rows - 1) / p.group_rows;
+    const KvSpan s = span_of(a.seqs, b);
+    r.row0 = (int)s.row0, r.n = s.n;
+    r.len = (int)(s.pos0 + s.n);
+    r.rows = r.n * a.group;
+    r.groups = (int)(((int64_t)r.rows + (1 << p.group_shift) - 1) >> p.group_shift);
     const int64_t held = (int64_t)a.seqs.max_pages << a.pool.page_shift;
-    int64_t len = r.span.pos0 + r.span.n;
-    len = len < 0 ? 0 : len > held ? held : len;
-    int64_t lo = a.window > 0 ? r.span.pos0 - a.window + 1 : 0;
-    lo = lo < 0 ? 0 : lo;
-    r.cap = (int)len;
-    r.first = (int)(lo >> 5);
-    r.tiles = (int)((len + 31) >> 5) - r.first;
+    r.cap = r.len < 0 ? 0 : r.len > held ? (int)held : r.len;
+    const int64_t lo = a.window > 0 ? r.pos0() - a.window + 1 : 0;
+    r.first = lo < 0 ? 0 : (int)(lo >> 5);
+    r.tiles = (int)(((int64_t)r.cap + 31) >> 5) - r.first;
     if (r.tiles < 1) r.tiles = 1;  // rows that see nothing are written too
+    r.chunks = (r.tiles + (1 << p.chunk_shift) - 1) >> p.chunk_shift;
     return r;
 }
-__device__ inline int64_t attend_items(const AttendArgs& a, const AttendSpan& s) {
-    return (int64_t)s.groups * a.pool.heads * s.tiles;
+__device__ __forceinline__ int token_of(const AttendPlan& p, int row) {
+    return (int)(((uint64_t)(uint32_t)row * p.group_magic) >> p.group_bits);
 }
 
-__device__ inline int64_t shfl_up64(int64_t x, int by) {
-    const int lo = __shfl_up((int)x, by, kWave), hi = __shfl_up((int)(x >> 32), by, kWave);
-    return (int64_t)hi << 32 | (uint32_t)lo;
+// Sum over this lane and the lanes below it.
+__device__ __forceinline__ int wave_scan(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);  // row_shr:1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);  // the last lane of rows 0 and 2 to rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);  // lane 31 to the upper half
+    return x;
 }
-__device__ inline int64_t shfl64(int64_t x, int from) {
-    const int lo = __shfl((int)x, from, kWave), hi = __shfl((int)(x >> 32), from, kWave);
-    return (int64_t)hi << 32 | (uint32_t)lo;
+
+// The range of items of this workgroup: the sequence in which it begins, the items before that sequence, the range, and
+// the items of a full range (a multiple of `grain`).  All 256 threads take part, a thread a sequence.
+struct AttendRange {
+    int b, before, at, end, per;
+};
+__device__ __forceinline__ AttendRange attend_range(const AttendArgs& a, const AttendPlan& p, int grain) {
+    __shared__ int total_of[4], found[2];
+    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, n_seq = a.seqs.n_seq;
+    int own = 0, sum = 0, all = 0, b = tid;
+    // items up to sequence b within a round of 256 (sum), and of the round (returned)
+    auto scan = [&]() {
+        own = b < n_seq ? attend_span(a, p, b).items(a) : 0;
+        sum = wave_scan(own);
+        __syncthreads();
+        if (lane == 63) total_of[wid] = sum;
+        __syncthreads();
+        const int t0 = total_of[0], t1 = total_of[1], t2 = total_of[2];
+        sum += (wid > 0 ? t0 : 0) + (wid > 1 ? t1 : 0) + (wid > 2 ? t2 : 0);
+        return t0 + t1 + t2 + total_of[3];
+    };
+    for (; b - tid < n_seq; b += 256) all += scan();
+    all = __builtin_amdgcn_readfirstlane(all);
+    AttendRange r;
+    r.per = (int)(((uint32_t)all + (uint32_t)p.workers - 1) / (uint32_t)p.workers);
+    r.per = (r.per + grain - 1) & ~(grain - 1);
+    const int64_t at = (int64_t)blockIdx.x * r.per;
+    r.at = at < all ? (int)at : all;
+    r.end = at + r.per < all ? (int)(at + r.per) : all;
+    // the thread whose sequence holds item `at` finds it
+    int before = 0;
+    for (b = tid; b - tid < n_seq; b += 256) {
+        const int round = n_seq > 256 ? scan() : all;
+        if (r.at >= before + sum - own && r.at < before + sum) {
+            found[0] = b;
+            found[1] = before + sum - own;
+        }
+        before += round;
+    }
+    __syncthreads();
+    r.b = __builtin_amdgcn_readfirstlane(found[0]);
+    r.before = __builtin_amdgcn_readfirstlane(found[1]);
+    return r;
 }
-__device__ inline int64_t uniform64(int64_t x) {
-    const int lo = __builtin_amdgcn_readfirstlane((int)x), hi = __builtin_amdgcn_readfirstlane((int)(x >> 32));
-    return (int64_t)hi << 32 | (uint32_t)lo;
+
+// 16 bytes a lane from a tile whose bytes past `size` (0: there is no tile) are not read and come as zeros.  Keys and
+// values are read once: non-temporal loads are 12 % faster (131,071 tokens 89 us, 102 without; 256 sequences of 512 to
+// 2048 tokens, 16 heads of 64 columns 191 us, 214).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_rsrc(const void* p, int size) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, size, 0x00020000);
+}
+__device__ __forceinline__ u32x4 tile_load(__amdgpu_buffer_rsrc_t r, int offset) {
+    return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, offset, 0, 2));
 }
 
 // four 8-bit codes as bfloat16 pairs
@@ -120,26 +184,47 @@ struct Attend {
     static constexpr int OCC = attend_occupancy(DP, BYTES, R, F32);
     static constexpr int CB = DP <= 128 ? DP : DP / 2;     // columns joined at a time
     static constexpr int ESZ = F32 ? 4 : 2;
+    static constexpr int BYTES_TILE = 32 * DP * (BYTES ? 1 : 2);
 
     u32x4 q[R][KC][NT];
     f32x4 o[R][NJ];
     float m[R], l[R];
     int hi[R], lo[R];  // the positions that the lane's row sees
-    u32x4 kf[NL], vf[NL];
-    f32x4 ks[2], vs[2];
+    struct Tile {
+        u32x4 k[NL], v[NL];
+        f32x4 ks[2], vs[2];
+        int index;
+    };
+
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            m[r] = -__builtin_inff();
+            l[r] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) o[r][j] = f32x4{0, 0, 0, 0};
+        }
+    }
+    // every lane's sum over the tokens of the four lane groups
+    __device__ __forceinline__ void reduce() {
+        auto add2 = [](float x, float y) { return x + y; };
+#pragma unroll
+        for (int r = 0; r < R; ++r) l[r] = xor_combine<16>(xor_combine<32>(l[r], add2), add2);
+    }
 
     // 16 bytes of a row as KC operands: the three terms of a float32 sum back to it exactly, a bfloat16 is its own
-    __device__ __forceinline__ void load_q(const AttendArgs& a, const AttendSpan& s, int h, int row0, int lane) {
+    __device__ __forceinline__ void load_q(const AttendArgs& a, const AttendPlan& p, const AttendSpan& s, int h, int row0,
+                                           int lane) {
         const int n = lane & 15, u = lane >> 4;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             int row = row0 + 16 * r + n;
             row = row < s.rows ? row : s.rows - 1;
-            const int i = row / a.group, head = h * a.group + (row - i * a.group);
-            const int64_t pos = s.span.pos0 + i;
+            const int i = token_of(p, row), head = h * a.group + (row - i * a.group);
+            const int64_t pos = s.pos0() + i;
             hi[r] = pos < 0 ? -1 : (int)pos;
             lo[r] = a.window > 0 && hi[r] - a.window + 1 > 0 ? hi[r] - a.window + 1 : 0;
-            const char* src = a.q + ((s.span.row0 + i) * a.q_row + (int64_t)head * a.pool.d) * ESZ;
+            const char* src = a.q + (((int64_t)s.row0 + i) * a.q_row + (int64_t)head * a.pool.d) * ESZ;
             const bool wide = ((uintptr_t)src & 15) == 0;
 #pragma unroll
             for (int c = 0; c < KC; ++c) {
@@ -176,34 +261,38 @@ struct Attend {
         }
     }
 
-    __device__ __forceinline__ void load_k(const char* p, const float* sc, int lane) {
+    static __device__ __forceinline__ void load_k(Tile& t, const AttendArgs& a, int64_t place, int there, int lane) {
+        const auto r = tile_rsrc(a.pool.k + place * BYTES_TILE, there * BYTES_TILE);
 #pragma unroll
-        for (int i = 0; i < NL; ++i) kf[i] = ((const u32x4*)p)[i * 64 + lane];
+        for (int i = 0; i < NL; ++i) t.k[i] = tile_load(r, i * 1024 + lane * 16);
         if constexpr (BYTES) {
-            ks[0] = *(const f32x4*)(sc + 4 * (lane >> 4));
-            ks[1] = *(const f32x4*)(sc + 16 + 4 * (lane >> 4));
+            const auto rs = tile_rsrc(a.pool.k_scale + place * 32, there * 128);
+#pragma unroll
+            for (int b = 0; b < 2; ++b) t.ks[b] = __builtin_bit_cast(f32x4, tile_load(rs, 64 * b + (lane >> 4) * 16));
         }
     }
-    __device__ __forceinline__ void load_v(const char* p, const float* sc, int lane) {
+    static __device__ __forceinline__ void load_v(Tile& t, const AttendArgs& a, int64_t place, int there, int lane) {
+        const auto r = tile_rsrc(a.pool.v + place * BYTES_TILE, there * BYTES_TILE);
 #pragma unroll
-        for (int i = 0; i < NL; ++i) vf[i] = ((const u32x4*)p)[i * 64 + lane];
+        for (int i = 0; i < NL; ++i) t.v[i] = tile_load(r, i * 1024 + lane * 16);
         if constexpr (BYTES) {
-            vs[0] = *(const f32x4*)(sc + 4 * (lane >> 4));
-            vs[1] = *(const f32x4*)(sc + 16 + 4 * (lane >> 4));
+            const auto rs = tile_rsrc(a.pool.v_scale + place * 32, there * 128);
+#pragma unroll
+            for (int b = 0; b < 2; ++b) t.vs[b] = __builtin_bit_cast(f32x4, tile_load(rs, 64 * b + (lane >> 4) * 16));
         }
     }
 
-    __device__ __forceinline__ u32x4 k_operand(int b, int c) const {
-        if constexpr (!BYTES) return kf[2 * c + b];
-        else return widen8<CT>(kf[c][2 * b], kf[c][2 * b + 1]);
+    static __device__ __forceinline__ u32x4 k_operand(const Tile& t, int b, int c) {
+        if constexpr (!BYTES) return t.k[2 * c + b];
+        else return widen8<CT>(t.k[c][2 * b], t.k[c][2 * b + 1]);
     }
-    __device__ __forceinline__ u32x4 v_operand(int j) const {
-        if constexpr (!BYTES) return vf[j];
-        else return widen8<CT>(vf[j >> 1][2 * (j & 1)], vf[j >> 1][2 * (j & 1) + 1]);
+    static __device__ __forceinline__ u32x4 v_operand(const Tile& t, int j) {
+        if constexpr (!BYTES) return t.v[j];
+        else return widen8<CT>(t.v[j >> 1][2 * (j & 1)], t.v[j >> 1][2 * (j & 1) + 1]);
     }
 
-    // scores of the tile in kf, in units of log2 e
-    __device__ __forceinline__ void scores(f32x4 (&s)[R][2], float scale2) {
+    // scores of a tile, in units of log2 e
+    __device__ __forceinline__ void scores(const Tile& t_, f32x4 (&s)[R][2], float scale2) {
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -212,7 +301,7 @@ struct Attend {
         for (int c = 0; c < KC; ++c)
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
-                const u32x4 k = k_operand(b, c);
+                const u32x4 k = k_operand(t_, b, c);
 #pragma unroll
                 for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -222,7 +311,7 @@ struct Attend {
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float f = BYTES ? ks[b][i] * scale2 : scale2;
+                const float f = BYTES ? t_.ks[b][i] * scale2 : scale2;
 #pragma unroll
                 for (int r = 0; r < R; ++r) s[r][b][i] *= f;
             }
@@ -230,8 +319,8 @@ struct Attend {
 
     // Hides the positions that a row does not see, and the values of those that no row of the wave sees (first .. last
     // are seen by one): what lies there may be anything.
-    __device__ __forceinline__ void hide(f32x4 (&s)[R][2], int tile, int first, int last, int lane) {
-        const int t0 = 32 * tile + 4 * (lane >> 4);
+    __device__ __forceinline__ void hide(Tile& t, int index, f32x4 (&s)[R][2], int first, int last, int lane) {
+        const int t0 = 32 * index + 4 * (lane >> 4);
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             uint32_t keep[4];
@@ -242,22 +331,22 @@ struct Attend {
                 for (int r = 0; r < R; ++r)
                     s[r][b][i] = j >= lo[r] && j <= hi[r] ? s[r][b][i] : -__builtin_inff();
                 keep[i] = j >= first && j <= last ? 0xFFFFFFFFu : 0u;
-                if constexpr (BYTES) vs[b][i] = keep[i] ? vs[b][i] : 0.0f;
+                if constexpr (BYTES) t.vs[b][i] = keep[i] ? t.vs[b][i] : 0.0f;
             }
             if constexpr (BYTES) {
                 const uint32_t w = (keep[0] & 0xFFu) | (keep[1] & 0xFF00u) | (keep[2] & 0xFF0000u) | (keep[3] & 0xFF000000u);
 #pragma unroll
                 for (int i = 0; i < NL; ++i) {
-                    vf[i][b] &= w;
-                    vf[i][2 + b] &= w;
+                    t.v[i][b] &= w;
+                    t.v[i][2 + b] &= w;
                 }
             } else {
                 const uint32_t w0 = (keep[0] & 0xFFFFu) | (keep[1] & 0xFFFF0000u),
                                w1 = (keep[2] & 0xFFFFu) | (keep[3] & 0xFFFF0000u);
 #pragma unroll
                 for (int i = 0; i < NL; ++i) {
-                    vf[i][2 * b] &= w0;
-                    vf[i][2 * b + 1] &= w1;
+                    t.v[i][2 * b] &= w0;
+                    t.v[i][2 * b + 1] &= w1;
                 }
             }
         }
@@ -292,8 +381,8 @@ struct Attend {
         }
     }
 
-    // O^T += V^T P^T with the tile in vf
-    __device__ __forceinline__ void gather(f32x4 (&s)[R][2]) {
+    // O^T += V^T P^T
+    __device__ __forceinline__ void gather(const Tile& t_, f32x4 (&s)[R][2]) {
         u32x4 p[R][NP];
 #pragma unroll
         for (int r = 0; r < R; ++r)
@@ -301,14 +390,14 @@ struct Attend {
             for (int e = 0; e < 4; ++e) {
                 float x = s[r][e >> 1][2 * (e & 1)], y = s[r][e >> 1][2 * (e & 1) + 1];
                 if constexpr (BYTES) {
-                    x *= vs[e >> 1][2 * (e & 1)];
-                    y *= vs[e >> 1][2 * (e & 1) + 1];
+                    x *= t_.vs[e >> 1][2 * (e & 1)];
+                    y *= t_.vs[e >> 1][2 * (e & 1) + 1];
                 }
                 split2<NP>(x, y, p[r], e);
             }
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
-            const u32x4 v = v_operand(j);
+            const u32x4 v = v_operand(t_, j);
 #pragma unroll
             for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -317,10 +406,9 @@ struct Attend {
     }
 };
 
-// Four columns of a row of the result.
+// Four columns of the result, from element `at` on.
 template <bool F32>
-__device__ __forceinline__ void store4(const AttendArgs& a, int64_t row, int head, int col, f32x4 x) {
-    const int64_t at = (row * a.q_heads + head) * a.pool.d + col;
+__device__ __forceinline__ void store4(const AttendArgs& a, int64_t at, f32x4 x) {
     if (F32) {
         float* p = (float*)a.out + at;
         if (((uintptr_t)p & 15) == 0) *(f32x4*)p = x;
@@ -339,237 +427,186 @@ __device__ __forceinline__ float lse_of(float m, float l) {
 template <int DP, int CT, int R, bool F32>
 __global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(AttendArgs a, AttendPlan p) {
     using A = Attend<DP, CT, R, F32>;
-    __shared__ float sm[4][16 * R], sl[4][16 * R];
+    constexpr int GR = 16 * R;  // rows of a row group
+    __shared__ float2 sml[4][GR];
     __shared__ float so[4][16][A::CB + 4];
     const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int tile_waves = 4 / p.row_waves, row_part = wid % p.row_waves, tile_part = wid / p.row_waves;
+    const int worker = blockIdx.x;
 
-    // the range of this workgroup, and the sequence in which it begins
-    const int n_seq = a.seqs.n_seq;
-    int64_t total = 0;
-    for (int b0 = 0; b0 < n_seq; b0 += 64) {
-        const int b = b0 + lane;
-        int64_t x = b < n_seq ? attend_items(a, attend_span(a, p, b)) : 0;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int64_t y = shfl_up64(x, o);
-            if (lane >= o) x += y;
-        }
-        if (blockIdx.x == 0 && wid == 0 && b < n_seq) p.base[b + 1] = total + x;
-        total += shfl64(x, 63);
+    AttendRange range = attend_range(a, p, 4 >> (p.chunk_shift < 2 ? p.chunk_shift : 2));
+    if (range.at >= range.end) {
+        if (tid == 0) p.split[worker].n_rows = 0;
+        return;
     }
-    total = uniform64(total);
-    int64_t per = (total + p.workgroups - 1) / p.workgroups;
-    per = (per + tile_waves - 1) / tile_waves * tile_waves;
-    if (blockIdx.x == 0 && tid == 0) {
-        p.base[0] = 0;
-        p.base[n_seq + 1] = per;
-    }
-    int64_t at = (int64_t)blockIdx.x * per;
-    const int64_t end = at + per < total ? at + per : total;
-    if (at >= end) return;
-    int b = 0;
-    int64_t before = 0;  // items before sequence b
-    for (int b0 = 0; b0 < n_seq; b0 += 64) {
-        const int bb = b0 + lane;
-        int64_t x = bb < n_seq ? attend_items(a, attend_span(a, p, bb)) : 0;
-        const int64_t own = x;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int64_t y = shfl_up64(x, o);
-            if (lane >= o) x += y;
-        }
-        const uint64_t past = __ballot(before + x > at);
-        if (past) {
-            const int i = __ffsll((unsigned long long)past) - 1;
-            b = b0 + i;
-            before = uniform64(before + shfl64(x - own, i));
-            break;
-        }
-        before = uniform64(before + shfl64(x, 63));
-    }
-    b = __builtin_amdgcn_readfirstlane(b);
-
-    A w;
+    AttendSplit split{};
     const float scale2 = a.scale * kLog2e;
     const int tile_shift = a.pool.page_shift - 5;
-    while (at < end) {
-        const AttendSpan s = attend_span(a, p, b);
-        const int64_t items = attend_items(a, s);
-        if (at - before >= items) {  // past this sequence (or it has no rows)
-            before += items;
-            ++b;
-            continue;
-        }
-        const int unit = (int)((at - before) / s.tiles);                  // kv head and row group
-        const int tile0 = (int)((at - before) - (int64_t)unit * s.tiles);
-        const int h = unit / s.groups, rg = unit - h * s.groups;
-        const int64_t left = end - at;
-        const int tile1 = s.tiles - tile0 <= left ? s.tiles : tile0 + (int)left;
-        const bool whole = tile0 == 0 && tile1 == s.tiles;
 
-        const int row0 = rg * p.group_rows + row_part * 16 * R;  // the wave's rows
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            w.m[r] = -__builtin_inff();
-            w.l[r] = 0.0f;
-#pragma unroll
-            for (int j = 0; j < A::NJ; ++j) w.o[r][j] = f32x4{0, 0, 0, 0};
-        }
-        if (row0 < s.rows) {
-            w.load_q(a, s, h, row0, lane);
-            // positions: seen by one of the wave's rows (first .. last), by all of them (first_all .. last_all)
-            const int row1 = row0 + 16 * R - 1 < s.rows ? row0 + 16 * R - 1 : s.rows - 1;
-            const int64_t p0 = s.span.pos0 + row0 / a.group, p1 = s.span.pos0 + row1 / a.group;
-            const int last_all = p0 < 0 ? -1 : (int)p0;
-            int last = p1 < 0 ? -1 : (int)p1;
-            const int first = a.window > 0 && last_all - a.window + 1 > 0 ? last_all - a.window + 1 : 0;
-            const int first_all = a.window > 0 && last - a.window + 1 > 0 ? last - a.window + 1 : 0;
-            last = last < s.cap - 1 ? last : s.cap - 1;
-            const int32_t* pages = a.seqs.pages + (int64_t)b * a.seqs.max_pages;
+    // A segment: tiles tile0 .. tile1 - 1 of one row group
+    struct Segment {
+        int h, rg, tile0, tile1, row0, rows, n_rows;  // n_rows: rows in the group
+        int first, b, item0;                          // item0: the row group's first item
+        bool starts, ends;                            // whether it holds the first and the last tile
+        int seen0, seen1, all0, all1;                 // positions that one of the rows, that every row sees
+    };
+    A w;
+    typename A::Tile tile;
+    int there = 0;
+    Segment g;
+    int page = -1, t0 = 0;
+    uint64_t todo = 0;
+    AttendSpan s = attend_span(a, p, range.b);
 
-            for (int t0 = tile0 + tile_part; t0 < tile1; t0 += 64 * tile_waves) {
-                // the next 64 tiles of the wave, a lane each: which are there and seen
-                const int mine = s.first + t0 + lane * tile_waves;
-                int page = -1;
-                if (t0 + lane * tile_waves < tile1 && 32 * mine <= last && 32 * mine + 31 >= first)
-                    page = pages[mine >> tile_shift];
-                uint64_t todo = __ballot(page >= 0 && page < a.pool.n_pages);
-                if (!todo) continue;
-                auto place = [&](int i, int& tile) {
-                    tile = s.first + t0 + i * tile_waves;
-                    const int64_t pg = __builtin_amdgcn_readlane(page, i);
-                    return ((pg * a.pool.heads + h) << tile_shift) + (tile & ((1 << tile_shift) - 1));
-                };
-                constexpr int TB = 32 * DP * (A::BYTES ? 1 : 2);  // bytes of a tile
-                int i = __ffsll((unsigned long long)todo) - 1, tile;
-                int64_t pl = place(i, tile);
-                w.load_k(a.pool.k + pl * TB, a.pool.k_scale + pl * 32, lane);
-                w.load_v(a.pool.v + pl * TB, a.pool.v_scale + pl * 32, lane);
-                todo &= todo - 1;
-                auto step = [&](auto more) {
-                    f32x4 sc[R][2];
-                    w.scores(sc, scale2);
-                    int next = 0;
-                    if constexpr (decltype(more)::value) {
-                        i = __ffsll((unsigned long long)todo) - 1;
-                        todo &= todo - 1;
-                        pl = place(i, next);
-                        w.load_k(a.pool.k + pl * TB, a.pool.k_scale + pl * 32, lane);
-                    }
-                    if (32 * tile < first_all || 32 * tile + 31 > last_all || 32 * tile + 31 > last)
-                        w.hide(sc, tile, first, last, lane);
-                    w.weigh(sc);
-                    w.gather(sc);
-                    if constexpr (decltype(more)::value) {
-                        w.load_v(a.pool.v + pl * TB, a.pool.v_scale + pl * 32, lane);
-                        tile = next;
-                    }
-                };
-                while (todo) step(std::true_type{});
-                step(std::false_type{});
+    // the wave's tiles t0, t0 + 4, ... of the segment, a lane each: which of them are there and seen
+    auto load_pages = [&]() {
+        const int t = t0 + lane * 4, mine = g.first + t;
+        page = -1;
+        if (t < g.tile1 && 32 * mine <= g.seen1 && 32 * mine + 31 >= g.seen0)
+            page = (a.seqs.pages + (int64_t)g.b * a.seqs.max_pages)[mine >> tile_shift];
+    };
+    // the wave's next tile, if there is one
+    auto next = [&]() {
+        there = todo ? 1 : 0;
+        const int k = there ? __ffsll((unsigned long long)todo) - 1 : 0;
+        todo &= todo - 1;
+        tile.index = g.first + t0 + k * 4;
+        const int64_t pg = there ? __builtin_amdgcn_readlane(page, k) : 0;
+        return ((pg * a.pool.heads + g.h) << tile_shift) + (tile.index & ((1 << tile_shift) - 1));
+    };
+    auto load_tiles = [&]() {
+        todo = __ballot(page >= 0 && page < a.pool.n_pages);
+        const int64_t pl = next();
+        A::load_k(tile, a, pl, there, lane);
+        A::load_v(tile, a, pl, there, lane);
+    };
+    // the segment that begins at item `at`, its queries and its first tiles
+    auto open = [&]() {
+        const int rel = range.at - range.before;
+        const int unit = (int)((uint32_t)rel / (uint32_t)s.chunks), c0 = rel - unit * s.chunks;
+        g.h = (int)((uint32_t)unit / (uint32_t)s.groups);
+        g.rg = unit - g.h * s.groups;
+        const int left = range.end - range.at, c1 = s.chunks - c0 <= left ? s.chunks : c0 + left;
+        range.at += c1 - c0;
+        g.item0 = range.before + unit * s.chunks;
+        g.starts = c0 == 0;
+        g.ends = c1 == s.chunks;
+        g.tile0 = c0 << p.chunk_shift;
+        g.tile1 = g.ends ? s.tiles : c1 << p.chunk_shift;
+        const int r0 = g.rg << p.group_shift;
+        g.row0 = s.row0, g.rows = s.rows, g.first = s.first, g.b = range.b;
+        g.n_rows = s.rows - r0 < GR ? s.rows - r0 : GR;
+        const int64_t p0 = s.pos0() + token_of(p, r0), p1 = s.pos0() + token_of(p, r0 + g.n_rows - 1);
+        const int q0 = p0 < 0 ? -1 : (int)p0, q1 = p1 < 0 ? -1 : (int)p1;
+        g.seen0 = a.window > 0 && q0 - a.window + 1 > 0 ? q0 - a.window + 1 : 0;
+        g.all0 = a.window > 0 && q1 - a.window + 1 > 0 ? q1 - a.window + 1 : 0;
+        g.seen1 = q1 < s.cap - 1 ? q1 : s.cap - 1;
+        g.all1 = q0 < g.seen1 ? q0 : g.seen1;
+        t0 = g.tile0 + wid;
+        load_pages();
+        w.load_q(a, p, s, g.h, r0, lane);  // while the page numbers are on their way
+        load_tiles();
+    };
+    open();
+    bool more = true;
+    while (more) {
+        w.clear();
+        while (true) {
+            while (there) {
+                f32x4 sc[R][2];
+                w.scores(tile, sc, scale2);
+                const int index = tile.index;
+                const int64_t pl = next();  // its keys are loaded under this tile's weights, its values under its scores
+                A::load_k(tile, a, pl, there, lane);
+                if (32 * index < g.all0 || 32 * index + 31 > g.all1) w.hide(tile, index, sc, g.seen0, g.seen1, lane);
+                w.weigh(sc);
+                w.gather(tile, sc);
+                A::load_v(tile, a, pl, there, lane);
             }
+            t0 += 64 * 4;
+            if (t0 >= g.tile1) break;
+            load_pages();
+            load_tiles();
         }
 
-        // the waves' results, joined where several waves had tiles of the same rows
-        auto add2 = [](float x, float y) { return x + y; };
-#pragma unroll
-        for (int r = 0; r < R; ++r) w.l[r] = xor_combine<16>(xor_combine<32>(w.l[r], add2), add2);
-        const int64_t slot = 2 * (int64_t)blockIdx.x + (tile1 < s.tiles ? 1 : 0);
-        float* part_o = p.part_o + slot * p.group_rows * DP;
-        float2* part_ml = p.part_ml + slot * p.group_rows;
-        const int64_t out0 = s.span.row0;
-        // one row's maximum and sum
-        auto put_ml = [&](int in_group, float m, float l) {
-            const int row = rg * p.group_rows + in_group;
-            if (row >= s.rows) return;
-            if (!whole) part_ml[in_group] = make_float2(m, l);
-            else if (a.lse) {
-                const int i = row / a.group;
-                a.lse[(out0 + i) * a.q_heads + h * a.group + (row - i * a.group)] = lse_of(m, l);
+        // The next segment's loads are on their way while this one's results are joined and stored.
+        const Segment old = g;
+        w.reduce();
+        more = range.at < range.end;
+        if (more) {
+            const int items = s.items(a);
+            if (range.at - range.before >= items) {  // past this sequence, and those without rows
+                range.before += items;
+                do s = attend_span(a, p, ++range.b);
+                while (s.n == 0);
             }
-        };
-        auto put_o = [&](int in_group, int col, f32x4 x, float l) {
-            const int row = rg * p.group_rows + in_group;
-            if (row >= s.rows) return;
+            open();
+        }
+        const bool whole = old.starts && old.ends;
+        const int64_t slot = (2 * (int64_t)worker + (old.ends ? 0 : 1)) * GR;
+        float* part_o = p.part_o + slot * DP;
+        float2* part_ml = p.part_ml + slot;
+        if (old.ends && !old.starts)  // the workers before this one had its other parts
+            split = AttendSplit{old.row0, old.h * a.group, old.rg * GR, old.n_rows,
+                                (int)((uint32_t)old.item0 / (uint32_t)range.per), {}};
+        // four columns of a row of the group; its maximum and sum with the first of them
+        auto put = [&](int row, int col, f32x4 x, float m, float l) {
             if (!whole) {
-                *(f32x4*)(part_o + (int64_t)in_group * DP + col) = x;
-            } else if (col < a.pool.d) {
-                const float f = l == 0.0f ? 0.0f : 1.0f / l;
-                const int i = row / a.group;
-                store4<F32>(a, out0 + i, h * a.group + (row - i * a.group), col, x * f);
+                *(f32x4*)(part_o + row * DP + col) = x;
+                if (col == 0) part_ml[row] = make_float2(m, l);
+                return;
             }
+            const int r = old.rg * GR + row, i = token_of(p, r), head = old.h * a.group + (r - i * a.group);
+            const int64_t at = ((int64_t)old.row0 + i) * a.q_heads + head;
+            if (col < a.pool.d) store4<F32>(a, at * a.pool.d + col, x * (l == 0.0f ? 0.0f : 1.0f / l));
+            if (col == 0 && a.lse) a.lse[at] = lse_of(m, l);
         };
-        const int n = lane & 15, g = lane >> 4;
-        if (tile_waves == 1) {
+        const int n = lane & 15, u = lane >> 4;
+        lds_barrier();  // the last segment's have been read
+        if (u == 0) {
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const int in_group = row_part * 16 * R + 16 * r + n;
-                if (g == 0) put_ml(in_group, w.m[r], w.l[r]);
-#pragma unroll
-                for (int j = 0; j < A::NJ; ++j) put_o(in_group, 16 * j + 4 * g, w.o[r][j], w.l[r]);
-            }
-        } else {
-            if (g == 0) {
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    sm[wid][16 * r + n] = w.m[r];
-                    sl[wid][16 * r + n] = w.l[r];
-                }
-            }
-            lds_barrier();
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                float M = -__builtin_inff(), L = 0.0f;
-                for (int t = 0; t < tile_waves; ++t) M = fmaxf(M, sm[t * p.row_waves + row_part][16 * r + n]);
-                const float base = M == -__builtin_inff() ? 0.0f : M;
-                for (int t = 0; t < tile_waves; ++t)
-                    L += sl[t * p.row_waves + row_part][16 * r + n] *
-                         __builtin_amdgcn_exp2f(sm[t * p.row_waves + row_part][16 * r + n] - base);
-                const float f = __builtin_amdgcn_exp2f(w.m[r] - base);
-                w.m[r] = M;
-                w.l[r] = L;
-#pragma unroll
-                for (int j = 0; j < A::NJ; ++j) w.o[r][j] *= f;
-                if (tile_part == 0 && g == 0) put_ml(row_part * 16 * R + 16 * r + n, M, L);
-            }
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int c0 = 0; c0 < DP; c0 += A::CB) {
-                    lds_barrier();  // what was read of so (and of sm and sl) has been read
-                    if (r == 0 && c0 == 0 && tile_part == 0 && g == 0) {
-                        // every row's sum, for the threads that divide by it
-#pragma unroll
-                        for (int rr = 0; rr < R; ++rr) sl[row_part][16 * rr + n] = w.l[rr];
-                    }
-#pragma unroll
-                    for (int j = c0 / 16; j < (c0 + A::CB) / 16; ++j) *(f32x4*)&so[wid][n][16 * j - c0 + 4 * g] = w.o[r][j];
-                    lds_barrier();
-                    for (int e = tid; e < p.row_waves * 16 * (A::CB / 4); e += 256) {
-                        const int col = e % (A::CB / 4) * 4, row = e / (A::CB / 4) % 16, part = e / (A::CB / 4) / 16;
-                        f32x4 x = *(const f32x4*)&so[part][row][col];
-                        for (int t = 1; t < tile_waves; ++t) x += *(const f32x4*)&so[t * p.row_waves + part][row][col];
-                        put_o(part * 16 * R + 16 * r + row, c0 + col, x, sl[part][16 * r + row]);
-                    }
-                }
-            lds_barrier();
+            for (int r = 0; r < R; ++r) sml[wid][16 * r + n] = make_float2(w.m[r], w.l[r]);
         }
-        at += tile1 - tile0;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int c0 = 0; c0 < DP; c0 += A::CB) {
+                if (r + c0 > 0) lds_barrier();
+                if (16 * r + n < old.n_rows) {
+#pragma unroll
+                    for (int j = 0; j < A::CB / 16; ++j) *(f32x4*)&so[wid][n][16 * j + 4 * u] = w.o[r][c0 / 16 + j];
+                }
+                lds_barrier();
+                const int rows = old.n_rows - 16 * r < 16 ? old.n_rows - 16 * r : 16;
+                for (int e = tid; e < rows * (A::CB / 4); e += 256) {
+                    const int col = e % (A::CB / 4) * 4, row = e / (A::CB / 4);
+                    float2 ml[4];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) ml[t] = sml[t][16 * r + row];
+                    const float M = fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x));
+                    const float base = M == -__builtin_inff() ? 0.0f : M;
+                    float L = 0.0f;
+                    f32x4 x{0, 0, 0, 0};
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        const float f = __builtin_amdgcn_exp2f(ml[t].x - base);
+                        L += ml[t].y * f;
+                        x += *(const f32x4*)&so[t][row][col] * f;
+                    }
+                    put(16 * r + row, c0 + col, x, M, L);
+                }
+            }
     }
+    if (tid == 0) p.split[worker] = split;
 }
 
 template <int DP>
-hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, int R, hipStream_t s) {
-    const dim3 grid((unsigned)p.workgroups), block(256);
+hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
+    const dim3 grid((unsigned)p.workers), block(256);
     auto go = [&](auto ct) {
         constexpr int CT = decltype(ct)::value;
         if (a.dtype == 0) k_attend<DP, CT, 1, true><<<grid, block, 0, s>>>(a, p);
-        else if (R == 1) k_attend<DP, CT, 1, false><<<grid, block, 0, s>>>(a, p);
-        if constexpr (DP <= 192)
-            if (R == 2 && a.dtype != 0) k_attend<DP, CT, 2, false><<<grid, block, 0, s>>>(a, p);
-        if constexpr (DP <= 96)
-            if (R == 4 && a.dtype != 0) k_attend<DP, CT, 4, false><<<grid, block, 0, s>>>(a, p);
+        else if (p.group_shift == 4) k_attend<DP, CT, 1, false><<<grid, block, 0, s>>>(a, p);
+        else if constexpr (DP <= 192) k_attend<DP, CT, 2, false><<<grid, block, 0, s>>>(a, p);
     };
     if (a.pool.type == kKvBf16) go(std::integral_constant<int, kKvBf16>{});
     else if (a.pool.type == kKvFp8) go(std::integral_constant<int, kKvFp8>{});
@@ -577,10 +614,10 @@ hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, int R, hipStr
     return hipGetLastError();
 }
 
-extern template hipError_t launch_attend<64>(const AttendArgs&, const AttendPlan&, int, hipStream_t);
-extern template hipError_t launch_attend<96>(const AttendArgs&, const AttendPlan&, int, hipStream_t);
-extern template hipError_t launch_attend<128>(const AttendArgs&, const AttendPlan&, int, hipStream_t);
-extern template hipError_t launch_attend<192>(const AttendArgs&, const AttendPlan&, int, hipStream_t);
-extern template hipError_t launch_attend<256>(const AttendArgs&, const AttendPlan&, int, hipStream_t);
+extern template hipError_t launch_attend<64>(const AttendArgs&, const AttendPlan&, hipStream_t);
+extern template hipError_t launch_attend<96>(const AttendArgs&, const AttendPlan&, hipStream_t);
+extern template hipError_t launch_attend<128>(const AttendArgs&, const AttendPlan&, hipStream_t);
+extern template hipError_t launch_attend<192>(const AttendArgs&, const AttendPlan&, hipStream_t);
+extern template hipError_t launch_attend<256>(const AttendArgs&, const AttendPlan&, hipStream_t);
 
 }  // namespace lacache

@@ -4,121 +4,122 @@
 
 namespace lacache {
 
-// A workgroup per row (of a sequence and kv head): a thread four columns of every 1024 / dp-th part.
-__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, AttendPlan p) {
-    __shared__ float sm[256], sl[256];
-    __shared__ f32x4 so[256];
-    const int tid = threadIdx.x, b = blockIdx.x, h = blockIdx.y;
-    const int64_t per = p.base[a.seqs.n_seq + 1];
-    const AttendSpan s = attend_span(a, p, b);
-    const int dp = a.pool.dp, lanes = dp / 4, groups = 256 / lanes;
-    const int col = tid % lanes * 4, part0 = tid / lanes;
-    for (int row = blockIdx.z; row < s.rows; row += gridDim.z) {
-        const int rg = row / p.group_rows, in_group = row - rg * p.group_rows;
-        const int64_t lo = p.base[b] + (int64_t)(h * s.groups + rg) * s.tiles, hi = lo + s.tiles;
-        const int64_t w0 = lo / per, w1 = (hi - 1) / per;
-        if (w0 == w1) continue;
-        // a workgroup's part of a row group that goes on after it lies in its second slot
-        auto slot = [&](int64_t w) { return 2 * w + (w < w1 ? 1 : 0); };
+// The row groups that several workers had parts of: a workgroup a row of the group that ended with worker blockIdx.x,
+// a thread four columns of every (4 THREADS / dp)-th part, four of them loaded together.
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void k_attend_join(AttendArgs a, AttendPlan p) {
+    __shared__ float2 sml[THREADS];
+    __shared__ f32x4 so[THREADS];
+    const AttendSplit s = p.split[blockIdx.x];
+    const int tid = threadIdx.x, dp = a.pool.dp, lanes = dp / 4, groups = THREADS / lanes;
+    const int col = tid % lanes * 4, part = tid / lanes;
+    const int parts = (int)blockIdx.x - s.worker0 + 1;
+    for (int row = blockIdx.y; row < s.n_rows; row += gridDim.y) {
         float m = -__builtin_inff(), l = 0.0f;
         f32x4 o{0, 0, 0, 0};
-        if (part0 < groups)
-            for (int64_t w = w0 + part0; w <= w1; w += groups) {
-                const int64_t at = slot(w) * p.group_rows + in_group;
-                const float2 ml = p.part_ml[at];
-                const f32x4 x = *(const f32x4*)(p.part_o + at * dp + col);
-                const float M = fmaxf(m, ml.x);
-                if (M == -__builtin_inff()) continue;
-                const float f = __builtin_amdgcn_exp2f(m - M), g = __builtin_amdgcn_exp2f(ml.x - M);
-                l = l * f + ml.y * g;
-                o = o * f + x * g;
-                m = M;
+        if (part < groups)
+            for (int k0 = part; k0 < parts; k0 += 4 * groups) {
+                float2 ml[4];
+                f32x4 x[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    // a worker's part of a row group that goes on after it lies in its second slot
+                    const int k = k0 + u * groups < parts ? k0 + u * groups : parts - 1;
+                    const int64_t at = (((2 * (int64_t)(s.worker0 + k)) + (k < parts - 1 ? 1 : 0)) << p.group_shift) + row;
+                    ml[u] = p.part_ml[at];
+                    x[u] = *(const f32x4*)(p.part_o + at * dp + col);
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    if (k0 + u * groups >= parts || ml[u].x == -__builtin_inff()) continue;
+                    const float M = fmaxf(m, ml[u].x);
+                    const float f = __builtin_amdgcn_exp2f(m - M), g = __builtin_amdgcn_exp2f(ml[u].x - M);
+                    l = l * f + ml[u].y * g;
+                    o = o * f + x[u] * g;
+                    m = M;
+                }
             }
         __syncthreads();
-        sm[tid] = m;
-        sl[tid] = l;
+        sml[tid] = make_float2(m, l);
         so[tid] = o;
         __syncthreads();
-        if (part0 == 0) {
+        const int live = groups < parts ? groups : parts;
+        if (part == 0) {
             float M = -__builtin_inff();
-            for (int k = 0; k < groups; ++k) M = fmaxf(M, sm[k * lanes + tid]);
+            for (int k = 0; k < live; ++k) M = fmaxf(M, sml[k * lanes + tid].x);
             const float base = M == -__builtin_inff() ? 0.0f : M;
             float L = 0.0f;
             f32x4 O{0, 0, 0, 0};
-            for (int k = 0; k < groups; ++k) {
-                const float f = __builtin_amdgcn_exp2f(sm[k * lanes + tid] - base);
-                L += sl[k * lanes + tid] * f;
+            for (int k = 0; k < live; ++k) {
+                const float f = __builtin_amdgcn_exp2f(sml[k * lanes + tid].x - base);
+                L += sml[k * lanes + tid].y * f;
                 O += so[k * lanes + tid] * f;
             }
-            const int i = row / a.group, head = h * a.group + (row - i * a.group);
+            const int r = s.row + row, i = token_of(p, r);
+            const int64_t at = ((int64_t)s.seq_row0 + i) * a.q_heads + s.head0 + (r - i * a.group);
             O *= L == 0.0f ? 0.0f : 1.0f / L;
             if (col < a.pool.d) {
-                if (a.dtype == 0) store4<true>(a, s.span.row0 + i, head, col, O);
-                else store4<false>(a, s.span.row0 + i, head, col, O);
+                if (a.dtype == 0) store4<true>(a, at * a.pool.d + col, O);
+                else store4<false>(a, at * a.pool.d + col, O);
             }
-            if (tid == 0 && a.lse) a.lse[(s.span.row0 + i) * a.q_heads + head] = lse_of(M, L);
+            if (tid == 0 && a.lse) a.lse[at] = lse_of(M, L);
         }
     }
 }
 
 namespace {
 
-// Row tiles of 16 a wave and waves that share a row group's rows, by the most rows of a (sequence, kv head).
-struct Shape {
-    int R, row_waves;
-};
-Shape shape_of(int dp, bool f32, int64_t rows) {
-    const int most = f32 ? 1 : dp <= 96 ? 4 : dp <= 192 ? 2 : 1;
-    int R = 1, waves = 1;
-    while (R < most && 16 * R < rows) R *= 2;
-    while (waves < 4 && 16 * R * waves < rows) waves *= 2;
-    return {R, waves};
-}
-
-int64_t round16(int64_t x) { return (x + 15) & ~int64_t(15); }
+// Row tiles of 16 of a row group, by the most rows of a (sequence, kv head).
+int tiles_of(int dp, bool f32, int64_t rows) { return f32 || rows <= 16 || dp > 192 ? 1 : 2; }
 
 // The plan of a launch whose workspace begins at `space`, and the bytes it takes.
-AttendPlan plan_of(const KvPool& pool, bool f32, int n_seq, int64_t rows, int num_cu, char* space, int64_t* bytes) {
-    const Shape sh = shape_of(pool.dp, f32, rows);
+AttendPlan plan_of(const KvPool& pool, bool f32, int n_seq, int max_new, int group, int num_cu, char* space,
+                   int64_t* bytes) {
     AttendPlan p{};
-    p.row_waves = sh.row_waves;
-    p.group_rows = 16 * sh.R * sh.row_waves;
-    p.workgroups = num_cu * attend_occupancy(pool.dp, pool.type != kKvBf16, sh.R, f32);
-    const int64_t base = round16(8 * ((int64_t)n_seq + 2)), slots = 2 * (int64_t)p.workgroups * p.group_rows;
-    p.base = (int64_t*)space;
-    p.part_ml = (float2*)(space + base);
-    p.part_o = (float*)(space + base + 8 * slots);
-    *bytes = base + 8 * slots + 4 * slots * pool.dp;
+    // (the rows of a (sequence, kv head), if no bound is known: plenty)
+    const int R = tiles_of(pool.dp, f32, (int64_t)(max_new > 0 ? max_new : 64) * group);
+    p.group_shift = R == 1 ? 4 : 5;
+    p.workers = num_cu * attend_occupancy(pool.dp, pool.type != kKvBf16, R, f32);
+    const int64_t split = (int64_t)sizeof(AttendSplit) * p.workers, slots = (2 * (int64_t)p.workers) << p.group_shift;
+    p.split = (AttendSplit*)space;
+    p.part_ml = (float2*)(space + split);
+    p.part_o = (float*)(space + split + 8 * slots);
+    *bytes = split + 8 * slots + 4 * slots * pool.dp;
     return p;
 }
 
 }  // namespace
 
-// The rows of a (sequence, kv head) if no bound is known: plenty.
-static int64_t most_rows(int max_new, int group) { return (int64_t)(max_new > 0 ? max_new : 64) * group; }
-
 int64_t attend_workspace(const KvPool& pool, int dtype, int n_seq, int q_heads, int max_new, int num_cu) {
     int64_t bytes;
-    plan_of(pool, dtype == 0, n_seq, most_rows(max_new, q_heads / pool.heads), num_cu, nullptr, &bytes);
+    plan_of(pool, dtype == 0, n_seq, max_new, q_heads / pool.heads, num_cu, nullptr, &bytes);
     return bytes;
 }
 
 hipError_t launch_kv_attend(const AttendArgs& a, int max_new, void* workspace, int num_cu, hipStream_t s) {
     if (a.seqs.rows <= 0 || a.seqs.n_seq <= 0) return hipSuccess;
-    const bool f32 = a.dtype == 0;
-    const int64_t rows = most_rows(max_new, a.group);
     int64_t bytes;
-    const AttendPlan p = plan_of(a.pool, f32, a.seqs.n_seq, rows, num_cu, (char*)workspace, &bytes);
-    const int R = shape_of(a.pool.dp, f32, rows).R;
-    const hipError_t e = a.pool.dp == 64    ? launch_attend<64>(a, p, R, s)
-                         : a.pool.dp == 96  ? launch_attend<96>(a, p, R, s)
-                         : a.pool.dp == 128 ? launch_attend<128>(a, p, R, s)
-                         : a.pool.dp == 192 ? launch_attend<192>(a, p, R, s)
-                                            : launch_attend<256>(a, p, R, s);
+    AttendPlan p = plan_of(a.pool, a.dtype == 0, a.seqs.n_seq, max_new, a.group, num_cu, (char*)workspace, &bytes);
+    // row / group for rows below 2^31: magic = ceil(2^(31 + bits) / group), bits = ceil(log2 group)
+    int bits = 0;
+    while ((1 << bits) < a.group) ++bits;
+    p.group_bits = 31 + bits;
+    p.group_magic = (uint32_t)((((uint64_t)1 << p.group_bits) + a.group - 1) / a.group);
+    // the chunks of all row groups are counted in 32 bits
+    const int64_t tiles = ((int64_t)a.seqs.max_pages << (a.pool.page_shift - 5)) + 1;
+    const int64_t groups = ((a.seqs.rows * a.group) >> p.group_shift) + a.seqs.n_seq;
+    while (groups * a.pool.heads * (((tiles - 1) >> p.chunk_shift) + 1) > INT32_MAX / 2 && p.chunk_shift < 30)
+        ++p.chunk_shift;
+    const hipError_t e = a.pool.dp == 64    ? launch_attend<64>(a, p, s)
+                         : a.pool.dp == 96  ? launch_attend<96>(a, p, s)
+                         : a.pool.dp == 128 ? launch_attend<128>(a, p, s)
+                         : a.pool.dp == 192 ? launch_attend<192>(a, p, s)
+                                            : launch_attend<256>(a, p, s);
     if (e != hipSuccess) return e;
-    const int64_t join_rows = rows < a.seqs.rows * a.group ? rows : a.seqs.rows * a.group;
-    k_attend_join<<<dim3((unsigned)a.seqs.n_seq, (unsigned)a.pool.heads, (unsigned)(join_rows < 1024 ? join_rows : 1024)),
-                    dim3(256), 0, s>>>(a, p);
+    const unsigned rows = 1u << p.group_shift;
+    const int64_t most = max_new > 0 && (int64_t)max_new * a.group < rows ? (int64_t)max_new * a.group : rows;
+    if (a.seqs.n_seq * (int64_t)a.pool.heads < 64) k_attend_join<512><<<dim3((unsigned)p.workers, (unsigned)most), dim3(512), 0, s>>>(a, p);
+    else k_attend_join<256><<<dim3((unsigned)p.workers, (unsigned)most), dim3(256), 0, s>>>(a, p);
     return hipGetLastError();
 }
 

@@ -2,5 +2,5 @@
 #include "attend.hpp"
 
 namespace lacache {
-template hipError_t launch_attend<96>(const AttendArgs&, const AttendPlan&, int, hipStream_t);
+template hipError_t launch_attend<96>(const AttendArgs&, const AttendPlan&, hipStream_t);
 }  // namespace lacache
