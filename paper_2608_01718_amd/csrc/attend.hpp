@@ -34,7 +34,7 @@ constexpr int attend_occupancy(int dp, bool bytes, int R, bool f32) {
 // What a launch works with besides the arguments: the shape of a row group, its workers, the workspace.
 struct AttendPlan {
     int group_shift;   // rows of a row group, as a shift
-    int workers;       // workgroups of the launch
+    int workers, waves;  // workgroups of the launch, and the waves of each
     int chunk_shift;   // the work is dealt out in chunks of this many tiles (a shift), so that counts fit in 32 bits
     uint32_t group_magic, group_bits;  // row / group = row * magic >> bits
     struct AttendSplit* split;  // [workers]: the row group whose last part a worker had
@@ -92,26 +92,33 @@ __device__ __forceinline__ int wave_scan(int x) {
 }
 
 // The range of items of this workgroup: the sequence in which it begins, the items before that sequence, the range, and
-// the items of a full range (a multiple of `grain`).  All 256 threads take part, a thread a sequence.
+// the items of a full range (a multiple of `grain`).  All threads take part, a thread a sequence.
 struct AttendRange {
     int b, before, at, end, per;
 };
+template <int WAVES>
 __device__ __forceinline__ AttendRange attend_range(const AttendArgs& a, const AttendPlan& p, int grain) {
-    __shared__ int total_of[4], found[2];
+    constexpr int THREADS = 64 * WAVES;
+    __shared__ int total_of[WAVES], found[2];
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, n_seq = a.seqs.n_seq;
     int own = 0, sum = 0, all = 0, b = tid;
-    // items up to sequence b within a round of 256 (sum), and of the round (returned)
+    // items up to sequence b within a round of THREADS (sum), and of the round (returned)
     auto scan = [&]() {
         own = b < n_seq ? attend_span(a, p, b).items(a) : 0;
         sum = wave_scan(own);
         __syncthreads();
         if (lane == 63) total_of[wid] = sum;
         __syncthreads();
-        const int t0 = total_of[0], t1 = total_of[1], t2 = total_of[2];
-        sum += (wid > 0 ? t0 : 0) + (wid > 1 ? t1 : 0) + (wid > 2 ? t2 : 0);
-        return t0 + t1 + t2 + total_of[3];
+        int round = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const int t = total_of[w];
+            sum += w < wid ? t : 0;
+            round += t;
+        }
+        return round;
     };
-    for (; b - tid < n_seq; b += 256) all += scan();
+    for (; b - tid < n_seq; b += THREADS) all += scan();
     all = __builtin_amdgcn_readfirstlane(all);
     AttendRange r;
     r.per = (int)(((uint32_t)all + (uint32_t)p.workers - 1) / (uint32_t)p.workers);
@@ -121,8 +128,8 @@ __device__ __forceinline__ AttendRange attend_range(const AttendArgs& a, const A
     r.end = at + r.per < all ? (int)(at + r.per) : all;
     // the thread whose sequence holds item `at` finds it
     int before = 0;
-    for (b = tid; b - tid < n_seq; b += 256) {
-        const int round = n_seq > 256 ? scan() : all;
+    for (b = tid; b - tid < n_seq; b += THREADS) {
+        const int round = n_seq > THREADS ? scan() : all;
         if (r.at >= before + sum - own && r.at < before + sum) {
             found[0] = b;
             found[1] = before + sum - own;
@@ -141,8 +148,9 @@ __device__ __forceinline__ AttendRange attend_range(const AttendArgs& a, const A
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_rsrc(const void* p, int size) {
     return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, size, 0x00020000);
 }
-__device__ __forceinline__ u32x4 tile_load(__amdgpu_buffer_rsrc_t r, int offset) {
-    return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, offset, 0, 2));
+// (The constant part of an offset fits in the instruction up to 4095 bytes; whole 4 KB go into a scalar register.)
+__device__ __forceinline__ u32x4 tile_load(__amdgpu_buffer_rsrc_t r, int at, int lane_offset) {
+    return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, lane_offset + (at & 4095), at & ~4095, 2));
 }
 
 // four 8-bit codes as bfloat16 pairs
@@ -213,39 +221,38 @@ struct Attend {
     }
 
     // 16 bytes of a row as KC operands: the three terms of a float32 sum back to it exactly, a bfloat16 is its own
+    // Row tile r is rows row0 + step r .. + 15 of the sequence's (its last row in the place of those that it has not).
     __device__ __forceinline__ void load_q(const AttendArgs& a, const AttendPlan& p, const AttendSpan& s, int h, int row0,
-                                           int lane) {
-        const int n = lane & 15, u = lane >> 4;
+                                           int step, int lane) {
+        const int u = lane >> 4;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            int row = row0 + 16 * r + n;
+            int row = row0 + step * r + (lane & 15);
             row = row < s.rows ? row : s.rows - 1;
             const int i = token_of(p, row), head = h * a.group + (row - i * a.group);
             const int64_t pos = s.pos0() + i;
             hi[r] = pos < 0 ? -1 : (int)pos;
             lo[r] = a.window > 0 && hi[r] - a.window + 1 > 0 ? hi[r] - a.window + 1 : 0;
             const char* src = a.q + (((int64_t)s.row0 + i) * a.q_row + (int64_t)head * a.pool.d) * ESZ;
-            const bool wide = ((uintptr_t)src & 15) == 0;
 #pragma unroll
             for (int c = 0; c < KC; ++c) {
                 const int col = 32 * c + 8 * u;
+                const bool in = col < a.pool.d;  // d is a multiple of 8
+                const char* at = src + (in ? col : 0) * ESZ;
                 u32x4 t[NT] = {};
-                if (col < a.pool.d) {
-                    if constexpr (F32) {
-                        float x[8];
-                        load8f(src, 0, a.pool.d, col, x);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) split2<NT>(x[2 * e], x[2 * e + 1], t, e);
-                    } else if (wide) {
-                        t[0] = *(const u32x4*)(src + col * 2);
-                    } else {
-                        const uint16_t* x = (const uint16_t*)src + col;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) t[0][e] = (uint32_t)x[2 * e] | (uint32_t)x[2 * e + 1] << 16;
-                    }
+                if constexpr (F32) {
+                    const f32x4 x = *(const f32x4_any*)at, y = *(const f32x4_any*)(at + 16);
+                    split2<NT>(x[0], x[1], t, 0);
+                    split2<NT>(x[2], x[3], t, 1);
+                    split2<NT>(y[0], y[1], t, 2);
+                    split2<NT>(y[2], y[3], t, 3);
+                } else {
+                    t[0] = *(const u32x4_any*)at;
                 }
 #pragma unroll
-                for (int k = 0; k < NT; ++k) q[r][c][k] = t[k];
+                for (int k = 0; k < NT; ++k)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) q[r][c][k][e] = in ? t[k][e] : 0u;
             }
         }
     }
@@ -264,21 +271,21 @@ struct Attend {
     static __device__ __forceinline__ void load_k(Tile& t, const AttendArgs& a, int64_t place, int there, int lane) {
         const auto r = tile_rsrc(a.pool.k + place * BYTES_TILE, there * BYTES_TILE);
 #pragma unroll
-        for (int i = 0; i < NL; ++i) t.k[i] = tile_load(r, i * 1024 + lane * 16);
+        for (int i = 0; i < NL; ++i) t.k[i] = tile_load(r, i * 1024, lane * 16);
         if constexpr (BYTES) {
             const auto rs = tile_rsrc(a.pool.k_scale + place * 32, there * 128);
 #pragma unroll
-            for (int b = 0; b < 2; ++b) t.ks[b] = __builtin_bit_cast(f32x4, tile_load(rs, 64 * b + (lane >> 4) * 16));
+            for (int b = 0; b < 2; ++b) t.ks[b] = __builtin_bit_cast(f32x4, tile_load(rs, 64 * b, (lane >> 4) * 16));
         }
     }
     static __device__ __forceinline__ void load_v(Tile& t, const AttendArgs& a, int64_t place, int there, int lane) {
         const auto r = tile_rsrc(a.pool.v + place * BYTES_TILE, there * BYTES_TILE);
 #pragma unroll
-        for (int i = 0; i < NL; ++i) t.v[i] = tile_load(r, i * 1024 + lane * 16);
+        for (int i = 0; i < NL; ++i) t.v[i] = tile_load(r, i * 1024, lane * 16);
         if constexpr (BYTES) {
             const auto rs = tile_rsrc(a.pool.v_scale + place * 32, there * 128);
 #pragma unroll
-            for (int b = 0; b < 2; ++b) t.vs[b] = __builtin_bit_cast(f32x4, tile_load(rs, 64 * b + (lane >> 4) * 16));
+            for (int b = 0; b < 2; ++b) t.vs[b] = __builtin_bit_cast(f32x4, tile_load(rs, 64 * b, (lane >> 4) * 16));
         }
     }
 
@@ -353,10 +360,11 @@ struct Attend {
     }
 
     // Weights of the tile (s becomes P), the running maximum and sum.  The sum stays a lane's own until the end.
+    template <int RA = R>
     __device__ __forceinline__ void weigh(f32x4 (&s)[R][2]) {
         auto max2 = [](float x, float y) { return fmaxf(x, y); };
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
+        for (int r = 0; r < RA; ++r) {
             float x = m[r];
 #pragma unroll
             for (int i = 0; i < 4; ++i) x = fmaxf(fmaxf(x, s[r][0][i]), s[r][1][i]);
@@ -379,6 +387,80 @@ struct Attend {
                     l[r] += s[r][b][i];
                 }
         }
+    }
+
+    // f(i, operand i) for COUNT operands in LDS, `at` this lane's 16 bytes of the first: G are read while the last G are
+    // worked with, and no more (the compiler would read them all, and keep sums in scratch memory for it).
+    template <int COUNT, class F>
+    static __device__ __forceinline__ void each_operand(const u32x4* at, F f) {
+        constexpr int G = COUNT % 4 == 0 ? 4 : 3;
+        static_assert(COUNT % G == 0, "whole groups");
+        u32x4 x[2][G];
+#pragma unroll
+        for (int g = 0; g < G; ++g) x[0][g] = at[g * 64];
+#pragma unroll
+        for (int i = 0; i < COUNT; i += G) {
+            if (i + G < COUNT) {
+#pragma unroll
+                for (int g = 0; g < G; ++g) x[(i / G + 1) & 1][g] = at[(i + G + g) * 64];
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int g = 0; g < G; ++g) f(i + g, x[(i / G) & 1][g]);
+        }
+    }
+    template <int RA>
+    __device__ __forceinline__ void scores_lds(const u32x4* k, const f32x4* ks, int u, f32x4 (&s)[R][2], float scale2) {
+#pragma unroll
+        for (int r = 0; r < RA; ++r)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) s[r][b] = f32x4{0, 0, 0, 0};
+        each_operand<2 * KC>(k, [&](int i, u32x4 x) {
+            const int c = i / 2, b = i % 2;
+#pragma unroll
+            for (int r = 0; r < RA; ++r)
+#pragma unroll
+                for (int t = NT - 1; t >= 0; --t) s[r][b] = mfma16x16x32(x, q[r][c][t], s[r][b]);
+        });
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            f32x4 f{scale2, scale2, scale2, scale2};
+            if constexpr (BYTES) f *= ks[4 * b + u];
+#pragma unroll
+            for (int r = 0; r < RA; ++r) s[r][b] *= f;
+        }
+    }
+    template <int RA>
+    __device__ __forceinline__ void hide_scores(int index, f32x4 (&s)[R][2], int lane) {
+        const int t0 = 32 * index + 4 * (lane >> 4);
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int j = t0 + 16 * b + i;
+#pragma unroll
+                for (int r = 0; r < RA; ++r)
+                    s[r][b][i] = j >= lo[r] && j <= hi[r] ? s[r][b][i] : -__builtin_inff();
+            }
+    }
+    template <int RA>
+    __device__ __forceinline__ void gather_lds(const u32x4* v, const f32x4* vs, int u, f32x4 (&s)[R][2]) {
+        u32x4 p[RA][NP];
+#pragma unroll
+        for (int r = 0; r < RA; ++r)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                f32x4 x = s[r][b];
+                if constexpr (BYTES) x *= vs[4 * b + u];
+                split2<NP>(x[0], x[1], p[r], 2 * b);
+                split2<NP>(x[2], x[3], p[r], 2 * b + 1);
+            }
+        each_operand<NJ>(v, [&](int j, u32x4 x) {
+#pragma unroll
+            for (int t = NP - 1; t >= 0; --t)
+#pragma unroll
+                for (int r = 0; r < RA; ++r) o[r][j] = mfma16x16x32(x, p[r][t], o[r][j]);
+        });
     }
 
     // O^T += V^T P^T
@@ -409,15 +491,8 @@ struct Attend {
 // Four columns of the result, from element `at` on.
 template <bool F32>
 __device__ __forceinline__ void store4(const AttendArgs& a, int64_t at, f32x4 x) {
-    if (F32) {
-        float* p = (float*)a.out + at;
-        if (((uintptr_t)p & 15) == 0) *(f32x4*)p = x;
-        else p[0] = x[0], p[1] = x[1], p[2] = x[2], p[3] = x[3];
-    } else {
-        uint16_t* p = (uint16_t*)a.out + at;
-        if (((uintptr_t)p & 7) == 0) *(uint2*)p = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
-        else p[0] = f32_to_bf16(x[0]), p[1] = f32_to_bf16(x[1]), p[2] = f32_to_bf16(x[2]), p[3] = f32_to_bf16(x[3]);
-    }
+    if (F32) *(f32x4_any*)((float*)a.out + at) = x;
+    else *(u32x2_any*)((uint16_t*)a.out + at) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
 }
 
 __device__ __forceinline__ float lse_of(float m, float l) {
@@ -433,7 +508,7 @@ __global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(A
     const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int worker = blockIdx.x;
 
-    AttendRange range = attend_range(a, p, 4 >> (p.chunk_shift < 2 ? p.chunk_shift : 2));
+    AttendRange range = attend_range<4>(a, p, 4 >> (p.chunk_shift < 2 ? p.chunk_shift : 2));
     if (range.at >= range.end) {
         if (tid == 0) p.split[worker].n_rows = 0;
         return;
@@ -464,20 +539,20 @@ __global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(A
         if (t < g.tile1 && 32 * mine <= g.seen1 && 32 * mine + 31 >= g.seen0)
             page = (a.seqs.pages + (int64_t)g.b * a.seqs.max_pages)[mine >> tile_shift];
     };
+    auto look = [&]() { todo = __ballot(page >= 0 && page < a.pool.n_pages); };
     // the wave's next tile, if there is one
     auto next = [&]() {
+        while (!todo && t0 + 256 < g.tile1) {
+            t0 += 256;
+            load_pages();
+            look();
+        }
         there = todo ? 1 : 0;
         const int k = there ? __ffsll((unsigned long long)todo) - 1 : 0;
         todo &= todo - 1;
         tile.index = g.first + t0 + k * 4;
         const int64_t pg = there ? __builtin_amdgcn_readlane(page, k) : 0;
         return ((pg * a.pool.heads + g.h) << tile_shift) + (tile.index & ((1 << tile_shift) - 1));
-    };
-    auto load_tiles = [&]() {
-        todo = __ballot(page >= 0 && page < a.pool.n_pages);
-        const int64_t pl = next();
-        A::load_k(tile, a, pl, there, lane);
-        A::load_v(tile, a, pl, there, lane);
     };
     // the segment that begins at item `at`, its queries and its first tiles
     auto open = [&]() {
@@ -503,29 +578,28 @@ __global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(A
         g.all1 = q0 < g.seen1 ? q0 : g.seen1;
         t0 = g.tile0 + wid;
         load_pages();
-        w.load_q(a, p, s, g.h, r0, lane);  // while the page numbers are on their way
-        load_tiles();
+        w.load_q(a, p, s, g.h, r0, 16, lane);  // while the page numbers are on their way
+        __builtin_amdgcn_sched_barrier(0);
+        look();
+        const int64_t pl = next();
+        A::load_k(tile, a, pl, there, lane);
+        A::load_v(tile, a, pl, there, lane);
+        __builtin_amdgcn_sched_barrier(0);
     };
     open();
     bool more = true;
     while (more) {
         w.clear();
-        while (true) {
-            while (there) {
-                f32x4 sc[R][2];
-                w.scores(tile, sc, scale2);
-                const int index = tile.index;
-                const int64_t pl = next();  // its keys are loaded under this tile's weights, its values under its scores
-                A::load_k(tile, a, pl, there, lane);
-                if (32 * index < g.all0 || 32 * index + 31 > g.all1) w.hide(tile, index, sc, g.seen0, g.seen1, lane);
-                w.weigh(sc);
-                w.gather(tile, sc);
-                A::load_v(tile, a, pl, there, lane);
-            }
-            t0 += 64 * 4;
-            if (t0 >= g.tile1) break;
-            load_pages();
-            load_tiles();
+        while (there) {
+            f32x4 sc[R][2];
+            w.scores(tile, sc, scale2);
+            const int index = tile.index;
+            const int64_t pl = next();  // its keys are loaded under this tile's weights, its values under its scores
+            A::load_k(tile, a, pl, there, lane);
+            if (32 * index < g.all0 || 32 * index + 31 > g.all1) w.hide(tile, index, sc, g.seen0, g.seen1, lane);
+            w.weigh(sc);
+            w.gather(tile, sc);
+            A::load_v(tile, a, pl, there, lane);
         }
 
         // The next segment's loads are on their way while this one's results are joined and stored.
@@ -598,26 +672,5 @@ __global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(A
     }
     if (tid == 0) p.split[worker] = split;
 }
-
-template <int DP>
-hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
-    const dim3 grid((unsigned)p.workers), block(256);
-    auto go = [&](auto ct) {
-        constexpr int CT = decltype(ct)::value;
-        if (a.dtype == 0) k_attend<DP, CT, 1, true><<<grid, block, 0, s>>>(a, p);
-        else if (p.group_shift == 4) k_attend<DP, CT, 1, false><<<grid, block, 0, s>>>(a, p);
-        else if constexpr (DP <= 192) k_attend<DP, CT, 2, false><<<grid, block, 0, s>>>(a, p);
-    };
-    if (a.pool.type == kKvBf16) go(std::integral_constant<int, kKvBf16>{});
-    else if (a.pool.type == kKvFp8) go(std::integral_constant<int, kKvFp8>{});
-    else go(std::integral_constant<int, kKvInt8>{});
-    return hipGetLastError();
-}
-
-extern template hipError_t launch_attend<64>(const AttendArgs&, const AttendPlan&, hipStream_t);
-extern template hipError_t launch_attend<96>(const AttendArgs&, const AttendPlan&, hipStream_t);
-extern template hipError_t launch_attend<128>(const AttendArgs&, const AttendPlan&, hipStream_t);
-extern template hipError_t launch_attend<192>(const AttendArgs&, const AttendPlan&, hipStream_t);
-extern template hipError_t launch_attend<256>(const AttendArgs&, const AttendPlan&, hipStream_t);
 
 }  // namespace lacache

@@ -1,6 +1,6 @@
 // k_attend.hip -- attention over the paged cache: the launches' shape, and the join of row groups that several
 // workgroups had tiles of.
-#include "attend.hpp"
+#include "attend_wide.hpp"
 
 namespace lacache {
 
@@ -69,17 +69,30 @@ __global__ __launch_bounds__(THREADS) void k_attend_join(AttendArgs a, AttendPla
 
 namespace {
 
-// Row tiles of 16 of a row group, by the most rows of a (sequence, kv head).
-int tiles_of(int dp, bool f32, int64_t rows) { return f32 || rows <= 16 || dp > 192 ? 1 : 2; }
+// The rows of a row group (as a shift) and the waves of a workgroup, by the most rows of a (sequence, kv head).
+struct Shape {
+    int group_shift, waves, occupancy;
+};
+Shape shape_of(const KvPool& pool, bool f32, int64_t rows) {
+    const bool bytes = pool.type != kKvBf16;
+    if (rows <= 16 || (f32 && pool.dp > 192)) return {4, 4, attend_occupancy(pool.dp, bytes, 1, f32)};
+    if (f32) return {6, 4, wide_occupancy(pool.dp, 4, 1, true)};
+    if (rows <= 32 && pool.dp <= 128) return {5, 4, attend_occupancy(pool.dp, bytes, 2, false)};
+    if (rows <= 64 && pool.dp <= 192) return {6, 4, wide_occupancy(pool.dp, 4, 1, false)};
+    if (pool.dp > 128) return {7, 8, wide_occupancy(pool.dp, 8, 1, false)};
+    if (rows <= 128) return {7, 4, wide_occupancy(pool.dp, 4, 2, false)};
+    return {8, 8, wide_occupancy(pool.dp, 8, 2, false)};
+}
 
 // The plan of a launch whose workspace begins at `space`, and the bytes it takes.
 AttendPlan plan_of(const KvPool& pool, bool f32, int n_seq, int max_new, int group, int num_cu, char* space,
                    int64_t* bytes) {
     AttendPlan p{};
     // (the rows of a (sequence, kv head), if no bound is known: plenty)
-    const int R = tiles_of(pool.dp, f32, (int64_t)(max_new > 0 ? max_new : 64) * group);
-    p.group_shift = R == 1 ? 4 : 5;
-    p.workers = num_cu * attend_occupancy(pool.dp, pool.type != kKvBf16, R, f32);
+    const Shape sh = shape_of(pool, f32, (int64_t)(max_new > 0 ? max_new : 64) * group);
+    p.group_shift = sh.group_shift;
+    p.waves = sh.waves;
+    p.workers = num_cu * sh.occupancy;
     const int64_t split = (int64_t)sizeof(AttendSplit) * p.workers, slots = (2 * (int64_t)p.workers) << p.group_shift;
     p.split = (AttendSplit*)space;
     p.part_ml = (float2*)(space + split);
@@ -117,7 +130,8 @@ hipError_t launch_kv_attend(const AttendArgs& a, int max_new, void* workspace, i
                                             : launch_attend<256>(a, p, s);
     if (e != hipSuccess) return e;
     const unsigned rows = 1u << p.group_shift;
-    const int64_t most = max_new > 0 && (int64_t)max_new * a.group < rows ? (int64_t)max_new * a.group : rows;
+    int64_t most = max_new > 0 && (int64_t)max_new * a.group < rows ? (int64_t)max_new * a.group : rows;
+    most = most < 32 ? most : 32;
     if (a.seqs.n_seq * (int64_t)a.pool.heads < 64) k_attend_join<512><<<dim3((unsigned)p.workers, (unsigned)most), dim3(512), 0, s>>>(a, p);
     else k_attend_join<256><<<dim3((unsigned)p.workers, (unsigned)most), dim3(256), 0, s>>>(a, p);
     return hipGetLastError();
