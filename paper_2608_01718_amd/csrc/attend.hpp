@@ -22,6 +22,10 @@ namespace lacache {
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 
+// A running maximum is raised only when a score passes it by more than this (in units of log2 e): weights then reach
+// 2^8 times the largest, which costs sums in float32 nothing, and the sums are rarely scaled.
+constexpr float kSlack = 8.0f;
+
 // Workgroups on a compute unit, by the registers of a lane: the sums, the queries, a tile's keys and values, the scores
 // and weights, and what goes around them.  (A wave of four has a SIMD's 512 registers to itself.)
 constexpr int attend_occupancy(int dp, bool bytes, int R, bool f32) {
@@ -178,7 +182,15 @@ __device__ __forceinline__ u32x4 widen8(uint32_t lo, uint32_t hi) {
 }
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-    return (uint32_t)f32_to_bf16(a) | (uint32_t)f32_to_bf16(b) << 16;
+    bf16x2 w;  // (converted as a pair: one instruction)
+    w[0] = (__bf16)a;
+    w[1] = (__bf16)b;
+    return __builtin_bit_cast(uint32_t, w);
+}
+
+// The scale of the scores in units of log2 e, always above 0 (its sign and its being 0 are in the queries: load_q).
+__device__ __forceinline__ float scale_of(const AttendArgs& a) {
+    return a.scale == 0.0f ? 1.0f : fabsf(a.scale) * kLog2e;
 }
 
 template <int DP, int CT, int R, bool F32>
@@ -252,7 +264,8 @@ struct Attend {
 #pragma unroll
                 for (int k = 0; k < NT; ++k)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) q[r][c][k][e] = in ? t[k][e] : 0u;
+                    for (int e = 0; e < 4; ++e)  // a negative scale's sign, and a scale of 0, go into the queries
+                        q[r][c][k][e] = in && a.scale != 0.0f ? t[k][e] ^ (a.scale < 0.0f ? 0x80008000u : 0u) : 0u;
             }
         }
     }
@@ -298,7 +311,7 @@ struct Attend {
         else return widen8<CT>(t.v[j >> 1][2 * (j & 1)], t.v[j >> 1][2 * (j & 1) + 1]);
     }
 
-    // scores of a tile, in units of log2 e
+    // scores of a tile: with 8-bit keys in units of log2 e, with bfloat16 ones before their scaling
     __device__ __forceinline__ void scores(const Tile& t_, f32x4 (&s)[R][2], float scale2) {
 #pragma unroll
         for (int r = 0; r < R; ++r)
@@ -314,14 +327,14 @@ struct Attend {
 #pragma unroll
                     for (int t = NT - 1; t >= 0; --t) s[r][b] = mfma16x16x32(k, q[r][c][t], s[r][b]);
             }
+        if constexpr (BYTES) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+            for (int b = 0; b < 2; ++b) {
+                const f32x4 f = t_.ks[b] * scale2;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float f = BYTES ? t_.ks[b][i] * scale2 : scale2;
-#pragma unroll
-                for (int r = 0; r < R; ++r) s[r][b][i] *= f;
+                for (int r = 0; r < R; ++r) s[r][b] *= f;
             }
+        }
     }
 
     // Hides the positions that a row does not see, and the values of those that no row of the wave sees (first .. last
@@ -359,31 +372,41 @@ struct Attend {
         }
     }
 
-    // Weights of the tile (s becomes P), the running maximum and sum.  The sum stays a lane's own until the end.
+    // Weights of the tile (s becomes P), the running maximum and sum.  The sum stays a lane's own until the end.  Scores
+    // are in units of log2 e times 1 / scale2 (8-bit keys: scaled already).
     template <int RA = R>
-    __device__ __forceinline__ void weigh(f32x4 (&s)[R][2]) {
+    __device__ __forceinline__ void weigh(f32x4 (&s)[R][2], float scale2) {
         auto max2 = [](float x, float y) { return fmaxf(x, y); };
+        const float c = BYTES ? 1.0f : scale2;
+        float x[RA];
+        bool raise = false;
 #pragma unroll
         for (int r = 0; r < RA; ++r) {
-            float x = m[r];
+            float y = fmaxf(s[r][0][0], s[r][1][0]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x = fmaxf(fmaxf(x, s[r][0][i]), s[r][1][i]);
-            x = xor_combine<16>(xor_combine<32>(x, max2), max2);
-            if (__any(x > m[r])) {
-                const float f = x > m[r] ? __builtin_amdgcn_exp2f(m[r] - x) : 1.0f;  // 0 where m was -infinity
+            for (int i = 1; i < 4; ++i) y = fmaxf(fmaxf(y, s[r][0][i]), s[r][1][i]);
+            x[r] = c * xor_combine<16>(xor_combine<32>(y, max2), max2);
+            raise |= x[r] > m[r] + kSlack;  // (from -infinity too)
+        }
+        if (__any(raise)) {
+#pragma unroll
+            for (int r = 0; r < RA; ++r) {
+                const float to = fmaxf(x[r], m[r]);
+                const float f = to > m[r] ? __builtin_amdgcn_exp2f(m[r] - to) : 1.0f;  // 0 where m was -infinity
                 l[r] *= f;
 #pragma unroll
-                for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) o[r][j][i] *= f;
-                m[r] = x;
+                for (int j = 0; j < NJ; ++j) o[r][j] *= f;
+                m[r] = to;
             }
+        }
+#pragma unroll
+        for (int r = 0; r < RA; ++r) {
             const float base = m[r] == -__builtin_inff() ? 0.0f : m[r];
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    s[r][b][i] = __builtin_amdgcn_exp2f(s[r][b][i] - base);
+                    s[r][b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][b][i], c, -base));
                     l[r] += s[r][b][i];
                 }
         }
@@ -409,6 +432,8 @@ struct Attend {
             for (int g = 0; g < G; ++g) f(i + g, x[(i / G) & 1][g]);
         }
     }
+    // scores, hide and gather for the first RA row tiles with a tile of operands in LDS (attend_wide.hpp): `k` and `v` this
+    // lane's 16 bytes of the first, `ks` and `vs` the scales of the tile's 32 tokens.
     template <int RA>
     __device__ __forceinline__ void scores_lds(const u32x4* k, const f32x4* ks, int u, f32x4 (&s)[R][2], float scale2) {
 #pragma unroll
@@ -422,12 +447,13 @@ struct Attend {
 #pragma unroll
                 for (int t = NT - 1; t >= 0; --t) s[r][b] = mfma16x16x32(x, q[r][c][t], s[r][b]);
         });
+        if constexpr (BYTES) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            f32x4 f{scale2, scale2, scale2, scale2};
-            if constexpr (BYTES) f *= ks[4 * b + u];
+            for (int b = 0; b < 2; ++b) {
+                const f32x4 f = ks[4 * b + u] * scale2;
 #pragma unroll
-            for (int r = 0; r < RA; ++r) s[r][b] *= f;
+                for (int r = 0; r < RA; ++r) s[r][b] *= f;
+            }
         }
     }
     template <int RA>
@@ -444,8 +470,7 @@ struct Attend {
             }
     }
     template <int RA>
-    __device__ __forceinline__ void gather_lds(const u32x4* v, const f32x4* vs, int u, f32x4 (&s)[R][2]) {
-        u32x4 p[RA][NP];
+    __device__ __forceinline__ void round_lds(const f32x4 (&s)[R][2], const f32x4* vs, int u, u32x4 (&p)[R][NP]) {
 #pragma unroll
         for (int r = 0; r < RA; ++r)
 #pragma unroll
@@ -455,6 +480,9 @@ struct Attend {
                 split2<NP>(x[0], x[1], p[r], 2 * b);
                 split2<NP>(x[2], x[3], p[r], 2 * b + 1);
             }
+    }
+    template <int RA>
+    __device__ __forceinline__ void gather_lds(const u32x4* v, const u32x4 (&p)[R][NP]) {
         each_operand<NJ>(v, [&](int j, u32x4 x) {
 #pragma unroll
             for (int t = NP - 1; t >= 0; --t)
@@ -514,7 +542,7 @@ __global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(A
         return;
     }
     AttendSplit split{};
-    const float scale2 = a.scale * kLog2e;
+    const float scale2 = scale_of(a);
     const int tile_shift = a.pool.page_shift - 5;
 
     // A segment: tiles tile0 .. tile1 - 1 of one row group
@@ -597,7 +625,7 @@ __global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(A
             const int64_t pl = next();  // its keys are loaded under this tile's weights, its values under its scores
             A::load_k(tile, a, pl, there, lane);
             if (32 * index < g.all0 || 32 * index + 31 > g.all1) w.hide(tile, index, sc, g.seen0, g.seen1, lane);
-            w.weigh(sc);
+            w.weigh(sc, scale2);
             w.gather(tile, sc);
             A::load_v(tile, a, pl, there, lane);
         }

@@ -3,9 +3,11 @@
 //
 // The mathematics and the division of the work are those of attend.hpp.  With many rows the matrix cores and the softmax
 // bound the time, not memory, and each tile is used by all of a workgroup's waves: it goes through registers into LDS
-// (two buffers, as bfloat16 whatever the cache's type), in the order of memory, which is that of the operands; each wave
-// reads every operand once for its R row tiles.  Row tiles are dealt out to the waves in turn, so that a group that is
-// not full leaves every SIMD about as much to do.
+// (as bfloat16 whatever the cache's type), in the order of memory, which is that of the operands; each wave reads every
+// operand once for its R row tiles.  Row tiles are dealt out to the waves in turn, so that a group that is not full leaves
+// every SIMD about as much to do.  One barrier a tile would keep eight waves in step, all of them at the matrix cores and
+// then all at the softmax; so the second wave of each SIMD multiplies a tile's weights and values only in the next step,
+// while the first computes that step's scores, and values stay for three steps.
 #pragma once
 
 #include "attend.hpp"
@@ -21,7 +23,8 @@ struct Wide {
     static constexpr int BYTES_TILE = 32 * DP * (BYTES ? 1 : 2);
     static constexpr int LOADS = 2 * BYTES_TILE / 1024;           // 16-byte loads a lane of keys and values, all waves
     static constexpr int PER_WAVE = (LOADS + WAVES - 1) / WAVES;
-    static constexpr int OPERANDS = 4 * KC;                       // 1 KB operands of a tile in LDS: keys, then values
+    static constexpr bool STAGGER = WAVES == 8;                   // the upper four waves are half a step behind
+    static constexpr int VBUF = STAGGER ? 3 : 2;                  // tiles of values in LDS
     // waves on a SIMD: two where the registers of the sums and queries leave room
     static constexpr int OCC = R * DP * (F32 ? 2 : 1) <= 256 ? 2 : 1;
 };
@@ -31,7 +34,7 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
                                                                                               AttendPlan p) {
     using W = Wide<DP, CT, WAVES, R, F32>;
     using A = Attend<DP, CT, R, F32>;
-    __shared__ u32x4 lds[2][W::OPERANDS * 64];
+    __shared__ u32x4 keys[2][2 * W::KC * 64], vals[W::VBUF][W::NJ * 64];  // operands of 1 KB each
     __shared__ f32x4 scales[2][16];  // 32 of the keys, 32 of the values
     const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int worker = blockIdx.x, n = lane & 15, u = lane >> 4;
@@ -42,7 +45,7 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
         return;
     }
     AttendSplit split{};
-    float scale2 = a.scale * kLog2e;
+    const float scale2 = scale_of(a);
     const int tile_shift = a.pool.page_shift - 5;
     AttendSpan s = attend_span(a, p, range.b);
     u32x4 stage[W::PER_WAVE];
@@ -105,8 +108,8 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
                 if (wid == 0) stage_scale = (lane < 32 ? a.pool.k_scale : a.pool.v_scale)[place * 32 + (lane & 31)];
             return index;
         };
-        // The loaded tile into buffer b; values that no row sees as zeros.
-        auto put_tile = [&](int b, int index) {
+        // The loaded tile into buffers b (keys, scales) and bv; values that no row sees as zeros.
+        auto put_tile = [&](int b, int bv, int index) {
             const bool edge = 32 * index < seen0 || 32 * index + 31 > seen1;
             auto shown = [&](int t) { return 32 * index + t >= seen0 && 32 * index + t <= seen1; };
 #pragma unroll
@@ -128,11 +131,13 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
                         x[d] &= keep;
                     }
                 }
+                u32x4* to = values ? &vals[bv][0] : &keys[b][0];
+                const int kb = values ? at - W::LOADS / 2 : at;
                 if constexpr (!W::BYTES) {
-                    lds[b][at * 64 + lane] = x;
+                    to[kb * 64 + lane] = x;
                 } else {
-                    lds[b][2 * at * 64 + lane] = widen8<CT>(x[0], x[1]);
-                    lds[b][(2 * at + 1) * 64 + lane] = widen8<CT>(x[2], x[3]);
+                    to[2 * kb * 64 + lane] = widen8<CT>(x[0], x[1]);
+                    to[(2 * kb + 1) * 64 + lane] = widen8<CT>(x[2], x[3]);
                 }
             }
             if constexpr (W::BYTES)
@@ -142,26 +147,34 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
         // All tiles, for a wave with RA row tiles.
         auto run = [&](auto count) {
             constexpr int RA = decltype(count)::value;
-            int now = fetch(), buf = 0;
+            const bool late = W::STAGGER && wid >= 4;
+            int now = fetch(), buf = 0, vbuf = 0, vlast = -1;
             if (now < 0) return;
-            put_tile(0, now);
+            put_tile(0, 0, now);
             int next = fetch();
+            u32x4 weights[R][W::NP];
             lds_barrier();
             while (true) {
                 if constexpr (RA > 0) {
+                    if (late && vlast >= 0) w.template gather_lds<RA>(&vals[vlast][lane], weights);
                     f32x4 sc[R][2];
-                    w.template scores_lds<RA>(&lds[buf][lane], scales[buf], u, sc, scale2);
+                    w.template scores_lds<RA>(&keys[buf][lane], scales[buf], u, sc, scale2);
                     if (32 * now < all0 || 32 * now + 31 > all1) w.template hide_scores<RA>(now, sc, lane);
-                    w.template weigh<RA>(sc);
-                    w.template gather_lds<RA>(&lds[buf][2 * W::KC * 64 + lane], scales[buf] + 8, u, sc);
+                    w.template weigh<RA>(sc, scale2);
+                    w.template round_lds<RA>(sc, scales[buf] + 8, u, weights);
+                    if (!late) w.template gather_lds<RA>(&vals[vbuf][lane], weights);
                 }
+                vlast = vbuf;
                 if (next < 0) break;
                 buf ^= 1;
-                put_tile(buf, next);
+                vbuf = vbuf + 1 == W::VBUF ? 0 : vbuf + 1;
+                put_tile(buf, vbuf, next);
                 now = next;
                 next = fetch();
                 lds_barrier();
             }
+            if constexpr (RA > 0)
+                if (late) w.template gather_lds<RA>(&vals[vlast][lane], weights);
         };
         if (R == 2 && active == 2) run(std::integral_constant<int, R>{});
         else if (active >= 1) run(std::integral_constant<int, 1>{});

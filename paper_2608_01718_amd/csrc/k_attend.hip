@@ -4,65 +4,93 @@
 
 namespace lacache {
 
-// The row groups that several workers had parts of: a workgroup a row of the group that ended with worker blockIdx.x,
-// a thread four columns of every (4 THREADS / dp)-th part, four of them loaded together.
-template <int THREADS>
-__global__ __launch_bounds__(THREADS) void k_attend_join(AttendArgs a, AttendPlan p) {
-    __shared__ float2 sml[THREADS];
-    __shared__ f32x4 so[THREADS];
+// The row groups that several workers had parts of: each of the workgroups (w, .) joins rows of the group that ended with
+// worker w.  A worker's part of a group that goes on after it lies in its second slot.
+__device__ __forceinline__ int64_t part_at(const AttendPlan& p, const AttendSplit& s, int parts, int k, int row) {
+    return (((2 * (int64_t)(s.worker0 + k)) + (k < parts - 1 ? 1 : 0)) << p.group_shift) + row;
+}
+struct Joined {
+    float m = -__builtin_inff(), l = 0.0f;
+    f32x4 o{0, 0, 0, 0};
+    __device__ __forceinline__ void add(float m2, float l2, f32x4 o2) {
+        if (m2 == -__builtin_inff()) return;
+        const float M = fmaxf(m, m2);
+        const float f = __builtin_amdgcn_exp2f(m - M), g = __builtin_amdgcn_exp2f(m2 - M);
+        l = l * f + l2 * g;
+        o = o * f + o2 * g;
+        m = M;
+    }
+};
+__device__ __forceinline__ void store_joined(const AttendArgs& a, const AttendPlan& p, const AttendSplit& s, int row,
+                                             int col, const Joined& x) {
+    const int r = s.row + row, i = token_of(p, r);
+    const int64_t at = ((int64_t)s.seq_row0 + i) * a.q_heads + s.head0 + (r - i * a.group);
+    const f32x4 o = x.o * (x.l == 0.0f ? 0.0f : 1.0f / x.l);
+    if (col < a.pool.d) {
+        if (a.dtype == 0) store4<true>(a, at * a.pool.d + col, o);
+        else store4<false>(a, at * a.pool.d + col, o);
+    }
+    if (col == 0 && a.lse) a.lse[at] = lse_of(x.m, x.l);
+}
+
+// Many row groups, of few parts each: a thread four columns of a row, part after part (four loaded together).
+__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, AttendPlan p) {
     const AttendSplit s = p.split[blockIdx.x];
-    const int tid = threadIdx.x, dp = a.pool.dp, lanes = dp / 4, groups = THREADS / lanes;
+    const int dp = a.pool.dp, lanes = dp / 4, rows = 256 / lanes;
+    const int col = threadIdx.x % lanes * 4, row_in = threadIdx.x / lanes;
+    const int parts = (int)blockIdx.x - s.worker0 + 1;
+    if (row_in >= rows) return;
+    for (int row = blockIdx.y * rows + row_in; row < s.n_rows; row += gridDim.y * rows) {
+        Joined x;
+        for (int k0 = 0; k0 < parts; k0 += 4) {
+            float2 ml[4];
+            f32x4 o[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int64_t at = part_at(p, s, parts, k0 + u < parts ? k0 + u : parts - 1, row);
+                ml[u] = p.part_ml[at];
+                o[u] = *(const f32x4*)(p.part_o + at * dp + col);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (k0 + u < parts) x.add(ml[u].x, ml[u].y, o[u]);
+        }
+        store_joined(a, p, s, row, col, x);
+    }
+}
+
+// Few row groups, of many parts each: a workgroup a row, a thread four columns of every (2048 / dp)-th part.
+__global__ __launch_bounds__(512) void k_attend_join_long(AttendArgs a, AttendPlan p) {
+    __shared__ float2 sml[512];
+    __shared__ f32x4 so[512];
+    const AttendSplit s = p.split[blockIdx.x];
+    const int tid = threadIdx.x, dp = a.pool.dp, lanes = dp / 4, groups = 512 / lanes;
     const int col = tid % lanes * 4, part = tid / lanes;
     const int parts = (int)blockIdx.x - s.worker0 + 1;
     for (int row = blockIdx.y; row < s.n_rows; row += gridDim.y) {
-        float m = -__builtin_inff(), l = 0.0f;
-        f32x4 o{0, 0, 0, 0};
+        Joined x;
         if (part < groups)
             for (int k0 = part; k0 < parts; k0 += 4 * groups) {
                 float2 ml[4];
-                f32x4 x[4];
+                f32x4 o[4];
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
-                    // a worker's part of a row group that goes on after it lies in its second slot
-                    const int k = k0 + u * groups < parts ? k0 + u * groups : parts - 1;
-                    const int64_t at = (((2 * (int64_t)(s.worker0 + k)) + (k < parts - 1 ? 1 : 0)) << p.group_shift) + row;
+                    const int64_t at = part_at(p, s, parts, k0 + u * groups < parts ? k0 + u * groups : parts - 1, row);
                     ml[u] = p.part_ml[at];
-                    x[u] = *(const f32x4*)(p.part_o + at * dp + col);
+                    o[u] = *(const f32x4*)(p.part_o + at * dp + col);
                 }
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    if (k0 + u * groups >= parts || ml[u].x == -__builtin_inff()) continue;
-                    const float M = fmaxf(m, ml[u].x);
-                    const float f = __builtin_amdgcn_exp2f(m - M), g = __builtin_amdgcn_exp2f(ml[u].x - M);
-                    l = l * f + ml[u].y * g;
-                    o = o * f + x[u] * g;
-                    m = M;
-                }
+                for (int u = 0; u < 4; ++u)
+                    if (k0 + u * groups < parts) x.add(ml[u].x, ml[u].y, o[u]);
             }
         __syncthreads();
-        sml[tid] = make_float2(m, l);
-        so[tid] = o;
+        sml[tid] = make_float2(x.m, x.l);
+        so[tid] = x.o;
         __syncthreads();
-        const int live = groups < parts ? groups : parts;
         if (part == 0) {
-            float M = -__builtin_inff();
-            for (int k = 0; k < live; ++k) M = fmaxf(M, sml[k * lanes + tid].x);
-            const float base = M == -__builtin_inff() ? 0.0f : M;
-            float L = 0.0f;
-            f32x4 O{0, 0, 0, 0};
-            for (int k = 0; k < live; ++k) {
-                const float f = __builtin_amdgcn_exp2f(sml[k * lanes + tid].x - base);
-                L += sml[k * lanes + tid].y * f;
-                O += so[k * lanes + tid] * f;
-            }
-            const int r = s.row + row, i = token_of(p, r);
-            const int64_t at = ((int64_t)s.seq_row0 + i) * a.q_heads + s.head0 + (r - i * a.group);
-            O *= L == 0.0f ? 0.0f : 1.0f / L;
-            if (col < a.pool.d) {
-                if (a.dtype == 0) store4<true>(a, at * a.pool.d + col, O);
-                else store4<false>(a, at * a.pool.d + col, O);
-            }
-            if (tid == 0 && a.lse) a.lse[at] = lse_of(M, L);
+            const int live = groups < parts ? groups : parts;
+            for (int k = 1; k < live; ++k) x.add(sml[k * lanes + tid].x, sml[k * lanes + tid].y, so[k * lanes + tid]);
+            store_joined(a, p, s, row, col, x);
         }
     }
 }
@@ -129,11 +157,15 @@ hipError_t launch_kv_attend(const AttendArgs& a, int max_new, void* workspace, i
                          : a.pool.dp == 192 ? launch_attend<192>(a, p, s)
                                             : launch_attend<256>(a, p, s);
     if (e != hipSuccess) return e;
-    const unsigned rows = 1u << p.group_shift;
-    int64_t most = max_new > 0 && (int64_t)max_new * a.group < rows ? (int64_t)max_new * a.group : rows;
-    most = most < 32 ? most : 32;
-    if (a.seqs.n_seq * (int64_t)a.pool.heads < 64) k_attend_join<512><<<dim3((unsigned)p.workers, (unsigned)most), dim3(512), 0, s>>>(a, p);
-    else k_attend_join<256><<<dim3((unsigned)p.workers, (unsigned)most), dim3(256), 0, s>>>(a, p);
+    // rows of a row group, row groups
+    int64_t rows = (int64_t)(max_new > 0 ? max_new : 64) * a.group, of_seq = ((rows - 1) >> p.group_shift) + 1;
+    rows = rows < (1 << p.group_shift) ? rows : 1 << p.group_shift;
+    if (a.seqs.n_seq * (int64_t)a.pool.heads * of_seq < 64) {
+        k_attend_join_long<<<dim3((unsigned)p.workers, (unsigned)(rows < 32 ? rows : 32)), dim3(512), 0, s>>>(a, p);
+    } else {
+        const int64_t at_once = 1024 / a.pool.dp;
+        k_attend_join<<<dim3((unsigned)p.workers, (unsigned)((rows + at_once - 1) / at_once)), dim3(256), 0, s>>>(a, p);
+    }
     return hipGetLastError();
 }
 
