@@ -146,15 +146,16 @@ __device__ __forceinline__ AttendRange attend_range(const AttendArgs& a, const A
     return r;
 }
 
-// 16 bytes a lane from a tile whose bytes past `size` (0: there is no tile) are not read and come as zeros.  Keys and
-// values are read once: non-temporal loads are 12 % faster (131,071 tokens 89 us, 102 without; 256 sequences of 512 to
+// 16 bytes a lane from a tile whose bytes past `size` (0: there is no tile) are not read and come as zeros.  With few rows
+// keys and values are read once (ONCE): non-temporal loads are 12 % faster (131,071 tokens 89 us, 102 without; 256 sequences of 512 to
 // 2048 tokens, 16 heads of 64 columns 191 us, 214).
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_rsrc(const void* p, int size) {
     return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, size, 0x00020000);
 }
 // (The constant part of an offset fits in the instruction up to 4095 bytes; whole 4 KB go into a scalar register.)
+template <bool ONCE = true>
 __device__ __forceinline__ u32x4 tile_load(__amdgpu_buffer_rsrc_t r, int at, int lane_offset) {
-    return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, lane_offset + (at & 4095), at & ~4095, 2));
+    return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, lane_offset + (at & 4095), at & ~4095, ONCE ? 2 : 0));
 }
 
 // four 8-bit codes as bfloat16 pairs

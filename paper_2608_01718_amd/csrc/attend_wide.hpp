@@ -23,6 +23,9 @@ struct Wide {
     static constexpr int BYTES_TILE = 32 * DP * (BYTES ? 1 : 2);
     static constexpr int LOADS = 2 * BYTES_TILE / 1024;           // 16-byte loads a lane of keys and values, all waves
     static constexpr int PER_WAVE = (LOADS + WAVES - 1) / WAVES;
+    // tiles on their way in registers: two hide the latency where one workgroup has the compute unit to itself (1.2 us a
+    // load under a step of 1.5 us)
+    static constexpr int AHEAD = WAVES == 8 ? 2 : 1;
     static constexpr bool STAGGER = WAVES == 8;                   // the upper four waves are half a step behind
     static constexpr int VBUF = STAGGER ? 3 : 2;                  // tiles of values in LDS
     // waves on a SIMD: two where the registers of the sums and queries leave room
@@ -48,8 +51,8 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
     const float scale2 = scale_of(a);
     const int tile_shift = a.pool.page_shift - 5;
     AttendSpan s = attend_span(a, p, range.b);
-    u32x4 stage[W::PER_WAVE];
-    float stage_scale = 0.0f;
+    u32x4 stage[W::AHEAD][W::PER_WAVE];
+    float stage_scale[W::AHEAD] = {};
 
     while (true) {
         // the segment that begins at item range.at
@@ -83,33 +86,36 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
             todo = __ballot(page >= 0 && page < a.pool.n_pages);
         };
         load_pages();
-        // Begins to load the next tile, the waves a part each; its number, or -1.
-        auto fetch = [&]() {
+        // Begins to load the next tile, the waves a part each; its number, or -1 (then nothing is read).
+        auto fetch = [&](u32x4 (&stage)[W::PER_WAVE], float& scale) {
             while (!todo && t0 + 64 < tile1) {
                 t0 += 64;
                 load_pages();
             }
-            if (!todo) return -1;
-            const int k = __ffsll((unsigned long long)todo) - 1;
+            const int there = todo ? 1 : 0, k = there ? __ffsll((unsigned long long)todo) - 1 : 0;
             todo &= todo - 1;
             const int index = s.first + t0 + k;
-            const int64_t place = (((int64_t)__builtin_amdgcn_readlane(page, k) * a.pool.heads + h) << tile_shift) +
-                                  (index & ((1 << tile_shift) - 1));
+            const int64_t pg = there ? __builtin_amdgcn_readlane(page, k) : 0;
+            const int64_t place = ((pg * a.pool.heads + h) << tile_shift) + (index & ((1 << tile_shift) - 1));
 #pragma unroll
             for (int i = 0; i < W::PER_WAVE; ++i) {
                 const int at = wid * W::PER_WAVE + i;  // which KB of the tile's keys and values
-                if (W::LOADS % W::PER_WAVE != 0 || W::LOADS < W::PER_WAVE * WAVES)
-                    if (at >= W::LOADS) continue;
-                const char* base = at < W::LOADS / 2 ? a.pool.k : a.pool.v;
-                const int kb = at < W::LOADS / 2 ? at : at - W::LOADS / 2;
-                stage[i] = *(const u32x4*)(base + place * W::BYTES_TILE + kb * 1024 + lane * 16);
+                const bool values = at >= W::LOADS / 2;
+                const auto r = tile_rsrc((values ? a.pool.v : a.pool.k) + place * W::BYTES_TILE,
+                                         at < W::LOADS ? there * W::BYTES_TILE : 0);
+                stage[i] = tile_load<false>(r, 0, (at - (values ? W::LOADS / 2 : 0)) * 1024 + lane * 16);
             }
-            if constexpr (W::BYTES)
-                if (wid == 0) stage_scale = (lane < 32 ? a.pool.k_scale : a.pool.v_scale)[place * 32 + (lane & 31)];
-            return index;
+            if constexpr (W::BYTES) {
+                const int size = wid == 0 ? there * 128 : 0, at = (lane & 31) * 4;
+                const auto rk = tile_rsrc(a.pool.k_scale + place * 32, size), rv = tile_rsrc(a.pool.v_scale + place * 32, size);
+                const uint32_t ks = __builtin_amdgcn_raw_buffer_load_b32(rk, at, 0, 0),
+                               vs = __builtin_amdgcn_raw_buffer_load_b32(rv, at, 0, 0);
+                scale = __uint_as_float(lane < 32 ? ks : vs);
+            }
+            return there ? index : -1;
         };
         // The loaded tile into buffers b (keys, scales) and bv; values that no row sees as zeros.
-        auto put_tile = [&](int b, int bv, int index) {
+        auto put_tile = [&](const u32x4 (&stage)[W::PER_WAVE], float scale, int b, int bv, int index) {
             const bool edge = 32 * index < seen0 || 32 * index + 31 > seen1;
             auto shown = [&](int t) { return 32 * index + t >= seen0 && 32 * index + t <= seen1; };
 #pragma unroll
@@ -142,19 +148,21 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
             }
             if constexpr (W::BYTES)
                 if (wid == 0)
-                    ((float*)scales[b])[lane] = lane >= 32 && edge && !shown(lane & 31) ? 0.0f : stage_scale;
+                    ((float*)scales[b])[lane] = lane >= 32 && edge && !shown(lane & 31) ? 0.0f : scale;
         };
         // All tiles, for a wave with RA row tiles.
         auto run = [&](auto count) {
             constexpr int RA = decltype(count)::value;
             const bool late = W::STAGGER && wid >= 4;
-            int now = fetch(), buf = 0, vbuf = 0, vlast = -1;
+            int now = fetch(stage[0], stage_scale[0]), buf = 0, vbuf = 0, vlast = -1;
             if (now < 0) return;
-            put_tile(0, 0, now);
-            int next = fetch();
+            put_tile(stage[0], stage_scale[0], 0, 0, now);
+            int next = fetch(stage[0], stage_scale[0]), after = -1;
+            if constexpr (W::AHEAD == 2) after = fetch(stage[1], stage_scale[1]);
             u32x4 weights[R][W::NP];
             lds_barrier();
-            while (true) {
+            // one tile; the next one, on its way in registers `k`, follows it into LDS
+            auto step = [&](int k) {
                 if constexpr (RA > 0) {
                     if (late && vlast >= 0) w.template gather_lds<RA>(&vals[vlast][lane], weights);
                     f32x4 sc[R][2];
@@ -165,14 +173,22 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
                     if (!late) w.template gather_lds<RA>(&vals[vbuf][lane], weights);
                 }
                 vlast = vbuf;
-                if (next < 0) break;
+                if (next < 0) return false;
                 buf ^= 1;
                 vbuf = vbuf + 1 == W::VBUF ? 0 : vbuf + 1;
-                put_tile(buf, vbuf, next);
+                put_tile(stage[k], stage_scale[k], buf, vbuf, next);
                 now = next;
-                next = fetch();
+                if constexpr (W::AHEAD == 2) {
+                    next = after;
+                    after = fetch(stage[k], stage_scale[k]);
+                } else {
+                    next = fetch(stage[k], stage_scale[k]);
+                }
                 lds_barrier();
-            }
+                return true;
+            };
+            while (step(0) && (W::AHEAD == 1 || step(W::AHEAD - 1)))
+                ;
             if constexpr (RA > 0)
                 if (late) w.template gather_lds<RA>(&vals[vlast][lane], weights);
         };
