@@ -95,13 +95,13 @@ __device__ __forceinline__ int wave_scan(int x) {
     return x;
 }
 
-// The range of items of this workgroup: the sequence in which it begins, the items before that sequence, the range, and
+// The range of items of a worker: the sequence in which it begins, the items before that sequence, the range, and
 // the items of a full range (a multiple of `grain`).  All threads take part, a thread a sequence.
 struct AttendRange {
     int b, before, at, end, per;
 };
 template <int WAVES>
-__device__ __forceinline__ AttendRange attend_range(const AttendArgs& a, const AttendPlan& p, int grain) {
+__device__ __forceinline__ AttendRange attend_range(const AttendArgs& a, const AttendPlan& p, int worker, int grain) {
     constexpr int THREADS = 64 * WAVES;
     __shared__ int total_of[WAVES], found[2];
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, n_seq = a.seqs.n_seq;
@@ -127,7 +127,7 @@ __device__ __forceinline__ AttendRange attend_range(const AttendArgs& a, const A
     AttendRange r;
     r.per = (int)(((uint32_t)all + (uint32_t)p.workers - 1) / (uint32_t)p.workers);
     r.per = (r.per + grain - 1) & ~(grain - 1);
-    const int64_t at = (int64_t)blockIdx.x * r.per;
+    const int64_t at = (int64_t)worker * r.per;
     r.at = at < all ? (int)at : all;
     r.end = at + r.per < all ? (int)(at + r.per) : all;
     // the thread whose sequence holds item `at` finds it
@@ -537,7 +537,7 @@ __global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(A
     const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int worker = blockIdx.x;
 
-    AttendRange range = attend_range<4>(a, p, 4 >> (p.chunk_shift < 2 ? p.chunk_shift : 2));
+    AttendRange range = attend_range<4>(a, p, worker, 4 >> (p.chunk_shift < 2 ? p.chunk_shift : 2));
     if (range.at >= range.end) {
         if (tid == 0) p.split[worker].n_rows = 0;
         return;

@@ -40,9 +40,13 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
     __shared__ u32x4 keys[2][2 * W::KC * 64], vals[W::VBUF][W::NJ * 64];  // operands of 1 KB each
     __shared__ f32x4 scales[2][16];  // 32 of the keys, 32 of the values
     const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int worker = blockIdx.x, n = lane & 15, u = lane >> 4;
+    const int n = lane & 15, u = lane >> 4;
+    // Workgroups go to the eight XCDs in turn; each XCD takes an eighth of the work in one piece, so that the row groups of
+    // a (sequence, kv head) share its L2.
+    const int eighth = (p.workers + 7) >> 3, worker = (blockIdx.x & 7) * eighth + (blockIdx.x >> 3);
+    if (worker >= p.workers) return;
 
-    AttendRange range = attend_range<WAVES>(a, p, 1);
+    AttendRange range = attend_range<WAVES>(a, p, worker, 1);
     if (range.at >= range.end) {
         if (tid == 0) p.split[worker].n_rows = 0;
         return;
@@ -76,25 +80,35 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
         w.clear();
         w.load_q(a, p, s, h, r0 + 16 * wid, 16 * WAVES, lane);
 
-        int t0 = tile0, page = -1;
+        // The segment's tiles in turn, from the first whose number is a multiple of a full range's length on, and then those
+        // before it: row groups of one (sequence, kv head), whose ranges begin anywhere, read the same tiles at about the
+        // same time.
+        const int64_t per = (int64_t)range.per << p.chunk_shift;
+        const int count = tile1 - tile0, off = (int)(tile0 % per);
+        const int from = off != 0 && per - off < count ? (int)(per - off) : 0;
+        int t0 = 0, page = -1;
         uint64_t todo = 0;
+        auto tile_at = [&](int i) {  // the segment's i-th tile in that order
+            i += from;
+            return s.first + tile0 + (i < count ? i : i - count);
+        };
         auto load_pages = [&]() {  // 64 tiles from t0 on, a lane each: which of them are there and seen
-            const int t = t0 + lane, mine = s.first + t;
+            const int t = t0 + lane, mine = tile_at(t);
             page = -1;
-            if (t < tile1 && 32 * mine <= seen1 && 32 * mine + 31 >= seen0)
+            if (t < count && 32 * mine <= seen1 && 32 * mine + 31 >= seen0)
                 page = (a.seqs.pages + (int64_t)range.b * a.seqs.max_pages)[mine >> tile_shift];
             todo = __ballot(page >= 0 && page < a.pool.n_pages);
         };
         load_pages();
         // Begins to load the next tile, the waves a part each; its number, or -1 (then nothing is read).
         auto fetch = [&](u32x4 (&stage)[W::PER_WAVE], float& scale) {
-            while (!todo && t0 + 64 < tile1) {
+            while (!todo && t0 + 64 < count) {
                 t0 += 64;
                 load_pages();
             }
             const int there = todo ? 1 : 0, k = there ? __ffsll((unsigned long long)todo) - 1 : 0;
             todo &= todo - 1;
-            const int index = s.first + t0 + k;
+            const int index = tile_at(t0 + k);
             const int64_t pg = there ? __builtin_amdgcn_readlane(page, k) : 0;
             const int64_t place = ((pg * a.pool.heads + h) << tile_shift) + (index & ((1 << tile_shift) - 1));
 #pragma unroll
@@ -161,19 +175,21 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
             if constexpr (W::AHEAD == 2) after = fetch(stage[1], stage_scale[1]);
             u32x4 weights[R][W::NP];
             lds_barrier();
-            // one tile; the next one, on its way in registers `k`, follows it into LDS
+            // One tile, if there is one; the next one, on its way in registers `k`, follows it into LDS.  (No way out of
+            // the middle: every step issues its loads, so that their number in flight is known and a wait is for its own.)
             auto step = [&](int k) {
-                if constexpr (RA > 0) {
-                    if (late && vlast >= 0) w.template gather_lds<RA>(&vals[vlast][lane], weights);
-                    f32x4 sc[R][2];
-                    w.template scores_lds<RA>(&keys[buf][lane], scales[buf], u, sc, scale2);
-                    if (32 * now < all0 || 32 * now + 31 > all1) w.template hide_scores<RA>(now, sc, lane);
-                    w.template weigh<RA>(sc, scale2);
-                    w.template round_lds<RA>(sc, scales[buf] + 8, u, weights);
-                    if (!late) w.template gather_lds<RA>(&vals[vbuf][lane], weights);
+                if (now >= 0) {
+                    if constexpr (RA > 0) {
+                        if (late && vlast >= 0) w.template gather_lds<RA>(&vals[vlast][lane], weights);
+                        f32x4 sc[R][2];
+                        w.template scores_lds<RA>(&keys[buf][lane], scales[buf], u, sc, scale2);
+                        if (32 * now < all0 || 32 * now + 31 > all1) w.template hide_scores<RA>(now, sc, lane);
+                        w.template weigh<RA>(sc, scale2);
+                        w.template round_lds<RA>(sc, scales[buf] + 8, u, weights);
+                        if (!late) w.template gather_lds<RA>(&vals[vbuf][lane], weights);
+                    }
+                    vlast = vbuf;
                 }
-                vlast = vbuf;
-                if (next < 0) return false;
                 buf ^= 1;
                 vbuf = vbuf + 1 == W::VBUF ? 0 : vbuf + 1;
                 put_tile(stage[k], stage_scale[k], buf, vbuf, next);
@@ -185,10 +201,11 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
                     next = fetch(stage[k], stage_scale[k]);
                 }
                 lds_barrier();
-                return true;
             };
-            while (step(0) && (W::AHEAD == 1 || step(W::AHEAD - 1)))
-                ;
+            while (now >= 0) {
+                step(0);
+                if constexpr (W::AHEAD == 2) step(1);
+            }
             if constexpr (RA > 0)
                 if (late) w.template gather_lds<RA>(&vals[vlast][lane], weights);
         };
@@ -234,7 +251,7 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
 
 template <int DP>
 hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
-    const dim3 grid((unsigned)p.workers), block(p.waves * 64);
+    const dim3 grid((unsigned)(p.group_shift < 6 ? p.workers : (p.workers + 7) & ~7)), block(p.waves * 64);
     auto go = [&](auto ct) {
         constexpr int CT = decltype(ct)::value;
         if (a.dtype == 0) {
