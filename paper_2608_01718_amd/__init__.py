@@ -8,7 +8,6 @@ fallback: importing this module fails if ``liblacache.so`` has not been built
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 
@@ -476,36 +475,45 @@ _KV_TYPES = {t: k for k, t in _KV_DTYPES.items()}
 _ROW_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 
 
-def _current(dev: torch.device):
-    """A context in which `dev` is the calling thread's current device."""
-    return contextlib.nullcontext() if torch.cuda.current_device() == dev.index else torch.cuda.device(dev)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # (torch.cuda.current_stream takes a microsecond more)
 
 
-def _rows(t: torch.Tensor, heads: int, d: int, dev: torch.device, dtype, name: str) -> int:
+def _on(index: int, stream, f, *args) -> int:
+    """f(*args, stream) with GPU `index` as the calling thread's current device."""
+    raw = _raw_stream(index) if stream is None and _raw_stream is not None else _stream(index, stream)
+    if torch.cuda.current_device() == index:
+        return f(*args, raw)
+    with torch.cuda.device(index):
+        return f(*args, raw)
+
+
+def _rows(t: torch.Tensor, heads: int, d: int, index: int, dtype, name: str) -> int:
     """The row stride of [rows, heads, d] activations whose rows are each contiguous."""
-    if t.dtype != dtype or t.device != dev:
-        raise ValueError(f"{name}: expected a {dtype} tensor on {dev}, got {t.dtype} on {t.device}")
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d or (
-            t.shape[0] and ((d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d))):
-        raise ValueError(f"{name}: expected [rows, {heads}, {d}] with contiguous rows, got {tuple(t.shape)} with strides "
-                         f"{t.stride()}")
-    return t.stride(0)
+    if t.dtype != dtype or t.get_device() != index:
+        raise ValueError(f"{name}: expected a {dtype} tensor on cuda:{index}, got {t.dtype} on {t.device}")
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[1] != heads or shape[2] != d or (
+            shape[0] and ((d > 1 and stride[2] != 1) or (heads > 1 and stride[1] != d))):
+        raise ValueError(f"{name}: expected [rows, {heads}, {d}] with contiguous rows, got {tuple(shape)} with strides "
+                         f"{stride}")
+    return stride[0]
 
 
-def _made(shape, dtype, dev, stream):
-    """An empty tensor that belongs to the stream the call runs on."""
+def _made(like: torch.Tensor, shape, dtype, stream):
+    """An empty tensor on the GPU of `like` that belongs to the stream the call runs on."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=dev)
+        return like.new_empty(shape, dtype=dtype)
     if not isinstance(stream, torch.cuda.Stream):
         handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
-        stream = torch.cuda.ExternalStream(handle, device=dev) if handle else torch.cuda.default_stream(dev)
+        stream = torch.cuda.ExternalStream(handle, device=like.device) if handle else \
+            torch.cuda.default_stream(like.device)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=dev)
+        return like.new_empty(shape, dtype=dtype)
 
 
-def _given(t: torch.Tensor, shape, dtype, dev, name: str) -> torch.Tensor:
-    if t.dtype != dtype or t.device != dev or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous {list(shape)} {dtype} tensor on {dev}")
+def _given(t: torch.Tensor, shape, dtype, index: int, name: str) -> torch.Tensor:
+    if t.dtype != dtype or t.get_device() != index or t.shape != torch.Size(shape) or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {list(shape)} {dtype} tensor on cuda:{index}")
     return t
 
 
@@ -517,7 +525,7 @@ class Rope:
         if table.dtype != torch.float32 or table.device.type != "cuda" or table.dim() != 3 or table.shape[2] != 2 or \
                 not table.is_contiguous():
             raise ValueError("table: expected a contiguous float32 [positions, rot / 2, 2] tensor on a GPU")
-        self.table, self.style, self.rot = table, style, 2 * table.shape[1]
+        self.table, self.style, self.rot, self.index = table, style, 2 * table.shape[1], table.get_device()
         self._c = _Rotary(table.data_ptr(), table.shape[0], self.rot, style)
         self._ref = ctypes.addressof(self._c)
 
@@ -533,7 +541,7 @@ class Sequences:
         _ints(start, (n + 1,), dev.index, "start")
         _ints(lens, (n,), dev.index, "lens")
         _ints(pages, (n, pages.shape[1]), dev.index, "pages")
-        self.start, self.lens, self.pages, self.device = start, lens, pages, dev
+        self.start, self.lens, self.pages, self.index = start, lens, pages, dev.index
         self._c = _Seqs(start.data_ptr(), lens.data_ptr(), pages.data_ptr(), n, pages.shape[1])
         self._ref = ctypes.addressof(self._c)
 
@@ -567,15 +575,15 @@ class KVCache:
             n_pages, heads, page = k.shape[0], k.shape[1], 32 * k.shape[2]
             if not 1 <= d <= 256 or k.shape[3] != 32 * _padded(d):
                 raise ValueError(f"pools: tiles of {k.shape[3]} elements do not fit d = {d}")
-            _given(k, k.shape, k.dtype, dev, "k")
-            _given(v, k.shape, k.dtype, dev, "v")
+            _given(k, k.shape, k.dtype, dev.index, "k")
+            _given(v, k.shape, k.dtype, dev.index, "v")
             for t, name in ((ks, "k_scale"), (vs, "v_scale")):
                 if type != KV_BF16:
-                    _given(t, (n_pages, heads, page), torch.float32, dev, name)
+                    _given(t, (n_pages, heads, page), torch.float32, dev.index, name)
                 elif t is not None:
                     raise ValueError(f"{name}: a bfloat16 cache has no scales")
         self.k, self.v, self.k_scale, self.v_scale = k, v, ks, vs
-        self.n_pages, self.heads, self.d, self.page, self.type, self.device = n_pages, heads, d, page, type, dev
+        self.n_pages, self.heads, self.d, self.page, self.type, self.index = n_pages, heads, d, page, type, k.get_device()
         self._c = _KV(k.data_ptr(), v.data_ptr(), *(0 if t is None else t.data_ptr() for t in (ks, vs)), n_pages, page,
                       heads, d, type)
         self._ref = ctypes.addressof(self._c)
@@ -600,12 +608,12 @@ def lacache_rope_table(n: int, rot: int, base: float = 10000.0, factor: float = 
                        out=None, stream=None):
     """(cos, sin) of positions first .. first+n-1 for rot / 2 pairs, [n, rot / 2, 2] float32, scaled by parts for long
     contexts if factor > 1."""
-    dev = torch.device("cuda", device)
     shape = (n, rot // 2, 2)
-    out = _made(shape, torch.float32, dev, stream) if out is None else _given(out, shape, torch.float32, dev, "out")
-    with _current(dev):
-        _check(_lib.lacache_rope_table(out.data_ptr(), first, n, rot, base, factor, original, low, high, magnitude,
-                                       _stream(dev.index, stream)), "lacache_rope_table")
+    if out is None:
+        out = _made(torch.empty(0, device=torch.device("cuda", device)), shape, torch.float32, stream)
+    _given(out, shape, torch.float32, device, "out")
+    _check(_on(device, stream, _lib.lacache_rope_table, out.data_ptr(), first, n, rot, base, factor, original, low, high,
+               magnitude), "lacache_rope_table")
     return out
 
 
@@ -613,69 +621,67 @@ def lacache_rope(x, pos, rope: Rope, backward: bool = False, out=None, stream=No
     """x [rows, H, d] float32 or bfloat16 (any strides, the last one 1), pos [rows] int32.  Returns the turned rows
     (`out`, which may be x; otherwise a new contiguous tensor); with backward=True the gradient of the input from that of
     the output."""
-    dev = x.device
-    if x.dim() != 3 or x.dtype not in _ROW_DTYPES or dev.type != "cuda" or (x.shape[2] > 1 and x.stride(2) != 1):
+    index, dtype, shape, xs = x.get_device(), _ROW_DTYPES.get(x.dtype), x.shape, x.stride()
+    if len(shape) != 3 or dtype is None or index < 0 or (shape[2] > 1 and xs[2] != 1):
         raise ValueError("x: expected a float32 or bfloat16 [rows, H, d] tensor on a GPU, its last stride 1")
-    rows, H, d = x.shape
+    rows, H, d = shape
     if out is None:
-        out = _made(x.shape, x.dtype, dev, stream)
-    elif out.shape != x.shape or out.dtype != x.dtype or out.device != dev or (d > 1 and out.stride(2) != 1):
-        raise ValueError(f"out: expected {tuple(x.shape)} {x.dtype} on {dev}, its last stride 1")
-    if rope.table.device != dev:
-        raise ValueError(f"rope: expected a table on {dev}")
-    with _current(dev):
-        _check(_lib.lacache_rope(x.data_ptr(), out.data_ptr(), _ROW_DTYPES[x.dtype], rows, H, d, x.stride(0), x.stride(1),
-                                 out.stride(0), out.stride(1), _ints(pos, (rows,), dev.index, "pos"), rope._ref,
-                                 int(backward), _stream(dev.index, stream)), "lacache_rope")
+        out = _made(x, shape, x.dtype, stream)
+    elif out.shape != shape or out.dtype != x.dtype or out.get_device() != index or (d > 1 and out.stride(2) != 1):
+        raise ValueError(f"out: expected {tuple(shape)} {x.dtype} on cuda:{index}, its last stride 1")
+    if rope.index != index or pos.dtype != torch.int32 or pos.get_device() != index or pos.shape != shape[:1] or \
+            not pos.is_contiguous():
+        raise ValueError(f"expected a table and {rows} contiguous int32 positions on cuda:{index}")
+    ys = out.stride()
+    _check(_on(index, stream, _lib.lacache_rope, x.data_ptr(), out.data_ptr(), dtype, rows, H, d, xs[0], xs[1], ys[0],
+               ys[1], pos.data_ptr(), rope._ref, int(backward)), "lacache_rope")
     return out
 
 
 def lacache_kv_append(c: KVCache, k, v, seqs: Sequences, q=None, rope=None, q_out=None, max_new: int = 0, stream=None):
     """Store the new tokens k, v [rows, heads, d] (float32 or bfloat16, for example parts of one projection's output) of
     every sequence; k and q [rows, q_heads, d] are turned by `rope`.  Returns the turned q (None without q)."""
-    dev, dtype = c.device, k.dtype
-    if dtype not in _ROW_DTYPES:
-        raise ValueError(f"k: unsupported dtype {dtype}")
+    index, kind = c.index, k.dtype
+    dtype = _ROW_DTYPES.get(kind)
+    if dtype is None:
+        raise ValueError(f"k: unsupported dtype {kind}")
+    k_row, v_row = _rows(k, c.heads, c.d, index, kind, "k"), _rows(v, c.heads, c.d, index, kind, "v")
     rows = k.shape[0]
-    k_row, v_row = _rows(k, c.heads, c.d, dev, dtype, "k"), _rows(v, c.heads, c.d, dev, dtype, "v")
-    if v.shape[0] != rows or seqs.device != dev or (rope is not None and rope.table.device != dev):
-        raise ValueError(f"expected {rows} rows of v, and sequences and table on {dev}")
+    if v.shape[0] != rows or seqs.index != index or (rope is not None and rope.index != index):
+        raise ValueError(f"expected {rows} rows of v, and sequences and table on cuda:{index}")
     q_ptr = o_ptr = None
     q_row = q_heads = 0
     if q is not None:
         q_heads = q.shape[1]
-        q_row = _rows(q, q_heads, c.d, dev, dtype, "q")
+        q_row = _rows(q, q_heads, c.d, index, kind, "q")
         if q.shape[0] != rows:
             raise ValueError(f"q: expected {rows} rows")
-        q_out = _made(q.shape, dtype, dev, stream) if q_out is None else _given(q_out, q.shape, dtype, dev, "q_out")
+        q_out = _made(q, q.shape, kind, stream) if q_out is None else _given(q_out, q.shape, kind, index, "q_out")
         q_ptr, o_ptr = q.data_ptr(), q_out.data_ptr()
-    with _current(dev):
-        _check(_lib.lacache_kv_append(c._ref, seqs._ref, k.data_ptr(), v.data_ptr(), _ROW_DTYPES[dtype], rows, k_row,
-                                      v_row, q_ptr, o_ptr, q_heads, q_row, None if rope is None else rope._ref, max_new,
-                                      _stream(dev.index, stream)), "lacache_kv_append")
+    _check(_on(index, stream, _lib.lacache_kv_append, c._ref, seqs._ref, k.data_ptr(), v.data_ptr(), dtype, rows, k_row,
+               v_row, q_ptr, o_ptr, q_heads, q_row, None if rope is None else rope._ref, max_new), "lacache_kv_append")
     return q_out if q is not None else None
 
 
 def lacache_kv_read(c: KVCache, seqs: Sequences, rows: int, dtype=torch.bfloat16, out=None, max_new: int = 0,
                     stream=None):
     """The newest tokens of every sequence as (k, v), each [rows, heads, d] of dtype; rows is start[-1]."""
-    dev = c.device
-    if dtype not in _ROW_DTYPES or seqs.device != dev:
-        raise ValueError(f"expected float32 or bfloat16, and sequences on {dev}")
+    index, kind = c.index, _ROW_DTYPES.get(dtype)
+    if kind is None or seqs.index != index:
+        raise ValueError(f"expected float32 or bfloat16, and sequences on cuda:{index}")
     shape = (rows, c.heads, c.d)
     if out is None:
-        out = (_made(shape, dtype, dev, stream), _made(shape, dtype, dev, stream))
-    for t, name in zip(out, ("k", "v")):
-        _given(t, shape, dtype, dev, name)
-    with _current(dev):
-        _check(_lib.lacache_kv_read(c._ref, seqs._ref, out[0].data_ptr(), out[1].data_ptr(), _ROW_DTYPES[dtype], rows,
-                                    max_new, _stream(dev.index, stream)), "lacache_kv_read")
-    return out
+        k, v = _made(c.k, shape, dtype, stream), _made(c.k, shape, dtype, stream)
+    else:
+        k, v = _given(out[0], shape, dtype, index, "k"), _given(out[1], shape, dtype, index, "v")
+    _check(_on(index, stream, _lib.lacache_kv_read, c._ref, seqs._ref, k.data_ptr(), v.data_ptr(), kind, rows, max_new),
+           "lacache_kv_read")
+    return k, v
 
 
 def lacache_kv_attend_workspace(c: KVCache, dtype: int, n_seq: int, q_heads: int, max_new: int = 0) -> int:
     """Bytes of scratch that lacache_kv_attend needs (dtype: F32 or BF16)."""
-    with _current(c.device):
+    with torch.cuda.device(c.index):
         n = int(_lib.lacache_kv_attend_workspace(c._ref, dtype, n_seq, q_heads, max_new))
     if n < 0:
         raise LaCacheError(n, "lacache_kv_attend_workspace")
@@ -686,28 +692,27 @@ def lacache_kv_attend(c: KVCache, q, seqs: Sequences, scale=None, window: int = 
                       stream=None):
     """Attention of the new rows q [rows, q_heads, d] (already turned) over the cached tokens.  scale defaults to
     1 / sqrt(d).  Returns (out [rows, q_heads, d] of q's dtype, lse [rows, q_heads] float32)."""
-    dev, dtype = c.device, q.dtype
-    if dtype not in _ROW_DTYPES or q.dim() != 3 or seqs.device != dev:
-        raise ValueError(f"q: expected float32 or bfloat16 [rows, q_heads, d], and sequences on {dev}")
-    rows, q_heads = q.shape[0], q.shape[1]
-    q_row = _rows(q, q_heads, c.d, dev, dtype, "q")
+    index, kind, shape = c.index, q.dtype, q.shape
+    dtype = _ROW_DTYPES.get(kind)
+    if dtype is None or len(shape) != 3 or seqs.index != index:
+        raise ValueError(f"q: expected float32 or bfloat16 [rows, q_heads, d], and sequences on cuda:{index}")
+    rows, q_heads = shape[0], shape[1]
+    q_row = _rows(q, q_heads, c.d, index, kind, "q")
     if out is None:
-        out = (_made(q.shape, dtype, dev, stream), _made((rows, q_heads), torch.float32, dev, stream))
+        out = (_made(q, shape, kind, stream), _made(q, shape[:2], torch.float32, stream))
     else:
-        _given(out[0], q.shape, dtype, dev, "out")
-        _given(out[1], (rows, q_heads), torch.float32, dev, "lse")
-    o, lse = out
-    key = (dtype, len(seqs), q_heads, max_new)
+        _given(out[0], shape, kind, index, "out")
+        _given(out[1], shape[:2], torch.float32, index, "lse")
+    key = (dtype, seqs._c.n_seq, q_heads, max_new)
     need = c._need.get(key)
     if need is None:
-        need = c._need[key] = lacache_kv_attend_workspace(c, _ROW_DTYPES[dtype], len(seqs), q_heads, max_new)
+        need = c._need[key] = lacache_kv_attend_workspace(c, *key)
     if c._space is None or c._space.numel() < need:
-        c._space = _made((need,), torch.uint8, dev, stream)
-    with _current(dev):
-        _check(_lib.lacache_kv_attend(c._ref, seqs._ref, q.data_ptr(), _ROW_DTYPES[dtype], rows, q_heads, q_row, max_new,
-                                      c.d ** -0.5 if scale is None else scale, window, o.data_ptr(), lse.data_ptr(),
-                                      c._space.data_ptr(), c._space.numel(), _stream(dev.index, stream)),
-               "lacache_kv_attend")
+        c._space = _made(q, (need,), torch.uint8, stream)
+    space = c._space
+    _check(_on(index, stream, _lib.lacache_kv_attend, c._ref, seqs._ref, q.data_ptr(), dtype, rows, q_heads, q_row,
+               max_new, c.d ** -0.5 if scale is None else scale, window, out[0].data_ptr(), out[1].data_ptr(),
+               space.data_ptr(), space.numel()), "lacache_kv_attend")
     return out
 
 

@@ -182,13 +182,6 @@ __device__ __forceinline__ u32x4 widen8(uint32_t lo, uint32_t hi) {
     return r;
 }
 
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-    bf16x2 w;  // (converted as a pair: one instruction)
-    w[0] = (__bf16)a;
-    w[1] = (__bf16)b;
-    return __builtin_bit_cast(uint32_t, w);
-}
-
 // The scale of the scores in units of log2 e, always above 0 (its sign and its being 0 are in the queries: load_q).
 __device__ __forceinline__ float scale_of(const AttendArgs& a) {
     return a.scale == 0.0f ? 1.0f : fabsf(a.scale) * kLog2e;

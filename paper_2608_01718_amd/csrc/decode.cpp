@@ -3,6 +3,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <atomic>
 #include <cmath>
 
 #include "kv.hpp"
@@ -49,15 +50,19 @@ bool to_rope(const lacache_rotary* r, int d, RopeArgs* out) {
     return true;
 }
 
-// Compute units of the current device; 0 on a HIP error.
+// Compute units of the current device; 0 on a HIP error.  (Asked once for each of the first 64 devices.)
 int compute_units() {
+    static std::atomic<int> known[64];
     int dev = 0, n = 0;
-    if (hipGetDevice(&dev) != hipSuccess ||
-        hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) {
-        (void)hipGetLastError();
-        return 0;
+    if (hipGetDevice(&dev) == hipSuccess) {
+        if (dev < 64 && (n = known[dev].load(std::memory_order_relaxed))) return n;
+        if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess) {
+            if (dev < 64) known[dev].store(n, std::memory_order_relaxed);
+            return n;
+        }
     }
-    return n;
+    (void)hipGetLastError();
+    return 0;
 }
 
 }  // namespace

@@ -2,6 +2,10 @@
 //
 // A token's keys of one head (turned by its position, if a table is given) or values are rounded once: to bfloat16, or
 // to 8-bit codes x * (top / m) with the scale m / top, m the largest magnitude of the d columns.
+//
+// Both are bound by memory: a tile of 32 tokens of one head passes through LDS, where its elements change from rows to
+// the tile's order, so that rows and tiles are read and written 16 bytes a lane.  A tile of which only some tokens are
+// concerned is written piece by piece, and read without LDS if they are few.
 #include "kv.hpp"
 #include "launch.hpp"
 
@@ -9,27 +13,55 @@ namespace lacache {
 
 namespace {
 
-// columns lane, lane + 64, ... of one head's row, turned
-__device__ inline void load_row(const char* src, int dtype, int d, int lane, const RopeArgs& rope, int64_t pos,
-                                float x[4]) {
-    auto get = [&](int c) { return dtype == 0 ? ((const float*)src)[c] : bf16_to_f32(((const uint16_t*)src)[c]); };
+// The tiles that new tokens of a sequence lie in: the first, how many.
+struct TileSpan {
+    KvSpan span;
+    int64_t first;
+    int count;
+};
+__device__ inline TileSpan tiles_of(const KvSeqs& s, int b) {
+    TileSpan t;
+    t.span = span_of(s, b);
+    const int64_t lo = t.span.pos0 < 0 ? 0 : t.span.pos0, hi = t.span.pos0 + t.span.n;  // positions lo .. hi - 1
+    t.first = lo >> 5;
+    t.count = hi > lo ? (int)(((hi - 1) >> 5) - t.first) + 1 : 0;
+    return t;
+}
+
+// A power of two of lanes that holds a head's columns by eights.
+constexpr int row_lanes(int dp) { return dp <= 64 ? 8 : dp <= 128 ? 16 : 32; }
+
+// Eight columns from c on of a row of keys, turned.
+template <bool F32>
+__device__ __forceinline__ void load_turned(const char* row, int c, const RopeArgs& rope, const float2* cs,
+                                            float (&x)[8]) {
+    load_row8<F32>(row, c, x);
     const int half = rope.rot / 2;
-    const int64_t p = pos < 0 ? 0 : pos >= rope.n_pos ? rope.n_pos - 1 : pos;
+    if (!rope.table || c >= rope.rot) return;
+    if (rope.pairs && c + 8 <= rope.rot) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const int c = lane + 64 * e;
-        x[e] = c < d ? get(c) : 0.0f;
-        if (rope.table && c < rope.rot) {
-            const int i = rope.pairs ? c >> 1 : c < half ? c : c - half;
-            const bool first = rope.pairs ? !(c & 1) : c < half;
-            const float2 cs = ((const float2*)rope.table)[p * half + i];
-            float a = x[e], b = get(rope.pairs ? c ^ 1 : first ? c + half : c - half);
-            if (!first) {
-                const float t = a;
-                a = b;
-                b = t;
-            }
-            turn(a, b, cs.x, cs.y);
+        for (int e = 0; e < 8; e += 2) turn(x[e], x[e + 1], cs[(c + e) / 2].x, cs[(c + e) / 2].y);
+    } else if (!rope.pairs && (c + 8 <= half || (c >= half && c + 8 <= rope.rot))) {
+        float other[8];
+        const bool first = c < half;
+        load_row8<F32>(row, first ? c + half : c - half, other);
+        const float2* w = cs + (first ? c : c - half);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float a = first ? x[e] : other[e], b = first ? other[e] : x[e];
+            turn(a, b, w[e].x, w[e].y);
+            x[e] = first ? a : b;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int col = c + e;
+            if (col >= rope.rot) break;
+            const bool first = rope.pairs ? !(col & 1) : col < half;
+            const int i = rope.pairs ? col >> 1 : first ? col : col - half;
+            const float o = load_row1<F32>(row, rope.pairs ? col ^ 1 : first ? col + half : col - half);
+            float a = first ? x[e] : o, b = first ? o : x[e];
+            turn(a, b, cs[i].x, cs[i].y);
             x[e] = first ? a : b;
         }
     }
@@ -37,105 +69,236 @@ __device__ inline void load_row(const char* src, int dtype, int d, int lane, con
 
 }  // namespace
 
-// A wave per (token, head): the query heads, the key heads, the value heads.  blockIdx.y steps through the new tokens
-// of sequence blockIdx.x.
-__global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
-    const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+// Workgroup x = parts b + part takes tile y (and every gridDim.y-th) of sequence b: the keys and values of head `part`,
+// or, from part `heads` on, a share of the queries of 32 rows.
+template <bool F32, int CT>
+__global__ __launch_bounds__(256) void k_kv_append(AppendArgs a, int parts, int turn_how) {
+    constexpr bool BYTES = CT != kKvBf16;
+    constexpr int CSZ = BYTES ? 1 : 2, ESZ = F32 ? 4 : 2;
+    __shared__ u32x4 tile[2][32 * 256 * CSZ / 16];  // keys, values, in the tile's order
     const KvPool& p = a.pool;
-    const bool bytes = p.type != kKvBf16;
-    const size_t esz = a.dtype == 0 ? 4 : 2;
-    const KvSpan span = span_of(a.seqs, blockIdx.x);
-    const int Hq = a.q ? a.q_heads : 0;
-    for (int i = blockIdx.y; i < span.n; i += gridDim.y) {
-        const int64_t row = span.row0 + i, pos = span.pos0 + i;
-        const int64_t page = pos < 0 ? -1 : page_of(p, a.seqs, blockIdx.x, pos);
+    const int tid = threadIdx.x, b = blockIdx.x / parts, part = blockIdx.x - b * parts;
+    const TileSpan t = tiles_of(a.seqs, b);
+
+    if (part >= p.heads) {  // queries
+        const int shares = parts - p.heads, share = part - p.heads;
+        const int items = turn_items(p.d, a.rope.rot, turn_how), of_row = a.q_heads * items;
+        for (int r0 = 32 * blockIdx.y; r0 < t.span.n; r0 += 32 * gridDim.y) {
+            const int rows = t.span.n - r0 < 32 ? t.span.n - r0 : 32;
+            for (int e = share * 256 + tid; e < rows * of_row; e += shares * 256) {
+                const int r = (int)((uint32_t)e / (uint32_t)of_row), in_row = e - r * of_row;
+                const int h = (int)((uint32_t)in_row / (uint32_t)items), i = in_row - h * items;
+                const int64_t row = t.span.row0 + r0 + r;
+                const char* x = a.q + (row * a.q_row + (int64_t)h * p.d) * ESZ;
+                char* y = a.q_out + (row * a.q_heads + h) * p.d * ESZ;
+                const float2* cs = table_row(a.rope, t.span.pos0 + r0 + r);
+                if (turn_how == kTurnHalves) turn_item<F32, kTurnHalves>(x, y, p.d, a.rope, cs, i, 1.0f);
+                else if (turn_how == kTurnPairs) turn_item<F32, kTurnPairs>(x, y, p.d, a.rope, cs, i, 1.0f);
+                else turn_item<F32, kTurnOne>(x, y, p.d, a.rope, cs, i, 1.0f);
+            }
+        }
+        return;
+    }
+
+    const int h = part, lanes = row_lanes(p.dp), at_once = 256 / lanes;
+    const int c = tid % lanes * 8, row_in = tid / lanes;
+    for (int k = blockIdx.y; k < t.count; k += gridDim.y) {
+        const int64_t pos = 32 * (t.first + k);  // of the tile's first token
+        const int64_t page = page_of(p, a.seqs, b, pos);
+        if (page < 0) continue;
+        // its tokens u0 .. u1 - 1 are new
+        const int64_t i0 = pos - t.span.pos0;  // row of the first token; may be negative
+        const int u0 = i0 < 0 ? (int)-i0 : 0, u1 = t.span.n - i0 < 32 ? (int)(t.span.n - i0) : 32, nu = u1 - u0;
         const int at = (int)(pos & ((1 << p.page_shift) - 1));
-        for (int h = wid; h < Hq + 2 * p.heads; h += 4) {
-            float x[4];
-            if (h < Hq) {
-                load_row(a.q + (row * a.q_row + (int64_t)h * p.d) * esz, a.dtype, p.d, lane, a.rope, pos, x);
+        __syncthreads();  // the last tile has been written
+        // rows of keys and then of values, a group of lanes each
+        for (int e = row_in; e < 2 * nu; e += at_once) {
+            const bool keys = e < nu;
+            const int u = u0 + (keys ? e : e - nu);
+            const int64_t row = t.span.row0 + i0 + u;
+            const char* src = keys ? a.k + (row * a.k_row + (int64_t)h * p.d) * ESZ
+                                   : a.v + (row * a.v_row + (int64_t)h * p.d) * ESZ;
+            float x[8] = {};
+            if (c < p.d) {
+                if (keys) load_turned<F32>(src, c, a.rope, a.rope.table ? table_row(a.rope, pos + u) : nullptr, x);
+                else load_row8<F32>(src, c, x);
+            }
+            if constexpr (BYTES) {
+                float m = 0.0f;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int64_t o = (row * a.q_heads + h) * p.d + lane + 64 * e;
-                    if (lane + 64 * e >= p.d) continue;
-                    if (a.dtype == 0) ((float*)a.q_out)[o] = x[e];
-                    else ((uint16_t*)a.q_out)[o] = f32_to_bf16(x[e]);
+                for (int q = 0; q < 8; ++q) m = fmaxf(m, fabsf(x[q]));
+                for (int o = lanes / 2; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, kWave));
+                const bool some = m >= kKvTiny;
+                const float top = CT == kKvFp8 ? 448.0f : 127.0f, inv = some ? top / m : 0.0f;
+                if (c == 0) (keys ? p.k_scale : p.v_scale)[scale_at(p, page, h, at + u)] = some ? m / top : 0.0f;
+                uint8_t code[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    const float y = fminf(fmaxf(x[q] * inv, -top), top);
+                    code[q] = CT == kKvInt8 ? (uint8_t)(int8_t)(int)rintf(y)
+                                            : (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(y, y, 0, false);
                 }
+                if (c < p.dp) {
+                    if (keys) {
+                        u32x2 w;
+                        __builtin_memcpy(&w, code, 8);
+                        *(u32x2*)((char*)tile[0] + k_place(u, c, true)) = w;
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) ((uint8_t*)tile[1])[v_place(u, c + q, true)] = code[q];
+                    }
+                }
+            } else if (c < p.dp) {
+                u32x4 w;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) w[q] = pack_bf16(x[2 * q], x[2 * q + 1]);
+                if (keys) {
+                    *(u32x4*)((char*)tile[0] + 2 * k_place(u, c, false)) = w;
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        ((uint16_t*)tile[1])[v_place(u, c + q, false)] = (uint16_t)(w[q >> 1] >> (16 * (q & 1)));
+                }
+            }
+        }
+        __syncthreads();
+        const int64_t base = tile_base(p, page, h, at) * CSZ;
+        const int pieces = 32 * p.dp * CSZ / 16;  // of 16 bytes
+        for (int e = tid; e < 2 * pieces; e += 256) {
+            const bool keys = e < pieces;
+            const int i = keys ? e : e - pieces;
+            const u32x4 w = tile[keys ? 0 : 1][i];
+            char* dst = (keys ? p.k : p.v) + base + (int64_t)i * 16;
+            if (nu == 32) {
+                *(u32x4*)dst = w;
                 continue;
             }
-            if (page < 0) continue;
-            const bool keys = h < Hq + p.heads;
-            const int hk = h - Hq - (keys ? 0 : p.heads);
-            RopeArgs rope = a.rope;
-            if (!keys) rope.table = nullptr;
-            load_row((keys ? a.k + row * a.k_row * esz : a.v + row * a.v_row * esz) + (int64_t)hk * p.d * esz, a.dtype,
-                     p.d, lane, rope, pos, x);
-            float m = fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3])));
-            m = wave_reduce(m, [](float u, float v) { return fmaxf(u, v); });
-            const bool some = m >= kKvTiny;
-            const float top = kv_top(p.type), inv = some ? top / m : 0.0f;
-            char* pool = (keys ? p.k : p.v);
-            const int64_t base = tile_base(p, page, hk, at);
+            auto is_new = [&](int u) { return u >= u0 && u < u1; };
+            // the tokens of the piece's 16 bytes (k_place, v_place)
+            if (keys) {
+                if constexpr (BYTES) {  // [b][e]
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int c = lane + 64 * e;
-                if (c >= p.dp) continue;
-                const int64_t o = base + (keys ? k_place(at & 31, c, bytes) : v_place(at & 31, c, bytes));
-                const float y = fminf(fmaxf(x[e] * inv, -top), top);
-                if (!bytes) ((uint16_t*)pool)[o] = f32_to_bf16(x[e]);
-                else if (p.type == kKvInt8) ((int8_t*)pool)[o] = (int8_t)(int)rintf(y);
-                else ((uint8_t*)pool)[o] = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(y, y, 0, false);
+                    for (int s = 0; s < 2; ++s)
+                        if (is_new(16 * s + (i & 15))) *(u32x2*)(dst + 8 * s) = u32x2{w[2 * s], w[2 * s + 1]};
+                } else if (is_new((i & 15) + 16 * ((i >> 6) & 1))) {
+                    *(u32x4*)dst = w;
+                }
+            } else {
+                const int g = (i >> 4) & 3;
+#pragma unroll
+                for (int q = 0; q < 16 / CSZ; ++q) {  // bfloat16 [s][i], 8 bits [y][s][i]
+                    if (!is_new(16 * ((q >> 2) & 1) + 4 * g + (q & 3))) continue;
+                    if constexpr (BYTES) ((uint8_t*)dst)[q] = (uint8_t)(w[q >> 2] >> (8 * (q & 3)));
+                    else ((uint16_t*)dst)[q] = (uint16_t)(w[q >> 1] >> (16 * (q & 1)));
+                }
             }
-            if (bytes && lane == 0)
-                (keys ? p.k_scale : p.v_scale)[scale_at(p, page, hk, at)] = some ? m / top : 0.0f;
         }
     }
 }
 
-// A wave per (token, head) of keys and of values.
-__global__ __launch_bounds__(256) void k_kv_read(KvPool p, KvSeqs s, void* k_out, void* v_out, int dtype) {
-    const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
-    const bool bytes = p.type != kKvBf16;
-    const KvSpan span = span_of(s, blockIdx.x);
-    for (int i = blockIdx.y; i < span.n; i += gridDim.y) {
-        const int64_t row = span.row0 + i, pos = span.pos0 + i;
-        const int64_t page = pos < 0 ? -1 : page_of(p, s, blockIdx.x, pos);
+// Workgroup x = heads b + h takes tile y (and every gridDim.y-th) of sequence b.
+template <bool F32, int CT>
+__global__ __launch_bounds__(256) void k_kv_read(KvPool p, KvSeqs s, char* k_out, char* v_out) {
+    constexpr bool BYTES = CT != kKvBf16;
+    constexpr int CSZ = BYTES ? 1 : 2, ESZ = F32 ? 4 : 2;
+    __shared__ u32x4 tile[2][32 * 256 * CSZ / 16];
+    const int tid = threadIdx.x, b = blockIdx.x / p.heads, h = blockIdx.x - b * p.heads;
+    const TileSpan t = tiles_of(s, b);
+    const int lanes = row_lanes(p.dp), at_once = 256 / lanes, c = tid % lanes * 8, row_in = tid / lanes;
+    // rows of positions that do not exist
+    const int before = t.span.pos0 < 0 ? (t.span.pos0 + t.span.n < 0 ? t.span.n : (int)-t.span.pos0) : 0;
+    for (int r = blockIdx.y * at_once + row_in; r < before; r += gridDim.y * at_once) {
+        const float zero[8] = {};
+        const int64_t o = ((t.span.row0 + r) * p.heads + h) * p.d * ESZ;
+        if (c < p.d && k_out) store_row8<F32>(k_out + o, c, zero);
+        if (c < p.d && v_out) store_row8<F32>(v_out + o, c, zero);
+    }
+    for (int k = blockIdx.y; k < t.count; k += gridDim.y) {
+        const int64_t pos = 32 * (t.first + k);
+        const int64_t page = page_of(p, s, b, pos);
+        const int64_t i0 = pos - t.span.pos0;
+        const int u0 = i0 < 0 ? (int)-i0 : 0, u1 = t.span.n - i0 < 32 ? (int)(t.span.n - i0) : 32, nu = u1 - u0;
         const int at = (int)(pos & ((1 << p.page_shift) - 1));
-        for (int h = wid; h < 2 * p.heads; h += 4) {
-            const bool keys = h < p.heads;
-            const int hk = keys ? h : h - p.heads;
-            void* out = keys ? k_out : v_out;
-            if (!out) continue;
-            const int64_t base = page < 0 ? 0 : tile_base(p, page, hk, at);
-            const float sc = bytes && page >= 0 ? (keys ? p.k_scale : p.v_scale)[scale_at(p, page, hk, at)] : 1.0f;
-            for (int c = lane; c < p.d; c += 64) {
-                float x = 0.0f;
-                if (page >= 0)
-                    x = kv_value(keys ? p.k : p.v, base + (keys ? k_place(at & 31, c, bytes) : v_place(at & 31, c, bytes)),
-                                 p.type) * sc;
-                const int64_t o = (row * p.heads + hk) * p.d + c;
-                if (dtype == 0) ((float*)out)[o] = x;
-                else ((uint16_t*)out)[o] = f32_to_bf16(x);
+        const int64_t base = page < 0 ? 0 : tile_base(p, page, h, at) * CSZ;
+        const bool shared = nu > 4 && page >= 0;  // (uniform)
+        if (shared) {
+            const int pieces = 32 * p.dp * CSZ / 16;
+            __syncthreads();
+            for (int e = tid; e < 2 * pieces; e += 256) {
+                const bool keys = e < pieces;
+                const int i = keys ? e : e - pieces;
+                tile[keys ? 0 : 1][i] = *(const u32x4*)((keys ? p.k : p.v) + base + (int64_t)i * 16);
             }
+            __syncthreads();
+        }
+        for (int e = row_in; e < 2 * nu; e += at_once) {
+            const bool keys = e < nu;
+            char* out = keys ? k_out : v_out;
+            if (!out || c >= p.d) continue;
+            const int u = u0 + (keys ? e : e - nu);
+            float x[8] = {};
+            if (page >= 0) {
+                const char* src = shared ? (const char*)tile[keys ? 0 : 1] : (keys ? p.k : p.v) + base;
+                const float sc = BYTES ? (keys ? p.k_scale : p.v_scale)[scale_at(p, page, h, at + u)] : 1.0f;
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    x[q] = kv_value(src, keys ? k_place(u, c + q, BYTES) : v_place(u, c + q, BYTES), CT);
+                    if constexpr (BYTES) x[q] *= sc;
+                }
+            }
+            store_row8<F32>(out + ((t.span.row0 + i0 + u) * p.heads + h) * p.d * ESZ, c, x);
         }
     }
 }
 
-static dim3 token_grid(const KvSeqs& s, int max_new) {
-    int64_t most = max_new > 0 && max_new < s.rows ? max_new : s.rows;
-    return dim3((unsigned)s.n_seq, (unsigned)(most > 1024 ? 1024 : most));
+namespace {
+
+// Tiles that the new tokens of a sequence can touch, for the launch shape (the kernels step on from there).
+unsigned tile_steps(const KvSeqs& s, int max_new) {
+    const int64_t most = max_new > 0 && max_new < s.rows ? max_new : s.rows;
+    const int64_t tiles = most <= 1 ? 1 : (most + 31) / 32 + 1;
+    return (unsigned)(tiles > 4096 ? 4096 : tiles);
 }
+
+template <class F>
+void by_types(int dtype, int type, F f) {
+    auto pick = [&](auto f32) {
+        if (type == kKvBf16) f(f32, std::integral_constant<int, kKvBf16>{});
+        else if (type == kKvFp8) f(f32, std::integral_constant<int, kKvFp8>{});
+        else f(f32, std::integral_constant<int, kKvInt8>{});
+    };
+    if (dtype == 0) pick(std::true_type{});
+    else pick(std::false_type{});
+}
+
+}  // namespace
 
 hipError_t launch_kv_append(const AppendArgs& a, int max_new, hipStream_t s) {
     if (a.seqs.rows <= 0 || a.seqs.n_seq <= 0) return hipSuccess;
-    k_kv_append<<<token_grid(a.seqs, max_new), dim3(256), 0, s>>>(a);
+    const unsigned steps = tile_steps(a.seqs, max_new);
+    const int how = a.q ? turn_by(a.pool.d, a.rope) : 0;
+    // workgroups that share the queries of 32 rows: two items a thread, if the rows are so many
+    const int64_t items = a.q ? (int64_t)(steps == 1 ? 1 : 32) * a.q_heads * turn_items(a.pool.d, a.rope.rot, how) : 0;
+    int64_t shares = (items + 511) / 512;
+    shares = shares > 64 ? 64 : shares;
+    const int parts = a.pool.heads + (int)shares;
+    if ((int64_t)a.seqs.n_seq * parts > INT32_MAX) return hipErrorInvalidValue;
+    by_types(a.dtype, a.pool.type, [&](auto f32, auto ct) {
+        k_kv_append<decltype(f32)::value, decltype(ct)::value>
+            <<<dim3((unsigned)(a.seqs.n_seq * parts), steps), dim3(256), 0, s>>>(a, parts, how);
+    });
     return hipGetLastError();
 }
 
 hipError_t launch_kv_read(const KvPool& pool, const KvSeqs& seqs, void* k_out, void* v_out, int dtype, int max_new,
                           hipStream_t s) {
     if (seqs.rows <= 0 || seqs.n_seq <= 0) return hipSuccess;
-    k_kv_read<<<token_grid(seqs, max_new), dim3(256), 0, s>>>(pool, seqs, k_out, v_out, dtype);
+    if ((int64_t)seqs.n_seq * pool.heads > INT32_MAX) return hipErrorInvalidValue;
+    by_types(dtype, pool.type, [&](auto f32, auto ct) {
+        k_kv_read<decltype(f32)::value, decltype(ct)::value>
+            <<<dim3((unsigned)(seqs.n_seq * pool.heads), tile_steps(seqs, max_new)), dim3(256), 0, s>>>(
+                pool, seqs, (char*)k_out, (char*)v_out);
+    });
     return hipGetLastError();
 }
 

@@ -23,36 +23,21 @@ __global__ __launch_bounds__(256) void k_rope_table(float2* __restrict__ table, 
     }
 }
 
-// One element a thread, whatever the strides and alignment.
-__global__ __launch_bounds__(256) void k_rope_any(const void* x, void* y, int dtype, int64_t rows, int H, int d,
-                                                  int64_t x_row, int64_t x_head, int64_t y_row, int64_t y_head,
-                                                  const int32_t* __restrict__ pos, RopeArgs rope, bool backward) {
-    // a pair, or a column that stays, is one item: y may be x
-    const int half = rope.rot / 2, items = d - half;
-    const int64_t total = rows * H * items, step = (int64_t)gridDim.x * 256;
+// A thread an item (turn_item) of a head of a row.
+template <bool F32, int BY>
+__global__ __launch_bounds__(256) void k_rope(const char* x, char* y, int64_t rows, int H, int d, int64_t x_row,
+                                              int64_t x_head, int64_t y_row, int64_t y_head,
+                                              const int32_t* __restrict__ pos, RopeArgs rope, float sign) {
+    constexpr int ESZ = F32 ? 4 : 2;
+    const int items = turn_items(d, rope.rot, BY);
+    const uint32_t of_row = (uint32_t)(H * items);
+    const int64_t total = rows * of_row, step = (int64_t)gridDim.x * 256;
     for (int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x; n < total; n += step) {
-        const int64_t r = n / items / H;
-        const int i = (int)(n % items), h = (int)(n / items % H);
-        const int64_t xi = r * x_row + h * x_head, yi = r * y_row + h * y_head;
-        auto get = [&](int c) {
-            return dtype == 0 ? ((const float*)x)[xi + c] : bf16_to_f32(((const uint16_t*)x)[xi + c]);
-        };
-        auto put = [&](int c, float v) {
-            if (dtype == 0) ((float*)y)[yi + c] = v;
-            else ((uint16_t*)y)[yi + c] = f32_to_bf16(v);
-        };
-        if (i >= half) {
-            put(i + half, get(i + half));
-            continue;
-        }
-        int64_t p = pos[r];
-        p = p < 0 ? 0 : p >= rope.n_pos ? rope.n_pos - 1 : p;
-        const float2 cs = ((const float2*)rope.table)[p * half + i];
-        const int ca = rope.pairs ? 2 * i : i, cb = rope.pairs ? 2 * i + 1 : i + half;
-        float a = get(ca), b = get(cb);
-        turn(a, b, cs.x, backward ? -cs.y : cs.y);
-        put(ca, a);
-        put(cb, b);
+        const int64_t r = (total >> 32) == 0 ? (int64_t)((uint32_t)n / of_row) : n / of_row;
+        const uint32_t in_row = (uint32_t)(n - r * of_row);
+        const int h = (int)(in_row / (uint32_t)items), i = (int)(in_row - h * items);
+        turn_item<F32, BY>(x + (r * x_row + h * x_head) * ESZ, y + (r * y_row + h * y_head) * ESZ, d, rope,
+                           table_row(rope, pos[r]), i, sign);
     }
 }
 
@@ -68,9 +53,21 @@ hipError_t launch_rope(const void* x, void* y, int dtype, int64_t rows, int H, i
                        int64_t y_row, int64_t y_head, const int32_t* pos, const RopeArgs& rope, bool backward,
                        hipStream_t s) {
     if (rows <= 0) return hipSuccess;
-    const int64_t items = rows * H * (d - rope.rot / 2);
-    k_rope_any<<<dim3((unsigned)grid_blocks((items + 255) / 256)), dim3(256), 0, s>>>(
-        x, y, dtype, rows, H, d, x_row, x_head, y_row, y_head, pos, rope, backward);
+    const TurnBy by = turn_by(d, rope);
+    const int64_t items = rows * H * turn_items(d, rope.rot, by);
+    const dim3 grid((unsigned)grid_blocks((items + 255) / 256)), block(256);
+    const float sign = backward ? -1.0f : 1.0f;
+    auto go = [&](auto f32, auto how) {
+        k_rope<decltype(f32)::value, decltype(how)::value><<<grid, block, 0, s>>>(
+            (const char*)x, (char*)y, rows, H, d, x_row, x_head, y_row, y_head, pos, rope, sign);
+    };
+    auto pick = [&](auto f32) {
+        if (by == kTurnHalves) go(f32, std::integral_constant<int, kTurnHalves>{});
+        else if (by == kTurnPairs) go(f32, std::integral_constant<int, kTurnPairs>{});
+        else go(f32, std::integral_constant<int, kTurnOne>{});
+    };
+    if (dtype == 0) pick(std::true_type{});
+    else pick(std::false_type{});
     return hipGetLastError();
 }
 

@@ -93,6 +93,13 @@ typedef u32x2 u32x2_any __attribute__((aligned(2)));
 
 __device__ inline uint16_t f32_to_bf16(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
 
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+    bf16x2 w;  // (converted as a pair: one instruction)
+    w[0] = (__bf16)a;
+    w[1] = (__bf16)b;
+    return __builtin_bit_cast(uint32_t, w);
+}
+
 // Largest code of the 8-bit types, and the magnitude below which a head is stored as zeros (its reciprocal, times the
 // largest code, would overflow).
 __device__ inline float kv_top(int type) { return type == kKvFp8 ? 448.0f : 127.0f; }
@@ -105,6 +112,101 @@ __device__ inline void turn(float& a, float& b, float c, float s) {
     const float x = a * c, y = b * s, z = b * c, w = a * s;
     a = x - y;
     b = z + w;
+}
+
+// Eight elements of activations, at any element boundary.
+template <bool F32>
+__device__ __forceinline__ void load_row8(const char* row, int c, float (&x)[8]) {
+    if constexpr (F32) {
+        const f32x4 a = *(const f32x4_any*)(row + c * 4), b = *(const f32x4_any*)(row + c * 4 + 16);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = a[e], x[4 + e] = b[e];
+    } else {
+        const u32x4 w = *(const u32x4_any*)(row + c * 2);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            x[2 * e] = __uint_as_float(w[e] << 16);
+            x[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+        }
+    }
+}
+template <bool F32>
+__device__ __forceinline__ void store_row8(char* row, int c, const float (&x)[8]) {
+    if constexpr (F32) {
+        *(f32x4_any*)(row + c * 4) = f32x4{x[0], x[1], x[2], x[3]};
+        *(f32x4_any*)(row + c * 4 + 16) = f32x4{x[4], x[5], x[6], x[7]};
+    } else {
+        u32x4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = pack_bf16(x[2 * e], x[2 * e + 1]);
+        *(u32x4_any*)(row + c * 2) = w;
+    }
+}
+template <bool F32>
+__device__ __forceinline__ float load_row1(const char* row, int c) {
+    return F32 ? ((const float*)row)[c] : bf16_to_f32(((const uint16_t*)row)[c]);
+}
+template <bool F32>
+__device__ __forceinline__ void store_row1(char* row, int c, float x) {
+    if constexpr (F32) ((float*)row)[c] = x;
+    else ((uint16_t*)row)[c] = f32_to_bf16(x);
+}
+
+// How a row of a head is turned, in items that no other item's columns overlap (the result may be written over the input):
+// eight columns each with their cosines and sines (pairs of neighbours), sixteen (two times eight, half a head apart), or
+// a pair at a time where the columns are not whole eights.
+enum TurnBy { kTurnOne = 0, kTurnPairs = 1, kTurnHalves = 2 };
+inline TurnBy turn_by(int d, const RopeArgs& r) {
+    return d % 8 != 0 ? kTurnOne : r.pairs ? (r.rot % 8 == 0 ? kTurnPairs : kTurnOne) : r.rot % 16 == 0 ? kTurnHalves : kTurnOne;
+}
+__host__ __device__ inline int turn_items(int d, int rot, int by) {
+    return by == kTurnPairs ? d / 8 : by == kTurnHalves ? d / 8 - rot / 16 : d - rot / 2;
+}
+// Item i of a head: from x to y, cs the table's row of its position, sign -1 for the transposed rotation.
+template <bool F32, int BY>
+__device__ __forceinline__ void turn_item(const char* x, char* y, int d, const RopeArgs& rope, const float2* cs, int i,
+                                          float sign) {
+    const int half = rope.rot / 2;
+    float a[8], b[8];
+    if constexpr (BY == kTurnOne) {
+        if (i >= half) {
+            store_row1<F32>(y, i + half, load_row1<F32>(x, i + half));
+            return;
+        }
+        const int ca = rope.pairs ? 2 * i : i, cb = rope.pairs ? 2 * i + 1 : i + half;
+        float u = load_row1<F32>(x, ca), v = load_row1<F32>(x, cb);
+        turn(u, v, cs[i].x, sign * cs[i].y);
+        store_row1<F32>(y, ca, u);
+        store_row1<F32>(y, cb, v);
+    } else if constexpr (BY == kTurnPairs) {
+        load_row8<F32>(x, 8 * i, a);
+        if (8 * i < rope.rot) {
+            const f32x4 p = *(const f32x4_any*)&cs[4 * i], q = *(const f32x4_any*)&cs[4 * i + 2];
+            turn(a[0], a[1], p[0], sign * p[1]);
+            turn(a[2], a[3], p[2], sign * p[3]);
+            turn(a[4], a[5], q[0], sign * q[1]);
+            turn(a[6], a[7], q[2], sign * q[3]);
+        }
+        store_row8<F32>(y, 8 * i, a);
+    } else {
+        const bool turns = 16 * i < rope.rot;
+        const int c = turns ? 8 * i : 8 * i + half;  // behind the turned columns: one eight an item
+        load_row8<F32>(x, c, a);
+        if (turns) {
+            load_row8<F32>(x, c + half, b);
+            f32x4 p[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) p[e] = *(const f32x4_any*)&cs[c + 2 * e];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) turn(a[e], b[e], p[e / 2][2 * (e & 1)], sign * p[e / 2][2 * (e & 1) + 1]);
+            store_row8<F32>(y, c + half, b);
+        }
+        store_row8<F32>(y, c, a);
+    }
+}
+__device__ inline const float2* table_row(const RopeArgs& rope, int64_t pos) {
+    pos = pos < 0 ? 0 : pos >= rope.n_pos ? rope.n_pos - 1 : pos;
+    return (const float2*)rope.table + pos * (rope.rot / 2);
 }
 
 hipError_t launch_rope_table(float* table, int64_t first, int64_t n, int rot, double base, double factor,
