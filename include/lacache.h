@@ -488,7 +488,10 @@ int lacache_kv_read(const lacache_kv *kv, const lacache_seqs *seqs, void *k_out,
  *   max_new    a bound on the new tokens of a sequence (for the launch shape
  *              alone; 0: not known)
  *   workspace  lacache_kv_attend_workspace bytes of device memory, 16-byte
- *              aligned, for this call alone while it runs
+ *              aligned, zero before the first call that uses them; a call
+ *              leaves its counters there at zero.  For one call at a time:
+ *              calls that overlap on one workspace give wrong results, until
+ *              it is cleared again
  * EINVAL too if workspace_bytes is less.
  */
 int64_t lacache_kv_attend_workspace(const lacache_kv *kv, lacache_dtype dtype, int32_t n_seq, int32_t q_heads,

@@ -499,16 +499,17 @@ def _rows(t: torch.Tensor, heads: int, d: int, index: int, dtype, name: str) -> 
     return stride[0]
 
 
-def _made(like: torch.Tensor, shape, dtype, stream):
-    """An empty tensor on the GPU of `like` that belongs to the stream the call runs on."""
+def _made(like: torch.Tensor, shape, dtype, stream, zeros=False):
+    """An empty (or zero) tensor on the GPU of `like` that belongs to the stream the call runs on."""
+    make = like.new_zeros if zeros else like.new_empty
     if stream is None:
-        return like.new_empty(shape, dtype=dtype)
+        return make(shape, dtype=dtype)
     if not isinstance(stream, torch.cuda.Stream):
         handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
         stream = torch.cuda.ExternalStream(handle, device=like.device) if handle else \
             torch.cuda.default_stream(like.device)
     with torch.cuda.stream(stream):
-        return like.new_empty(shape, dtype=dtype)
+        return make(shape, dtype=dtype)
 
 
 def _given(t: torch.Tensor, shape, dtype, index: int, name: str) -> torch.Tensor:
@@ -708,7 +709,7 @@ def lacache_kv_attend(c: KVCache, q, seqs: Sequences, scale=None, window: int = 
     if need is None:
         need = c._need[key] = lacache_kv_attend_workspace(c, *key)
     if c._space is None or c._space.numel() < need:
-        c._space = _made(q, (need,), torch.uint8, stream)
+        c._space = _made(q, (need,), torch.uint8, stream, zeros=True)
     space = c._space
     _check(_on(index, stream, _lib.lacache_kv_attend, c._ref, seqs._ref, q.data_ptr(), dtype, rows, q_heads, q_row,
                max_new, c.d ** -0.5 if scale is None else scale, window, out[0].data_ptr(), out[1].data_ptr(),

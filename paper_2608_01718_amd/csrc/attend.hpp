@@ -11,7 +11,8 @@
 //
 // The work is the linear space (sequence, kv head, row group, tile), cut into equal ranges, one a workgroup, from the
 // lengths on the device: ragged batches and single long contexts alike fill the chip.  A row group whose tiles lie in
-// more than one range is joined by k_attend_join from the partial sums that the ranges leave in the workspace.
+// more than one range is joined from the partial sums that the ranges leave in the workspace: by the launch that follows
+// (k_attend.hip), or, where there is little to do, by whichever of its workgroups ends last.
 #pragma once
 
 #include "kv.hpp"
@@ -41,17 +42,21 @@ struct AttendPlan {
     int workers, waves;  // workgroups of the launch, and the waves of each
     int chunk_shift;   // the work is dealt out in chunks of this many tiles (a shift), so that counts fit in 32 bits
     uint32_t group_magic, group_bits;  // row / group = row * magic >> bits
+    int join_here;     // parts are joined by the workgroup that ends last; otherwise by the launch that follows
+    uint32_t* done;    // [kMaxWorkers] parts that are there of the row group that begins with a worker; 0 between launches
     struct AttendSplit* split;  // [workers]: the row group whose last part a worker had
     float* part_o;     // [2 workers][group rows][dp] partial sums of values
     float2* part_ml;   // [2 workers][group rows] their maxima and sums of weights
 };
 
-// A row group of which several workers had a part, the last of them the one whose entry this is.
+constexpr int kMaxWorkers = 4096;
+
+// A row group that several workers have parts of, the last of them the one whose entry in AttendPlan::split this is.
 struct alignas(16) AttendSplit {
     int seq_row0, head0;   // the sequence's first row, the first query head
     int row, n_rows;       // rows row .. row + n_rows - 1 of the sequence's (0: there is no such row group)
-    int worker0;           // the first of its workers
-    int unused[3];
+    int worker0, parts;    // the first of its workers, their number
+    int unused[2];
 };
 
 // What the work of a sequence is: its rows and their groups, its tiles.
@@ -521,7 +526,108 @@ __device__ __forceinline__ float lse_of(float m, float l) {
     return l == 0.0f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-template <int DP, int CT, int R, bool F32>
+// Where a worker's part lies: its second slot if the row group goes on after it.
+__device__ __forceinline__ int64_t part_of(const AttendPlan& p, int worker, bool goes_on) {
+    return (2 * (int64_t)worker + (goes_on ? 1 : 0)) << p.group_shift;
+}
+
+struct Joined {
+    float m = -__builtin_inff(), l = 0.0f;
+    f32x4 o{0, 0, 0, 0};
+    __device__ __forceinline__ void add(float m2, float l2, f32x4 o2) {
+        if (m2 == -__builtin_inff()) return;
+        const float M = fmaxf(m, m2);
+        const float f = __builtin_amdgcn_exp2f(m - M), g = __builtin_amdgcn_exp2f(m2 - M);
+        l = l * f + l2 * g;
+        o = o * f + o2 * g;
+        m = M;
+    }
+};
+
+// ---------------------------------------------------------------------------
+// The join within the launch, for small calls (AttendPlan::join_here).  Parts are written and read with device-wide (sc1)
+// accesses alone, so the hand-over of last_workgroup_wait holds for them: every workgroup of a row group waits for its
+// stores, counts itself, and the one that counts last reads all parts and leaves the counter at 0.  Nobody waits for
+// another.
+// ---------------------------------------------------------------------------
+constexpr int kDeviceWide = 16;  // the sc1 bit of a buffer access
+
+template <int DP>
+__device__ __forceinline__ void store_part(const AttendPlan& p, int64_t part, int row, int col, f32x4 x) {
+    const auto r = __builtin_amdgcn_make_buffer_rsrc(p.part_o + part * DP, 0, DP * 4 << p.group_shift, 0x00020000);
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), r, (row * DP + col) * 4, 0, kDeviceWide);
+}
+__device__ __forceinline__ void store_part_ml(const AttendPlan& p, int64_t part, int row, float m, float l) {
+    const auto r = __builtin_amdgcn_make_buffer_rsrc(p.part_ml + part, 0, 8 << p.group_shift, 0x00020000);
+    __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(m), __float_as_uint(l)}, r, row * 8, 0, kDeviceWide);
+}
+
+// After a workgroup's part of a row group has been stored: counts it, and joins the parts if it is the last.  scratch:
+// THREADS f32x4 and float2 of LDS that nothing else uses meanwhile.  A group of dp / 4 lanes takes a row, or, with few
+// rows, every so many parts of one.
+template <int THREADS, int DP, bool F32>
+__device__ __forceinline__ void join_parts(const AttendArgs& a, const AttendPlan& p, const AttendSplit& s,
+                                           f32x4* scratch) {
+    __shared__ int last;
+    const int tid = fresh_lane() + (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) << 6);  // (nothing kept from before)
+    last_workgroup_wait();
+    __syncthreads();
+    if (tid == 0) {
+        uint32_t* done = p.done + s.worker0;
+        last = __hip_atomic_fetch_add(done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)s.parts - 1;
+        if (last) __hip_atomic_store(done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (!last) return;
+    constexpr int LANES = DP / 4, GROUPS = THREADS / LANES;
+    int of_row = 1;  // lane groups on a row
+    while (2 * of_row * s.n_rows <= GROUPS) of_row *= 2;
+    const int rows = GROUPS / of_row, g = tid / LANES, col = tid % LANES * 4, sub = g % of_row;
+    float2* ml_of = (float2*)(scratch + THREADS);
+    for (int row0 = 0; row0 < s.n_rows; row0 += rows) {
+        const int row = row0 + g / of_row;
+        const bool live = g < rows * of_row && row < s.n_rows;
+        Joined x;
+        if (live)
+            for (int k0 = sub; k0 < s.parts; k0 += 4 * of_row) {
+                float2 ml[4];
+                f32x4 o[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int k = k0 + u * of_row < s.parts ? k0 + u * of_row : s.parts - 1;
+                    const int64_t at = part_of(p, s.worker0 + k, k < s.parts - 1) + row;
+                    const uint64_t w = __hip_atomic_load((uint64_t*)(p.part_ml + at), __ATOMIC_RELAXED,
+                                                         __HIP_MEMORY_SCOPE_AGENT);
+                    ml[u] = make_float2(__uint_as_float((uint32_t)w), __uint_as_float((uint32_t)(w >> 32)));
+                    const uint64_t* src = (const uint64_t*)(p.part_o + at * DP + col);
+                    const uint64_t v0 = __hip_atomic_load(src, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT),
+                                   v1 = __hip_atomic_load(src + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    o[u] = f32x4{__uint_as_float((uint32_t)v0), __uint_as_float((uint32_t)(v0 >> 32)),
+                                 __uint_as_float((uint32_t)v1), __uint_as_float((uint32_t)(v1 >> 32))};
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    if (k0 + u * of_row < s.parts) x.add(ml[u].x, ml[u].y, o[u]);
+            }
+        if (of_row > 1) {  // (then there is one round)
+            ml_of[tid] = make_float2(x.m, x.l);
+            scratch[tid] = x.o;
+            __syncthreads();
+            if (sub == 0 && live)
+                for (int k = 1; k < of_row; ++k)
+                    x.add(ml_of[tid + k * LANES].x, ml_of[tid + k * LANES].y, scratch[tid + k * LANES]);
+        }
+        if (live && sub == 0) {
+            const int r = s.row + row, i = token_of(p, r);
+            const int64_t at = ((int64_t)s.seq_row0 + i) * a.q_heads + s.head0 + (r - i * a.group);
+            if (col < a.pool.d) store4<F32>(a, at * a.pool.d + col, x.o * (x.l == 0.0f ? 0.0f : 1.0f / x.l));
+            if (col == 0 && a.lse) a.lse[at] = lse_of(x.m, x.l);
+        }
+    }
+}
+
+// HERE: parts are joined within the launch.
+template <int DP, int CT, int R, bool F32, bool HERE>
 __global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(AttendArgs a, AttendPlan p) {
     using A = Attend<DP, CT, R, F32>;
     constexpr int GR = 16 * R;  // rows of a row group
@@ -532,7 +638,7 @@ __global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(A
 
     AttendRange range = attend_range<4>(a, p, worker, 4 >> (p.chunk_shift < 2 ? p.chunk_shift : 2));
     if (range.at >= range.end) {
-        if (tid == 0) p.split[worker].n_rows = 0;
+        if (!HERE && tid == 0) p.split[worker].n_rows = 0;
         return;
     }
     AttendSplit split{};
@@ -542,7 +648,7 @@ __global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(A
     // A segment: tiles tile0 .. tile1 - 1 of one row group
     struct Segment {
         int h, rg, tile0, tile1, row0, rows, n_rows;  // n_rows: rows in the group
-        int first, b, item0;                          // item0: the row group's first item
+        int first, b, item0, items;                   // the row group's first item, its items
         bool starts, ends;                            // whether it holds the first and the last tile
         int seen0, seen1, all0, all1;                 // positions that one of the rows, that every row sees
     };
@@ -585,6 +691,7 @@ __global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(A
         const int left = range.end - range.at, c1 = s.chunks - c0 <= left ? s.chunks : c0 + left;
         range.at += c1 - c0;
         g.item0 = range.before + unit * s.chunks;
+        g.items = s.chunks;
         g.starts = c0 == 0;
         g.ends = c1 == s.chunks;
         g.tile0 = c0 << p.chunk_shift;
@@ -638,17 +745,24 @@ __global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(A
             open();
         }
         const bool whole = old.starts && old.ends;
-        const int64_t slot = (2 * (int64_t)worker + (old.ends ? 0 : 1)) * GR;
-        float* part_o = p.part_o + slot * DP;
-        float2* part_ml = p.part_ml + slot;
-        if (old.ends && !old.starts)  // the workers before this one had its other parts
-            split = AttendSplit{old.row0, old.h * a.group, old.rg * GR, old.n_rows,
-                                (int)((uint32_t)old.item0 / (uint32_t)range.per), {}};
+        const int64_t part = part_of(p, worker, !old.ends);
+        AttendSplit u0{};
+        if (!whole) {
+            const int first = (int)((uint32_t)old.item0 / (uint32_t)range.per);
+            const int end = (int)((uint32_t)(old.item0 + old.items - 1) / (uint32_t)range.per);
+            u0 = AttendSplit{old.row0, old.h * a.group, old.rg * GR, old.n_rows, first, end - first + 1, {}};
+            if (old.ends) split = u0;
+        }
         // four columns of a row of the group; its maximum and sum with the first of them
         auto put = [&](int row, int col, f32x4 x, float m, float l) {
             if (!whole) {
-                *(f32x4*)(part_o + row * DP + col) = x;
-                if (col == 0) part_ml[row] = make_float2(m, l);
+                if constexpr (HERE) {
+                    store_part<DP>(p, part, row, col, x);
+                    if (col == 0) store_part_ml(p, part, row, m, l);
+                } else {
+                    *(f32x4*)(p.part_o + (part + row) * DP + col) = x;
+                    if (col == 0) p.part_ml[part + row] = make_float2(m, l);
+                }
                 return;
             }
             const int r = old.rg * GR + row, i = token_of(p, r), head = old.h * a.group + (r - i * a.group);
@@ -691,8 +805,12 @@ __global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(A
                     put(16 * r + row, c0 + col, x, M, L);
                 }
             }
+        if constexpr (HERE) {
+            static_assert(sizeof(so) >= 256 * 24, "the join's scratch");
+            if (!whole) join_parts<256, DP, F32>(a, p, u0, (f32x4*)&so[0][0][0]);
+        }
     }
-    if (tid == 0) p.split[worker] = split;
+    if (!HERE && tid == 0) p.split[worker] = split;
 }
 
 }  // namespace lacache

@@ -215,10 +215,11 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
         w.reduce();
 
         const bool whole = starts && ends;
-        const int64_t slot = (2 * (int64_t)worker + (ends ? 0 : 1)) * W::ROWS;
-        if (ends && !starts)
-            split = AttendSplit{s.row0, h * a.group, r0, n_rows,
-                                (int)((uint32_t)(range.before + unit * s.chunks) / (uint32_t)range.per), {}};
+        const int64_t slot = part_of(p, worker, !ends);
+        if (ends && !starts) {
+            const int first = (int)((uint32_t)(range.before + unit * s.chunks) / (uint32_t)range.per);
+            split = AttendSplit{s.row0, h * a.group, r0, n_rows, first, worker - first + 1, {}};
+        }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int row = 16 * (r * WAVES + wid) + n;
@@ -255,14 +256,18 @@ hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t s
     auto go = [&](auto ct) {
         constexpr int CT = decltype(ct)::value;
         if (a.dtype == 0) {
-            if (p.group_shift == 4) k_attend<DP, CT, 1, true><<<grid, block, 0, s>>>(a, p);
+            if (p.join_here) k_attend<DP, CT, 1, true, true><<<grid, block, 0, s>>>(a, p);
+            else if (p.group_shift == 4) k_attend<DP, CT, 1, true, false><<<grid, block, 0, s>>>(a, p);
             else if constexpr (DP <= 192) k_attend_wide<DP, CT, 4, 1, true><<<grid, block, 0, s>>>(a, p);
             return;
         }
         switch (p.group_shift) {
-            case 4: k_attend<DP, CT, 1, false><<<grid, block, 0, s>>>(a, p); break;
+            case 4:
+                if (p.join_here) k_attend<DP, CT, 1, false, true><<<grid, block, 0, s>>>(a, p);
+                else k_attend<DP, CT, 1, false, false><<<grid, block, 0, s>>>(a, p);
+                break;
             case 5:
-                if constexpr (DP <= 128) k_attend<DP, CT, 2, false><<<grid, block, 0, s>>>(a, p);
+                if constexpr (DP <= 128) k_attend<DP, CT, 2, false, false><<<grid, block, 0, s>>>(a, p);
                 break;
             case 6:
                 if constexpr (DP <= 192) k_attend_wide<DP, CT, 4, 1, false><<<grid, block, 0, s>>>(a, p);

@@ -5,22 +5,10 @@
 namespace lacache {
 
 // The row groups that several workers had parts of: each of the workgroups (w, .) joins rows of the group that ended with
-// worker w.  A worker's part of a group that goes on after it lies in its second slot.
-__device__ __forceinline__ int64_t part_at(const AttendPlan& p, const AttendSplit& s, int parts, int k, int row) {
-    return (((2 * (int64_t)(s.worker0 + k)) + (k < parts - 1 ? 1 : 0)) << p.group_shift) + row;
+// worker w.
+__device__ __forceinline__ int64_t part_at(const AttendPlan& p, const AttendSplit& s, int k, int row) {
+    return part_of(p, s.worker0 + k, k < s.parts - 1) + row;
 }
-struct Joined {
-    float m = -__builtin_inff(), l = 0.0f;
-    f32x4 o{0, 0, 0, 0};
-    __device__ __forceinline__ void add(float m2, float l2, f32x4 o2) {
-        if (m2 == -__builtin_inff()) return;
-        const float M = fmaxf(m, m2);
-        const float f = __builtin_amdgcn_exp2f(m - M), g = __builtin_amdgcn_exp2f(m2 - M);
-        l = l * f + l2 * g;
-        o = o * f + o2 * g;
-        m = M;
-    }
-};
 __device__ __forceinline__ void store_joined(const AttendArgs& a, const AttendPlan& p, const AttendSplit& s, int row,
                                              int col, const Joined& x) {
     const int r = s.row + row, i = token_of(p, r);
@@ -38,7 +26,7 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, AttendPlan p)
     const AttendSplit s = p.split[blockIdx.x];
     const int dp = a.pool.dp, lanes = dp / 4, rows = 256 / lanes;
     const int col = threadIdx.x % lanes * 4, row_in = threadIdx.x / lanes;
-    const int parts = (int)blockIdx.x - s.worker0 + 1;
+    const int parts = s.parts;
     if (row_in >= rows) return;
     for (int row = blockIdx.y * rows + row_in; row < s.n_rows; row += gridDim.y * rows) {
         Joined x;
@@ -47,7 +35,7 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, AttendPlan p)
             f32x4 o[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const int64_t at = part_at(p, s, parts, k0 + u < parts ? k0 + u : parts - 1, row);
+                const int64_t at = part_at(p, s, k0 + u < parts ? k0 + u : parts - 1, row);
                 ml[u] = p.part_ml[at];
                 o[u] = *(const f32x4*)(p.part_o + at * dp + col);
             }
@@ -66,7 +54,7 @@ __global__ __launch_bounds__(512) void k_attend_join_long(AttendArgs a, AttendPl
     const AttendSplit s = p.split[blockIdx.x];
     const int tid = threadIdx.x, dp = a.pool.dp, lanes = dp / 4, groups = 512 / lanes;
     const int col = tid % lanes * 4, part = tid / lanes;
-    const int parts = (int)blockIdx.x - s.worker0 + 1;
+    const int parts = s.parts;
     for (int row = blockIdx.y; row < s.n_rows; row += gridDim.y) {
         Joined x;
         if (part < groups)
@@ -75,7 +63,7 @@ __global__ __launch_bounds__(512) void k_attend_join_long(AttendArgs a, AttendPl
                 f32x4 o[4];
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
-                    const int64_t at = part_at(p, s, parts, k0 + u * groups < parts ? k0 + u * groups : parts - 1, row);
+                    const int64_t at = part_at(p, s, k0 + u * groups < parts ? k0 + u * groups : parts - 1, row);
                     ml[u] = p.part_ml[at];
                     o[u] = *(const f32x4*)(p.part_o + at * dp + col);
                 }
@@ -121,11 +109,15 @@ AttendPlan plan_of(const KvPool& pool, bool f32, int n_seq, int max_new, int gro
     p.group_shift = sh.group_shift;
     p.waves = sh.waves;
     p.workers = num_cu * sh.occupancy;
-    const int64_t split = (int64_t)sizeof(AttendSplit) * p.workers, slots = (2 * (int64_t)p.workers) << p.group_shift;
-    p.split = (AttendSplit*)space;
-    p.part_ml = (float2*)(space + split);
-    p.part_o = (float*)(space + split + 8 * slots);
-    *bytes = split + 8 * slots + 4 * slots * pool.dp;
+    p.workers = p.workers < kMaxWorkers ? p.workers : kMaxWorkers;
+    // (the counters first: at the same place in every launch)
+    const int64_t done = 4 * kMaxWorkers, split = (int64_t)sizeof(AttendSplit) * p.workers;
+    const int64_t slots = (2 * (int64_t)p.workers) << p.group_shift;
+    p.done = (uint32_t*)space;
+    p.split = (AttendSplit*)(space + done);
+    p.part_ml = (float2*)(space + done + split);
+    p.part_o = (float*)(space + done + split + 8 * slots);
+    *bytes = done + split + 8 * slots + 4 * slots * pool.dp;
     return p;
 }
 
@@ -151,12 +143,19 @@ hipError_t launch_kv_attend(const AttendArgs& a, int max_new, void* workspace, i
     const int64_t groups = ((a.seqs.rows * a.group) >> p.group_shift) + a.seqs.n_seq;
     while (groups * a.pool.heads * (((tiles - 1) >> p.chunk_shift) + 1) > INT32_MAX / 2 && p.chunk_shift < 30)
         ++p.chunk_shift;
+    // Small calls join their parts in the launch: where each wave has a tile at most, by what the page tables (or the
+    // window) can hold.  One launch less is 2 us on the host and 1 us on the GPU (one sequence of 777 tokens, 8 heads 11.5 us,
+    // 13.7 in two); with more parts to join, or parts of many rows, the launch is faster (131,071 tokens 88 us, 93 joined in
+    // the launch; 64 sequences in fp8 99, 103; 151 new tokens 174, 208).
+    const int64_t seen = a.window > 0 && a.window / 32 + 2 + (int64_t)max_new / 32 < tiles && max_new > 0
+                             ? a.window / 32 + 2 + max_new / 32 : tiles;
+    p.join_here = p.group_shift == 4 && groups * a.pool.heads * seen <= 4 * (int64_t)p.workers;
     const hipError_t e = a.pool.dp == 64    ? launch_attend<64>(a, p, s)
                          : a.pool.dp == 96  ? launch_attend<96>(a, p, s)
                          : a.pool.dp == 128 ? launch_attend<128>(a, p, s)
                          : a.pool.dp == 192 ? launch_attend<192>(a, p, s)
                                             : launch_attend<256>(a, p, s);
-    if (e != hipSuccess) return e;
+    if (e != hipSuccess || p.join_here) return e;
     // rows of a row group, row groups
     int64_t rows = (int64_t)(max_new > 0 ? max_new : 64) * a.group, of_seq = ((rows - 1) >> p.group_shift) + 1;
     rows = rows < (1 << p.group_shift) ? rows : 1 << p.group_shift;
