@@ -5,9 +5,10 @@
 // bound the time, not memory, and each tile is used by all of a workgroup's waves: it goes through registers into LDS
 // (as bfloat16 whatever the cache's type), in the order of memory, which is that of the operands; each wave reads every
 // operand once for its R row tiles.  Row tiles are dealt out to the waves in turn, so that a group that is not full leaves
-// every SIMD about as much to do.  One barrier a tile would keep eight waves in step, all of them at the matrix cores and
-// then all at the softmax; so the second wave of each SIMD multiplies a tile's weights and values only in the next step,
-// while the first computes that step's scores, and values stay for three steps.
+// every SIMD about as much to do.  Four waves and two workgroups on a compute unit where the registers allow it (up to 128
+// columns), so that one is at the matrix cores while the other is at the softmax; eight waves of one row tile each for
+// wider heads.  (Tried without gain: eight waves of two row tiles, with 256 rows a group; the upper four waves half a step
+// behind; two tiles on their way instead of one; three workgroups.)
 #pragma once
 
 #include "attend.hpp"
@@ -23,11 +24,6 @@ struct Wide {
     static constexpr int BYTES_TILE = 32 * DP * (BYTES ? 1 : 2);
     static constexpr int LOADS = 2 * BYTES_TILE / 1024;           // 16-byte loads a lane of keys and values, all waves
     static constexpr int PER_WAVE = (LOADS + WAVES - 1) / WAVES;
-    // tiles on their way in registers: two hide the latency where one workgroup has the compute unit to itself (1.2 us a
-    // load under a step of 1.5 us)
-    static constexpr int AHEAD = WAVES == 8 ? 2 : 1;
-    static constexpr bool STAGGER = WAVES == 8;                   // the upper four waves are half a step behind
-    static constexpr int VBUF = STAGGER ? 3 : 2;                  // tiles of values in LDS
     // waves on a SIMD: two where the registers of the sums and queries leave room
     static constexpr int OCC = R * DP * (F32 ? 2 : 1) <= 256 ? 2 : 1;
 };
@@ -37,7 +33,7 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
                                                                                               AttendPlan p) {
     using W = Wide<DP, CT, WAVES, R, F32>;
     using A = Attend<DP, CT, R, F32>;
-    __shared__ u32x4 keys[2][2 * W::KC * 64], vals[W::VBUF][W::NJ * 64];  // operands of 1 KB each
+    __shared__ u32x4 keys[2][2 * W::KC * 64], vals[2][W::NJ * 64];  // operands of 1 KB each
     __shared__ f32x4 scales[2][16];  // 32 of the keys, 32 of the values
     const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15, u = lane >> 4;
@@ -55,8 +51,6 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
     const float scale2 = scale_of(a);
     const int tile_shift = a.pool.page_shift - 5;
     AttendSpan s = attend_span(a, p, range.b);
-    u32x4 stage[W::AHEAD][W::PER_WAVE];
-    float stage_scale[W::AHEAD] = {};
 
     while (true) {
         // the segment that begins at item range.at
@@ -128,8 +122,8 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
             }
             return there ? index : -1;
         };
-        // The loaded tile into buffers b (keys, scales) and bv; values that no row sees as zeros.
-        auto put_tile = [&](const u32x4 (&stage)[W::PER_WAVE], float scale, int b, int bv, int index) {
+        // The loaded tile into buffer b; values that no row sees as zeros.
+        auto put_tile = [&](const u32x4 (&stage)[W::PER_WAVE], float scale, int b, int index) {
             const bool edge = 32 * index < seen0 || 32 * index + 31 > seen1;
             auto shown = [&](int t) { return 32 * index + t >= seen0 && 32 * index + t <= seen1; };
 #pragma unroll
@@ -151,7 +145,7 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
                         x[d] &= keep;
                     }
                 }
-                u32x4* to = values ? &vals[bv][0] : &keys[b][0];
+                u32x4* to = values ? &vals[b][0] : &keys[b][0];
                 const int kb = values ? at - W::LOADS / 2 : at;
                 if constexpr (!W::BYTES) {
                     to[kb * 64 + lane] = x;
@@ -167,47 +161,30 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
         // All tiles, for a wave with RA row tiles.
         auto run = [&](auto count) {
             constexpr int RA = decltype(count)::value;
-            const bool late = W::STAGGER && wid >= 4;
-            int now = fetch(stage[0], stage_scale[0]), buf = 0, vbuf = 0, vlast = -1;
+            u32x4 stage[W::PER_WAVE];  // the next tile, on its way
+            float stage_scale = 0.0f;
+            int now = fetch(stage, stage_scale), buf = 0;
             if (now < 0) return;
-            put_tile(stage[0], stage_scale[0], 0, 0, now);
-            int next = fetch(stage[0], stage_scale[0]), after = -1;
-            if constexpr (W::AHEAD == 2) after = fetch(stage[1], stage_scale[1]);
-            u32x4 weights[R][W::NP];
+            put_tile(stage, stage_scale, 0, now);
+            int next = fetch(stage, stage_scale);
             lds_barrier();
-            // One tile, if there is one; the next one, on its way in registers `k`, follows it into LDS.  (No way out of
-            // the middle: every step issues its loads, so that their number in flight is known and a wait is for its own.)
-            auto step = [&](int k) {
-                if (now >= 0) {
-                    if constexpr (RA > 0) {
-                        if (late && vlast >= 0) w.template gather_lds<RA>(&vals[vlast][lane], weights);
-                        f32x4 sc[R][2];
-                        w.template scores_lds<RA>(&keys[buf][lane], scales[buf], u, sc, scale2);
-                        if (32 * now < all0 || 32 * now + 31 > all1) w.template hide_scores<RA>(now, sc, lane);
-                        w.template weigh<RA>(sc, scale2);
-                        w.template round_lds<RA>(sc, scales[buf] + 8, u, weights);
-                        if (!late) w.template gather_lds<RA>(&vals[vbuf][lane], weights);
-                    }
-                    vlast = vbuf;
+            while (true) {
+                if constexpr (RA > 0) {
+                    f32x4 sc[R][2];
+                    u32x4 weights[R][W::NP];
+                    w.template scores_lds<RA>(&keys[buf][lane], scales[buf], u, sc, scale2);
+                    if (32 * now < all0 || 32 * now + 31 > all1) w.template hide_scores<RA>(now, sc, lane);
+                    w.template weigh<RA>(sc, scale2);
+                    w.template round_lds<RA>(sc, scales[buf] + 8, u, weights);
+                    w.template gather_lds<RA>(&vals[buf][lane], weights);
                 }
+                if (next < 0) break;
                 buf ^= 1;
-                vbuf = vbuf + 1 == W::VBUF ? 0 : vbuf + 1;
-                put_tile(stage[k], stage_scale[k], buf, vbuf, next);
+                put_tile(stage, stage_scale, buf, next);
                 now = next;
-                if constexpr (W::AHEAD == 2) {
-                    next = after;
-                    after = fetch(stage[k], stage_scale[k]);
-                } else {
-                    next = fetch(stage[k], stage_scale[k]);
-                }
+                next = fetch(stage, stage_scale);
                 lds_barrier();
-            };
-            while (now >= 0) {
-                step(0);
-                if constexpr (W::AHEAD == 2) step(1);
             }
-            if constexpr (RA > 0)
-                if (late) w.template gather_lds<RA>(&vals[vlast][lane], weights);
         };
         if (R == 2 && active == 2) run(std::integral_constant<int, R>{});
         else if (active >= 1) run(std::integral_constant<int, 1>{});
@@ -276,8 +253,6 @@ hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t s
                 if constexpr (DP <= 128) k_attend_wide<DP, CT, 4, 2, false><<<grid, block, 0, s>>>(a, p);
                 else k_attend_wide<DP, CT, 8, 1, false><<<grid, block, 0, s>>>(a, p);
                 break;
-            default:
-                if constexpr (DP <= 128) k_attend_wide<DP, CT, 8, 2, false><<<grid, block, 0, s>>>(a, p);
         }
     };
     if (a.pool.type == kKvBf16) go(std::integral_constant<int, kKvBf16>{});

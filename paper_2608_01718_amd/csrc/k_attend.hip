@@ -96,8 +96,7 @@ Shape shape_of(const KvPool& pool, bool f32, int64_t rows) {
     if (rows <= 32 && pool.dp <= 128) return {5, 4, attend_occupancy(pool.dp, bytes, 2, false)};
     if (rows <= 64 && pool.dp <= 192) return {6, 4, wide_occupancy(pool.dp, 4, 1, false)};
     if (pool.dp > 128) return {7, 8, wide_occupancy(pool.dp, 8, 1, false)};
-    if (rows <= 128) return {7, 4, wide_occupancy(pool.dp, 4, 2, false)};
-    return {8, 8, wide_occupancy(pool.dp, 8, 2, false)};
+    return {7, 4, wide_occupancy(pool.dp, 4, 2, false)};
 }
 
 // The plan of a launch whose workspace begins at `space`, and the bytes it takes.
