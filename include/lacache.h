@@ -450,7 +450,8 @@ int lacache_rope(const void *x, void *y, lacache_dtype dtype, int64_t rows, int3
  * rope is given) and v is taken as it is, in float32; both are rounded once, to
  * nearest-even, to bfloat16, or to 8-bit codes x * (top / m), m the largest
  * magnitude of the token's head, top = 448 (fp8) or 127 (int8), with the scale
- * m / top (m below 2^-100 stores zeros).
+ * m / top (m below 2^-100 stores zeros; a head that holds an infinity or NaN
+ * has a scale of NaN, and all of it reads as NaN).
  *   k, v   [rows][heads][d] (dtype), rows k_row and v_row elements apart
  *   q      [rows][q_heads][d], rows q_row elements apart: turned by its
  *          position and written to q_out [rows][q_heads][d], contiguous; q_out

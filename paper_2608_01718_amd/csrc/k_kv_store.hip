@@ -124,17 +124,22 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a, int parts, int 
                 else load_row8<F32>(src, c, x);
             }
             if constexpr (BYTES) {
-                float m = 0.0f;
+                // the largest magnitude by its bits, so that a NaN is above everything: a head that holds one, or an infinity,
+                // has no codes, and a scale that says so
+                uint32_t m_bits = 0;
 #pragma unroll
-                for (int q = 0; q < 8; ++q) m = fmaxf(m, fabsf(x[q]));
-                for (int o = lanes / 2; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, kWave));
-                const bool some = m >= kKvTiny;
+                for (int q = 0; q < 8; ++q) m_bits = max(m_bits, __float_as_uint(x[q]) & 0x7FFFFFFFu);
+                for (int o = lanes / 2; o >= 1; o >>= 1) m_bits = max(m_bits, (uint32_t)__shfl_xor((int)m_bits, o, kWave));
+                const float m = __uint_as_float(m_bits);
+                const bool none = m_bits >= 0x7F800000u, some = m >= kKvTiny && !none;
                 const float top = CT == kKvFp8 ? 448.0f : 127.0f, inv = some ? top / m : 0.0f;
-                if (c == 0) (keys ? p.k_scale : p.v_scale)[scale_at(p, page, h, at + u)] = some ? m / top : 0.0f;
+                if (c == 0)
+                    (keys ? p.k_scale : p.v_scale)[scale_at(p, page, h, at + u)] =
+                        none ? __builtin_nanf("") : some ? m / top : 0.0f;
                 uint8_t code[8];
 #pragma unroll
                 for (int q = 0; q < 8; ++q) {
-                    const float y = fminf(fmaxf(x[q] * inv, -top), top);
+                    const float y = none ? 0.0f : fminf(fmaxf(x[q] * inv, -top), top);
                     code[q] = CT == kKvInt8 ? (uint8_t)(int8_t)(int)rintf(y)
                                             : (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(y, y, 0, false);
                 }

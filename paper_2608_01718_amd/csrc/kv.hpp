@@ -100,9 +100,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     return __builtin_bit_cast(uint32_t, w);
 }
 
-// Largest code of the 8-bit types, and the magnitude below which a head is stored as zeros (its reciprocal, times the
-// largest code, would overflow).
-__device__ inline float kv_top(int type) { return type == kKvFp8 ? 448.0f : 127.0f; }
+// The magnitude below which a head is stored as zeros (its reciprocal, times the largest code, would overflow).
 constexpr float kKvTiny = 0x1p-100f;
 
 // a c - b s and b c + a s, every product and sum rounded (no fused multiply-add: the codes of the 8-bit types are then

@@ -232,6 +232,27 @@ def test_codes_of_tiny_and_huge_heads(lc, kind, spread):
 
 
 @pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_values_that_are_no_numbers_are_not_lost(lc, kind, dtype, bad):
+    """bfloat16 keeps them where they are; 8 bits have none, the whole head of the token reads as NaN.  Other heads and
+    tokens are as ever."""
+    g = torch.Generator().manual_seed(4)
+    k, v = (torch.randn((40, 3, 80), generator=g).to(dtype) for _ in range(2))
+    pg = Paged(lc, kind, 3, 80, 32, 1, 2)
+    seqs = pg.seqs([40], [40])
+    want = [ref.values(*ref.coded(x.float(), kind)) for x in (k, v)]
+    for x, w in zip((k, v), want):
+        for t, h, c in ((0, 1, 0), (31, 0, 79), (39, 2, 41)):
+            x[t, h, c] = bad
+            w[t, h, slice(None) if kind != "bf16" else c] = bad if kind == "bf16" else math.nan
+    pg.cache.append(k.to(DEV), v.to(DEV), seqs)
+    for got, w in zip(pg.cache.read(seqs, 40, dtype=torch.float32), want):
+        got = got.cpu()
+        assert torch.equal(got.isnan(), w.isnan()) and torch.equal(got[~w.isnan()], w[~w.isnan()])
+
+
+@pytest.mark.parametrize("kind", KINDS)
 def test_positions_that_do_not_exist(lc, kind):
     """Pages outside the pool, positions beyond the page table and negative positions: not stored, read as zeros, their
     queries turned all the same; no other page changes."""
