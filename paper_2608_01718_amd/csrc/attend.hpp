@@ -535,7 +535,7 @@ struct Joined {
     float m = -__builtin_inff(), l = 0.0f;
     f32x4 o{0, 0, 0, 0};
     __device__ __forceinline__ void add(float m2, float l2, f32x4 o2) {
-        if (m2 == -__builtin_inff()) return;
+        if (m2 == -__builtin_inff() && l2 == 0.0f) return;  // nothing was seen (scores that are all NaN raise no maximum)
         const float M = fmaxf(m, m2);
         const float f = __builtin_amdgcn_exp2f(m - M), g = __builtin_amdgcn_exp2f(m2 - M);
         l = l * f + l2 * g;

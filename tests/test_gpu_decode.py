@@ -445,6 +445,22 @@ def test_attend_pages_that_are_not_there(lc, kind):
     check_attend(lc, pg, held, q, news, lens, table=cut, gone=gone)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("lens,new", [([70], 1), ([20_001, 40], 1), ([9000], 25)])
+def test_attend_of_queries_that_are_no_numbers(lc, kind, dtype, lens, new):
+    """A query with a NaN has NaN for a result, also where its context is joined of parts; no other row changes."""
+    pg, _ = filled(lc, kind, 1, 64, 32, lens, seed=9)
+    q = torch.randn((new * len(lens), 4, 64), generator=torch.Generator(DEV).manual_seed(2), device=DEV).to(dtype)
+    seqs = pg.seqs([new] * len(lens), lens)
+    want = [x.clone() for x in pg.cache.attend(q, seqs, max_new=new)]
+    q[0, 2, 7] = math.nan
+    for x in want:
+        x[0, 2] = math.nan
+    for got, x in zip(pg.cache.attend(q, seqs, max_new=new), want):
+        assert torch.equal(got.isnan(), x.isnan()) and torch.equal(got[~x.isnan()], x[~x.isnan()])
+
+
 def test_attend_rows_before_the_first_position(lc):
     """More rows than the sequence has tokens: the first rows see nothing."""
     pg, held = filled(lc, "bf16", 1, 64, 32, [5, 40], seed=2)
