@@ -512,6 +512,13 @@ def _made(like: torch.Tensor, shape, dtype, stream, zeros=False):
         return make(shape, dtype=dtype)
 
 
+def _capturing(index: int, stream) -> bool:
+    """Whether the stream of the call is recording a graph."""
+    handle = _stream(index, stream)
+    with torch.cuda.stream(torch.cuda.ExternalStream(handle, device=index) if handle else torch.cuda.default_stream(index)):
+        return torch.cuda.is_current_stream_capturing()
+
+
 def _given(t: torch.Tensor, shape, dtype, index: int, name: str) -> torch.Tensor:
     if t.dtype != dtype or t.get_device() != index or t.shape != torch.Size(shape) or not t.is_contiguous():
         raise ValueError(f"{name}: expected a contiguous {list(shape)} {dtype} tensor on cuda:{index}")
@@ -588,7 +595,18 @@ class KVCache:
         self._c = _KV(k.data_ptr(), v.data_ptr(), *(0 if t is None else t.data_ptr() for t in (ks, vs)), n_pages, page,
                       heads, d, type)
         self._ref = ctypes.addressof(self._c)
-        self._need, self._space = {}, None
+        self._need, self._space, self._outgrown = {}, None, []
+
+    def _scratch(self, like, need: int, stream):
+        """Larger scratch.  What it replaces stays: a captured graph may have it among its arguments.  Scratch made while a
+        graph is captured is that graph's alone, since its zeros are written when the graph runs, not before."""
+        space = _made(like, (need,), torch.uint8, stream, zeros=True)
+        if _capturing(self.index, stream):
+            return space
+        if self._space is not None:
+            self._outgrown.append(self._space)
+        self._space = space
+        return space
 
     def append(self, k, v, seqs, q=None, rope=None, q_out=None, max_new=0, stream=None):
         return lacache_kv_append(self, k, v, seqs, q, rope, q_out, max_new, stream)
@@ -708,9 +726,9 @@ def lacache_kv_attend(c: KVCache, q, seqs: Sequences, scale=None, window: int = 
     need = c._need.get(key)
     if need is None:
         need = c._need[key] = lacache_kv_attend_workspace(c, *key)
-    if c._space is None or c._space.numel() < need:
-        c._space = _made(q, (need,), torch.uint8, stream, zeros=True)
     space = c._space
+    if space is None or space.numel() < need:
+        space = c._scratch(q, need, stream)
     _check(_on(index, stream, _lib.lacache_kv_attend, c._ref, seqs._ref, q.data_ptr(), dtype, rows, q_heads, q_row,
                max_new, c.d ** -0.5 if scale is None else scale, window, out[0].data_ptr(), out[1].data_ptr(),
                space.data_ptr(), space.numel()), "lacache_kv_attend")

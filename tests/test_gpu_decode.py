@@ -449,16 +449,19 @@ def test_attend_pages_that_are_not_there(lc, kind):
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("lens,new", [([70], 1), ([20_001, 40], 1), ([9000], 25)])
 def test_attend_of_queries_that_are_no_numbers(lc, kind, dtype, lens, new):
-    """A query with a NaN has NaN for a result, also where its context is joined of parts; no other row changes."""
-    pg, _ = filled(lc, kind, 1, 64, 32, lens, seed=9)
-    q = torch.randn((new * len(lens), 4, 64), generator=torch.Generator(DEV).manual_seed(2), device=DEV).to(dtype)
-    seqs = pg.seqs([new] * len(lens), lens)
-    want = [x.clone() for x in pg.cache.attend(q, seqs, max_new=new)]
-    q[0, 2, 7] = math.nan
-    for x in want:
-        x[0, 2] = math.nan
-    for got, x in zip(pg.cache.attend(q, seqs, max_new=new), want):
-        assert torch.equal(got.isnan(), x.isnan()) and torch.equal(got[~x.isnan()], x[~x.isnan()])
+    """A query with a NaN has NaN for a result, also where its context is joined of parts; other rows are as ever."""
+    pg, held = filled(lc, kind, 1, 64, 32, lens, seed=9)
+    news = [new] * len(lens)
+    q = torch.randn((sum(news), 4, 64), generator=torch.Generator(DEV).manual_seed(2), device=DEV).to(dtype)
+    seqs = pg.seqs(news, lens)
+    want = pg.cache.attend(q, seqs, max_new=new)
+    odd = q.clone()
+    odd[0, 2, 7] = math.nan
+    got = pg.cache.attend(odd, seqs, max_new=new)
+    for x, w in zip(got, want):
+        assert bool(x[0, 2].isnan().all()) and int(x.isnan().sum()) == x[0, 2].numel()
+        x[0, 2] = w[0, 2]
+    check_attend(lc, pg, held, q, news, lens, out=got)
 
 
 def test_attend_rows_before_the_first_position(lc):
@@ -537,6 +540,43 @@ def test_decode_on_another_stream_and_in_a_graph(lc):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(outs[0], want) and torch.equal(outs[1], want_lse), r
+
+
+def test_graphs_keep_their_scratch(lc):
+    """A graph captured before any eager call, eager calls before its first replay, and eager calls that need more scratch
+    than the graph was captured with: each gives what a cache of its own gives."""
+    lens = [3000, 40, 64]
+    pg, _ = filled(lc, "bf16", 2, 64, 32, lens, seed=40)
+    other, _ = filled(lc, "bf16", 2, 64, 32, lens, seed=40)
+    g = torch.Generator(DEV).manual_seed(1)
+    q = torch.randn((3, 8, 64), generator=g, device=DEV).to(torch.bfloat16)
+    many = torch.randn((90, 8, 64), generator=g, device=DEV).to(torch.bfloat16)
+    one, thirty = (lambda p: p.seqs([1, 1, 1], lens)), (lambda p: p.seqs([30, 30, 30], lens))
+    want = [x.clone() for x in other.cache.attend(q, one(other), max_new=1)]
+    want_many = [x.clone() for x in other.cache.attend(many, thirty(other), max_new=30)]
+
+    def captured(pg):
+        outs, seqs, graph = (torch.zeros_like(want[0]), torch.zeros_like(want[1])), one(pg), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            pg.cache.attend(q, seqs, max_new=1, out=outs)
+        return graph, outs, seqs
+
+    first = captured(pg)
+    for _ in range(3):
+        assert all(torch.equal(a, b) for a, b in zip(pg.cache.attend(q, one(pg), max_new=1), want))
+    second = captured(pg)                    # with the scratch of the eager calls
+    assert pg.cache._space is not None
+    for r in range(3):
+        assert all(torch.equal(a, b) for a, b in zip(pg.cache.attend(many, thirty(pg), max_new=30), want_many))
+        fill = [torch.full((1 << n,), 255, dtype=torch.uint8, device=DEV) for n in range(12, 27)]  # takes what was freed
+        for graph, outs, _ in (first, second):
+            for x in outs:
+                x.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(outs, want)), r
+        assert all(bool((x == 255).all()) for x in fill)
+        del fill
 
 
 # ---- refusals of the binding ---------------------------------------------------------------------------------
