@@ -484,6 +484,8 @@ int lacache_kv_read(const lacache_kv *kv, const lacache_seqs *seqs, void *k_out,
  *   out   [rows][q_heads][d] (dtype) = sum_j w_j v_j, w = softmax(scale q.k_j)
  *   lse   [rows][q_heads] float = log sum_j exp(scale q.k_j); NULL: not wanted.
  *         A row that sees nothing has out = 0 and lse = -infinity.
+ *         Infinities and NaN make the results of the rows that see them
+ *         infinite or NaN (a value in its column alone), and no others.
  * Products are exact and sums are in float32; with bfloat16 rows the weights
  * are rounded to 16 bits before they multiply the values.
  *   max_new    a bound on the new tokens of a sequence (for the launch shape

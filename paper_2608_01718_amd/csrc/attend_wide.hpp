@@ -169,6 +169,12 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
             int next = fetch(stage, stage_scale);
             lds_barrier();
             while (true) {
+                if ((seen0 < all0 && 32 * now < all0) || (seen1 > all1 && 32 * now + 31 > all1))  // (the same for all waves)
+                    if (w.template spoil_lds<RA>(&vals[buf][lane], scales[buf] + 8, now, lane)) {
+                        lds_barrier();
+                        A::clear_lds(&vals[buf][lane], (float*)(scales[buf] + 8), wid, WAVES, lane);
+                        lds_barrier();
+                    }
                 if constexpr (RA > 0) {
                     f32x4 sc[R][2];
                     u32x4 weights[R][W::NP];

@@ -447,6 +447,49 @@ def test_attend_pages_that_are_not_there(lc, kind):
 
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("window", [0, 45])
+@pytest.mark.parametrize("length,new,heads,Hq,d", [(75, 3, 2, 4, 64), (130, 9, 2, 6, 96), (300, 21, 2, 8, 128),
+                                                   (96, 40, 2, 4, 256), (3000, 150, 2, 2, 64), (64, 64, 2, 2, 192)])
+def test_attend_hidden_values_that_are_no_numbers(lc, kind, dtype, bad, window, length, new, heads, Hq, d):
+    """An infinity or NaN among the keys or values of a token that some rows see and others do not (later new tokens, and
+    tokens that the window has passed): the rows that see it get it (8 bits: in all columns of its head, as a NaN), the
+    others are as if it were not there."""
+    say(f"[case] no numbers {kind} {dtype} {bad} window={window} {length, new, heads, Hq, d}")
+    g = torch.Generator(DEV).manual_seed(d + new)
+    k, v = (torch.randn((length, heads, d), generator=g, device=DEV) for _ in range(2))
+    pg, clean = (Paged(lc, kind, heads, d, 32, 1, -(-length // 32), seed=d) for _ in range(2))
+    seqs = pg.seqs([length], [length])
+    clean.cache.append(k, v, seqs)
+    keys, vals = (x.double() for x in clean.cache.read(seqs, length, dtype=torch.float32))
+    spoiled = torch.zeros((length, heads, d), dtype=torch.bool, device=DEV)   # values that are no numbers
+    for t, h, c in ((length - 1, 0, 5), (length - new // 2 - 1, 0, 5), (length - new // 2 - 1, 1, d - 1),
+                    (max(0, length - new - 40), 1, 0)):
+        v[t, h, c] = bad
+        spoiled[t, h, slice(None) if kind != "bf16" else c] = True
+    key_at = length - 1 - new // 3
+    k[key_at, 1, 3] = math.nan
+    pg.cache.append(k, v, seqs)
+    q = torch.randn((new, Hq, d), generator=g, device=DEV).to(dtype)
+    o, lse = pg.cache.attend(q, pg.seqs([new], [length]), window=window, max_new=new)
+    j, p = torch.arange(length, device=DEV), torch.arange(length - new, length, device=DEV)[:, None]
+    seen = (j <= p) & ((p - j < window) if window else (j >= 0))
+    want = ref.attention(q.double(), keys, vals, seen, d ** -0.5)
+    eo, el = ref.bounds(want, d, dtype == torch.float32)
+    of = Hq // heads
+    no_number = ((seen.double() @ spoiled.double().flatten(1)).view(new, heads, d) > 0).repeat_interleave(of, 1)
+    lost = torch.zeros((new, heads), dtype=torch.bool, device=DEV)            # rows without a sum
+    lost[:, 1] = seen[:, key_at]
+    lost = lost.repeat_interleave(of, 1)
+    no_number |= lost[..., None]
+    assert torch.equal(~o.isfinite(), no_number)
+    assert torch.equal(lse.isnan(), lost)
+    assert bool(((o.double() - want[0]).abs() <= eo)[~no_number].all())
+    assert bool(((lse.double() - want[1]).abs() <= el)[~lost].all())
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("lens,new", [([70], 1), ([20_001, 40], 1), ([9000], 25)])
 def test_attend_of_queries_that_are_no_numbers(lc, kind, dtype, lens, new):
     """A query with a NaN has NaN for a result, also where its context is joined of parts; other rows are as ever."""
