@@ -411,75 +411,96 @@ struct Attend {
         }
     }
 
-    // Tiles of which some rows see more than others: 0 times an infinity or a NaN is NaN, so a value that is no number must
-    // not meet the weight 0 of a row that does not see its token.  It is taken out, and rows that see it become NaN by a
-    // product of their own: (is no number) times (is seen).
+    // Values that are no numbers.  0 times an infinity or a NaN is NaN, so in a tile that some rows see more of than others
+    // they must not meet the weight 0 of a row that does not see their token.  They are taken out of such tiles (hide,
+    // put_tile in attend_wide.hpp), and if there were any, the rows that see them are made NaN when the segment is through,
+    // by another look at its tiles and a product (is no number) times (is seen).
     //
-    // The tokens of which the scale is no number, as halves 0x4000 of two bfloat16 a dword; the scale becomes 0.
-    static __device__ __forceinline__ u32x4 odd_scales(f32x4 (&vs)[2]) {
-        u32x4 odd{};
+    // The top bits of a dword's elements that are no numbers: of two bfloat16, of the cache's type (no integer is none);
+    // without: the dword without them.
+    static __device__ __forceinline__ uint32_t no_numbers(uint32_t w) {
+        return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+    }
+    static __device__ __forceinline__ uint32_t no_codes(uint32_t w) {
+        if constexpr (CT == kKvInt8) return 0;
+        return CT == kKvFp8 ? ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u : no_numbers(w);
+    }
+    static __device__ __forceinline__ uint32_t without(uint32_t w, uint32_t n) {
+        return w & ~(n | (n - (n >> (CT == kKvFp8 ? 7 : 15))));
+    }
+    static __device__ __forceinline__ bool no_scale(float x) { return (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u; }
+    // Whether rows see more of a tile than others: seen0 .. seen1 are seen by one of them, all0 .. all1 by every one.
+    static __device__ __forceinline__ bool mixed(int index, int seen0, int seen1, int all0, int all1) {
+        return (seen0 < all0 && 32 * index < all0) || (seen1 > all1 && 32 * index + 31 > all1);
+    }
+    // Takes them out of a tile; whether there were any.
+    static __device__ __forceinline__ uint32_t take_out(Tile& t) {
+        uint32_t some = 0;
+#pragma unroll
+        for (int i = 0; i < NL; ++i)
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                const uint32_t n = no_codes(t.v[i][d]);
+                t.v[i][d] = without(t.v[i][d], n);
+                some |= n;
+            }
         if constexpr (BYTES) {
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const bool is = (__float_as_uint(vs[b][i]) & 0x7F800000u) == 0x7F800000u;
-                    odd[2 * b + (i >> 1)] |= is ? 0x4000u << (16 * (i & 1)) : 0u;
-                    vs[b][i] = is ? 0.0f : vs[b][i];
+                    some |= no_scale(t.vs[b][i]);
+                    t.vs[b][i] = no_scale(t.vs[b][i]) ? 0.0f : t.vs[b][i];
                 }
         }
-        return odd;
+        return some;
     }
-    // Which of the tile's tokens the rows of row tile r see, as bfloat16 ones.
-    __device__ __forceinline__ u32x4 seen_ones(int r, int index, int lane) {
-        u32x4 seen{};
+    // The mixed tiles t0, t0 + step, ... < t1 of a segment: rows that see what is no number become NaN in its column.
+    __device__ __forceinline__ void spoil(const AttendArgs& a, const int32_t* pages, int h, int first, int t0, int t1, int step,
+                                          int seen0, int seen1, int all0, int all1, int lane) {
+        const int shift = a.pool.page_shift - 5;
+#pragma unroll 1
+        for (int t = t0; t < t1; t += step) {
+            const int index = first + t;
+            if (32 * index > seen1 || 32 * index + 31 < seen0 || !mixed(index, seen0, seen1, all0, all1)) continue;
+            const int64_t page = __builtin_amdgcn_readfirstlane(pages[index >> shift]);
+            if (page < 0 || page >= a.pool.n_pages) continue;
+            const int64_t place = ((page * a.pool.heads + h) << shift) + (index & ((1 << shift) - 1));
+            const auto values = tile_rsrc(a.pool.v + place * BYTES_TILE, BYTES_TILE);
+            u32x4 seen[R], odd{};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int j = 32 * index + 16 * (e >> 2) + 4 * (lane >> 4) + (e & 3);
-            seen[e >> 1] |= j >= lo[r] && j <= hi[r] ? 0x3F80u << (16 * (e & 1)) : 0u;
-        }
-        return seen;
-    }
-    // The top bits of the halves of two bfloat16 that are no numbers, and the pair without them.
-    static __device__ __forceinline__ uint32_t no_numbers(uint32_t w) {
-        return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
-    }
-    static __device__ __forceinline__ uint32_t without(uint32_t w, uint32_t n) { return w & ~(n | (n - (n >> 15))); }
-    // Operand j of the values (bfloat16) holds something that is no number, or the tile has an odd token: rows that see one
-    // become NaN there.
-    template <int RA>
-    __device__ __forceinline__ bool spoil(int j, u32x4 x, u32x4 odd, int index, int lane) {
-        u32x4 none;
+            for (int e = 0; e < 8; ++e) {
+                const int j = 32 * index + 16 * (e >> 2) + 4 * (lane >> 4) + (e & 3);
 #pragma unroll
-        for (int d = 0; d < 4; ++d) none[d] = no_numbers(x[d]) >> 1 | odd[d];
-        if (!__any((none[0] | none[1] | none[2] | none[3]) != 0)) return false;
-#pragma unroll
-        for (int r = 0; r < RA; ++r) {
-            const f32x4 hit = mfma16x16x32(none, seen_ones(r, index, lane), f32x4{0, 0, 0, 0});
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[r][j][i] = hit[i] > 0.0f ? __builtin_nanf("") : o[r][j][i];
-        }
-        return true;
-    }
-    // For a tile in registers, which then holds numbers only.
-    __device__ __forceinline__ void take_out(Tile& t, int index, int lane) {
-        const u32x4 odd = odd_scales(t.vs);
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            spoil<R>(j, v_operand(t, j), odd, index, lane);
-            if constexpr (!BYTES) {
-#pragma unroll
-                for (int d = 0; d < 4; ++d) t.v[j][d] = without(t.v[j][d], no_numbers(t.v[j][d]));
+                for (int r = 0; r < R; ++r) {
+                    const uint32_t one = j >= lo[r] && j <= hi[r] ? 0x3F80u << (16 * (e & 1)) : 0u;
+                    seen[r][e >> 1] = e & 1 ? seen[r][e >> 1] | one : one;
+                }
+                if constexpr (BYTES)
+                    odd[e >> 1] |= no_scale(a.pool.v_scale[place * 32 + (j & 31)]) ? 0x4000u << (16 * (e & 1)) : 0u;
             }
-        }
-        if constexpr (CT == kKvFp8) {
+            // (a few loads at a time, for the registers)
+            constexpr int G = BYTES ? 2 : 8, EACH = BYTES ? 2 : 1;
 #pragma unroll
-            for (int i = 0; i < NL; ++i)
+            for (int i0 = 0; i0 < NL; i0 += G) {
+                Tile x;
 #pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                    const uint32_t n = ((t.v[i][d] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
-                    t.v[i][d] &= ~(n | (n - (n >> 7)));
+                for (int i = i0; i < i0 + G && i < NL; ++i) x.v[i] = tile_load(values, i * 1024, lane * 16);
+#pragma unroll
+                for (int j = EACH * i0; j < EACH * (i0 + G) && j < NJ; ++j) {
+                    const u32x4 v = v_operand(x, j);
+                    u32x4 none;  // twos (0x4000), from the value or from the token's scale
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) none[d] = no_numbers(v[d]) >> 1 | odd[d];
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        const f32x4 hit = mfma16x16x32(none, seen[r], f32x4{0, 0, 0, 0});
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[r][j][i] = hit[i] > 0.0f ? __builtin_nanf("") : o[r][j][i];
+                    }
                 }
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
     }
 
@@ -526,27 +547,6 @@ struct Attend {
                 for (int r = 0; r < RA; ++r) s[r][b] *= f;
             }
         }
-    }
-    // take_out for that tile: spoils this wave's rows and returns whether there is anything to be taken out (the same in
-    // every wave); then `clear_lds`, when all waves have been here: operands of a part of the waves, and the scales.
-    template <int RA>
-    __device__ __forceinline__ bool spoil_lds(const u32x4* v, const f32x4* vs, int index, int lane) {
-        f32x4 f[2] = {};
-        if constexpr (BYTES) f[0] = vs[lane >> 4], f[1] = vs[4 + (lane >> 4)];
-        const u32x4 odd = odd_scales(f);
-        bool some = false;
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) some |= spoil<RA>(j, v[j * 64], odd, index, lane);
-        return some;
-    }
-    static __device__ __forceinline__ void clear_lds(u32x4* v, float* vs, int wid, int waves, int lane) {
-        for (int j = wid; j < NJ; j += waves) {
-            u32x4 x = v[j * 64];
-#pragma unroll
-            for (int d = 0; d < 4; ++d) x[d] = without(x[d], no_numbers(x[d]));
-            v[j * 64] = x;
-        }
-        if (BYTES && wid == 0 && lane < 32 && (__float_as_uint(vs[lane]) & 0x7F800000u) == 0x7F800000u) vs[lane] = 0.0f;
     }
     template <int RA>
     __device__ __forceinline__ void hide_scores(int index, f32x4 (&s)[R][2], int lane) {
@@ -812,13 +812,14 @@ __global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(A
     bool more = true;
     while (more) {
         w.clear();
+        int odd = 0;  // whether something that is no number was taken out
         while (there) {
             f32x4 sc[R][2];
             w.scores(tile, sc, scale2);
             const int index = tile.index;
-            if ((g.seen0 < g.all0 && 32 * index < g.all0) || (g.seen1 > g.all1 && 32 * index + 31 > g.all1)) {
-                w.take_out(tile, index, lane);  // here the registers of the keys are free
-                __builtin_amdgcn_sched_barrier(0);
+            if (A::mixed(index, g.seen0, g.seen1, g.all0, g.all1)) {
+                const uint32_t some = A::take_out(tile);
+                odd = __any(some != 0) ? 1 : odd;
             }
             const int64_t pl = next();  // its keys are loaded under this tile's weights, its values under its scores
             A::load_k(tile, a, pl, there, lane);
@@ -828,6 +829,9 @@ __global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(A
             A::load_v(tile, a, pl, there, lane);
         }
 
+        if (odd)
+            w.spoil(a, a.seqs.pages + (int64_t)g.b * a.seqs.max_pages, g.h, g.first, g.tile0 + wid, g.tile1, 4, g.seen0, g.seen1,
+                    g.all0, g.all1, lane);
         // The next segment's loads are on their way while this one's results are joined and stored.
         const Segment old = g;
         w.reduce();

@@ -35,6 +35,7 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
     using A = Attend<DP, CT, R, F32>;
     __shared__ u32x4 keys[2][2 * W::KC * 64], vals[2][W::NJ * 64];  // operands of 1 KB each
     __shared__ f32x4 scales[2][16];  // 32 of the keys, 32 of the values
+    __shared__ int odd_of[WAVES];    // whether a wave has taken out something that is no number
     const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15, u = lane >> 4;
     // Workgroups go to the eight XCDs in turn; each XCD takes an eighth of the work in one piece, so that the row groups of
@@ -122,9 +123,12 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
             }
             return there ? index : -1;
         };
-        // The loaded tile into buffer b; values that no row sees as zeros.
+        uint32_t odd = 0;
+        // The loaded tile into buffer b; values that no row sees as zeros, and those that are no numbers taken out of tiles
+        // that rows see different parts of.
         auto put_tile = [&](const u32x4 (&stage)[W::PER_WAVE], float scale, int b, int index) {
             const bool edge = 32 * index < seen0 || 32 * index + 31 > seen1;
+            const bool takes = A::mixed(index, seen0, seen1, all0, all1);
             auto shown = [&](int t) { return 32 * index + t >= seen0 && 32 * index + t <= seen1; };
 #pragma unroll
             for (int i = 0; i < W::PER_WAVE; ++i) {
@@ -145,6 +149,14 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
                         x[d] &= keep;
                     }
                 }
+                if (takes && values) {
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) {
+                        const uint32_t none = A::no_codes(x[d]);
+                        x[d] = A::without(x[d], none);
+                        odd |= none;
+                    }
+                }
                 u32x4* to = values ? &vals[b][0] : &keys[b][0];
                 const int kb = values ? at - W::LOADS / 2 : at;
                 if constexpr (!W::BYTES) {
@@ -155,8 +167,14 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
                 }
             }
             if constexpr (W::BYTES)
-                if (wid == 0)
-                    ((float*)scales[b])[lane] = lane >= 32 && edge && !shown(lane & 31) ? 0.0f : scale;
+                if (wid == 0) {
+                    float f = lane >= 32 && edge && !shown(lane & 31) ? 0.0f : scale;
+                    if (takes && lane >= 32 && A::no_scale(f)) {
+                        f = 0.0f;
+                        odd = 1;
+                    }
+                    ((float*)scales[b])[lane] = f;
+                }
         };
         // All tiles, for a wave with RA row tiles.
         auto run = [&](auto count) {
@@ -169,12 +187,6 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
             int next = fetch(stage, stage_scale);
             lds_barrier();
             while (true) {
-                if ((seen0 < all0 && 32 * now < all0) || (seen1 > all1 && 32 * now + 31 > all1))  // (the same for all waves)
-                    if (w.template spoil_lds<RA>(&vals[buf][lane], scales[buf] + 8, now, lane)) {
-                        lds_barrier();
-                        A::clear_lds(&vals[buf][lane], (float*)(scales[buf] + 8), wid, WAVES, lane);
-                        lds_barrier();
-                    }
                 if constexpr (RA > 0) {
                     f32x4 sc[R][2];
                     u32x4 weights[R][W::NP];
@@ -195,6 +207,17 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
         if (R == 2 && active == 2) run(std::integral_constant<int, R>{});
         else if (active >= 1) run(std::integral_constant<int, 1>{});
         else run(std::integral_constant<int, 0>{});
+        if (seen0 < all0 || seen1 > all1) {  // (the same for all waves)
+            const int any = __any(odd != 0);
+            if (lane == 0) odd_of[wid] = any;
+            lds_barrier();
+            int some = 0;
+#pragma unroll
+            for (int t = 0; t < WAVES; ++t) some |= odd_of[t];
+            if (__builtin_amdgcn_readfirstlane(some))
+                w.spoil(a, a.seqs.pages + (int64_t)range.b * a.seqs.max_pages, h, s.first, tile0, tile1, 1, seen0, seen1, all0, all1,
+                        lane);
+        }
         w.reduce();
 
         const bool whole = starts && ends;
