@@ -101,12 +101,12 @@ __device__ __forceinline__ int wave_scan(int x) {
 }
 
 // The range of items of a worker: the sequence in which it begins, the items before that sequence, the range, and
-// the items of a full range (a multiple of `grain`).  All threads take part, a thread a sequence.
+// the items of a full range (a multiple of `grain`, and `least` or more).  All threads take part, a thread a sequence.
 struct AttendRange {
     int b, before, at, end, per;
 };
 template <int WAVES>
-__device__ __forceinline__ AttendRange attend_range(const AttendArgs& a, const AttendPlan& p, int worker, int grain) {
+__device__ __forceinline__ AttendRange attend_range(const AttendArgs& a, const AttendPlan& p, int worker, int grain, int least) {
     constexpr int THREADS = 64 * WAVES;
     __shared__ int total_of[WAVES], found[2];
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, n_seq = a.seqs.n_seq;
@@ -131,6 +131,7 @@ __device__ __forceinline__ AttendRange attend_range(const AttendArgs& a, const A
     all = __builtin_amdgcn_readfirstlane(all);
     AttendRange r;
     r.per = (int)(((uint32_t)all + (uint32_t)p.workers - 1) / (uint32_t)p.workers);
+    r.per = r.per < least ? least : r.per;
     r.per = (r.per + grain - 1) & ~(grain - 1);
     const int64_t at = (int64_t)worker * r.per;
     r.at = at < all ? (int)at : all;
@@ -637,6 +638,57 @@ struct Joined {
     }
 };
 
+__device__ __forceinline__ void store_joined(const AttendArgs& a, const AttendPlan& p, const AttendSplit& s, int row,
+                                             int col, const Joined& x) {
+    const int r = s.row + row, i = token_of(p, r);
+    const int64_t at = ((int64_t)s.seq_row0 + i) * a.q_heads + s.head0 + (r - i * a.group);
+    const f32x4 o = x.o * (x.l == 0.0f ? 0.0f : 1.0f / x.l);
+    if (col < a.pool.d) {
+        if (a.dtype == 0) store4<true>(a, at * a.pool.d + col, o);
+        else store4<false>(a, at * a.pool.d + col, o);
+    }
+    if (col == 0 && a.lse) a.lse[at] = lse_of(x.m, x.l);
+}
+
+// Joins the parts of a row group: of_row groups (a power of two) of dp / 4 lanes on a row, four parts loaded together.  The workgroup takes rows first, first + 1, ... as many as it has lane groups for, and
+// again from `step` times as many on.  load(part's first row + row, column, ml, o) loads four columns.  scratch: THREADS f32x4 and
+// float2 of LDS.
+template <int THREADS, class Load>
+__device__ __forceinline__ void join_rows(const AttendArgs& a, const AttendPlan& p, const AttendSplit& s, int dp, int of_row, int tid,
+                                          int first, int step, f32x4* scratch, Load load) {
+    const int lanes = dp / 4, groups = THREADS / lanes;
+    const int rows = groups / of_row, g = tid / lanes, col = tid % lanes * 4, sub = g % of_row;
+    float2* ml_of = (float2*)(scratch + THREADS);
+    for (int row0 = first * rows; row0 < s.n_rows; row0 += step * rows) {
+        const int row = row0 + g / of_row;
+        const bool live = g < rows * of_row && row < s.n_rows;
+        Joined x;
+        if (live)
+            for (int k0 = sub; k0 < s.parts; k0 += 4 * of_row) {
+                float2 ml[4];
+                f32x4 o[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int k = k0 + u * of_row < s.parts ? k0 + u * of_row : s.parts - 1;
+                    load(part_of(p, s.worker0 + k, k < s.parts - 1) + row, col, ml[u], o[u]);
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    if (k0 + u * of_row < s.parts) x.add(ml[u].x, ml[u].y, o[u]);
+            }
+        if (of_row > 1) {
+            ml_of[tid] = make_float2(x.m, x.l);
+            scratch[tid] = x.o;
+            __syncthreads();
+            if (sub == 0 && live)
+                for (int k = 1; k < of_row; ++k)
+                    x.add(ml_of[tid + k * lanes].x, ml_of[tid + k * lanes].y, scratch[tid + k * lanes]);
+            __syncthreads();
+        }
+        if (live && sub == 0) store_joined(a, p, s, row, col, x);
+    }
+}
+
 // ---------------------------------------------------------------------------
 // The join within the launch, for small calls (AttendPlan::join_here).  Parts are written and read with device-wide (sc1)
 // accesses alone, so the hand-over of last_workgroup_wait holds for them: every workgroup of a row group waits for its
@@ -656,9 +708,8 @@ __device__ __forceinline__ void store_part_ml(const AttendPlan& p, int64_t part,
 }
 
 // After a workgroup's part of a row group has been stored: counts it, and joins the parts if it is the last.  scratch:
-// THREADS f32x4 and float2 of LDS that nothing else uses meanwhile.  A group of dp / 4 lanes takes a row, or, with few
-// rows, every so many parts of one.
-template <int THREADS, int DP, bool F32>
+// THREADS f32x4 and float2 of LDS that nothing else uses meanwhile.
+template <int THREADS, int DP>
 __device__ __forceinline__ void join_parts(const AttendArgs& a, const AttendPlan& p, const AttendSplit& s,
                                            f32x4* scratch) {
     __shared__ int last;
@@ -672,51 +723,18 @@ __device__ __forceinline__ void join_parts(const AttendArgs& a, const AttendPlan
     }
     __syncthreads();
     if (!last) return;
-    constexpr int LANES = DP / 4, GROUPS = THREADS / LANES;
-    int of_row = 1;  // lane groups on a row
-    while (2 * of_row * s.n_rows <= GROUPS) of_row *= 2;
-    const int rows = GROUPS / of_row, g = tid / LANES, col = tid % LANES * 4, sub = g % of_row;
-    float2* ml_of = (float2*)(scratch + THREADS);
-    for (int row0 = 0; row0 < s.n_rows; row0 += rows) {
-        const int row = row0 + g / of_row;
-        const bool live = g < rows * of_row && row < s.n_rows;
-        Joined x;
-        if (live)
-            for (int k0 = sub; k0 < s.parts; k0 += 4 * of_row) {
-                float2 ml[4];
-                f32x4 o[4];
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const int k = k0 + u * of_row < s.parts ? k0 + u * of_row : s.parts - 1;
-                    const int64_t at = part_of(p, s.worker0 + k, k < s.parts - 1) + row;
-                    const uint64_t w = __hip_atomic_load((uint64_t*)(p.part_ml + at), __ATOMIC_RELAXED,
-                                                         __HIP_MEMORY_SCOPE_AGENT);
-                    ml[u] = make_float2(__uint_as_float((uint32_t)w), __uint_as_float((uint32_t)(w >> 32)));
-                    const uint64_t* src = (const uint64_t*)(p.part_o + at * DP + col);
-                    const uint64_t v0 = __hip_atomic_load(src, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT),
-                                   v1 = __hip_atomic_load(src + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                    o[u] = f32x4{__uint_as_float((uint32_t)v0), __uint_as_float((uint32_t)(v0 >> 32)),
-                                 __uint_as_float((uint32_t)v1), __uint_as_float((uint32_t)(v1 >> 32))};
-                }
-#pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    if (k0 + u * of_row < s.parts) x.add(ml[u].x, ml[u].y, o[u]);
-            }
-        if (of_row > 1) {  // (then there is one round)
-            ml_of[tid] = make_float2(x.m, x.l);
-            scratch[tid] = x.o;
-            __syncthreads();
-            if (sub == 0 && live)
-                for (int k = 1; k < of_row; ++k)
-                    x.add(ml_of[tid + k * LANES].x, ml_of[tid + k * LANES].y, scratch[tid + k * LANES]);
-        }
-        if (live && sub == 0) {
-            const int r = s.row + row, i = token_of(p, r);
-            const int64_t at = ((int64_t)s.seq_row0 + i) * a.q_heads + s.head0 + (r - i * a.group);
-            if (col < a.pool.d) store4<F32>(a, at * a.pool.d + col, x.o * (x.l == 0.0f ? 0.0f : 1.0f / x.l));
-            if (col == 0 && a.lse) a.lse[at] = lse_of(x.m, x.l);
-        }
-    }
+    // (all rows at once where they are few; a choice by the parts too costs more than it gains here)
+    int of_row = 1;
+    while (2 * of_row * s.n_rows <= THREADS / (DP / 4)) of_row *= 2;
+    join_rows<THREADS>(a, p, s, DP, of_row, tid, 0, 1, scratch, [&](int64_t at, int col, float2& ml, f32x4& o) {
+        auto load8 = [](const void* from) {
+            const uint64_t w = __hip_atomic_load((const uint64_t*)from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            return make_float2(__uint_as_float((uint32_t)w), __uint_as_float((uint32_t)(w >> 32)));
+        };
+        ml = load8(p.part_ml + at);
+        const float2 x = load8(p.part_o + at * DP + col), y = load8(p.part_o + at * DP + col + 2);
+        o = f32x4{x.x, x.y, y.x, y.y};
+    });
 }
 
 // HERE: parts are joined within the launch.
@@ -729,7 +747,7 @@ __global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(A
     const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int worker = blockIdx.x;
 
-    AttendRange range = attend_range<4>(a, p, worker, 4 >> (p.chunk_shift < 2 ? p.chunk_shift : 2));
+    AttendRange range = attend_range<4>(a, p, worker, 4 >> (p.chunk_shift < 2 ? p.chunk_shift : 2), 1);
     if (range.at >= range.end) {
         if (!HERE && tid == 0) p.split[worker].n_rows = 0;
         return;
@@ -908,7 +926,7 @@ __global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(A
             }
         if constexpr (HERE) {
             static_assert(sizeof(so) >= 256 * 24, "the join's scratch");
-            if (!whole) join_parts<256, DP, F32>(a, p, u0, (f32x4*)&so[0][0][0]);
+            if (!whole) join_parts<256, DP>(a, p, u0, (f32x4*)&so[0][0][0]);
         }
     }
     if (!HERE && tid == 0) p.split[worker] = split;

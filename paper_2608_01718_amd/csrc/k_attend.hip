@@ -4,22 +4,7 @@
 
 namespace lacache {
 
-// The row groups that several workers had parts of: each of the workgroups (w, .) joins rows of the group that ended with
-// worker w.
-__device__ __forceinline__ int64_t part_at(const AttendPlan& p, const AttendSplit& s, int k, int row) {
-    return part_of(p, s.worker0 + k, k < s.parts - 1) + row;
-}
-__device__ __forceinline__ void store_joined(const AttendArgs& a, const AttendPlan& p, const AttendSplit& s, int row,
-                                             int col, const Joined& x) {
-    const int r = s.row + row, i = token_of(p, r);
-    const int64_t at = ((int64_t)s.seq_row0 + i) * a.q_heads + s.head0 + (r - i * a.group);
-    const f32x4 o = x.o * (x.l == 0.0f ? 0.0f : 1.0f / x.l);
-    if (col < a.pool.d) {
-        if (a.dtype == 0) store4<true>(a, at * a.pool.d + col, o);
-        else store4<false>(a, at * a.pool.d + col, o);
-    }
-    if (col == 0 && a.lse) a.lse[at] = lse_of(x.m, x.l);
-}
+constexpr int kJoinThreads = 256;
 
 // Many row groups, of few parts each: a thread four columns of a row, part after part (four loaded together).
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, AttendPlan p) {
@@ -35,7 +20,7 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, AttendPlan p)
             f32x4 o[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const int64_t at = part_at(p, s, k0 + u < parts ? k0 + u : parts - 1, row);
+                const int64_t at = part_of(p, s.worker0 + (k0 + u < parts ? k0 + u : parts - 1), k0 + u < parts - 1) + row;
                 ml[u] = p.part_ml[at];
                 o[u] = *(const f32x4*)(p.part_o + at * dp + col);
             }
@@ -47,39 +32,25 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, AttendPlan p)
     }
 }
 
-// Few row groups, of many parts each: a workgroup a row, a thread four columns of every (2048 / dp)-th part.
-__global__ __launch_bounds__(512) void k_attend_join_long(AttendArgs a, AttendPlan p) {
-    __shared__ float2 sml[512];
-    __shared__ f32x4 so[512];
-    const AttendSplit s = p.split[blockIdx.x];
-    const int tid = threadIdx.x, dp = a.pool.dp, lanes = dp / 4, groups = 512 / lanes;
-    const int col = tid % lanes * 4, part = tid / lanes;
-    const int parts = s.parts;
-    for (int row = blockIdx.y; row < s.n_rows; row += gridDim.y) {
-        Joined x;
-        if (part < groups)
-            for (int k0 = part; k0 < parts; k0 += 4 * groups) {
-                float2 ml[4];
-                f32x4 o[4];
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const int64_t at = part_at(p, s, k0 + u * groups < parts ? k0 + u * groups : parts - 1, row);
-                    ml[u] = p.part_ml[at];
-                    o[u] = *(const f32x4*)(p.part_o + at * dp + col);
-                }
-#pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    if (k0 + u * groups < parts) x.add(ml[u].x, ml[u].y, o[u]);
-            }
-        __syncthreads();
-        sml[tid] = make_float2(x.m, x.l);
-        so[tid] = x.o;
-        __syncthreads();
-        if (part == 0) {
-            const int live = groups < parts ? groups : parts;
-            for (int k = 1; k < live; ++k) x.add(sml[k * lanes + tid].x, sml[k * lanes + tid].y, so[k * lanes + tid]);
-            store_joined(a, p, s, row, col, x);
-        }
+// Few row groups, often of many parts each: the workgroups (x, .) join those that ended with one of `of` workers, each a
+// share of the rows.  The j-th of these workers is number (x + j) mod gridDim.x of the j-th gridDim.x of all, so that
+// neighbours among the workers, and those in regular steps, go to different workgroups.
+__global__ __launch_bounds__(kJoinThreads) void k_attend_join_few(AttendArgs a, AttendPlan p, int of) {
+    __shared__ f32x4 scratch[kJoinThreads * 3 / 2];
+    auto worker = [&](int j) { return j * (int)gridDim.x + (int)((blockIdx.x + j) % gridDim.x); };
+    const int mine = worker(threadIdx.x & 63);
+    uint64_t todo = __ballot((int)(threadIdx.x & 63) < of && mine < p.workers && p.split[mine].n_rows > 0);
+    for (; todo; todo &= todo - 1) {
+        const AttendSplit s = p.split[worker(__ffsll((unsigned long long)todo) - 1)];
+        const int groups = kJoinThreads / (a.pool.dp / 4);
+        int of_row = 1;
+        while (2 * of_row <= groups && (8 * of_row <= s.parts || (4 * of_row <= s.parts && 2 * of_row * s.n_rows <= groups)))
+            of_row *= 2;
+        join_rows<kJoinThreads>(a, p, s, a.pool.dp, of_row, threadIdx.x, blockIdx.y, gridDim.y, scratch,
+                                [&](int64_t at, int col, float2& ml, f32x4& o) {
+                                    ml = p.part_ml[at];
+                                    o = *(const f32x4*)(p.part_o + at * a.pool.dp + col);
+                                });
     }
 }
 
@@ -156,13 +127,27 @@ hipError_t launch_kv_attend(const AttendArgs& a, int max_new, void* workspace, i
                                             : launch_attend<256>(a, p, s);
     if (e != hipSuccess || p.join_here) return e;
     // rows of a row group, row groups
-    int64_t rows = (int64_t)(max_new > 0 ? max_new : 64) * a.group, of_seq = ((rows - 1) >> p.group_shift) + 1;
+    int64_t rows = (int64_t)(max_new > 0 ? max_new : 64) * a.group;
+    const int64_t groups_most = a.seqs.n_seq * (int64_t)a.pool.heads * (((rows - 1) >> p.group_shift) + 1);
     rows = rows < (1 << p.group_shift) ? rows : 1 << p.group_shift;
-    if (a.seqs.n_seq * (int64_t)a.pool.heads * of_seq < 64) {
-        k_attend_join_long<<<dim3((unsigned)p.workers, (unsigned)(rows < 32 ? rows : 32)), dim3(512), 0, s>>>(a, p);
+    const int64_t lane_groups = kJoinThreads / (a.pool.dp / 4);
+    if (groups_most >= 64) {
+        k_attend_join<<<dim3((unsigned)p.workers, (unsigned)((rows + lane_groups - 1) / lane_groups)), dim3(kJoinThreads), 0,
+                        s>>>(a, p);
     } else {
-        const int64_t at_once = 1024 / a.pool.dp;
-        k_attend_join<<<dim3((unsigned)p.workers, (unsigned)((rows + at_once - 1) / at_once)), dim3(256), 0, s>>>(a, p);
+        // About one row group that was split for each workgroup in x, and one pass over its rows, but no more than 2048
+        // workgroups: of a launch of 16,384 that find nothing most of the time is theirs (4 sequences of 1024 tokens, 16 new
+        // ones, 4 kv heads: 24 us for the whole call, 189 with a workgroup of 512 threads for each worker and 4 rows).  With
+        // more row groups that end anywhere, workgroups would get several of them in turn (32 sequences of 512 to 4096
+        // tokens, 21 new ones: 75 us this way, 65 with a launch for all workers).
+        int of = 1;
+        while (of < 16 && 2 * of * groups_most <= p.workers) of *= 2;
+        const int64_t x = (p.workers + of - 1) / of, parts = p.workers / groups_most + 1;
+        int64_t at_once = lane_groups;
+        for (int64_t of_row = 1; at_once > 1 && 8 * of_row <= parts; of_row *= 2) at_once /= 2;
+        int64_t y = (rows + at_once - 1) / at_once;
+        y = y < 2048 / x ? y : 2048 / x;
+        k_attend_join_few<<<dim3((unsigned)x, (unsigned)(y > 1 ? y : 1)), dim3(kJoinThreads), 0, s>>>(a, p, of);
     }
     return hipGetLastError();
 }
