@@ -114,12 +114,13 @@ hipError_t launch_kv_attend(const AttendArgs& a, int max_new, void* workspace, i
     while (groups * a.pool.heads * (((tiles - 1) >> p.chunk_shift) + 1) > INT32_MAX / 2 && p.chunk_shift < 30)
         ++p.chunk_shift;
     // Small calls join their parts in the launch: where each wave has a tile at most, by what the page tables (or the
-    // window) can hold.  One launch less is 2 us on the host and 1 us on the GPU (one sequence of 777 tokens, 8 heads 11.5 us,
-    // 13.7 in two); with more parts to join, or parts of many rows, the launch is faster (131,071 tokens 88 us, 93 joined in
-    // the launch; 64 sequences in fp8 99, 103; 151 new tokens 174, 208).
+    // window) can hold, and a row group has few parts.  One launch less is 2 us on the host and 1 us on the GPU (one sequence of
+    // 777 tokens, 8 heads 11.5 us, 13.7 in two); with more parts to join, or parts of many rows, the launch is faster (131,071
+    // tokens 88 us, 93 joined in the launch; 64 sequences in fp8 99, 103; 151 new tokens 174, 208; 7 heads on one of 33,000
+    // tokens, 260 parts 19, 53; of 1000 tokens 13.4, 10.5).
     const int64_t seen = a.window > 0 && a.window / 32 + 2 + (int64_t)max_new / 32 < tiles && max_new > 0
                              ? a.window / 32 + 2 + max_new / 32 : tiles;
-    p.join_here = p.group_shift == 4 && groups * a.pool.heads * seen <= 4 * (int64_t)p.workers;
+    p.join_here = p.group_shift == 4 && seen <= 64 && groups * a.pool.heads * seen <= 4 * (int64_t)p.workers;
     const hipError_t e = a.pool.dp == 64    ? launch_attend<64>(a, p, s)
                          : a.pool.dp == 96  ? launch_attend<96>(a, p, s)
                          : a.pool.dp == 128 ? launch_attend<128>(a, p, s)
