@@ -113,15 +113,22 @@ struct AttendRange {
 template <int WAVES>
 __device__ __forceinline__ AttendRange attend_range(const AttendArgs& a, const AttendPlan& p, int worker, int grain, int least) {
     constexpr int THREADS = 64 * WAVES;
-    __shared__ int total_of[WAVES], found[2];
+    __shared__ int total_of[WAVES], found[2], longest_of[WAVES];
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, n_seq = a.seqs.n_seq;
-    int own = 0, sum = 0, all = 0, b = tid;
+    int own = 0, sum = 0, all = 0, b = tid, longest = 1;
     // items up to sequence b within a round of THREADS (sum), and of the round (returned)
     auto scan = [&]() {
-        own = b < n_seq ? attend_span(a, p, b).items(a) : 0;
+        int chunks = 0;
+        own = 0;
+        if (b < n_seq) {
+            const AttendSpan s = attend_span(a, p, b);
+            own = s.items(a);
+            chunks = own > 0 ? s.chunks : 0;
+        }
         sum = wave_scan(own);
+        const int length = __any(chunks > 2) ? 4 : __any(chunks == 2) ? 2 : 1;  // of a row group, up to 4
         __syncthreads();
-        if (lane == 63) total_of[wid] = sum;
+        if (lane == 63) total_of[wid] = sum, longest_of[wid] = length;
         __syncthreads();
         int round = 0;
 #pragma unroll
@@ -129,6 +136,7 @@ __device__ __forceinline__ AttendRange attend_range(const AttendArgs& a, const A
             const int t = total_of[w];
             sum += w < wid ? t : 0;
             round += t;
+            longest = max(longest, longest_of[w]);
         }
         return round;
     };
@@ -136,6 +144,9 @@ __device__ __forceinline__ AttendRange attend_range(const AttendArgs& a, const A
     all = __builtin_amdgcn_readfirstlane(all);
     AttendRange r;
     r.per = (int)(((uint32_t)all + (uint32_t)p.workers - 1) / (uint32_t)p.workers);
+    // (no multiple of more than a row group has: a workgroup would get several of them)
+    longest = __builtin_amdgcn_readfirstlane(longest);
+    grain = grain < longest ? grain : longest;
     r.per = r.per < least ? least : r.per;
     r.per = (r.per + grain - 1) & ~(grain - 1);
     const int64_t at = (int64_t)worker * r.per;
