@@ -495,7 +495,9 @@ int lacache_kv_read(const lacache_kv *kv, const lacache_seqs *seqs, void *k_out,
  *              leaves its counters there at zero.  For one call at a time:
  *              calls that overlap on one workspace give wrong results, until
  *              it is cleared again
- * EINVAL too if workspace_bytes is less.
+ * EINVAL too if workspace_bytes is less, if rows q_heads / heads is 2^31 or more,
+ * or if there could be more than 2^30 row groups (a row group is 16 rows or more
+ * of one sequence and kv head; the pieces of work are counted in 32 bits).
  */
 int64_t lacache_kv_attend_workspace(const lacache_kv *kv, lacache_dtype dtype, int32_t n_seq, int32_t q_heads,
                                     int32_t max_new);

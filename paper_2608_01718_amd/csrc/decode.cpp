@@ -142,7 +142,8 @@ int lacache_kv_attend(const lacache_kv* kv, const lacache_seqs* seqs, const void
     AttendArgs a{};
     if (!to_pool(kv, true, &a.pool) || !to_seqs(seqs, rows, &a.seqs) || !is_dtype(dtype) || q_heads < 1 ||
         q_heads > 65535 || q_heads % kv->heads != 0 || q_row < 0 || max_new < 0 || !std::isfinite(scale) ||
-        rows * (q_heads / kv->heads) > INT32_MAX || window < 0 || workspace_bytes < 0)
+        rows * (q_heads / kv->heads) > INT32_MAX || window < 0 || workspace_bytes < 0 ||
+        !attend_fits(a.pool, (int)dtype, rows, seqs->n_seq, q_heads / kv->heads, max_new))
         return LACACHE_EINVAL;
     if (rows == 0 || seqs->n_seq == 0) return LACACHE_OK;
     const uintptr_t esz = dtype == LACACHE_F32 ? 4 : 2;

@@ -5,6 +5,7 @@
 namespace lacache {
 
 constexpr int kJoinThreads = 256;
+constexpr int64_t kMostItems = INT32_MAX / 2;  // chunks of tiles of all row groups
 
 // Many row groups, of few parts each: a thread four columns of a row, part after part (four loaded together).
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, AttendPlan p) {
@@ -91,7 +92,17 @@ AttendPlan plan_of(const KvPool& pool, bool f32, int n_seq, int max_new, int gro
     return p;
 }
 
+// More than the row groups of all (sequence, kv head) together.  Sequences without rows have none.
+int64_t row_groups(const KvPool& pool, int64_t rows, int n_seq, int group, int group_shift) {
+    return (((rows * group) >> group_shift) + (n_seq < rows ? n_seq : rows)) * pool.heads;
+}
+
 }  // namespace
+
+bool attend_fits(const KvPool& pool, int dtype, int64_t rows, int n_seq, int group, int max_new) {
+    const Shape sh = shape_of(pool, dtype == 0, (int64_t)(max_new > 0 ? max_new : 64) * group);
+    return row_groups(pool, rows, n_seq, group, sh.group_shift) <= kMostItems;
+}
 
 int64_t attend_workspace(const KvPool& pool, int dtype, int n_seq, int q_heads, int max_new, int num_cu) {
     int64_t bytes;
@@ -108,11 +119,10 @@ hipError_t launch_kv_attend(const AttendArgs& a, int max_new, void* workspace, i
     while ((1 << bits) < a.group) ++bits;
     p.group_bits = 31 + bits;
     p.group_magic = (uint32_t)((((uint64_t)1 << p.group_bits) + a.group - 1) / a.group);
-    // the chunks of all row groups are counted in 32 bits
+    // the chunks of all row groups are counted in 32 bits (a chunk holds a whole sequence at the latest: attend_fits)
     const int64_t tiles = ((int64_t)a.seqs.max_pages << (a.pool.page_shift - 5)) + 1;
-    const int64_t groups = ((a.seqs.rows * a.group) >> p.group_shift) + a.seqs.n_seq;
-    while (groups * a.pool.heads * (((tiles - 1) >> p.chunk_shift) + 1) > INT32_MAX / 2 && p.chunk_shift < 30)
-        ++p.chunk_shift;
+    const int64_t units = row_groups(a.pool, a.seqs.rows, a.seqs.n_seq, a.group, p.group_shift);
+    while (units * (((tiles - 1) >> p.chunk_shift) + 1) > kMostItems && p.chunk_shift < 30) ++p.chunk_shift;
     // Small calls join their parts in the launch: where each wave has a tile at most, by what the page tables (or the
     // window) can hold, and a row group has few parts.  One launch less is 2 us on the host and 1 us on the GPU (one sequence of
     // 777 tokens, 8 heads 11.5 us, 13.7 in two); with more parts to join, or parts of many rows, the launch is faster (131,071
@@ -120,7 +130,7 @@ hipError_t launch_kv_attend(const AttendArgs& a, int max_new, void* workspace, i
     // tokens, 260 parts 19, 53; of 1000 tokens 13.4, 10.5).
     const int64_t seen = a.window > 0 && a.window / 32 + 2 + (int64_t)max_new / 32 < tiles && max_new > 0
                              ? a.window / 32 + 2 + max_new / 32 : tiles;
-    p.join_here = p.group_shift == 4 && seen <= 64 && groups * a.pool.heads * seen <= 4 * (int64_t)p.workers;
+    p.join_here = p.group_shift == 4 && seen <= 64 && units * seen <= 4 * (int64_t)p.workers;
     const hipError_t e = a.pool.dp == 64    ? launch_attend<64>(a, p, s)
                          : a.pool.dp == 96  ? launch_attend<96>(a, p, s)
                          : a.pool.dp == 128 ? launch_attend<128>(a, p, s)
@@ -128,8 +138,9 @@ hipError_t launch_kv_attend(const AttendArgs& a, int max_new, void* workspace, i
                                             : launch_attend<256>(a, p, s);
     if (e != hipSuccess || p.join_here) return e;
     // rows of a row group, row groups
-    int64_t rows = (int64_t)(max_new > 0 ? max_new : 64) * a.group;
-    const int64_t groups_most = a.seqs.n_seq * (int64_t)a.pool.heads * (((rows - 1) >> p.group_shift) + 1);
+    int64_t rows = (max_new <= 0 ? 64 : max_new < a.seqs.rows ? max_new : a.seqs.rows) * a.group;
+    const int64_t live = a.seqs.n_seq < a.seqs.rows ? a.seqs.n_seq : a.seqs.rows;
+    const int64_t groups_most = live * a.pool.heads * (((rows - 1) >> p.group_shift) + 1);
     rows = rows < (1 << p.group_shift) ? rows : 1 << p.group_shift;
     const int64_t lane_groups = kJoinThreads / (a.pool.dp / 4);
     if (groups_most >= 64) {

@@ -234,6 +234,8 @@ struct AttendArgs {
     int64_t q_row;
     float scale;
 };
+// Whether the row groups of a call can be counted in 32 bits.
+bool attend_fits(const KvPool& pool, int dtype, int64_t rows, int n_seq, int group, int max_new);
 int64_t attend_workspace(const KvPool& pool, int dtype, int n_seq, int q_heads, int max_new, int num_cu);
 hipError_t launch_kv_attend(const AttendArgs& a, int max_new, void* workspace, int num_cu, hipStream_t s);
 
