@@ -636,10 +636,31 @@ def lacache_rope_table(n: int, rot: int, base: float = 10000.0, factor: float = 
     return out
 
 
+class _RopeGrad(torch.autograd.Function):
+    """lacache_rope under autograd: the gradient is the other rotation of the two."""
+
+    @staticmethod
+    def forward(ctx, x, pos, rope, backward, stream):
+        ctx.rope, ctx.turns_back = rope, backward
+        ctx.save_for_backward(pos, rope.table)
+        return lacache_rope(x, pos, rope, backward, None, stream)
+
+    @staticmethod
+    def backward(ctx, dy):
+        pos, _ = ctx.saved_tensors
+        dy = dy if dy.stride(2) == 1 else dy.contiguous()
+        return lacache_rope(dy, pos, ctx.rope, not ctx.turns_back), None, None, None, None
+
+
 def lacache_rope(x, pos, rope: Rope, backward: bool = False, out=None, stream=None):
     """x [rows, H, d] float32 or bfloat16 (any strides, the last one 1), pos [rows] int32.  Returns the turned rows
     (`out`, which may be x; otherwise a new contiguous tensor); with backward=True the gradient of the input from that of
-    the output."""
+    the output.  autograd differentiates it with respect to x (not through `out`, and not with respect to the table)."""
+    if torch.is_grad_enabled():
+        if rope.table.requires_grad or (out is not None and (x.requires_grad or out.requires_grad)):
+            raise ValueError("a table that needs a gradient has none, nor does a result written into `out`")
+        if x.requires_grad:
+            return _RopeGrad.apply(x, pos, rope, bool(backward), stream)
     index, dtype, shape, xs = x.get_device(), _ROW_DTYPES.get(x.dtype), x.shape, x.stride()
     if len(shape) != 3 or dtype is None or index < 0 or (shape[2] > 1 and xs[2] != 1):
         raise ValueError("x: expected a float32 or bfloat16 [rows, H, d] tensor on a GPU, its last stride 1")
