@@ -557,12 +557,19 @@ class Sequences:
         return self._c.n_seq
 
 
+def _no_gradient(name: str) -> ValueError:
+    """What autograd would want to follow: the cache keeps numbers, and no graph."""
+    return ValueError(f"{name}: has no gradient, and a tensor requires one (torch.no_grad() or detach() say that none is "
+                      "wanted)")
+
+
 class KVCache:
     """A paged key-value cache: the pools of lacache_kv in torch tensors, and the scratch of its attention.  Without
     `pools` they are allocated here (zeros): k and v [n_pages, heads, page / 32, 32 D] (D: d padded to 64, 96, 128, 192 or
     256) bfloat16, float8_e4m3fn or int8, and for the last two k_scale and v_scale [n_pages, heads, page] float32.  With
     pools = (k, v, k_scale, v_scale) these tensors are used.  Calls on one cache are ordered on one stream (or by events):
-    they share the pools and the scratch."""
+    they share the pools and the scratch.  No gradient passes through a cache: with autograd on, its calls refuse tensors that
+    require one."""
 
     def __init__(self, n_pages: int = 0, heads: int = 0, d: int = 0, page: int = 64, type: int = KV_BF16, device: int = 0,
                  pools=None):
@@ -685,6 +692,10 @@ def lacache_kv_append(c: KVCache, k, v, seqs: Sequences, q=None, rope=None, q_ou
     dtype = _ROW_DTYPES.get(kind)
     if dtype is None:
         raise ValueError(f"k: unsupported dtype {kind}")
+    if torch.is_grad_enabled() and (k.requires_grad or v.requires_grad or (q is not None and q.requires_grad) or
+                                    (q_out is not None and q_out.requires_grad) or
+                                    (rope is not None and rope.table.requires_grad)):
+        raise _no_gradient("lacache_kv_append")
     k_row, v_row = _rows(k, c.heads, c.d, index, kind, "k"), _rows(v, c.heads, c.d, index, kind, "v")
     rows = k.shape[0]
     if v.shape[0] != rows or seqs.index != index or (rope is not None and rope.index != index):
@@ -714,6 +725,8 @@ def lacache_kv_read(c: KVCache, seqs: Sequences, rows: int, dtype=torch.bfloat16
         k, v = _made(c.k, shape, dtype, stream), _made(c.k, shape, dtype, stream)
     else:
         k, v = _given(out[0], shape, dtype, index, "k"), _given(out[1], shape, dtype, index, "v")
+        if torch.is_grad_enabled() and (k.requires_grad or v.requires_grad):
+            raise _no_gradient("lacache_kv_read")
     _check(_on(index, stream, _lib.lacache_kv_read, c._ref, seqs._ref, k.data_ptr(), v.data_ptr(), kind, rows, max_new),
            "lacache_kv_read")
     return k, v
@@ -738,6 +751,8 @@ def lacache_kv_attend(c: KVCache, q, seqs: Sequences, scale=None, window: int = 
         raise ValueError(f"q: expected float32 or bfloat16 [rows, q_heads, d], and sequences on cuda:{index}")
     rows, q_heads = shape[0], shape[1]
     q_row = _rows(q, q_heads, c.d, index, kind, "q")
+    if torch.is_grad_enabled() and (q.requires_grad or (out is not None and (out[0].requires_grad or out[1].requires_grad))):
+        raise _no_gradient("lacache_kv_attend")
     if out is None:
         out = (_made(q, shape, kind, stream), _made(q, shape[:2], torch.float32, stream))
     else:

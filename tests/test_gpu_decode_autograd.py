@@ -83,3 +83,19 @@ def test_rope_refuses_where_a_gradient_would_be_lost(lc, rope):
             call()
         with torch.no_grad():
             call()
+
+
+def test_the_cache_refuses_where_a_gradient_would_be_lost(lc):
+    cache, seqs, q, k, v = made(lc)
+    rope = lc.Rope(lc.lacache_rope_table(50, 48))
+    table = lc.Rope(rope.table.clone().requires_grad_())
+    grad = lambda t: t.clone().requires_grad_()  # noqa: E731
+    for call in (lambda: cache.append(grad(k), v, seqs), lambda: cache.append(k, grad(v), seqs),
+                 lambda: cache.append(k, v, seqs, q=grad(q), rope=rope), lambda: cache.append(k, v, seqs, rope=table),
+                 lambda: cache.append(k, v, seqs, q=q, rope=rope, q_out=grad(q)), lambda: cache.attend(grad(q), seqs),
+                 lambda: cache.attend(q, seqs, out=(grad(q), torch.zeros((3, 4), device=DEV))),
+                 lambda: cache.read(seqs, 3, dtype=torch.float32, out=(grad(k), v.clone()))):
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+        with torch.no_grad():
+            call()
