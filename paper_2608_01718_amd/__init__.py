@@ -525,6 +525,9 @@ def _given(t: torch.Tensor, shape, dtype, index: int, name: str) -> torch.Tensor
     return t
 
 
+_written = torch.autograd.graph.increment_version  # what autograd goes by to see that a tensor it keeps was written into
+
+
 class Rope:
     """A rotary table [positions, rot / 2, 2] (cos, sin; float32, for example from lacache_rope_table) and the layout of
     the pairs."""
@@ -602,6 +605,7 @@ class KVCache:
         self._c = _KV(k.data_ptr(), v.data_ptr(), *(0 if t is None else t.data_ptr() for t in (ks, vs)), n_pages, page,
                       heads, d, type)
         self._ref = ctypes.addressof(self._c)
+        self._pools = tuple(t for t in (k, v, ks, vs) if t is not None)
         self._need, self._space, self._outgrown = {}, None, []
 
     def _scratch(self, like, need: int, stream):
@@ -640,6 +644,7 @@ def lacache_rope_table(n: int, rot: int, base: float = 10000.0, factor: float = 
     _given(out, shape, torch.float32, device, "out")
     _check(_on(device, stream, _lib.lacache_rope_table, out.data_ptr(), first, n, rot, base, factor, original, low, high,
                magnitude), "lacache_rope_table")
+    _written(out)
     return out
 
 
@@ -672,7 +677,8 @@ def lacache_rope(x, pos, rope: Rope, backward: bool = False, out=None, stream=No
     if len(shape) != 3 or dtype is None or index < 0 or (shape[2] > 1 and xs[2] != 1):
         raise ValueError("x: expected a float32 or bfloat16 [rows, H, d] tensor on a GPU, its last stride 1")
     rows, H, d = shape
-    if out is None:
+    given = out is not None
+    if not given:
         out = _made(x, shape, x.dtype, stream)
     elif out.shape != shape or out.dtype != x.dtype or out.get_device() != index or (d > 1 and out.stride(2) != 1):
         raise ValueError(f"out: expected {tuple(shape)} {x.dtype} on cuda:{index}, its last stride 1")
@@ -682,6 +688,8 @@ def lacache_rope(x, pos, rope: Rope, backward: bool = False, out=None, stream=No
     ys = out.stride()
     _check(_on(index, stream, _lib.lacache_rope, x.data_ptr(), out.data_ptr(), dtype, rows, H, d, xs[0], xs[1], ys[0],
                ys[1], pos.data_ptr(), rope._ref, int(backward)), "lacache_rope")
+    if given:
+        _written(out)
     return out
 
 
@@ -711,6 +719,7 @@ def lacache_kv_append(c: KVCache, k, v, seqs: Sequences, q=None, rope=None, q_ou
         q_ptr, o_ptr = q.data_ptr(), q_out.data_ptr()
     _check(_on(index, stream, _lib.lacache_kv_append, c._ref, seqs._ref, k.data_ptr(), v.data_ptr(), dtype, rows, k_row,
                v_row, q_ptr, o_ptr, q_heads, q_row, None if rope is None else rope._ref, max_new), "lacache_kv_append")
+    _written(c._pools if q is None else (*c._pools, q_out))
     return q_out if q is not None else None
 
 
@@ -729,6 +738,8 @@ def lacache_kv_read(c: KVCache, seqs: Sequences, rows: int, dtype=torch.bfloat16
             raise _no_gradient("lacache_kv_read")
     _check(_on(index, stream, _lib.lacache_kv_read, c._ref, seqs._ref, k.data_ptr(), v.data_ptr(), kind, rows, max_new),
            "lacache_kv_read")
+    if out is not None:
+        _written((k, v))
     return k, v
 
 
@@ -751,9 +762,10 @@ def lacache_kv_attend(c: KVCache, q, seqs: Sequences, scale=None, window: int = 
         raise ValueError(f"q: expected float32 or bfloat16 [rows, q_heads, d], and sequences on cuda:{index}")
     rows, q_heads = shape[0], shape[1]
     q_row = _rows(q, q_heads, c.d, index, kind, "q")
-    if torch.is_grad_enabled() and (q.requires_grad or (out is not None and (out[0].requires_grad or out[1].requires_grad))):
+    given = out is not None
+    if torch.is_grad_enabled() and (q.requires_grad or (given and (out[0].requires_grad or out[1].requires_grad))):
         raise _no_gradient("lacache_kv_attend")
-    if out is None:
+    if not given:
         out = (_made(q, shape, kind, stream), _made(q, shape[:2], torch.float32, stream))
     else:
         _given(out[0], shape, kind, index, "out")
@@ -768,6 +780,8 @@ def lacache_kv_attend(c: KVCache, q, seqs: Sequences, scale=None, window: int = 
     _check(_on(index, stream, _lib.lacache_kv_attend, c._ref, seqs._ref, q.data_ptr(), dtype, rows, q_heads, q_row,
                max_new, c.d ** -0.5 if scale is None else scale, window, out[0].data_ptr(), out[1].data_ptr(),
                space.data_ptr(), space.numel()), "lacache_kv_attend")
+    if given:
+        _written(out)
     return out
 
 

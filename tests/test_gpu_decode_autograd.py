@@ -99,3 +99,36 @@ def test_the_cache_refuses_where_a_gradient_would_be_lost(lc):
             call()
         with torch.no_grad():
             call()
+
+
+def test_written_tensors_are_known_to_have_changed(lc, rope):
+    """autograd keeps a tensor for its backward pass and checks then that nothing has been written into it."""
+    cache, seqs, q, k, v = made(lc)
+    full = lc.Rope(lc.lacache_rope_table(50, 48))
+    pos = torch.zeros(3, dtype=torch.int32, device=DEV)
+
+    def changes(t, call):
+        w = torch.ones_like(t).requires_grad_()
+        y = (w * t).sum()      # keeps t
+        call()
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward()
+
+    x = torch.randn((3, 2, 48), device=DEV)
+    changes(x, lambda: lc.lacache_rope(x, pos, rope, out=x))
+    changes(q, lambda: cache.append(k, v, seqs, q=q, rope=full, q_out=q))
+    out = torch.zeros_like(q), torch.zeros((3, 4), device=DEV)
+    for t in out:
+        changes(t, lambda: cache.attend(q, seqs, out=out))
+    back = torch.zeros_like(k), torch.zeros_like(v)
+    for t in back:
+        changes(t, lambda: cache.read(seqs, 3, dtype=torch.float32, out=back))
+    table = torch.zeros((4, 16, 2), device=DEV)
+    changes(table, lambda: lc.lacache_rope_table(4, 32, out=table))
+    coded = lc.KVCache(4, 2, 48, page=32, type=lc.KV_INT8)
+    for t in (cache.k, cache.v, coded.k_scale, coded.v_scale):
+        changes(t, lambda: (cache if t.dtype == torch.bfloat16 else coded).append(k, v, seqs))
+    with torch.inference_mode():  # tensors without versions
+        x = torch.randn((3, 2, 48), device=DEV)
+        assert lc.lacache_rope(x, pos, rope, out=x) is x
+        cache.append(x.new_zeros((3, 2, 48)), x, seqs)
