@@ -577,8 +577,9 @@ class KVCache:
     def __init__(self, n_pages: int = 0, heads: int = 0, d: int = 0, page: int = 64, type: int = KV_BF16, device: int = 0,
                  pools=None):
         if pools is None:
-            if type not in _KV_DTYPES or page not in (32, 64, 128, 256) or d < 1 or d > 256:
-                raise ValueError("KVCache: expected a KV_ type, a page of 32, 64, 128 or 256 tokens and 1 <= d <= 256")
+            if type not in _KV_DTYPES or not _kv_fits(n_pages, heads, d, page):
+                raise ValueError("KVCache: expected a KV_ type, at least one head, a page of 32, 64, 128 or 256 tokens and d as a "
+                                 "multiple of 8 up to 256")
             dev = torch.device("cuda", device)
             shape = (n_pages, heads, page // 32, 32 * _padded(d))
             # (zeros of a one-byte type: fp8 has no fill everywhere, its zero is the byte 0)
@@ -593,6 +594,8 @@ class KVCache:
             n_pages, heads, page = k.shape[0], k.shape[1], 32 * k.shape[2]
             if not 1 <= d <= 256 or k.shape[3] != 32 * _padded(d):
                 raise ValueError(f"pools: tiles of {k.shape[3]} elements do not fit d = {d}")
+            if not _kv_fits(n_pages, heads, d, page):
+                raise LaCacheError(EINVAL, f"pools of {n_pages} pages, {heads} heads, d = {d}, {page} tokens a page")
             _given(k, k.shape, k.dtype, dev.index, "k")
             _given(v, k.shape, k.dtype, dev.index, "v")
             for t, name in ((ks, "k_scale"), (vs, "v_scale")):
@@ -627,6 +630,11 @@ class KVCache:
 
     def attend(self, q, seqs, scale=None, window=0, max_new=0, out=None, stream=None):
         return lacache_kv_attend(self, q, seqs, scale, window, max_new, out, stream)
+
+
+def _kv_fits(n_pages: int, heads: int, d: int, page: int) -> bool:
+    """What the calls take (lacache_kv)."""
+    return 0 <= n_pages < 1 << 31 and 1 <= heads <= 65535 and 8 <= d <= 256 and d % 8 == 0 and page in (32, 64, 128, 256)
 
 
 def _padded(d: int) -> int:
