@@ -434,8 +434,9 @@ int lacache_rope_table(float *table, int64_t first, int64_t n, int32_t rot, doub
 /*
  * y = x turned by the positions of its rows; columns from rot on are copied.
  *   x, y   rows of H heads of d columns (dtype), row t at x + t * x_row, head h
- *          at + h * x_head elements (y likewise); y may be x itself, and must
- *          not overlap it otherwise
+ *          at + h * x_head elements (y likewise, and no two of its rows and
+ *          heads share elements); y may be x itself with the same strides, and
+ *          must not overlap it otherwise
  *   pos    [rows] int32
  *   backward != 0: the transposed rotation, so that with dy in x the result is
  *          dx: the gradient with respect to the input

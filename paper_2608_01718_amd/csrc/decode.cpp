@@ -91,6 +91,9 @@ int lacache_rope(const void* x, void* y, lacache_dtype dtype, int64_t rows, int3
     if (rows == 0) return LACACHE_OK;
     const uintptr_t esz = dtype == LACACHE_F32 ? 4 : 2;
     if (!x || !y || !pos || !aligned(x, esz) || !aligned(y, esz)) return LACACHE_EINVAL;
+    // rows and heads of the result that share elements; a result over its input in another order
+    if ((rows > 1 && (y_row < d || (x == y && x_row != y_row))) || (H > 1 && (y_head < d || (x == y && x_head != y_head))))
+        return LACACHE_EINVAL;
     return launch_rope(x, y, (int)dtype, rows, H, d, x_row, x_head, y_row, y_head, pos, r, backward != 0,
                        (hipStream_t)stream) == hipSuccess ? LACACHE_OK : LACACHE_EHIP;
 }

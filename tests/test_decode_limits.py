@@ -32,3 +32,14 @@ def test_attention_of_more_row_groups_than_are_counted(lc, rows, n_seq, heads, q
 def test_a_cache_that_no_call_would_take_is_not_allocated(lc, kw):
     with pytest.raises(ValueError):
         lc.KVCache(**{**dict(n_pages=4, heads=2, d=64, page=64, type=lc.KV_BF16), **kw})
+
+
+@pytest.mark.parametrize("x,y,strides", [(FAKE, 2 * FAKE, (512, 128, 0, 128)), (FAKE, 2 * FAKE, (512, 128, 512, 0)),
+                                         (FAKE, 2 * FAKE, (512, 128, 127, 1024)), (FAKE, 2 * FAKE, (512, 128, 512, 64)),
+                                         (FAKE, FAKE, (512, 128, 1024, 128)), (FAKE, FAKE, (512, 128, 512, 256)),
+                                         (FAKE, FAKE, (0, 128, 0, 128))])
+def test_rotated_rows_that_would_overlap_are_refused(lc, x, y, strides):
+    """Rows or heads of the result that share elements, and a result over the input in another order."""
+    rope = lc._Rotary(FAKE, 100, 64, 0)
+    turn = lc.raw_library().lacache_rope
+    assert turn(x, y, 1, 3, 4, 128, *strides, FAKE, ref(rope), 0, None) == EINVAL
