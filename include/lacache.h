@@ -484,9 +484,13 @@ int lacache_kv_read(const lacache_kv *kv, const lacache_seqs *seqs, void *k_out,
  *   p - j < window if window > 0:
  *   out   [rows][q_heads][d] (dtype) = sum_j w_j v_j, w = softmax(scale q.k_j)
  *   lse   [rows][q_heads] float = log sum_j exp(scale q.k_j); NULL: not wanted.
- *         A row that sees nothing has out = 0 and lse = -infinity.
- *         Infinities and NaN make the results of the rows that see them
- *         infinite or NaN (a value in its column alone), and no others.
+ *         A row that sees nothing, or whose every score is -infinity, has
+ *         out = 0 and lse = -infinity.
+ *         An infinity or NaN among the values makes its column of the rows
+ *         that see it infinite or NaN; a query or key that makes a score NaN
+ *         or +infinity makes the row NaN.  A score of -infinity is the weight
+ *         0; with float32 rows, whose queries are sums of terms, an infinite
+ *         key may make it NaN.  No other row's results change.
  * Products are exact and sums are in float32; with bfloat16 rows the weights
  * are rounded to 16 bits before they multiply the values.
  *   max_new    a bound on the new tokens of a sequence (for the launch shape

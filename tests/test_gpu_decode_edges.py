@@ -3,6 +3,7 @@ up to 32 rows, calls that do not take the wide ones.  Results are held to bounds
 from __future__ import annotations
 
 import ctypes
+import math
 
 import pytest
 import torch
@@ -240,3 +241,47 @@ def test_append_and_read_of_a_prompt_among_single_tokens(lc, kind, dtype, max_ne
     kb, vb = pg.cache.read(seqs, T, dtype=torch.float32, max_new=max_new)
     assert same(kb, ref.values(*ref.coded(ref.turned(k, at, False), kind)))
     assert same(vb, ref.values(*ref.coded(v.float(), kind)))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("shape", ROWS)
+def test_keys_that_are_infinite(lc, dtype, shape):
+    """A score of -infinity is the weight 0 (with float32 rows, whose queries are sums of terms, it may be a NaN too), one of
+    +infinity makes the row NaN.  Rows that do not see the key are as if it were not there."""
+    new, heads, Hq, d = shape
+    say(f"[case] infinite keys {dtype} {shape}")
+    length, at = 300, 300 - 1 - new // 2
+    pg, held = filled(lc, "bf16", heads, d, 32, [length], seed=9)
+    q = queries(new, Hq, d, dtype)
+    q[..., 3] = q[..., 3].abs() + 1
+    j, p = torch.arange(length, device=DEV)[None], torch.arange(length - new, length, device=DEV)[:, None]
+    for bad in (-math.inf, math.inf):
+        k, v = (x.float().clone() for x in held[0])
+        k[at, :, 3] = bad
+        pg.cache.append(k, v, pg.seqs([length], [length]))
+        o, lse = pg.cache.attend(q, pg.seqs([new], [length]), max_new=new)
+        without = (j <= p) & (j != at)
+        want = ref.attention(q.double(), *held[0], without, d ** -0.5)
+        eo, el = ex.bounds(want, d, dtype == torch.float32)
+        near = ((o.double() - want[0]).abs() <= eo).all(2) & ((lse.double() - want[1]).abs() <= el)
+        nan = o.isnan().all(2) & lse.isnan()
+        sees = (p[:, 0] >= at)[:, None].expand_as(near)
+        assert bool(near[~sees].all())
+        if bad > 0:
+            assert bool(nan[sees].all())
+        else:
+            assert bool((near | nan if dtype == torch.float32 else near)[sees].all())
+
+
+def test_rows_whose_every_score_is_minus_infinity(lc):
+    """They are as rows that see nothing."""
+    pg, held = filled(lc, "bf16", 2, 64, 32, [70, 5000], seed=9)
+    k, v = (torch.cat([h[i] for h in held]).float() for i in (0, 1))
+    k[:, 0, 3] = -math.inf
+    pg.cache.append(k, v, pg.seqs([70, 5000], [70, 5000]))
+    for new in (1, 21):
+        q = queries(2 * new, 4, 64, torch.bfloat16)
+        q[..., 3] = q[..., 3].abs() + 1
+        o, lse = pg.cache.attend(q, pg.seqs([new, new], [70, 5000]), max_new=new)
+        assert bool((o[:, :2] == 0).all()) and bool((lse[:, :2] == -math.inf).all())
+        assert bool(o[:, 2:].isfinite().all()) and bool(lse[:, 2:].isfinite().all())
