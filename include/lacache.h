@@ -495,11 +495,11 @@ int lacache_kv_read(const lacache_kv *kv, const lacache_seqs *seqs, void *k_out,
  * are rounded to 16 bits before they multiply the values.
  *   max_new    a bound on the new tokens of a sequence (for the launch shape
  *              alone; 0: not known)
- *   workspace  lacache_kv_attend_workspace bytes of device memory, 16-byte
- *              aligned, zero before the first call that uses them; a call
- *              leaves its counters there at zero.  For one call at a time:
- *              calls that overlap on one workspace give wrong results, until
- *              it is cleared again
+ *   workspace  lacache_kv_attend_workspace bytes of device memory (the same for
+ *              any number of sequences), 16-byte aligned, zero before the first
+ *              call that uses them; a call leaves its counters there at zero.
+ *              For one call at a time: calls that overlap on one workspace
+ *              give wrong results, until it is cleared again
  * EINVAL too if workspace_bytes is less, if rows q_heads / heads is 2^31 or more,
  * or if there could be more than 2^30 row groups (a row group is 16 rows or more
  * of one sequence and kv head; the pieces of work are counted in 32 bits).

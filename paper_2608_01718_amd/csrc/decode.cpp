@@ -136,7 +136,7 @@ int64_t lacache_kv_attend_workspace(const lacache_kv* kv, lacache_dtype dtype, i
         q_heads % kv->heads != 0 || max_new < 0)
         return LACACHE_EINVAL;
     const int cu = compute_units();
-    return cu ? attend_workspace(p, (int)dtype, n_seq, q_heads, max_new, cu) : LACACHE_EHIP;
+    return cu ? attend_workspace(p, (int)dtype, q_heads, max_new, cu) : LACACHE_EHIP;
 }
 
 int lacache_kv_attend(const lacache_kv* kv, const lacache_seqs* seqs, const void* q, lacache_dtype dtype, int64_t rows,
@@ -153,7 +153,7 @@ int lacache_kv_attend(const lacache_kv* kv, const lacache_seqs* seqs, const void
     if (!q || !out || !aligned(q, esz) || !aligned(out, esz) || !aligned(lse, 4)) return LACACHE_EINVAL;
     const int cu = compute_units();
     if (!cu) return LACACHE_EHIP;
-    const int64_t need = attend_workspace(a.pool, (int)dtype, seqs->n_seq, q_heads, max_new, cu);
+    const int64_t need = attend_workspace(a.pool, (int)dtype, q_heads, max_new, cu);
     if (workspace_bytes < need || (need > 0 && (!workspace || !aligned(workspace, 16)))) return LACACHE_EINVAL;
     a.q = (const char*)q, a.out = (char*)out, a.lse = lse;
     a.dtype = (int)dtype, a.q_heads = q_heads, a.group = q_heads / kv->heads, a.window = window;

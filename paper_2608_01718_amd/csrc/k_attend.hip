@@ -72,8 +72,7 @@ Shape shape_of(const KvPool& pool, bool f32, int64_t rows) {
 }
 
 // The plan of a launch whose workspace begins at `space`, and the bytes it takes.
-AttendPlan plan_of(const KvPool& pool, bool f32, int n_seq, int max_new, int group, int num_cu, char* space,
-                   int64_t* bytes) {
+AttendPlan plan_of(const KvPool& pool, bool f32, int max_new, int group, int num_cu, char* space, int64_t* bytes) {
     AttendPlan p{};
     // (the rows of a (sequence, kv head), if no bound is known: plenty)
     const Shape sh = shape_of(pool, f32, (int64_t)(max_new > 0 ? max_new : 64) * group);
@@ -104,16 +103,16 @@ bool attend_fits(const KvPool& pool, int dtype, int64_t rows, int n_seq, int gro
     return row_groups(pool, rows, n_seq, group, sh.group_shift) <= kMostItems;
 }
 
-int64_t attend_workspace(const KvPool& pool, int dtype, int n_seq, int q_heads, int max_new, int num_cu) {
+int64_t attend_workspace(const KvPool& pool, int dtype, int q_heads, int max_new, int num_cu) {
     int64_t bytes;
-    plan_of(pool, dtype == 0, n_seq, max_new, q_heads / pool.heads, num_cu, nullptr, &bytes);
+    plan_of(pool, dtype == 0, max_new, q_heads / pool.heads, num_cu, nullptr, &bytes);
     return bytes;
 }
 
 hipError_t launch_kv_attend(const AttendArgs& a, int max_new, void* workspace, int num_cu, hipStream_t s) {
     if (a.seqs.rows <= 0 || a.seqs.n_seq <= 0) return hipSuccess;
     int64_t bytes;
-    AttendPlan p = plan_of(a.pool, a.dtype == 0, a.seqs.n_seq, max_new, a.group, num_cu, (char*)workspace, &bytes);
+    AttendPlan p = plan_of(a.pool, a.dtype == 0, max_new, a.group, num_cu, (char*)workspace, &bytes);
     // row / group for rows below 2^31: magic = ceil(2^(31 + bits) / group), bits = ceil(log2 group)
     int bits = 0;
     while ((1 << bits) < a.group) ++bits;

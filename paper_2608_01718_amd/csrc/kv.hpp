@@ -236,7 +236,7 @@ struct AttendArgs {
 };
 // Whether the row groups of a call can be counted in 32 bits.
 bool attend_fits(const KvPool& pool, int dtype, int64_t rows, int n_seq, int group, int max_new);
-int64_t attend_workspace(const KvPool& pool, int dtype, int n_seq, int q_heads, int max_new, int num_cu);
+int64_t attend_workspace(const KvPool& pool, int dtype, int q_heads, int max_new, int num_cu);
 hipError_t launch_kv_attend(const AttendArgs& a, int max_new, void* workspace, int num_cu, hipStream_t s);
 
 }  // namespace lacache
