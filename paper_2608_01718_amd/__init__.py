@@ -718,16 +718,20 @@ def lacache_kv_append(c: KVCache, k, v, seqs: Sequences, q=None, rope=None, q_ou
         raise ValueError(f"expected {rows} rows of v, and sequences and table on cuda:{index}")
     q_ptr = o_ptr = None
     q_row = q_heads = 0
+    given = False
     if q is not None:
         q_heads = q.shape[1]
         q_row = _rows(q, q_heads, c.d, index, kind, "q")
         if q.shape[0] != rows:
             raise ValueError(f"q: expected {rows} rows")
-        q_out = _made(q, q.shape, kind, stream) if q_out is None else _given(q_out, q.shape, kind, index, "q_out")
+        given = q_out is not None
+        q_out = _given(q_out, q.shape, kind, index, "q_out") if given else _made(q, q.shape, kind, stream)
         q_ptr, o_ptr = q.data_ptr(), q_out.data_ptr()
     _check(_on(index, stream, _lib.lacache_kv_append, c._ref, seqs._ref, k.data_ptr(), v.data_ptr(), dtype, rows, k_row,
                v_row, q_ptr, o_ptr, q_heads, q_row, None if rope is None else rope._ref, max_new), "lacache_kv_append")
-    _written(c._pools if q is None else (*c._pools, q_out))
+    _written(c._pools)
+    if given:
+        _written(q_out)
     return q_out if q is not None else None
 
 
