@@ -12,9 +12,10 @@
 // time as it was.)
 //
 // 21 new tokens of 32 sequences of 512 to 4096, 32 query heads on 4, d = 128: 55 us, and 10 for the join of 30 MB of parts; the
-// matrix cores are busy for 17 % of it, the vector unit 23 %: it waits for its tiles (16 KB on their way for each workgroup), 27 us
-// are start, parts and join whatever the length.  151 new tokens of 4 sequences of 5000 to 20,000, 16 heads on 2, d = 256:
-// 160 to 188 us by card, 0.52 to 0.61 PFLOP/s beside which the weights' second term is half as much again.
+// matrix cores are busy for 17 % of it, the vector unit 23 %; 27 us are start, parts and join whatever the length.  151 new
+// tokens of 4 sequences of 5000 to 20,000, 16 heads on 2, d = 256: 160 to 188 us by card, 0.52 to 0.61 PFLOP/s beside which the
+// weights' second term is half as much again.  There LDS is the busiest unit: the eight waves read each operand for one row tile each,
+// 256 KB a tile of tokens, 61 bytes a clock of 128, beside 36 % of the matrix cores.
 #pragma once
 
 #include "attend.hpp"

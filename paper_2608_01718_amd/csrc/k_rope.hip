@@ -3,7 +3,9 @@
 // Pair i of a head's first rot columns is turned by the angle position * f_i (a 2 x 2 rotation, times the table's
 // magnitude); its transpose, with -sin, is the gradient.  Both are bound by reading x and writing y: a thread turns eight or
 // sixteen columns, 16 bytes a lane, so that all of a head's pairs are loaded once whatever the layout.  8192 x 32 x 128 float32,
-// half of the columns turned: 51 us, 5.2 TB/s (a large copy 4.8); 64 x 40 x 128 bfloat16: 3.1 us, the launch.
+// half of the columns turned: 51 us, 5.2 TB/s (a large copy 4.8); 64 x 40 x 128 bfloat16: 3.1 us, the launch.  Where the pairs do not
+// come in whole eights a thread turns one: 8192 x 32 x 80 bfloat16, 40 columns in halves 60 us, 1.4 TB/s (pairs 17 us).  The table
+// is bound by cosines and sines in double: 131,072 x 64 pairs 75 us.
 #include "kv.hpp"
 #include "launch.hpp"
 
