@@ -251,6 +251,44 @@ int lacache_accept_length(const void *logits, lacache_dtype dtype, int32_t V, co
                           void *stream);
 
 /*
+ * Sampled verification of drafted tokens: the acceptance of speculative
+ * sampling, after which every token has the target model's distribution.
+ * Sequence b has n_draft[b] drafts x_j (all k if n_draft is NULL; a count outside
+ * 0 .. k is taken as the nearest of them), drawn from q_j = softmax(draft_logits
+ * [b][j] / T); with p_j = softmax(logits[b][j] / T), T = temperature[b] (1 if
+ * NULL), draft j is taken if u_accept[b][j] q_j(x_j) < p_j(x_j) and all before it
+ * were.  Behind the n = accept_len[b] that were taken the next token is drawn: the
+ * first v with r(0) + ... + r(v) > u_next[b] sum r (the last with r > 0 if there
+ * is none), where r = max(0, p_n - q_n), and r = p_n if n = n_draft[b] or if
+ * sum r <= 2^-30.
+ *   logits        rows of V logits (dtype): sequence b's j-th at b t_seq + j t_row
+ *                 elements, j <= n_draft[b]; draft_logits likewise with d_seq and
+ *                 d_row, j < n_draft[b].  Other rows are not read.
+ *   draft_tokens  [B][k] int32; one outside [0, V) has p = q = 0
+ *   u_accept      [B][k], u_next [B]: numbers from [0, 1)
+ *   temperature   [B]; a sequence whose temperature is not in 2^-60 .. 2^60 (0, for
+ *                 one) is greedy: a draft is taken if its logit is one of the
+ *                 largest, the next token is the first of the largest; its rows of
+ *                 draft_logits are not read
+ *   1 <= V, 0 <= B <= 65535, 0 <= k <= 4096
+ * Outputs: accept_len [B], next_token [B] int32, p_target and p_draft [B][k] the
+ * p_j(x_j) and q_j(x_j) in float32 (a greedy sequence's: 1 or 0, and 1; those from
+ * n_draft[b] on: 0).  accept_len and next_token are those of 64-bit arithmetic.
+ * Logits of -infinity have probability 0.  A row without a finite logit, or with
+ * +infinity or NaN, has no probabilities: its draft is not taken (p or q 0); if it
+ * is the target's row n the next token is -1, if it is the draft model's r = p_n.
+ *   workspace     lacache_verify_workspace bytes of device memory, 16-byte aligned,
+ *                 in any state, for one call at a time
+ * B == 0 is a no-op.  k == 0 draws a token from each target row.
+ */
+int64_t lacache_verify_workspace(int32_t V, int32_t B, int32_t k);
+int lacache_verify(const void *logits, const void *draft_logits, lacache_dtype dtype, int32_t V, int64_t t_seq,
+                   int64_t t_row, int64_t d_seq, int64_t d_row, const int32_t *draft_tokens, const float *u_accept,
+                   const float *u_next, const float *temperature, const int32_t *n_draft, int32_t B, int32_t k,
+                   int32_t *accept_len, int32_t *next_token, float *p_target, float *p_draft, void *workspace,
+                   int64_t workspace_bytes, void *stream);
+
+/*
  * Locality-sensitive index for stage 1 (Section 3, Eq. (1): the cache key is
  * an LSH of the embedding, colliding with probability above p1 for close
  * pairs and below p2 for far ones; Algorithm 1 searches the cache with it).

@@ -77,6 +77,10 @@ _lib.lacache_kv_read.argtypes = [_P, _P, _P, _P, ctypes.c_int, _i64, _i32, _P]
 _lib.lacache_kv_attend_workspace.argtypes = [_P, ctypes.c_int, _i32, _i32, _i32]
 _lib.lacache_kv_attend_workspace.restype = _i64
 _lib.lacache_kv_attend.argtypes = [_P, _P, _P, ctypes.c_int, _i64, _i32, _i64, _i32, _f32, _i32, _P, _P, _P, _i64, _P]
+_lib.lacache_verify_workspace.argtypes = [_i32, _i32, _i32]
+_lib.lacache_verify_workspace.restype = _i64
+_lib.lacache_verify.argtypes = [_P, _P, ctypes.c_int, _i32, _i64, _i64, _i64, _i64, _P, _P, _P, _P, _P, _i32, _i32, _P, _P,
+                                _P, _P, _P, _i64, _P]
 _lib.lacache_strerror.argtypes = [ctypes.c_int]
 _lib.lacache_strerror.restype = ctypes.c_char_p
 
@@ -88,7 +92,7 @@ EXPORTED = ("lacache_create", "lacache_create_ensemble", "lacache_models", "laca
             "lacache_set_small_batch",
             "lacache_profile", "lacache_profile_read", "lacache_replay_fallbacks", "lacache_strerror",
             "lacache_rope_table", "lacache_rope", "lacache_kv_append", "lacache_kv_read",
-            "lacache_kv_attend_workspace", "lacache_kv_attend")
+            "lacache_kv_attend_workspace", "lacache_kv_attend", "lacache_verify_workspace", "lacache_verify")
 
 
 class LaCacheError(RuntimeError):
@@ -795,6 +799,63 @@ def lacache_kv_attend(c: KVCache, q, seqs: Sequences, scale=None, window: int = 
     if given:
         _written(out)
     return out
+
+
+def lacache_verify_workspace(V: int, B: int, k: int) -> int:
+    """Bytes of scratch that lacache_verify needs."""
+    n = int(_lib.lacache_verify_workspace(V, B, k))
+    if n < 0:
+        raise LaCacheError(n, "lacache_verify_workspace")
+    return n
+
+
+def _logits(t, rows: int, V: int, like, name: str):
+    """The strides of [B, rows, V] logits whose rows are each contiguous."""
+    if t.dtype != like.dtype or t.device != like.device or tuple(t.shape) != (like.shape[0], rows, V) or \
+            (V > 1 and t.numel() and t.stride(2) != 1):
+        raise ValueError(f"{name}: expected [{like.shape[0]}, {rows}, {V}] {like.dtype} on {like.device} with contiguous "
+                         f"rows, got {tuple(t.shape)} {t.dtype} on {t.device} with strides {t.stride()}")
+    return t.stride(0), t.stride(1)
+
+
+def lacache_verify(logits, draft_logits, draft_tokens, u_accept, u_next, temperature=None, n_draft=None, out=None,
+                   stream=None):
+    """Verification of drafted tokens by rejection: logits [B, k + 1, V] of the target model and draft_logits [B, k, V] of
+    the draft model (float32 or bfloat16, rows contiguous), draft_tokens [B, k] int32, u_accept [B, k] and u_next [B]
+    float32 random numbers from [0, 1), temperature [B] float32 (1 where it is not given; 0 is greedy), n_draft [B] int32
+    (k where it is not given).  Returns (accept_len [B] int32, next_token [B] int32, p_target [B, k], p_draft [B, k])."""
+    kind = _ROW_DTYPES.get(logits.dtype)
+    if logits.dim() != 3 or logits.device.type != "cuda" or kind is None or logits.shape[1] < 1:
+        raise ValueError("logits: expected a float32 or bfloat16 [B, k + 1, V] tensor on a GPU")
+    B, k, V, index = logits.shape[0], logits.shape[1] - 1, logits.shape[2], logits.get_device()
+    t_seq, t_row = _logits(logits, k + 1, V, logits, "logits")
+    d_seq, d_row = _logits(draft_logits, k, V, logits, "draft_logits")
+    _given(draft_tokens, (B, k), torch.int32, index, "draft_tokens")
+    _given(u_accept, (B, k), torch.float32, index, "u_accept")
+    _given(u_next, (B,), torch.float32, index, "u_next")
+    if temperature is not None:
+        _given(temperature, (B,), torch.float32, index, "temperature")
+    if n_draft is not None:
+        _given(n_draft, (B,), torch.int32, index, "n_draft")
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in
+                                       (logits, draft_logits, u_accept, u_next, temperature, *(out or ()))):
+        raise _no_gradient("lacache_verify")
+    shapes = (((B,), torch.int32, "accept_len"), ((B,), torch.int32, "next_token"), ((B, k), torch.float32, "p_target"),
+              ((B, k), torch.float32, "p_draft"))
+    given = out is not None
+    if given:
+        for t, (shape, dtype, name) in zip(out, shapes, strict=True):
+            _given(t, shape, dtype, index, name)
+    else:
+        out = tuple(_made(logits, shape, dtype, stream) for shape, dtype, _ in shapes)
+    space = _made(logits, (lacache_verify_workspace(V, B, k),), torch.uint8, stream)
+    _check(_on(index, stream, _lib.lacache_verify, logits.data_ptr(), draft_logits.data_ptr(), kind, V, t_seq, t_row, d_seq,
+               d_row, draft_tokens.data_ptr(), u_accept.data_ptr(), u_next.data_ptr(),
+               None if temperature is None else temperature.data_ptr(), None if n_draft is None else n_draft.data_ptr(), B, k,
+               *(t.data_ptr() for t in out), space.data_ptr(), space.numel()), "lacache_verify")
+    if given:
+        _written(out)
+    return tuple(out)
 
 
 def raw_library() -> ctypes.CDLL:

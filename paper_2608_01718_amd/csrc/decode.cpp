@@ -6,6 +6,7 @@
 #include <atomic>
 #include <cmath>
 
+#include "draft.hpp"
 #include "kv.hpp"
 
 using namespace lacache;
@@ -159,6 +160,36 @@ int lacache_kv_attend(const lacache_kv* kv, const lacache_seqs* seqs, const void
     a.dtype = (int)dtype, a.q_heads = q_heads, a.group = q_heads / kv->heads, a.window = window;
     a.q_row = q_row, a.scale = scale;
     return launch_kv_attend(a, max_new, workspace, cu, (hipStream_t)stream) == hipSuccess ? LACACHE_OK : LACACHE_EHIP;
+}
+
+int64_t lacache_verify_workspace(int32_t V, int32_t B, int32_t k) {
+    return V < 1 || B < 0 || B > 65535 || k < 0 || k > 4096 ? LACACHE_EINVAL : draft_workspace(V, B, k);
+}
+
+int lacache_verify(const void* logits, const void* draft_logits, lacache_dtype dtype, int32_t V, int64_t t_seq,
+                   int64_t t_row, int64_t d_seq, int64_t d_row, const int32_t* draft_tokens, const float* u_accept,
+                   const float* u_next, const float* temperature, const int32_t* n_draft, int32_t B, int32_t k,
+                   int32_t* accept_len, int32_t* next_token, float* p_target, float* p_draft, void* workspace,
+                   int64_t workspace_bytes, void* stream) {
+    if (!is_dtype(dtype) || V < 1 || B < 0 || B > 65535 || k < 0 || k > 4096 || t_seq < 0 || t_row < 0 || d_seq < 0 ||
+        d_row < 0 || workspace_bytes < 0)
+        return LACACHE_EINVAL;
+    if (B == 0) return LACACHE_OK;
+    const uintptr_t esz = dtype == LACACHE_F32 ? 4 : 2;
+    if (!logits || !u_next || !accept_len || !next_token || !workspace || !aligned(logits, esz) || !aligned(u_next, 4) ||
+        !aligned(accept_len, 4) || !aligned(next_token, 4) || !aligned(temperature, 4) || !aligned(n_draft, 4) ||
+        !aligned(workspace, 16) || workspace_bytes < draft_workspace(V, B, k))
+        return LACACHE_EINVAL;
+    if (k > 0 && (!draft_logits || !draft_tokens || !u_accept || !p_target || !p_draft || !aligned(draft_logits, esz) ||
+                  !aligned(draft_tokens, 4) || !aligned(u_accept, 4) || !aligned(p_target, 4) || !aligned(p_draft, 4)))
+        return LACACHE_EINVAL;
+    DraftArgs a{};
+    a.logits = (const char*)logits, a.draft_logits = (const char*)draft_logits;
+    a.dtype = (int)dtype, a.V = V, a.B = B, a.k = k;
+    a.t_seq = t_seq, a.t_row = t_row, a.d_seq = d_seq, a.d_row = d_row;
+    a.tokens = draft_tokens, a.n_draft = n_draft, a.u_accept = u_accept, a.u_next = u_next, a.temperature = temperature;
+    a.accept_len = accept_len, a.next_token = next_token, a.p_target = p_target, a.p_draft = p_draft;
+    return launch_verify_drafts(a, workspace, (hipStream_t)stream) == hipSuccess ? LACACHE_OK : LACACHE_EHIP;
 }
 
 }  // extern "C"

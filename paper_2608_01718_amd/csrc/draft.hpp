@@ -1,0 +1,38 @@
+// draft.hpp -- sampled verification of drafted tokens: arguments and launcher.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace lacache {
+
+// The row behind the last draft that was taken: whether it has probabilities, and whether the draft model's are taken off
+// them; the largest logits of both.
+struct DraftRow {
+    int n, has_p, has_q;
+    float mt, md;
+};
+
+struct DraftArgs {
+    const char *logits, *draft_logits;
+    int dtype, V, B, k;
+    int64_t t_seq, t_row, d_seq, d_row;
+    const int32_t *tokens, *n_draft;
+    const float *u_accept, *u_next, *temperature;
+    int32_t *accept_len, *next_token;
+    float *p_target, *p_draft;
+    // the workspace
+    float2* stats;    // [B (2 k + 1)][chunks] maxima and sums
+    int chunks;
+    int64_t wide;     // logits of a chunk of the row that follows
+    int wides;
+    double2* sums;    // [B][wides] of both models
+    double* rest;     // [B][wides] of r
+    DraftRow* rows;   // [B]
+    uint32_t* done;   // [B] workgroups of k_draft_pick that are through
+};
+
+int64_t draft_workspace(int V, int B, int k);
+hipError_t launch_verify_drafts(DraftArgs a, void* workspace, hipStream_t s);
+
+}  // namespace lacache
