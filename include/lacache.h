@@ -548,6 +548,85 @@ int lacache_kv_attend(const lacache_kv *kv, const lacache_seqs *seqs, const void
                       int64_t rows, int32_t q_heads, int64_t q_row, int32_t max_new, float scale, int32_t window,
                       void *out, float *lse, void *workspace, int64_t workspace_bytes, void *stream);
 
+/*
+ * Attention over chosen pages.  A long context costs what is read of it: the
+ * three calls below keep bounds of each page's keys, choose for every new token
+ * and kv head the pages whose keys may give it its largest scores, and attend
+ * over these alone.
+ *
+ * Bounds of the pages of a pool: for each (page, head) the largest and the
+ * smallest value of every key column over the page's tokens, in 8 bits rounded
+ * outwards: with m the largest magnitude of them,
+ *     code[0][c] = ceil(127 max_c / m), code[1][c] = floor(127 min_c / m),
+ *     scale = m / 127
+ * (exact but for the rounding of scale to float32).  m below 2^-100: zeros.  A
+ * page that holds an infinity or NaN for a head: zeros, and a scale of NaN.
+ * code is [n_pages][heads][2][D], 16-byte aligned, scale [n_pages][heads].
+ */
+typedef struct {
+    int8_t *code;
+    float *scale;
+} lacache_bounds;
+
+/*
+ * Bounds of the pages that the newest tokens of every sequence lie in, over all
+ * of the sequence's tokens there: after each lacache_kv_append.  rows and
+ * max_new as in that call.  n_seq is at most 2^20 here and in the two calls below,
+ * and max_pages too.
+ */
+int lacache_kv_bound(const lacache_kv *kv, const lacache_bounds *bounds, const lacache_seqs *seqs, int64_t rows,
+                     int32_t max_new, void *stream);
+
+/*
+ * Bounds of given pages (pages [n] int32) as the values that they stand for:
+ * most and least [n][heads][d] float32, either may be NULL; zeros for a page that
+ * is not in the pool.
+ */
+int lacache_kv_bounds_read(const lacache_kv *kv, const lacache_bounds *bounds, const int32_t *pages, int64_t n,
+                           float *most, float *least, void *stream);
+
+/*
+ * The pages for the newest tokens: blocks [rows][heads][n_blocks] int32, for the
+ * row of position p the indices i <= p / page into its sequence's page table of
+ * the pages that are there and have the largest scores, in rising order, -1 behind
+ * them if there are fewer.  The score of page i for kv head h is the largest over
+ * h's query heads g of
+ *     ((float) (c+ . code[0] + c- . code[1]) * scale) * unit
+ * rounded step by step to float32, where unit = max |q_g| / 127 and c = q_g / unit
+ * rounded to the nearest whole number (all in float32), c+ and c- its positive and
+ * its negative columns: to the roundings of q_g and of the bounds a bound of
+ * q_g . k over the page (so scale > 0 in the attention that follows).  NaN counts
+ * as the largest of numbers; of equal pages the first ones are taken.  The first
+ * `first` pages of a table and the `last` newest ones of a row are taken before
+ * others (first, last >= 0, first + last <= n_blocks).
+ *   q, q_heads, q_row, max_new   as in lacache_kv_attend
+ *   workspace   lacache_kv_select_workspace bytes of device memory, 16-byte
+ *               aligned, in any state, for one call at a time
+ * 1 <= n_blocks <= 2^20.  Rows of no sequence are left as they were.  kv's pools
+ * are not read.
+ */
+int64_t lacache_kv_select_workspace(const lacache_kv *kv, int64_t rows, int32_t max_pages);
+int lacache_kv_select(const lacache_kv *kv, const lacache_bounds *bounds, const lacache_seqs *seqs, const void *q,
+                      lacache_dtype dtype, int64_t rows, int32_t q_heads, int64_t q_row, int32_t n_blocks, int32_t first,
+                      int32_t last, int32_t max_new, int32_t *blocks, void *workspace, int64_t workspace_bytes,
+                      void *stream);
+
+/*
+ * lacache_kv_attend where the row of position p and kv head h see those positions
+ * j <= p alone that lie in a page whose index stands in blocks [rows][heads]
+ * [n_blocks] (int32, in any order; a number outside 0 .. max_pages - 1 stands for
+ * nothing; a page that is listed twice counts twice).
+ *   workspace  lacache_kv_attend_blocks_workspace bytes, under the rules of
+ *              lacache_kv_attend's; the two calls may share one.
+ * Rows of no sequence are left as they were.  rows heads ceil(q_heads / heads / 16)
+ * is below 2^24, 1 <= n_blocks <= 2^20.
+ */
+int64_t lacache_kv_attend_blocks_workspace(const lacache_kv *kv, int64_t rows, int32_t q_heads, int32_t n_blocks);
+int lacache_kv_attend_blocks(const lacache_kv *kv, const lacache_seqs *seqs, const void *q, lacache_dtype dtype,
+                             int64_t rows, int32_t q_heads, int64_t q_row, const int32_t *blocks, int32_t n_blocks,
+                             float scale, void *out, float *lse, void *workspace, int64_t workspace_bytes,
+                             void *stream);
+
 /* Static text for a return code. */
 const char *lacache_strerror(int code);
 

@@ -65,6 +65,10 @@ class _Seqs(ctypes.Structure):
     _fields_ = [("start", _P), ("lens", _P), ("pages", _P), ("n_seq", _i32), ("max_pages", _i32)]
 
 
+class _Bounds(ctypes.Structure):
+    _fields_ = [("code", _P), ("scale", _P)]
+
+
 class _Rotary(ctypes.Structure):
     _fields_ = [("table", _P), ("n_pos", _i64), ("rot", _i32), ("style", ctypes.c_int)]
 
@@ -77,6 +81,14 @@ _lib.lacache_kv_read.argtypes = [_P, _P, _P, _P, ctypes.c_int, _i64, _i32, _P]
 _lib.lacache_kv_attend_workspace.argtypes = [_P, ctypes.c_int, _i32, _i32, _i32]
 _lib.lacache_kv_attend_workspace.restype = _i64
 _lib.lacache_kv_attend.argtypes = [_P, _P, _P, ctypes.c_int, _i64, _i32, _i64, _i32, _f32, _i32, _P, _P, _P, _i64, _P]
+_lib.lacache_kv_bound.argtypes = [_P, _P, _P, _i64, _i32, _P]
+_lib.lacache_kv_bounds_read.argtypes = [_P, _P, _P, _i64, _P, _P, _P]
+_lib.lacache_kv_select_workspace.argtypes = [_P, _i64, _i32]
+_lib.lacache_kv_select_workspace.restype = _i64
+_lib.lacache_kv_select.argtypes = [_P, _P, _P, _P, ctypes.c_int, _i64, _i32, _i64, _i32, _i32, _i32, _i32, _P, _P, _i64, _P]
+_lib.lacache_kv_attend_blocks_workspace.argtypes = [_P, _i64, _i32, _i32]
+_lib.lacache_kv_attend_blocks_workspace.restype = _i64
+_lib.lacache_kv_attend_blocks.argtypes = [_P, _P, _P, ctypes.c_int, _i64, _i32, _i64, _P, _i32, _f32, _P, _P, _P, _i64, _P]
 _lib.lacache_verify_workspace.argtypes = [_i32, _i32, _i32]
 _lib.lacache_verify_workspace.restype = _i64
 _lib.lacache_verify.argtypes = [_P, _P, ctypes.c_int, _i32, _i64, _i64, _i64, _i64, _P, _P, _P, _P, _P, _i32, _i32, _P, _P,
@@ -92,7 +104,9 @@ EXPORTED = ("lacache_create", "lacache_create_ensemble", "lacache_models", "laca
             "lacache_set_small_batch",
             "lacache_profile", "lacache_profile_read", "lacache_replay_fallbacks", "lacache_strerror",
             "lacache_rope_table", "lacache_rope", "lacache_kv_append", "lacache_kv_read",
-            "lacache_kv_attend_workspace", "lacache_kv_attend", "lacache_verify_workspace", "lacache_verify")
+            "lacache_kv_attend_workspace", "lacache_kv_attend", "lacache_verify_workspace", "lacache_verify",
+            "lacache_kv_bound", "lacache_kv_bounds_read", "lacache_kv_select_workspace", "lacache_kv_select",
+            "lacache_kv_attend_blocks_workspace", "lacache_kv_attend_blocks")
 
 
 class LaCacheError(RuntimeError):
@@ -635,6 +649,33 @@ class KVCache:
     def attend(self, q, seqs, scale=None, window=0, max_new=0, out=None, stream=None):
         return lacache_kv_attend(self, q, seqs, scale, window, max_new, out, stream)
 
+    def attend_blocks(self, q, seqs, blocks, scale=None, out=None, stream=None):
+        return lacache_kv_attend_blocks(self, q, seqs, blocks, scale, out, stream)
+
+
+class KVBounds:
+    """Bounds of the keys of a cache's pages, in 8 bits: code [n_pages, heads, 2, D] int8 (the largest value of each column,
+    then the smallest) and scale [n_pages, heads] float32.  Allocated here (zeros) if they are not given."""
+
+    def __init__(self, cache: KVCache, code=None, scale=None):
+        shape = (cache.n_pages, cache.heads, 2, _padded(cache.d))
+        self.code = cache.k.new_zeros(shape, dtype=torch.int8) if code is None else \
+            _given(code, shape, torch.int8, cache.index, "code")
+        self.scale = cache.k.new_zeros(shape[:2], dtype=torch.float32) if scale is None else \
+            _given(scale, shape[:2], torch.float32, cache.index, "scale")
+        self.cache = cache
+        self._c = _Bounds(self.code.data_ptr(), self.scale.data_ptr())
+        self._ref = ctypes.addressof(self._c)
+
+    def update(self, seqs, rows, max_new=0, stream=None):
+        return lacache_kv_bound(self, seqs, rows, max_new, stream)
+
+    def read(self, pages, out=None, stream=None):
+        return lacache_kv_bounds_read(self, pages, out, stream)
+
+    def select(self, q, seqs, n_blocks, first=1, last=1, max_new=0, out=None, stream=None):
+        return lacache_kv_select(self, q, seqs, n_blocks, first, last, max_new, out, stream)
+
 
 def _kv_fits(n_pages: int, heads: int, d: int, page: int) -> bool:
     """What the calls take (lacache_kv)."""
@@ -796,6 +837,112 @@ def lacache_kv_attend(c: KVCache, q, seqs: Sequences, scale=None, window: int = 
     _check(_on(index, stream, _lib.lacache_kv_attend, c._ref, seqs._ref, q.data_ptr(), dtype, rows, q_heads, q_row,
                max_new, c.d ** -0.5 if scale is None else scale, window, out[0].data_ptr(), out[1].data_ptr(),
                space.data_ptr(), space.numel()), "lacache_kv_attend")
+    if given:
+        _written(out)
+    return out
+
+
+def lacache_kv_bound(b: KVBounds, seqs: Sequences, rows: int, max_new: int = 0, stream=None) -> None:
+    """Bounds of the pages that the newest tokens of every sequence lie in (rows is start[-1]), after each append."""
+    c = b.cache
+    if seqs.index != c.index:
+        raise ValueError(f"expected sequences on cuda:{c.index}")
+    _check(_on(c.index, stream, _lib.lacache_kv_bound, c._ref, b._ref, seqs._ref, rows, max_new), "lacache_kv_bound")
+    _written((b.code, b.scale))
+
+
+def lacache_kv_bounds_read(b: KVBounds, pages, out=None, stream=None):
+    """The bounds of pages [n] (int32) as (most, least), each [n, heads, d] float32."""
+    c = b.cache
+    n = pages.shape[0] if pages.dim() == 1 else -1
+    _given(pages, (n,) if n >= 0 else (0,), torch.int32, c.index, "pages")
+    shape = (n, c.heads, c.d)
+    given = out is not None
+    if not given:
+        out = (_made(c.k, shape, torch.float32, stream), _made(c.k, shape, torch.float32, stream))
+    else:
+        _given(out[0], shape, torch.float32, c.index, "most")
+        _given(out[1], shape, torch.float32, c.index, "least")
+        if torch.is_grad_enabled() and (out[0].requires_grad or out[1].requires_grad):
+            raise _no_gradient("lacache_kv_bounds_read")
+    _check(_on(c.index, stream, _lib.lacache_kv_bounds_read, c._ref, b._ref, pages.data_ptr(), n, out[0].data_ptr(),
+               out[1].data_ptr()), "lacache_kv_bounds_read")
+    if given:
+        _written(out)
+    return out
+
+
+def lacache_kv_select_workspace(c: KVCache, rows: int, max_pages: int) -> int:
+    """Bytes of scratch that lacache_kv_select needs."""
+    n = int(_lib.lacache_kv_select_workspace(c._ref, rows, max_pages))
+    if n < 0:
+        raise LaCacheError(n, "lacache_kv_select_workspace")
+    return n
+
+
+def lacache_kv_select(b: KVBounds, q, seqs: Sequences, n_blocks: int, first: int = 1, last: int = 1, max_new: int = 0,
+                      out=None, stream=None):
+    """The pages whose keys may give the new rows q [rows, q_heads, d] their largest scores: [rows, heads, n_blocks] int32
+    indices into the page tables, rising, -1 behind them.  The first `first` pages and the `last` newest are always there."""
+    c = b.cache
+    index, kind, shape = c.index, q.dtype, q.shape
+    dtype = _ROW_DTYPES.get(kind)
+    if dtype is None or len(shape) != 3 or seqs.index != index:
+        raise ValueError(f"q: expected float32 or bfloat16 [rows, q_heads, d], and sequences on cuda:{index}")
+    q_row = _rows(q, shape[1], c.d, index, kind, "q")
+    given = out is not None
+    if n_blocks < 1:
+        raise ValueError("n_blocks: expected at least one")
+    out = _given(out, (shape[0], c.heads, n_blocks), torch.int32, index, "out") if given else \
+        _made(q, (shape[0], c.heads, n_blocks), torch.int32, stream)
+    space = _made(q, (lacache_kv_select_workspace(c, shape[0], seqs._c.max_pages),), torch.uint8, stream)
+    _check(_on(index, stream, _lib.lacache_kv_select, c._ref, b._ref, seqs._ref, q.data_ptr(), dtype, shape[0], shape[1], q_row,
+               n_blocks, first, last, max_new, out.data_ptr(), space.data_ptr(), space.numel()), "lacache_kv_select")
+    if given:
+        _written(out)
+    return out
+
+
+def lacache_kv_attend_blocks_workspace(c: KVCache, rows: int, q_heads: int, n_blocks: int) -> int:
+    """Bytes of scratch that lacache_kv_attend_blocks needs."""
+    with torch.cuda.device(c.index):
+        n = int(_lib.lacache_kv_attend_blocks_workspace(c._ref, rows, q_heads, n_blocks))
+    if n < 0:
+        raise LaCacheError(n, "lacache_kv_attend_blocks_workspace")
+    return n
+
+
+def lacache_kv_attend_blocks(c: KVCache, q, seqs: Sequences, blocks, scale=None, out=None, stream=None):
+    """Attention of the new rows q [rows, q_heads, d] (already turned) over the pages of their lists, blocks [rows, heads, n]
+    int32 indices into the page tables (for example of KVBounds.select).  Returns (out, lse) as lacache_kv_attend."""
+    index, kind, shape = c.index, q.dtype, q.shape
+    dtype = _ROW_DTYPES.get(kind)
+    if dtype is None or len(shape) != 3 or seqs.index != index:
+        raise ValueError(f"q: expected float32 or bfloat16 [rows, q_heads, d], and sequences on cuda:{index}")
+    rows, q_heads = shape[0], shape[1]
+    q_row = _rows(q, q_heads, c.d, index, kind, "q")
+    if blocks.dim() != 3 or blocks.shape[2] < 1:
+        raise ValueError(f"blocks: expected [{rows}, {c.heads}, n] with n >= 1, got {tuple(blocks.shape)}")
+    n = blocks.shape[2]
+    _given(blocks, (rows, c.heads, n), torch.int32, index, "blocks")
+    given = out is not None
+    if torch.is_grad_enabled() and (q.requires_grad or (given and (out[0].requires_grad or out[1].requires_grad))):
+        raise _no_gradient("lacache_kv_attend_blocks")
+    if not given:
+        out = (_made(q, shape, kind, stream), _made(q, shape[:2], torch.float32, stream))
+    else:
+        _given(out[0], shape, kind, index, "out")
+        _given(out[1], shape[:2], torch.float32, index, "lse")
+    key = ("blocks", rows, q_heads, n)
+    need = c._need.get(key)
+    if need is None:
+        need = c._need[key] = lacache_kv_attend_blocks_workspace(c, rows, q_heads, n)
+    space = c._space
+    if need and (space is None or space.numel() < need):
+        space = c._scratch(q, need, stream)
+    _check(_on(index, stream, _lib.lacache_kv_attend_blocks, c._ref, seqs._ref, q.data_ptr(), dtype, rows, q_heads, q_row,
+               blocks.data_ptr(), n, c.d ** -0.5 if scale is None else scale, out[0].data_ptr(), out[1].data_ptr(),
+               space.data_ptr() if need else None, space.numel() if need else 0), "lacache_kv_attend_blocks")
     if given:
         _written(out)
     return out

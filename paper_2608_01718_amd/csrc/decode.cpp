@@ -51,6 +51,14 @@ bool to_rope(const lacache_rotary* r, int d, RopeArgs* out) {
     return true;
 }
 
+constexpr int kMostChosen = 1 << 20;  // sequences, pages of a table and of a list where pages are chosen
+
+bool to_bounds(const lacache_bounds* b, KvBounds* out) {
+    if (!b || !b->code || !b->scale || !aligned(b->code, 16) || !aligned(b->scale, 4)) return false;
+    *out = {b->code, b->scale};
+    return true;
+}
+
 // Compute units of the current device; 0 on a HIP error.  (Asked once for each of the first 64 devices.)
 int compute_units() {
     static std::atomic<int> known[64];
@@ -160,6 +168,91 @@ int lacache_kv_attend(const lacache_kv* kv, const lacache_seqs* seqs, const void
     a.dtype = (int)dtype, a.q_heads = q_heads, a.group = q_heads / kv->heads, a.window = window;
     a.q_row = q_row, a.scale = scale;
     return launch_kv_attend(a, max_new, workspace, cu, (hipStream_t)stream) == hipSuccess ? LACACHE_OK : LACACHE_EHIP;
+}
+
+int lacache_kv_bound(const lacache_kv* kv, const lacache_bounds* bounds, const lacache_seqs* seqs, int64_t rows,
+                     int32_t max_new, void* stream) {
+    KvPool p;
+    KvSeqs s;
+    KvBounds b;
+    if (!to_pool(kv, true, &p) || !to_seqs(seqs, rows, &s) || s.n_seq > kMostChosen || s.max_pages > kMostChosen || max_new < 0)
+        return LACACHE_EINVAL;
+    if (rows == 0 || s.n_seq == 0 || p.n_pages == 0) return LACACHE_OK;
+    if (!to_bounds(bounds, &b)) return LACACHE_EINVAL;
+    return launch_kv_bound(p, b, s, max_new, (hipStream_t)stream) == hipSuccess ? LACACHE_OK : LACACHE_EHIP;
+}
+
+int lacache_kv_bounds_read(const lacache_kv* kv, const lacache_bounds* bounds, const int32_t* pages, int64_t n,
+                           float* most, float* least, void* stream) {
+    KvPool p;
+    KvBounds b;
+    if (!to_pool(kv, false, &p) || n < 0 || n > INT32_MAX || !aligned(pages, 4) || !aligned(most, 4) || !aligned(least, 4))
+        return LACACHE_EINVAL;
+    if (n == 0 || (!most && !least)) return LACACHE_OK;
+    if (!pages || (p.n_pages > 0 && !to_bounds(bounds, &b))) return LACACHE_EINVAL;
+    return launch_kv_bounds_read(p, b, pages, n, most, least, (hipStream_t)stream) == hipSuccess ? LACACHE_OK : LACACHE_EHIP;
+}
+
+int64_t lacache_kv_select_workspace(const lacache_kv* kv, int64_t rows, int32_t max_pages) {
+    KvPool p;
+    if (!to_pool(kv, false, &p) || rows < 0 || rows > INT32_MAX || max_pages < 0 || max_pages > kMostChosen)
+        return LACACHE_EINVAL;
+    return 4 * rows * p.heads * select_stride(max_pages);
+}
+
+int lacache_kv_select(const lacache_kv* kv, const lacache_bounds* bounds, const lacache_seqs* seqs, const void* q,
+                      lacache_dtype dtype, int64_t rows, int32_t q_heads, int64_t q_row, int32_t n_blocks, int32_t first,
+                      int32_t last, int32_t max_new, int32_t* blocks, void* workspace, int64_t workspace_bytes,
+                      void* stream) {
+    SelectArgs a{};
+    if (!to_pool(kv, false, &a.pool) || !to_seqs(seqs, rows, &a.seqs) || !is_dtype(dtype) || q_heads < 1 ||
+        q_heads > 65535 || q_heads % kv->heads != 0 || q_row < 0 || max_new < 0 || a.seqs.n_seq > kMostChosen ||
+        a.seqs.max_pages > kMostChosen || n_blocks < 1 || n_blocks > kMostChosen || first < 0 || last < 0 ||
+        (int64_t)first + last > n_blocks || workspace_bytes < 0)
+        return LACACHE_EINVAL;
+    if (rows == 0 || a.seqs.n_seq == 0) return LACACHE_OK;
+    const int64_t need = 4 * rows * a.pool.heads * select_stride(a.seqs.max_pages);
+    if (!q || !blocks || !aligned(q, dtype == LACACHE_F32 ? 4 : 2) || !aligned(blocks, 4) || workspace_bytes < need ||
+        (need > 0 && (!workspace || !aligned(workspace, 16))) || (a.pool.n_pages > 0 && !to_bounds(bounds, &a.bounds)))
+        return LACACHE_EINVAL;
+    a.q = (const char*)q, a.dtype = (int)dtype, a.group = q_heads / kv->heads, a.q_row = q_row;
+    a.n_blocks = n_blocks, a.first = first, a.last = last, a.blocks = blocks, a.scores = (float*)workspace;
+    return launch_kv_select(a, max_new, (hipStream_t)stream) == hipSuccess ? LACACHE_OK : LACACHE_EHIP;
+}
+
+int64_t lacache_kv_attend_blocks_workspace(const lacache_kv* kv, int64_t rows, int32_t q_heads, int32_t n_blocks) {
+    KvPool p;
+    if (!to_pool(kv, false, &p) || rows < 0 || rows > INT32_MAX || q_heads < 1 || q_heads > 65535 ||
+        q_heads % kv->heads != 0 || n_blocks < 1 || n_blocks > kMostChosen)
+        return LACACHE_EINVAL;
+    const int cu = compute_units();
+    return cu ? blocks_workspace(p, rows, q_heads / kv->heads, n_blocks, cu) : LACACHE_EHIP;
+}
+
+int lacache_kv_attend_blocks(const lacache_kv* kv, const lacache_seqs* seqs, const void* q, lacache_dtype dtype,
+                             int64_t rows, int32_t q_heads, int64_t q_row, const int32_t* blocks, int32_t n_blocks,
+                             float scale, void* out, float* lse, void* workspace, int64_t workspace_bytes,
+                             void* stream) {
+    BlocksArgs x{};
+    AttendArgs& a = x.a;
+    if (!to_pool(kv, true, &a.pool) || !to_seqs(seqs, rows, &a.seqs) || !is_dtype(dtype) || q_heads < 1 ||
+        q_heads > 65535 || q_heads % kv->heads != 0 || q_row < 0 || !std::isfinite(scale) || a.seqs.n_seq > kMostChosen ||
+        a.seqs.max_pages > kMostChosen || n_blocks < 1 || n_blocks > kMostChosen || workspace_bytes < 0)
+        return LACACHE_EINVAL;
+    a.group = q_heads / kv->heads;
+    if (rows * kv->heads * ((a.group + 15) / 16) >= 1 << 24) return LACACHE_EINVAL;
+    if (rows == 0 || a.seqs.n_seq == 0) return LACACHE_OK;
+    const uintptr_t esz = dtype == LACACHE_F32 ? 4 : 2;
+    if (!q || !out || !blocks || !aligned(q, esz) || !aligned(out, esz) || !aligned(lse, 4) || !aligned(blocks, 4))
+        return LACACHE_EINVAL;
+    const int cu = compute_units();
+    if (!cu) return LACACHE_EHIP;
+    const int64_t need = blocks_workspace(a.pool, rows, a.group, n_blocks, cu);
+    if (workspace_bytes < need || (need > 0 && (!workspace || !aligned(workspace, 16)))) return LACACHE_EINVAL;
+    a.q = (const char*)q, a.out = (char*)out, a.lse = lse;
+    a.dtype = (int)dtype, a.q_heads = q_heads, a.window = 0, a.q_row = q_row, a.scale = scale;
+    x.blocks = blocks, x.n_blocks = n_blocks;
+    return launch_attend_blocks(x, workspace, cu, (hipStream_t)stream) == hipSuccess ? LACACHE_OK : LACACHE_EHIP;
 }
 
 int64_t lacache_verify_workspace(int32_t V, int32_t B, int32_t k) {

@@ -78,6 +78,16 @@ __device__ inline KvSpan span_of(const KvSeqs& s, int b) {
     return {a, (int)(e - a), (int64_t)s.lens[b] - (e - a)};
 }
 
+// The sequence of a row, by all lanes of a wave: -1 if it is none's.
+__device__ __forceinline__ int sequence_of(const KvSeqs& s, int64_t row, int lane) {
+    int count = 0;
+    for (int i = 0; i <= s.n_seq; i += 64) {
+        const bool at = i + lane <= s.n_seq && s.start[i + lane] <= row;
+        count += __popcll(__ballot(at));
+    }
+    return count > s.n_seq ? -1 : count - 1;
+}
+
 __device__ inline float kv_value(const char* pool, int64_t i, int type) {
     if (type == kKvBf16) return bf16_to_f32(((const uint16_t*)pool)[i]);
     if (type == kKvInt8) return (float)((const int8_t*)pool)[i];
@@ -238,5 +248,44 @@ struct AttendArgs {
 bool attend_fits(const KvPool& pool, int dtype, int64_t rows, int n_seq, int group, int max_new);
 int64_t attend_workspace(const KvPool& pool, int dtype, int q_heads, int max_new, int num_cu);
 hipError_t launch_kv_attend(const AttendArgs& a, int max_new, void* workspace, int num_cu, hipStream_t s);
+
+
+// Bounds of the pages of a pool (lacache_kv_bounds): [pages][heads][2][dp] codes, [pages][heads] scales.
+struct KvBounds {
+    int8_t* code;
+    float* scale;
+};
+struct SelectArgs {
+    KvPool pool;
+    KvBounds bounds;
+    KvSeqs seqs;
+    const char* q;
+    int dtype, group;
+    int64_t q_row;
+    int n_blocks, first, last;
+    int32_t* blocks;   // [rows][heads][n_blocks]
+    float* scores;     // [rows][heads][stride]; -infinity: there is no such page
+    int64_t stride;
+    int fold, slots;   // columns of a token; workgroups in x of a sequence
+};
+hipError_t launch_kv_bound(const KvPool& pool, const KvBounds& bounds, const KvSeqs& seqs, int max_new, hipStream_t s);
+hipError_t launch_kv_bounds_read(const KvPool& pool, const KvBounds& bounds, const int32_t* pages, int64_t n, float* hi,
+                                 float* lo, hipStream_t s);
+int64_t select_stride(int max_pages);
+hipError_t launch_kv_select(SelectArgs a, int max_new, hipStream_t s);
+
+// Attention over lists of pages: the arguments of attention, the lists, and how a list's tiles are split.
+struct BlocksArgs {
+    AttendArgs a;
+    const int32_t* blocks;  // [rows][heads][n_blocks]
+    int n_blocks;
+    int splits, per;        // workgroups of a (row, head, row tile), the tiles of each
+    uint32_t magic, bits;   // AttendPlan::group_magic, group_bits
+    uint32_t* done;         // [units] parts that are there; 0 between launches
+    float* part_o;          // [units][splits][16][dp]
+    float2* part_ml;        // [units][splits][16]
+};
+int64_t blocks_workspace(const KvPool& pool, int64_t rows, int group, int n_blocks, int num_cu);
+hipError_t launch_attend_blocks(BlocksArgs x, void* workspace, int num_cu, hipStream_t s);
 
 }  // namespace lacache
