@@ -549,6 +549,35 @@ int lacache_kv_attend(const lacache_kv *kv, const lacache_seqs *seqs, const void
                       void *out, float *lse, void *workspace, int64_t workspace_bytes, void *stream);
 
 /*
+ * Prefixes that sequences share (device arrays): sequences group[g] ..
+ * group[g+1]-1 (non-decreasing; those outside all groups share nothing) hold the
+ * same first len[g] tokens, rounded down to whole pages, in the same pages: the
+ * first entries of their page tables are equal.  A group of one sequence shares
+ * nothing.
+ */
+typedef struct {
+    const int32_t *group;  /* [n_groups + 1] */
+    const int32_t *len;    /* [n_groups] */
+    int32_t n_groups;
+} lacache_prefixes;
+
+/*
+ * lacache_kv_attend of sequences of which groups share a prefix: the same
+ * results to rounding, the prefix of a group read once for all of its rows
+ * (through the page table of its first sequence).  The other arguments are those
+ * of lacache_kv_attend.
+ *   workspace  lacache_kv_attend_shared_workspace bytes, under the rules of
+ *              lacache_kv_attend's; the calls may share one.
+ * n_groups is at most 2^20, n_seq too.
+ */
+int64_t lacache_kv_attend_shared_workspace(const lacache_kv *kv, lacache_dtype dtype, int64_t rows, int32_t n_seq,
+                                           int32_t n_groups, int32_t q_heads, int32_t max_new);
+int lacache_kv_attend_shared(const lacache_kv *kv, const lacache_seqs *seqs, const lacache_prefixes *prefixes,
+                             const void *q, lacache_dtype dtype, int64_t rows, int32_t q_heads, int64_t q_row,
+                             int32_t max_new, float scale, int32_t window, void *out, float *lse, void *workspace,
+                             int64_t workspace_bytes, void *stream);
+
+/*
  * Attention over chosen pages.  A long context costs what is read of it: the
  * three calls below keep bounds of each page's keys, choose for every new token
  * and kv head the pages whose keys may give it its largest scores, and attend

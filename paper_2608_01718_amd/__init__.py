@@ -69,6 +69,10 @@ class _Bounds(ctypes.Structure):
     _fields_ = [("code", _P), ("scale", _P)]
 
 
+class _Prefixes(ctypes.Structure):
+    _fields_ = [("group", _P), ("len", _P), ("n_groups", _i32)]
+
+
 class _Rotary(ctypes.Structure):
     _fields_ = [("table", _P), ("n_pos", _i64), ("rot", _i32), ("style", ctypes.c_int)]
 
@@ -81,6 +85,10 @@ _lib.lacache_kv_read.argtypes = [_P, _P, _P, _P, ctypes.c_int, _i64, _i32, _P]
 _lib.lacache_kv_attend_workspace.argtypes = [_P, ctypes.c_int, _i32, _i32, _i32]
 _lib.lacache_kv_attend_workspace.restype = _i64
 _lib.lacache_kv_attend.argtypes = [_P, _P, _P, ctypes.c_int, _i64, _i32, _i64, _i32, _f32, _i32, _P, _P, _P, _i64, _P]
+_lib.lacache_kv_attend_shared_workspace.argtypes = [_P, ctypes.c_int, _i64, _i32, _i32, _i32, _i32]
+_lib.lacache_kv_attend_shared_workspace.restype = _i64
+_lib.lacache_kv_attend_shared.argtypes = [_P, _P, _P, _P, ctypes.c_int, _i64, _i32, _i64, _i32, _f32, _i32, _P, _P, _P, _i64,
+                                          _P]
 _lib.lacache_kv_bound.argtypes = [_P, _P, _P, _i64, _i32, _P]
 _lib.lacache_kv_bounds_read.argtypes = [_P, _P, _P, _i64, _P, _P, _P]
 _lib.lacache_kv_select_workspace.argtypes = [_P, _i64, _i32]
@@ -105,7 +113,7 @@ EXPORTED = ("lacache_create", "lacache_create_ensemble", "lacache_models", "laca
             "lacache_profile", "lacache_profile_read", "lacache_replay_fallbacks", "lacache_strerror",
             "lacache_rope_table", "lacache_rope", "lacache_kv_append", "lacache_kv_read",
             "lacache_kv_attend_workspace", "lacache_kv_attend", "lacache_verify_workspace", "lacache_verify",
-            "lacache_kv_bound", "lacache_kv_bounds_read", "lacache_kv_select_workspace", "lacache_kv_select",
+            "lacache_kv_attend_shared_workspace", "lacache_kv_attend_shared", "lacache_kv_bound", "lacache_kv_bounds_read", "lacache_kv_select_workspace", "lacache_kv_select",
             "lacache_kv_attend_blocks_workspace", "lacache_kv_attend_blocks")
 
 
@@ -578,6 +586,21 @@ class Sequences:
         return self._c.n_seq
 
 
+class Prefixes:
+    """Tokens that sequences share: sequences group[g] .. group[g + 1] - 1 begin with the same len[g] tokens (whole pages of
+    them), and their page tables with the same pages.  group [n + 1] and len [n], int32 on one GPU."""
+
+    def __init__(self, group: torch.Tensor, len: torch.Tensor):
+        n, dev = len.shape[0], len.device
+        if dev.type != "cuda":
+            raise ValueError("prefixes: expected tensors on a GPU")
+        _ints(group, (n + 1,), dev.index, "group")
+        _ints(len, (n,), dev.index, "len")
+        self.group, self.len, self.index = group, len, dev.index
+        self._c = _Prefixes(group.data_ptr(), len.data_ptr(), n)
+        self._ref = ctypes.addressof(self._c)
+
+
 def _no_gradient(name: str) -> ValueError:
     """What autograd would want to follow: the cache keeps numbers, and no graph."""
     return ValueError(f"{name}: has no gradient, and a tensor requires one (torch.no_grad() or detach() say that none is "
@@ -648,6 +671,9 @@ class KVCache:
 
     def attend(self, q, seqs, scale=None, window=0, max_new=0, out=None, stream=None):
         return lacache_kv_attend(self, q, seqs, scale, window, max_new, out, stream)
+
+    def attend_shared(self, q, seqs, prefixes, scale=None, window=0, max_new=0, out=None, stream=None):
+        return lacache_kv_attend_shared(self, q, seqs, prefixes, scale, window, max_new, out, stream)
 
     def attend_blocks(self, q, seqs, blocks, scale=None, out=None, stream=None):
         return lacache_kv_attend_blocks(self, q, seqs, blocks, scale, out, stream)
@@ -837,6 +863,49 @@ def lacache_kv_attend(c: KVCache, q, seqs: Sequences, scale=None, window: int = 
     _check(_on(index, stream, _lib.lacache_kv_attend, c._ref, seqs._ref, q.data_ptr(), dtype, rows, q_heads, q_row,
                max_new, c.d ** -0.5 if scale is None else scale, window, out[0].data_ptr(), out[1].data_ptr(),
                space.data_ptr(), space.numel()), "lacache_kv_attend")
+    if given:
+        _written(out)
+    return out
+
+
+def lacache_kv_attend_shared_workspace(c: KVCache, dtype: int, rows: int, n_seq: int, n_groups: int, q_heads: int,
+                                       max_new: int = 0) -> int:
+    """Bytes of scratch that lacache_kv_attend_shared needs (dtype: F32 or BF16)."""
+    with torch.cuda.device(c.index):
+        n = int(_lib.lacache_kv_attend_shared_workspace(c._ref, dtype, rows, n_seq, n_groups, q_heads, max_new))
+    if n < 0:
+        raise LaCacheError(n, "lacache_kv_attend_shared_workspace")
+    return n
+
+
+def lacache_kv_attend_shared(c: KVCache, q, seqs: Sequences, prefixes: Prefixes, scale=None, window: int = 0, max_new: int = 0,
+                             out=None, stream=None):
+    """lacache_kv_attend of sequences of which groups begin with the same pages, which are read once for all of a group's
+    rows.  Returns (out, lse) as that call."""
+    index, kind, shape = c.index, q.dtype, q.shape
+    dtype = _ROW_DTYPES.get(kind)
+    if dtype is None or len(shape) != 3 or seqs.index != index or prefixes.index != index:
+        raise ValueError(f"q: expected float32 or bfloat16 [rows, q_heads, d], and sequences and prefixes on cuda:{index}")
+    rows, q_heads = shape[0], shape[1]
+    q_row = _rows(q, q_heads, c.d, index, kind, "q")
+    given = out is not None
+    if torch.is_grad_enabled() and (q.requires_grad or (given and (out[0].requires_grad or out[1].requires_grad))):
+        raise _no_gradient("lacache_kv_attend_shared")
+    if not given:
+        out = (_made(q, shape, kind, stream), _made(q, shape[:2], torch.float32, stream))
+    else:
+        _given(out[0], shape, kind, index, "out")
+        _given(out[1], shape[:2], torch.float32, index, "lse")
+    key = ("shared", dtype, rows, seqs._c.n_seq, prefixes._c.n_groups, q_heads, max_new)
+    need = c._need.get(key)
+    if need is None:
+        need = c._need[key] = lacache_kv_attend_shared_workspace(c, *key[1:])
+    space = c._space
+    if space is None or space.numel() < need:
+        space = c._scratch(q, need, stream)
+    _check(_on(index, stream, _lib.lacache_kv_attend_shared, c._ref, seqs._ref, prefixes._ref, q.data_ptr(), dtype, rows, q_heads,
+               q_row, max_new, c.d ** -0.5 if scale is None else scale, window, out[0].data_ptr(), out[1].data_ptr(),
+               space.data_ptr(), space.numel()), "lacache_kv_attend_shared")
     if given:
         _written(out)
     return out

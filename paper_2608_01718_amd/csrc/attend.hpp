@@ -41,6 +41,21 @@ constexpr int attend_occupancy(int dp, bool bytes, int R, bool f32) {
     return regs <= 136 ? 4 : regs <= 170 ? 3 : regs <= 256 ? 2 : 1;
 }
 
+// What an attention launch is: all of it; the part over the prefixes that groups of sequences share, whose "sequences" are
+// the groups; the part over each sequence's own tokens, which takes up the other's results.
+enum AttendMode { kWhole = 0, kPrefix = 1, kOwn = 2 };
+
+// The shared prefixes of a call, as k_attend_share has laid them out.
+struct AttendShare {
+    int n_groups;
+    int4* span;        // [n_groups] first row, rows, shared tokens (whole pages), first sequence
+    int32_t* first;    // [n_groups] the first tile that any row sees
+    int32_t* held;     // [n_seq] tokens that a sequence shares (0: it is in no group)
+    int32_t* row_pos;  // [rows] positions of rows (-1 before the first)
+    float* o;          // [rows q_heads][dp] sums of values over the prefix
+    float2* ml;        // [rows q_heads] their maxima and sums of weights
+};
+
 // What a launch works with besides the arguments: the shape of a row group, its workers, the workspace.
 struct AttendPlan {
     int group_shift;   // rows of a row group, as a shift
@@ -52,6 +67,7 @@ struct AttendPlan {
     struct AttendSplit* split;  // [workers]: the row group whose last part a worker had
     float* part_o;     // [2 workers][group rows][dp] partial sums of values
     float2* part_ml;   // [2 workers][group rows] their maxima and sums of weights
+    AttendShare share;
 };
 
 constexpr int kMaxWorkers = 4096;
@@ -61,7 +77,8 @@ struct alignas(16) AttendSplit {
     int seq_row0, head0;   // the sequence's first row, the first query head
     int row, n_rows;       // rows row .. row + n_rows - 1 of the sequence's (0: there is no such row group)
     int worker0, parts;    // the first of its workers, their number
-    int unused[2];
+    int held;              // whether there is a part over a prefix (kOwn)
+    int unused;
 };
 
 // What the work of a sequence is: its rows and their groups, its tiles.
@@ -71,20 +88,33 @@ struct AttendSpan {
     int first, tiles;    // the first tile that any row sees, the number of tiles
     int cap;             // positions that exist
     int chunks;          // the tiles in chunks
+    int table;           // the sequence whose page table holds them
+    int held;            // positions that another launch sees to
     __device__ int64_t pos0() const { return (int64_t)len - n; }  // of the first row
     __device__ int items(const AttendArgs& a) const { return groups * a.pool.heads * chunks; }
 };
+template <int MODE = kWhole>
 __device__ inline AttendSpan attend_span(const AttendArgs& a, const AttendPlan& p, int b) {
     AttendSpan r;
-    const KvSpan s = span_of(a.seqs, b);
-    r.row0 = (int)s.row0, r.n = s.n;
-    r.len = (int)(s.pos0 + s.n);
+    if constexpr (MODE == kPrefix) {
+        const int4 g = p.share.span[b];
+        r.row0 = g.x, r.n = g.y, r.len = r.cap = g.z, r.table = g.w;
+        r.first = p.share.first[b];
+        r.held = 0;
+    } else {
+        const KvSpan s = span_of(a.seqs, b);
+        r.row0 = (int)s.row0, r.n = s.n;
+        r.len = (int)(s.pos0 + s.n);
+        const int64_t held = (int64_t)a.seqs.max_pages << a.pool.page_shift;
+        r.cap = r.len < 0 ? 0 : r.len > held ? (int)held : r.len;
+        const int64_t lo = a.window > 0 ? r.pos0() - a.window + 1 : 0;
+        r.first = lo < 0 ? 0 : (int)(lo >> 5);
+        r.table = b;
+        r.held = MODE == kOwn ? p.share.held[b] : 0;
+        if (MODE == kOwn && r.first < r.held >> 5) r.first = r.held >> 5;  // (whole pages)
+    }
     r.rows = r.n * a.group;
     r.groups = (int)(((int64_t)r.rows + (1 << p.group_shift) - 1) >> p.group_shift);
-    const int64_t held = (int64_t)a.seqs.max_pages << a.pool.page_shift;
-    r.cap = r.len < 0 ? 0 : r.len > held ? (int)held : r.len;
-    const int64_t lo = a.window > 0 ? r.pos0() - a.window + 1 : 0;
-    r.first = lo < 0 ? 0 : (int)(lo >> 5);
     r.tiles = (int)(((int64_t)r.cap + 31) >> 5) - r.first;
     if (r.tiles < 1) r.tiles = 1;  // rows that see nothing are written too
     r.chunks = (r.tiles + (1 << p.chunk_shift) - 1) >> p.chunk_shift;
@@ -92,6 +122,30 @@ __device__ inline AttendSpan attend_span(const AttendArgs& a, const AttendPlan& 
 }
 __device__ __forceinline__ int token_of(const AttendPlan& p, int row) {
     return (int)(((uint64_t)(uint32_t)row * p.group_magic) >> p.group_bits);
+}
+
+// The positions of the first and the last of rows r0 .. r0 + n - 1 of a sequence, of those of the least and the greatest one where
+// rows of several sequences are together (all lanes of the wave take part); -1 for those before the first position.
+struct AttendEnds {
+    int least, most;
+};
+template <int MODE>
+__device__ __forceinline__ AttendEnds ends_of(const AttendPlan& p, const AttendSpan& s, int r0, int n, int lane) {
+    const int i0 = token_of(p, r0), i1 = token_of(p, r0 + n - 1);
+    if constexpr (MODE == kPrefix) {
+        int least = INT32_MAX, most = -1;
+        for (int i = i0 + lane; i <= i1; i += 64) {
+            const int pos = p.share.row_pos[s.row0 + i];
+            least = min(least, pos);
+            most = max(most, pos);
+        }
+        least = wave_reduce(least, [](int x, int y) { return min(x, y); });
+        most = wave_reduce(most, [](int x, int y) { return max(x, y); });
+        return {__builtin_amdgcn_readfirstlane(least), __builtin_amdgcn_readfirstlane(most)};
+    } else {
+        const int64_t p0 = s.pos0() + i0, p1 = s.pos0() + i1;
+        return {p0 < 0 ? -1 : (int)p0, p1 < 0 ? -1 : (int)p1};
+    }
 }
 
 // Sum over this lane and the lanes below it.
@@ -110,18 +164,18 @@ __device__ __forceinline__ int wave_scan(int x) {
 struct AttendRange {
     int b, before, at, end, per;
 };
-template <int WAVES>
+template <int WAVES, int MODE = kWhole>
 __device__ __forceinline__ AttendRange attend_range(const AttendArgs& a, const AttendPlan& p, int worker, int grain, int least) {
     constexpr int THREADS = 64 * WAVES;
     __shared__ int total_of[WAVES], found[2], longest_of[WAVES];
-    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, n_seq = a.seqs.n_seq;
+    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, n_seq = MODE == kPrefix ? p.share.n_groups : a.seqs.n_seq;
     int own = 0, sum = 0, all = 0, b = tid, longest = 1;
     // items up to sequence b within a round of THREADS (sum), and of the round (returned)
     auto scan = [&]() {
         int chunks = 0;
         own = 0;
         if (b < n_seq) {
-            const AttendSpan s = attend_span(a, p, b);
+            const AttendSpan s = attend_span<MODE>(a, p, b);
             own = s.items(a);
             chunks = own > 0 ? s.chunks : 0;
         }
@@ -250,6 +304,7 @@ struct Attend {
 
     // 16 bytes of a row as KC operands: the three terms of a float32 sum back to it exactly, a bfloat16 is its own
     // Row tile r is rows row0 + step r .. + 15 of the sequence's (its last row in the place of those that it has not).
+    template <int MODE = kWhole>
     __device__ __forceinline__ void load_q(const AttendArgs& a, const AttendPlan& p, const AttendSpan& s, int h, int row0,
                                            int step, int lane) {
         const int u = lane >> 4;
@@ -258,9 +313,10 @@ struct Attend {
             int row = row0 + step * r + (lane & 15);
             row = row < s.rows ? row : s.rows - 1;
             const int i = token_of(p, row), head = h * a.group + (row - i * a.group);
-            const int64_t pos = s.pos0() + i;
+            const int64_t pos = MODE == kPrefix ? p.share.row_pos[s.row0 + i] : s.pos0() + i;
             hi[r] = pos < 0 ? -1 : (int)pos;
             lo[r] = a.window > 0 && hi[r] - a.window + 1 > 0 ? hi[r] - a.window + 1 : 0;
+            if (MODE == kOwn) lo[r] = lo[r] > s.held ? lo[r] : s.held;
             const char* src = a.q + (((int64_t)s.row0 + i) * a.q_row + (int64_t)head * a.pool.d) * ESZ;
 #pragma unroll
             for (int c = 0; c < KC; ++c) {
@@ -654,10 +710,24 @@ struct Joined {
     }
 };
 
+// Takes up the part over the prefix: of element `at` of the results, four columns from col on.
+template <int DP>
+__device__ __forceinline__ void add_prefix(const AttendPlan& p, Joined& x, int64_t at, int dp, int col) {
+    const float2 ml = p.share.ml[at];
+    x.add(ml.x, ml.y, *(const f32x4*)(p.share.o + at * (DP > 0 ? DP : dp) + col));
+}
+
+template <int MODE = kWhole>
 __device__ __forceinline__ void store_joined(const AttendArgs& a, const AttendPlan& p, const AttendSplit& s, int row,
-                                             int col, const Joined& x) {
+                                             int col, Joined x) {
     const int r = s.row + row, i = token_of(p, r);
     const int64_t at = ((int64_t)s.seq_row0 + i) * a.q_heads + s.head0 + (r - i * a.group);
+    if constexpr (MODE == kPrefix) {
+        *(f32x4*)(p.share.o + at * a.pool.dp + col) = x.o;
+        if (col == 0) p.share.ml[at] = make_float2(x.m, x.l);
+        return;
+    }
+    if (MODE == kOwn && s.held) add_prefix<0>(p, x, at, a.pool.dp, col);
     const f32x4 o = x.o * (x.l == 0.0f ? 0.0f : 1.0f / x.l);
     if (col < a.pool.d) {
         if (a.dtype == 0) store4<true>(a, at * a.pool.d + col, o);
@@ -669,7 +739,7 @@ __device__ __forceinline__ void store_joined(const AttendArgs& a, const AttendPl
 // Joins the parts of a row group: of_row groups (a power of two) of dp / 4 lanes on a row, four parts loaded together.  The workgroup takes rows first, first + 1, ... as many as it has lane groups for, and
 // again from `step` times as many on.  load(part's first row + row, column, ml, o) loads four columns.  scratch: THREADS f32x4 and
 // float2 of LDS.
-template <int THREADS, class Load>
+template <int THREADS, int MODE, class Load>
 __device__ __forceinline__ void join_rows(const AttendArgs& a, const AttendPlan& p, const AttendSplit& s, int dp, int of_row, int tid,
                                           int first, int step, f32x4* scratch, Load load) {
     const int lanes = dp / 4, groups = THREADS / lanes;
@@ -701,7 +771,7 @@ __device__ __forceinline__ void join_rows(const AttendArgs& a, const AttendPlan&
                     x.add(ml_of[tid + k * lanes].x, ml_of[tid + k * lanes].y, scratch[tid + k * lanes]);
             __syncthreads();
         }
-        if (live && sub == 0) store_joined(a, p, s, row, col, x);
+        if (live && sub == 0) store_joined<MODE>(a, p, s, row, col, x);
     }
 }
 
@@ -725,7 +795,7 @@ __device__ __forceinline__ void store_part_ml(const AttendPlan& p, int64_t part,
 
 // After a workgroup's part of a row group has been stored: counts it, and joins the parts if it is the last.  scratch:
 // THREADS f32x4 and float2 of LDS that nothing else uses meanwhile.
-template <int THREADS, int DP>
+template <int THREADS, int DP, int MODE>
 __device__ __forceinline__ void join_parts(const AttendArgs& a, const AttendPlan& p, const AttendSplit& s,
                                            f32x4* scratch) {
     __shared__ int last;
@@ -742,7 +812,7 @@ __device__ __forceinline__ void join_parts(const AttendArgs& a, const AttendPlan
     // (all rows at once where they are few; a choice by the parts too costs more than it gains here)
     int of_row = 1;
     while (2 * of_row * s.n_rows <= THREADS / (DP / 4)) of_row *= 2;
-    join_rows<THREADS>(a, p, s, DP, of_row, tid, 0, 1, scratch, [&](int64_t at, int col, float2& ml, f32x4& o) {
+    join_rows<THREADS, MODE>(a, p, s, DP, of_row, tid, 0, 1, scratch, [&](int64_t at, int col, float2& ml, f32x4& o) {
         auto load8 = [](const void* from) {
             const uint64_t w = __hip_atomic_load((const uint64_t*)from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             return make_float2(__uint_as_float((uint32_t)w), __uint_as_float((uint32_t)(w >> 32)));
@@ -753,9 +823,10 @@ __device__ __forceinline__ void join_parts(const AttendArgs& a, const AttendPlan
     });
 }
 
-// HERE: parts are joined within the launch.
-template <int DP, int CT, int R, bool F32, bool HERE>
-__global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(AttendArgs a, AttendPlan p) {
+// HERE: parts are joined within the launch (for sequences' own tokens with three workgroups on a compute unit at most: two
+// registers of the narrowest heads would be kept in memory with four).
+template <int DP, int CT, int R, bool F32, bool HERE, int MODE = kWhole>
+__global__ __launch_bounds__(256, (HERE && MODE == kOwn && Attend<DP, CT, R, F32>::OCC > 3 ? 3 : Attend<DP, CT, R, F32>::OCC)) void k_attend(AttendArgs a, AttendPlan p) {
     using A = Attend<DP, CT, R, F32>;
     constexpr int GR = 16 * R;  // rows of a row group
     __shared__ float2 sml[4][GR];
@@ -763,7 +834,7 @@ __global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(A
     const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int worker = blockIdx.x;
 
-    AttendRange range = attend_range<4>(a, p, worker, 4 >> (p.chunk_shift < 2 ? p.chunk_shift : 2), 1);
+    AttendRange range = attend_range<4, MODE>(a, p, worker, 4 >> (p.chunk_shift < 2 ? p.chunk_shift : 2), 1);
     if (range.at >= range.end) {
         if (!HERE && tid == 0) p.split[worker].n_rows = 0;
         return;
@@ -775,7 +846,7 @@ __global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(A
     // A segment: tiles tile0 .. tile1 - 1 of one row group
     struct Segment {
         int h, rg, tile0, tile1, row0, rows, n_rows;  // n_rows: rows in the group
-        int first, b, item0, items;                   // the row group's first item, its items
+        int first, table, held, item0, items;         // the row group's first item, its items
         bool starts, ends;                            // whether it holds the first and the last tile
         int seen0, seen1, all0, all1;                 // positions that one of the rows, that every row sees
     };
@@ -785,14 +856,14 @@ __global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(A
     Segment g;
     int page = -1, t0 = 0;
     uint64_t todo = 0;
-    AttendSpan s = attend_span(a, p, range.b);
+    AttendSpan s = attend_span<MODE>(a, p, range.b);
 
     // the wave's tiles t0, t0 + 4, ... of the segment, a lane each: which of them are there and seen
     auto load_pages = [&]() {
         const int t = t0 + lane * 4, mine = g.first + t;
         page = -1;
         if (t < g.tile1 && 32 * mine <= g.seen1 && 32 * mine + 31 >= g.seen0)
-            page = (a.seqs.pages + (int64_t)g.b * a.seqs.max_pages)[mine >> tile_shift];
+            page = (a.seqs.pages + (int64_t)g.table * a.seqs.max_pages)[mine >> tile_shift];
     };
     auto look = [&]() { todo = __ballot(page >= 0 && page < a.pool.n_pages); };
     // the wave's next tile, if there is one
@@ -824,17 +895,18 @@ __global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(A
         g.tile0 = c0 << p.chunk_shift;
         g.tile1 = g.ends ? s.tiles : c1 << p.chunk_shift;
         const int r0 = g.rg << p.group_shift;
-        g.row0 = s.row0, g.rows = s.rows, g.first = s.first, g.b = range.b;
+        g.row0 = s.row0, g.rows = s.rows, g.first = s.first, g.table = s.table, g.held = s.held;
         g.n_rows = s.rows - r0 < GR ? s.rows - r0 : GR;
-        const int64_t p0 = s.pos0() + token_of(p, r0), p1 = s.pos0() + token_of(p, r0 + g.n_rows - 1);
-        const int q0 = p0 < 0 ? -1 : (int)p0, q1 = p1 < 0 ? -1 : (int)p1;
+        const AttendEnds ends = ends_of<MODE>(p, s, r0, g.n_rows, lane);
+        const int q0 = ends.least, q1 = ends.most;
         g.seen0 = a.window > 0 && q0 - a.window + 1 > 0 ? q0 - a.window + 1 : 0;
         g.all0 = a.window > 0 && q1 - a.window + 1 > 0 ? q1 - a.window + 1 : 0;
+        if (MODE == kOwn) g.seen0 = max(g.seen0, s.held), g.all0 = max(g.all0, s.held);
         g.seen1 = q1 < s.cap - 1 ? q1 : s.cap - 1;
         g.all1 = q0 < g.seen1 ? q0 : g.seen1;
         t0 = g.tile0 + wid;
         load_pages();
-        w.load_q(a, p, s, g.h, r0, 16, lane);  // while the page numbers are on their way
+        w.template load_q<MODE>(a, p, s, g.h, r0, 16, lane);  // while the page numbers are on their way
         __builtin_amdgcn_sched_barrier(0);
         look();
         const int64_t pl = next();
@@ -864,7 +936,7 @@ __global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(A
         }
 
         if (odd)
-            w.spoil(a, a.seqs.pages + (int64_t)g.b * a.seqs.max_pages, g.h, g.first, g.tile0 + wid, g.tile1, 4, g.seen0, g.seen1,
+            w.spoil(a, a.seqs.pages + (int64_t)g.table * a.seqs.max_pages, g.h, g.first, g.tile0 + wid, g.tile1, 4, g.seen0, g.seen1,
                     g.all0, g.all1, lane);
         // The next segment's loads are on their way while this one's results are joined and stored.
         const Segment old = g;
@@ -874,7 +946,7 @@ __global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(A
             const int items = s.items(a);
             if (range.at - range.before >= items) {  // past this sequence, and those without rows
                 range.before += items;
-                do s = attend_span(a, p, ++range.b);
+                do s = attend_span<MODE>(a, p, ++range.b);
                 while (s.n == 0);
             }
             open();
@@ -885,7 +957,7 @@ __global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(A
         if (!whole) {
             const int first = (int)((uint32_t)old.item0 / (uint32_t)range.per);
             const int end = (int)((uint32_t)(old.item0 + old.items - 1) / (uint32_t)range.per);
-            u0 = AttendSplit{old.row0, old.h * a.group, old.rg * GR, old.n_rows, first, end - first + 1, {}};
+            u0 = AttendSplit{old.row0, old.h * a.group, old.rg * GR, old.n_rows, first, end - first + 1, old.held, 0};
             if (old.ends) split = u0;
         }
         // four columns of a row of the group; its maximum and sum with the first of them
@@ -902,6 +974,16 @@ __global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(A
             }
             const int r = old.rg * GR + row, i = token_of(p, r), head = old.h * a.group + (r - i * a.group);
             const int64_t at = ((int64_t)old.row0 + i) * a.q_heads + head;
+            if constexpr (MODE == kPrefix) {
+                *(f32x4*)(p.share.o + at * DP + col) = x;
+                if (col == 0) p.share.ml[at] = make_float2(m, l);
+                return;
+            }
+            if (MODE == kOwn && old.held) {
+                Joined j{m, l, x};
+                add_prefix<DP>(p, j, at, DP, col);
+                m = j.m, l = j.l, x = j.o;
+            }
             if (col < a.pool.d) store4<F32>(a, at * a.pool.d + col, x * (l == 0.0f ? 0.0f : 1.0f / l));
             if (col == 0 && a.lse) a.lse[at] = lse_of(m, l);
         };
@@ -942,7 +1024,7 @@ __global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(A
             }
         if constexpr (HERE) {
             static_assert(sizeof(so) >= 256 * 24, "the join's scratch");
-            if (!whole) join_parts<256, DP>(a, p, u0, (f32x4*)&so[0][0][0]);
+            if (!whole) join_parts<256, DP, MODE>(a, p, u0, (f32x4*)&so[0][0][0]);
         }
     }
     if (!HERE && tid == 0) p.split[worker] = split;

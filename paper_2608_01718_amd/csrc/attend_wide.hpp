@@ -35,7 +35,7 @@ struct Wide {
     static constexpr int OCC = R * DP * (F32 ? 2 : 1) <= 256 ? 2 : 1;
 };
 
-template <int DP, int CT, int WAVES, int R, bool F32>
+template <int DP, int CT, int WAVES, int R, bool F32, int MODE = kWhole>
 __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) void k_attend_wide(AttendArgs a,
                                                                                               AttendPlan p) {
     using W = Wide<DP, CT, WAVES, R, F32>;
@@ -52,7 +52,7 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
 
     // (two tiles or more: a part of 128 rows is four times the bytes of a tile to write, and again to read in the join; one
     // sequence of 4096 tokens, 16 new ones 40 us, 50 with one)
-    AttendRange range = attend_range<WAVES>(a, p, worker, 1, 2);
+    AttendRange range = attend_range<WAVES, MODE>(a, p, worker, 1, 2);
     if (range.at >= range.end) {
         if (tid == 0) p.split[worker].n_rows = 0;
         return;
@@ -60,7 +60,7 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
     AttendSplit split{};
     const float scale2 = scale_of(a);
     const int tile_shift = a.pool.page_shift - 5;
-    AttendSpan s = attend_span(a, p, range.b);
+    AttendSpan s = attend_span<MODE>(a, p, range.b);
 
     while (true) {
         // the segment that begins at item range.at
@@ -73,16 +73,17 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
         const int tile0 = c0 << p.chunk_shift, tile1 = ends ? s.tiles : c1 << p.chunk_shift;
         const int r0 = rg << p.group_shift, n_rows = s.rows - r0 < W::ROWS ? s.rows - r0 : W::ROWS;
         // positions that one of the rows, that every row sees
-        const int64_t p0 = s.pos0() + token_of(p, r0), p1 = s.pos0() + token_of(p, r0 + n_rows - 1);
-        const int q0 = p0 < 0 ? -1 : (int)p0, q1 = p1 < 0 ? -1 : (int)p1;
-        const int seen0 = a.window > 0 && q0 - a.window + 1 > 0 ? q0 - a.window + 1 : 0;
-        const int all0 = a.window > 0 && q1 - a.window + 1 > 0 ? q1 - a.window + 1 : 0;
+        const AttendEnds of_rows = ends_of<MODE>(p, s, r0, n_rows, lane);
+        const int q0 = of_rows.least, q1 = of_rows.most;
+        int seen0 = a.window > 0 && q0 - a.window + 1 > 0 ? q0 - a.window + 1 : 0;
+        int all0 = a.window > 0 && q1 - a.window + 1 > 0 ? q1 - a.window + 1 : 0;
+        if (MODE == kOwn) seen0 = max(seen0, s.held), all0 = max(all0, s.held);
         const int seen1 = q1 < s.cap - 1 ? q1 : s.cap - 1, all1 = q0 < seen1 ? q0 : seen1;
         const int tiles_here = (n_rows + 15) >> 4, active = tiles_here > wid ? (tiles_here - wid + WAVES - 1) / WAVES : 0;
 
         A w;
         w.clear();
-        w.load_q(a, p, s, h, r0 + 16 * wid, 16 * WAVES, lane);
+        w.template load_q<MODE>(a, p, s, h, r0 + 16 * wid, 16 * WAVES, lane);
 
         // The segment's tiles in turn, from the first whose number is a multiple of a full range's length on, and then those
         // before it: row groups of one (sequence, kv head), whose ranges begin anywhere, read the same tiles at about the
@@ -100,7 +101,7 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
             const int t = t0 + lane, mine = tile_at(t);
             page = -1;
             if (t < count && 32 * mine <= seen1 && 32 * mine + 31 >= seen0)
-                page = (a.seqs.pages + (int64_t)range.b * a.seqs.max_pages)[mine >> tile_shift];
+                page = (a.seqs.pages + (int64_t)s.table * a.seqs.max_pages)[mine >> tile_shift];
             todo = __ballot(page >= 0 && page < a.pool.n_pages);
         };
         load_pages();
@@ -224,7 +225,7 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
 #pragma unroll
             for (int t = 0; t < WAVES; ++t) some |= odd_of[t];
             if (__builtin_amdgcn_readfirstlane(some))
-                w.spoil(a, a.seqs.pages + (int64_t)range.b * a.seqs.max_pages, h, s.first, tile0, tile1, 1, seen0, seen1, all0, all1,
+                w.spoil(a, a.seqs.pages + (int64_t)s.table * a.seqs.max_pages, h, s.first, tile0, tile1, 1, seen0, seen1, all0, all1,
                         lane);
         }
         w.reduce();
@@ -233,7 +234,7 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
         const int64_t slot = part_of(p, worker, !ends);
         if (ends && !starts) {
             const int first = (int)((uint32_t)(range.before + unit * s.chunks) / (uint32_t)range.per);
-            split = AttendSplit{s.row0, h * a.group, r0, n_rows, first, worker - first + 1, {}};
+            split = AttendSplit{s.row0, h * a.group, r0, n_rows, first, worker - first + 1, s.held, 0};
         }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -247,6 +248,22 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
             } else {
                 const int i = token_of(p, r0 + row), head = h * a.group + (r0 + row - i * a.group);
                 const int64_t at = ((int64_t)s.row0 + i) * a.q_heads + head;
+                if constexpr (MODE == kPrefix) {
+#pragma unroll
+                    for (int j = 0; j < W::NJ; ++j) *(f32x4*)(p.share.o + at * DP + 16 * j + 4 * u) = w.o[r][j];
+                    if (u == 0) p.share.ml[at] = make_float2(w.m[r], w.l[r]);
+                    continue;
+                }
+                if (MODE == kOwn && s.held) {
+                    Joined x{w.m[r], w.l[r], {}};
+#pragma unroll
+                    for (int j = 0; j < W::NJ; ++j) {
+                        x = Joined{w.m[r], w.l[r], w.o[r][j]};
+                        add_prefix<DP>(p, x, at, DP, 16 * j + 4 * u);
+                        w.o[r][j] = x.o;
+                    }
+                    w.m[r] = x.m, w.l[r] = x.l;
+                }
                 const float f = w.l[r] == 0.0f ? 0.0f : 1.0f / w.l[r];
 #pragma unroll
                 for (int j = 0; j < W::NJ; ++j)
@@ -257,7 +274,7 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
         if (range.at >= range.end) break;
         if (range.at - range.before >= s.items(a)) {  // past this sequence, and those without rows
             range.before += s.items(a);
-            do s = attend_span(a, p, ++range.b);
+            do s = attend_span<MODE>(a, p, ++range.b);
             while (s.n == 0);
         }
         lds_barrier();  // the buffers have been read
@@ -265,31 +282,32 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
     if (tid == 0) p.split[worker] = split;
 }
 
-template <int DP>
+template <int DP, int MODE>
 hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
     const dim3 grid((unsigned)(p.group_shift < 6 ? p.workers : (p.workers + 7) & ~7)), block(p.waves * 64);
     auto go = [&](auto ct) {
         constexpr int CT = decltype(ct)::value;
+        constexpr bool HERE = MODE != kPrefix;
         if (a.dtype == 0) {
-            if (p.join_here) k_attend<DP, CT, 1, true, true><<<grid, block, 0, s>>>(a, p);
-            else if (p.group_shift == 4) k_attend<DP, CT, 1, true, false><<<grid, block, 0, s>>>(a, p);
-            else if constexpr (DP <= 192) k_attend_wide<DP, CT, 4, 1, true><<<grid, block, 0, s>>>(a, p);
+            if (HERE && p.join_here) k_attend<DP, CT, 1, true, HERE, MODE><<<grid, block, 0, s>>>(a, p);
+            else if (p.group_shift == 4) k_attend<DP, CT, 1, true, false, MODE><<<grid, block, 0, s>>>(a, p);
+            else if constexpr (DP <= 192) k_attend_wide<DP, CT, 4, 1, true, MODE><<<grid, block, 0, s>>>(a, p);
             return;
         }
         switch (p.group_shift) {
             case 4:
-                if (p.join_here) k_attend<DP, CT, 1, false, true><<<grid, block, 0, s>>>(a, p);
-                else k_attend<DP, CT, 1, false, false><<<grid, block, 0, s>>>(a, p);
+                if (HERE && p.join_here) k_attend<DP, CT, 1, false, HERE, MODE><<<grid, block, 0, s>>>(a, p);
+                else k_attend<DP, CT, 1, false, false, MODE><<<grid, block, 0, s>>>(a, p);
                 break;
             case 5:
-                if constexpr (DP <= 128) k_attend<DP, CT, 2, false, false><<<grid, block, 0, s>>>(a, p);
+                if constexpr (DP <= 128) k_attend<DP, CT, 2, false, false, MODE><<<grid, block, 0, s>>>(a, p);
                 break;
             case 6:
-                if constexpr (DP <= 192) k_attend_wide<DP, CT, 4, 1, false><<<grid, block, 0, s>>>(a, p);
+                if constexpr (DP <= 192) k_attend_wide<DP, CT, 4, 1, false, MODE><<<grid, block, 0, s>>>(a, p);
                 break;
             case 7:
-                if constexpr (DP <= 128) k_attend_wide<DP, CT, 4, 2, false><<<grid, block, 0, s>>>(a, p);
-                else k_attend_wide<DP, CT, 8, 1, false><<<grid, block, 0, s>>>(a, p);
+                if constexpr (DP <= 128) k_attend_wide<DP, CT, 4, 2, false, MODE><<<grid, block, 0, s>>>(a, p);
+                else k_attend_wide<DP, CT, 8, 1, false, MODE><<<grid, block, 0, s>>>(a, p);
                 break;
         }
     };
@@ -302,10 +320,20 @@ hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t s
 // Workgroups of the wide kernels on a compute unit.
 constexpr int wide_occupancy(int dp, int waves, int R, bool f32) { return (R * dp * (f32 ? 2 : 1) <= 256 ? 2 : 1) * 4 / waves; }
 
-extern template hipError_t launch_attend<64>(const AttendArgs&, const AttendPlan&, hipStream_t);
-extern template hipError_t launch_attend<96>(const AttendArgs&, const AttendPlan&, hipStream_t);
-extern template hipError_t launch_attend<128>(const AttendArgs&, const AttendPlan&, hipStream_t);
-extern template hipError_t launch_attend<192>(const AttendArgs&, const AttendPlan&, hipStream_t);
-extern template hipError_t launch_attend<256>(const AttendArgs&, const AttendPlan&, hipStream_t);
+extern template hipError_t launch_attend<64, kWhole>(const AttendArgs&, const AttendPlan&, hipStream_t);
+extern template hipError_t launch_attend<96, kWhole>(const AttendArgs&, const AttendPlan&, hipStream_t);
+extern template hipError_t launch_attend<128, kWhole>(const AttendArgs&, const AttendPlan&, hipStream_t);
+extern template hipError_t launch_attend<192, kWhole>(const AttendArgs&, const AttendPlan&, hipStream_t);
+extern template hipError_t launch_attend<256, kWhole>(const AttendArgs&, const AttendPlan&, hipStream_t);
+extern template hipError_t launch_attend<64, kPrefix>(const AttendArgs&, const AttendPlan&, hipStream_t);
+extern template hipError_t launch_attend<96, kPrefix>(const AttendArgs&, const AttendPlan&, hipStream_t);
+extern template hipError_t launch_attend<128, kPrefix>(const AttendArgs&, const AttendPlan&, hipStream_t);
+extern template hipError_t launch_attend<192, kPrefix>(const AttendArgs&, const AttendPlan&, hipStream_t);
+extern template hipError_t launch_attend<256, kPrefix>(const AttendArgs&, const AttendPlan&, hipStream_t);
+extern template hipError_t launch_attend<64, kOwn>(const AttendArgs&, const AttendPlan&, hipStream_t);
+extern template hipError_t launch_attend<96, kOwn>(const AttendArgs&, const AttendPlan&, hipStream_t);
+extern template hipError_t launch_attend<128, kOwn>(const AttendArgs&, const AttendPlan&, hipStream_t);
+extern template hipError_t launch_attend<192, kOwn>(const AttendArgs&, const AttendPlan&, hipStream_t);
+extern template hipError_t launch_attend<256, kOwn>(const AttendArgs&, const AttendPlan&, hipStream_t);
 
 }  // namespace lacache

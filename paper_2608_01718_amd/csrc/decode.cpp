@@ -170,6 +170,43 @@ int lacache_kv_attend(const lacache_kv* kv, const lacache_seqs* seqs, const void
     return launch_kv_attend(a, max_new, workspace, cu, (hipStream_t)stream) == hipSuccess ? LACACHE_OK : LACACHE_EHIP;
 }
 
+int64_t lacache_kv_attend_shared_workspace(const lacache_kv* kv, lacache_dtype dtype, int64_t rows, int32_t n_seq,
+                                           int32_t n_groups, int32_t q_heads, int32_t max_new) {
+    KvPool p;
+    if (!to_pool(kv, false, &p) || !is_dtype(dtype) || rows < 0 || rows > INT32_MAX || n_seq < 0 || n_seq > kMostChosen ||
+        n_groups < 0 || n_groups > kMostChosen || q_heads < 1 || q_heads > 65535 || q_heads % kv->heads != 0 || max_new < 0)
+        return LACACHE_EINVAL;
+    const int cu = compute_units();
+    return cu ? attend_shared_workspace(p, (int)dtype, rows, n_seq, n_groups, q_heads, max_new, cu) : LACACHE_EHIP;
+}
+
+int lacache_kv_attend_shared(const lacache_kv* kv, const lacache_seqs* seqs, const lacache_prefixes* prefixes,
+                             const void* q, lacache_dtype dtype, int64_t rows, int32_t q_heads, int64_t q_row,
+                             int32_t max_new, float scale, int32_t window, void* out, float* lse, void* workspace,
+                             int64_t workspace_bytes, void* stream) {
+    AttendArgs a{};
+    if (!to_pool(kv, true, &a.pool) || !to_seqs(seqs, rows, &a.seqs) || !is_dtype(dtype) || q_heads < 1 ||
+        q_heads > 65535 || q_heads % kv->heads != 0 || q_row < 0 || max_new < 0 || !std::isfinite(scale) ||
+        rows * (q_heads / kv->heads) > INT32_MAX || window < 0 || workspace_bytes < 0 || !prefixes || prefixes->n_groups < 0 ||
+        prefixes->n_groups > kMostChosen || a.seqs.n_seq > kMostChosen ||
+        (prefixes->n_groups > 0 && (!prefixes->group || !prefixes->len || !aligned(prefixes->group, 4) || !aligned(prefixes->len, 4))) ||
+        !attend_fits(a.pool, (int)dtype, rows, seqs->n_seq, q_heads / kv->heads, max_new) ||
+        !attend_shared_fits(a.pool, (int)dtype, rows, prefixes->n_groups, q_heads / kv->heads))
+        return LACACHE_EINVAL;
+    if (rows == 0 || seqs->n_seq == 0) return LACACHE_OK;
+    const uintptr_t esz = dtype == LACACHE_F32 ? 4 : 2;
+    if (!q || !out || !aligned(q, esz) || !aligned(out, esz) || !aligned(lse, 4)) return LACACHE_EINVAL;
+    const int cu = compute_units();
+    if (!cu) return LACACHE_EHIP;
+    const int64_t need = attend_shared_workspace(a.pool, (int)dtype, rows, seqs->n_seq, prefixes->n_groups, q_heads, max_new, cu);
+    if (workspace_bytes < need || (need > 0 && (!workspace || !aligned(workspace, 16)))) return LACACHE_EINVAL;
+    a.q = (const char*)q, a.out = (char*)out, a.lse = lse;
+    a.dtype = (int)dtype, a.q_heads = q_heads, a.group = q_heads / kv->heads, a.window = window;
+    a.q_row = q_row, a.scale = scale;
+    return launch_kv_attend_shared(a, prefixes->group, prefixes->len, prefixes->n_groups, max_new, workspace, cu,
+                                   (hipStream_t)stream) == hipSuccess ? LACACHE_OK : LACACHE_EHIP;
+}
+
 int lacache_kv_bound(const lacache_kv* kv, const lacache_bounds* bounds, const lacache_seqs* seqs, int64_t rows,
                      int32_t max_new, void* stream) {
     KvPool p;

@@ -8,6 +8,7 @@ constexpr int kJoinThreads = 256;
 constexpr int64_t kMostItems = INT32_MAX / 2;  // chunks of tiles of all row groups
 
 // Many row groups, of few parts each: a thread four columns of a row, part after part (four loaded together).
+template <int MODE>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, AttendPlan p) {
     const AttendSplit s = p.split[blockIdx.x];
     const int dp = a.pool.dp, lanes = dp / 4, rows = 256 / lanes;
@@ -29,13 +30,14 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, AttendPlan p)
             for (int u = 0; u < 4; ++u)
                 if (k0 + u < parts) x.add(ml[u].x, ml[u].y, o[u]);
         }
-        store_joined(a, p, s, row, col, x);
+        store_joined<MODE>(a, p, s, row, col, x);
     }
 }
 
 // Few row groups, often of many parts each: the workgroups (x, .) join those that ended with one of `of` workers, each a
 // share of the rows.  The j-th of these workers is number (x + j) mod gridDim.x of the j-th gridDim.x of all, so that
 // neighbours among the workers, and those in regular steps, go to different workgroups.
+template <int MODE>
 __global__ __launch_bounds__(kJoinThreads) void k_attend_join_few(AttendArgs a, AttendPlan p, int of) {
     __shared__ f32x4 scratch[kJoinThreads * 3 / 2];
     auto worker = [&](int j) { return j * (int)gridDim.x + (int)((blockIdx.x + j) % gridDim.x); };
@@ -47,7 +49,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_attend_join_few(AttendArgs a, 
         int of_row = 1;
         while (2 * of_row <= groups && (8 * of_row <= s.parts || (4 * of_row <= s.parts && 2 * of_row * s.n_rows <= groups)))
             of_row *= 2;
-        join_rows<kJoinThreads>(a, p, s, a.pool.dp, of_row, threadIdx.x, blockIdx.y, gridDim.y, scratch,
+        join_rows<kJoinThreads, MODE>(a, p, s, a.pool.dp, of_row, threadIdx.x, blockIdx.y, gridDim.y, scratch,
                                 [&](int64_t at, int col, float2& ml, f32x4& o) {
                                     ml = p.part_ml[at];
                                     o = *(const f32x4*)(p.part_o + at * a.pool.dp + col);
@@ -109,10 +111,11 @@ int64_t attend_workspace(const KvPool& pool, int dtype, int q_heads, int max_new
     return bytes;
 }
 
-hipError_t launch_kv_attend(const AttendArgs& a, int max_new, void* workspace, int num_cu, hipStream_t s) {
-    if (a.seqs.rows <= 0 || a.seqs.n_seq <= 0) return hipSuccess;
-    int64_t bytes;
-    AttendPlan p = plan_of(a.pool, a.dtype == 0, max_new, a.group, num_cu, (char*)workspace, &bytes);
+namespace {
+
+// The launches of one mode.  n_seq: what the mode counts as sequences; max_new: a bound (kPrefix: an average) on the rows of each.
+template <int MODE>
+hipError_t launch_mode(const AttendArgs& a, AttendPlan p, int n_seq, int64_t max_new, hipStream_t s) {
     // row / group for rows below 2^31: magic = ceil(2^(31 + bits) / group), bits = ceil(log2 group)
     int bits = 0;
     while ((1 << bits) < a.group) ++bits;
@@ -120,31 +123,31 @@ hipError_t launch_kv_attend(const AttendArgs& a, int max_new, void* workspace, i
     p.group_magic = (uint32_t)((((uint64_t)1 << p.group_bits) + a.group - 1) / a.group);
     // the chunks of all row groups are counted in 32 bits (a chunk holds a whole sequence at the latest: attend_fits)
     const int64_t tiles = ((int64_t)a.seqs.max_pages << (a.pool.page_shift - 5)) + 1;
-    const int64_t units = row_groups(a.pool, a.seqs.rows, a.seqs.n_seq, a.group, p.group_shift);
+    const int64_t units = row_groups(a.pool, a.seqs.rows, n_seq, a.group, p.group_shift);
     while (units * (((tiles - 1) >> p.chunk_shift) + 1) > kMostItems && p.chunk_shift < 30) ++p.chunk_shift;
     // Small calls join their parts in the launch: where each wave has a tile at most, by what the page tables (or the
     // window) can hold, and a row group has few parts.  One launch less is 2 us on the host and 1 us on the GPU (one sequence of
     // 777 tokens, 8 heads 11.5 us, 13.7 in two); with more parts to join, or parts of many rows, the launch is faster (131,071
     // tokens 88 us, 93 joined in the launch; 64 sequences in fp8 99, 103; 151 new tokens 174, 208; 7 heads on one of 33,000
     // tokens, 260 parts 19, 53; of 1000 tokens 13.4, 10.5).
-    const int64_t seen = a.window > 0 && a.window / 32 + 2 + (int64_t)max_new / 32 < tiles && max_new > 0
+    const int64_t seen = a.window > 0 && a.window / 32 + 2 + max_new / 32 < tiles && max_new > 0
                              ? a.window / 32 + 2 + max_new / 32 : tiles;
-    p.join_here = p.group_shift == 4 && seen <= 64 && units * seen <= 4 * (int64_t)p.workers;
-    const hipError_t e = a.pool.dp == 64    ? launch_attend<64>(a, p, s)
-                         : a.pool.dp == 96  ? launch_attend<96>(a, p, s)
-                         : a.pool.dp == 128 ? launch_attend<128>(a, p, s)
-                         : a.pool.dp == 192 ? launch_attend<192>(a, p, s)
-                                            : launch_attend<256>(a, p, s);
+    p.join_here = MODE != kPrefix && p.group_shift == 4 && seen <= 64 && units * seen <= 4 * (int64_t)p.workers;
+    const hipError_t e = a.pool.dp == 64    ? launch_attend<64, MODE>(a, p, s)
+                         : a.pool.dp == 96  ? launch_attend<96, MODE>(a, p, s)
+                         : a.pool.dp == 128 ? launch_attend<128, MODE>(a, p, s)
+                         : a.pool.dp == 192 ? launch_attend<192, MODE>(a, p, s)
+                                            : launch_attend<256, MODE>(a, p, s);
     if (e != hipSuccess || p.join_here) return e;
     // rows of a row group, row groups
     int64_t rows = (max_new <= 0 ? 64 : max_new < a.seqs.rows ? max_new : a.seqs.rows) * a.group;
-    const int64_t live = a.seqs.n_seq < a.seqs.rows ? a.seqs.n_seq : a.seqs.rows;
+    const int64_t live = n_seq < a.seqs.rows ? n_seq : a.seqs.rows;
     const int64_t groups_most = live * a.pool.heads * (((rows - 1) >> p.group_shift) + 1);
     rows = rows < (1 << p.group_shift) ? rows : 1 << p.group_shift;
     const int64_t lane_groups = kJoinThreads / (a.pool.dp / 4);
     if (groups_most >= 64) {
-        k_attend_join<<<dim3((unsigned)p.workers, (unsigned)((rows + lane_groups - 1) / lane_groups)), dim3(kJoinThreads), 0,
-                        s>>>(a, p);
+        k_attend_join<MODE><<<dim3((unsigned)p.workers, (unsigned)((rows + lane_groups - 1) / lane_groups)), dim3(kJoinThreads),
+                              0, s>>>(a, p);
     } else {
         // About one row group that was split for each workgroup in x, and one pass over its rows, but no more than 2048
         // workgroups: of a launch of 16,384 that find nothing most of the time is theirs (4 sequences of 1024 tokens, 16 new
@@ -158,9 +161,122 @@ hipError_t launch_kv_attend(const AttendArgs& a, int max_new, void* workspace, i
         for (int64_t of_row = 1; at_once > 1 && 8 * of_row <= parts; of_row *= 2) at_once /= 2;
         int64_t y = (rows + at_once - 1) / at_once;
         y = y < 2048 / x ? y : 2048 / x;
-        k_attend_join_few<<<dim3((unsigned)x, (unsigned)(y > 1 ? y : 1)), dim3(kJoinThreads), 0, s>>>(a, p, of);
+        k_attend_join_few<MODE><<<dim3((unsigned)x, (unsigned)(y > 1 ? y : 1)), dim3(kJoinThreads), 0, s>>>(a, p, of);
     }
     return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_kv_attend(const AttendArgs& a, int max_new, void* workspace, int num_cu, hipStream_t s) {
+    if (a.seqs.rows <= 0 || a.seqs.n_seq <= 0) return hipSuccess;
+    int64_t bytes;
+    return launch_mode<kWhole>(a, plan_of(a.pool, a.dtype == 0, max_new, a.group, num_cu, (char*)workspace, &bytes), a.seqs.n_seq,
+                               max_new, s);
+}
+
+// ---------------------------------------------------------------------------
+// Groups of sequences that share a prefix.  The prefix of a group is attended to once, by all of the group's rows together: a
+// tile is read for up to 128 of them instead of for one sequence's.  A launch over the prefixes leaves each row's sums in the
+// workspace, a launch over the sequences' own tokens takes them up before it divides.
+// ---------------------------------------------------------------------------
+
+// What the two launches need: workgroup b < n_seq the positions of sequence b's rows and what it shares, the others a group each.
+__global__ __launch_bounds__(64) void k_attend_share(AttendArgs a, AttendShare x, const int32_t* group, const int32_t* len) {
+    const int lane = threadIdx.x, n_seq = a.seqs.n_seq;
+    const int64_t known = (int64_t)a.seqs.max_pages << a.pool.page_shift;
+    // sequences and tokens of group g (one sequence shares nothing)
+    auto group_of = [&](int g, int& from, int& to) {
+        from = group[g], to = group[g + 1];
+        from = from < 0 ? 0 : from > n_seq ? n_seq : from;
+        to = to < from ? from : to > n_seq ? n_seq : to;
+        const int64_t n = len[g] < 0 ? 0 : len[g] < known ? len[g] : known;
+        return to - from > 1 ? (int)(n >> a.pool.page_shift << a.pool.page_shift) : 0;
+    };
+    if ((int)blockIdx.x < n_seq) {
+        const int b = blockIdx.x;
+        int count = 0;  // groups that begin at b or before
+        for (int i = 0; i < x.n_groups; i += 64) count += __popcll(__ballot(i + lane < x.n_groups && group[i + lane] <= b));
+        int from = 0, to = 0;
+        const int held = count > 0 ? group_of(count - 1, from, to) : 0;
+        if (lane == 0) x.held[b] = b >= from && b < to ? held : 0;
+        const KvSpan s = span_of(a.seqs, b);
+        for (int i = lane; i < s.n; i += 64) x.row_pos[s.row0 + i] = s.pos0 + i < 0 ? -1 : (int)(s.pos0 + i);
+        return;
+    }
+    const int g = blockIdx.x - n_seq;
+    int from, to, least = INT32_MAX;
+    const int held = group_of(g, from, to);
+    for (int b = from + lane; b < to; b += 64) {
+        const KvSpan s = span_of(a.seqs, b);
+        const int64_t first = s.pos0 < 0 ? 0 : s.pos0;
+        if (s.n > 0 && s.pos0 + s.n > 0) least = first < least ? (int)first : least;
+    }
+    least = wave_reduce(least, [](int p, int q) { return p < q ? p : q; });
+    if (lane == 0) {
+        const int64_t row0 = from < n_seq ? span_of(a.seqs, from).row0 : 0, end = to > from ? span_of(a.seqs, to - 1).row0 + span_of(a.seqs, to - 1).n : row0;
+        x.span[g] = make_int4((int)row0, held > 0 && end > row0 ? (int)(end - row0) : 0, held, from);
+        const int64_t lo = a.window > 0 && least < INT32_MAX ? (int64_t)least - a.window + 1 : 0;
+        x.first[g] = lo > 0 ? (int)(lo >> 5) : 0;
+    }
+}
+
+namespace {
+
+int prefix_rows(int64_t rows, int n_groups) {  // of a group, on average
+    const int64_t each = n_groups > 0 ? (rows + n_groups - 1) / n_groups : 1;
+    return each < 1 ? 1 : (int)each;
+}
+
+// The plans of both launches, which use the same memory one after the other, and what lies behind it.
+int64_t shared_plan(const KvPool& pool, bool f32, int64_t rows, int n_seq, int n_groups, int q_heads, int max_new, int num_cu,
+                    char* space, AttendPlan* prefix, AttendPlan* own) {
+    const int group = q_heads / pool.heads;
+    int64_t one, two;
+    *prefix = plan_of(pool, f32, prefix_rows(rows, n_groups), group, num_cu, space, &one);
+    *own = plan_of(pool, f32, max_new, group, num_cu, space, &two);
+    int64_t at = one > two ? one : two;
+    auto take = [&](int64_t n) {
+        at = (at + 15) & ~int64_t(15);
+        char* p = space + at;
+        at += n;
+        return p;
+    };
+    AttendShare x{};
+    x.n_groups = n_groups;
+    x.span = (int4*)take(16 * (int64_t)n_groups);
+    x.first = (int32_t*)take(4 * (int64_t)n_groups);
+    x.held = (int32_t*)take(4 * (int64_t)n_seq);
+    x.row_pos = (int32_t*)take(4 * rows);
+    x.ml = (float2*)take(8 * rows * q_heads);
+    x.o = (float*)take(4 * rows * q_heads * pool.dp);
+    prefix->share = own->share = x;
+    return at;
+}
+
+}  // namespace
+
+bool attend_shared_fits(const KvPool& pool, int dtype, int64_t rows, int n_groups, int group) {
+    const Shape sh = shape_of(pool, dtype == 0, (int64_t)prefix_rows(rows, n_groups) * group);
+    return row_groups(pool, rows, n_groups, group, sh.group_shift) <= kMostItems;
+}
+
+int64_t attend_shared_workspace(const KvPool& pool, int dtype, int64_t rows, int n_seq, int n_groups, int q_heads, int max_new,
+                                int num_cu) {
+    AttendPlan p, o;
+    return shared_plan(pool, dtype == 0, rows, n_seq, n_groups, q_heads, max_new, num_cu, nullptr, &p, &o);
+}
+
+hipError_t launch_kv_attend_shared(const AttendArgs& a, const int32_t* group, const int32_t* len, int n_groups, int max_new,
+                                   void* workspace, int num_cu, hipStream_t s) {
+    if (a.seqs.rows <= 0 || a.seqs.n_seq <= 0) return hipSuccess;
+    AttendPlan prefix, own;
+    shared_plan(a.pool, a.dtype == 0, a.seqs.rows, a.seqs.n_seq, n_groups, a.q_heads, max_new, num_cu, (char*)workspace, &prefix, &own);
+    k_attend_share<<<dim3((unsigned)(a.seqs.n_seq + n_groups)), dim3(64), 0, s>>>(a, prefix.share, group, len);
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && n_groups > 0) e = launch_mode<kPrefix>(a, prefix, n_groups, prefix_rows(a.seqs.rows, n_groups), s);
+    if (e == hipSuccess) e = launch_mode<kOwn>(a, own, a.seqs.n_seq, max_new, s);
+    return e;
 }
 
 }  // namespace lacache

@@ -2,5 +2,5 @@
 #include "attend_wide.hpp"
 
 namespace lacache {
-template hipError_t launch_attend<128>(const AttendArgs&, const AttendPlan&, hipStream_t);
+template hipError_t launch_attend<128, kWhole>(const AttendArgs&, const AttendPlan&, hipStream_t);
 }  // namespace lacache

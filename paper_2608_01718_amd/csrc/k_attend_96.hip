@@ -2,5 +2,5 @@
 #include "attend_wide.hpp"
 
 namespace lacache {
-template hipError_t launch_attend<96>(const AttendArgs&, const AttendPlan&, hipStream_t);
+template hipError_t launch_attend<96, kWhole>(const AttendArgs&, const AttendPlan&, hipStream_t);
 }  // namespace lacache

@@ -1,0 +1,7 @@
+// k_attend_shared_128.hip -- the attention kernels of batches that share prefixes, heads padded to 128 columns.
+#include "attend_wide.hpp"
+
+namespace lacache {
+template hipError_t launch_attend<128, kPrefix>(const AttendArgs&, const AttendPlan&, hipStream_t);
+template hipError_t launch_attend<128, kOwn>(const AttendArgs&, const AttendPlan&, hipStream_t);
+}  // namespace lacache

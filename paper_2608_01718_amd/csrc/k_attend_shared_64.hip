@@ -1,0 +1,7 @@
+// k_attend_shared_64.hip -- the attention kernels of batches that share prefixes, heads padded to 64 columns.
+#include "attend_wide.hpp"
+
+namespace lacache {
+template hipError_t launch_attend<64, kPrefix>(const AttendArgs&, const AttendPlan&, hipStream_t);
+template hipError_t launch_attend<64, kOwn>(const AttendArgs&, const AttendPlan&, hipStream_t);
+}  // namespace lacache

@@ -1,0 +1,7 @@
+// k_attend_shared_96.hip -- the attention kernels of batches that share prefixes, heads padded to 96 columns.
+#include "attend_wide.hpp"
+
+namespace lacache {
+template hipError_t launch_attend<96, kPrefix>(const AttendArgs&, const AttendPlan&, hipStream_t);
+template hipError_t launch_attend<96, kOwn>(const AttendArgs&, const AttendPlan&, hipStream_t);
+}  // namespace lacache

@@ -249,6 +249,12 @@ bool attend_fits(const KvPool& pool, int dtype, int64_t rows, int n_seq, int gro
 int64_t attend_workspace(const KvPool& pool, int dtype, int q_heads, int max_new, int num_cu);
 hipError_t launch_kv_attend(const AttendArgs& a, int max_new, void* workspace, int num_cu, hipStream_t s);
 
+// Attention of sequences of which groups share their first tokens (lacache_prefixes).
+bool attend_shared_fits(const KvPool& pool, int dtype, int64_t rows, int n_groups, int group);
+int64_t attend_shared_workspace(const KvPool& pool, int dtype, int64_t rows, int n_seq, int n_groups, int q_heads, int max_new,
+                                int num_cu);
+hipError_t launch_kv_attend_shared(const AttendArgs& a, const int32_t* group, const int32_t* len, int n_groups, int max_new,
+                                   void* workspace, int num_cu, hipStream_t s);
 
 // Bounds of the pages of a pool (lacache_kv_bounds): [pages][heads][2][dp] codes, [pages][heads] scales.
 struct KvBounds {
