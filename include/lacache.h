@@ -270,7 +270,7 @@ int lacache_accept_length(const void *logits, lacache_dtype dtype, int32_t V, co
  *                 one) is greedy: a draft is taken if its logit is one of the
  *                 largest, the next token is the first of the largest; its rows of
  *                 draft_logits are not read
- *   1 <= V, 0 <= B <= 65535, 0 <= k <= 4096
+ *   1 <= V, 0 <= B <= 65535, 0 <= k <= 4096, B (V / 2048 + 1) below 2^24
  * Outputs: accept_len [B], next_token [B] int32, p_target and p_draft [B][k] the
  * p_j(x_j) and q_j(x_j) in float32 (a greedy sequence's: 1 or 0, and 1; those from
  * n_draft[b] on: 0).  accept_len and next_token are those of 64-bit arithmetic.
@@ -621,9 +621,9 @@ int lacache_kv_bounds_read(const lacache_kv *kv, const lacache_bounds *bounds, c
  * them if there are fewer.  The score of page i for kv head h is the largest over
  * h's query heads g of
  *     ((float) (c+ . code[0] + c- . code[1]) * scale) * unit
- * rounded step by step to float32, where unit = max |q_g| / 127 and c = q_g / unit
- * rounded to the nearest whole number (all in float32), c+ and c- its positive and
- * its negative columns: to the roundings of q_g and of the bounds a bound of
+ * rounded step by step to float32, where unit = max |q_g| (1 / 127) and c = q_g /
+ * unit, at most 127, rounded to the nearest whole number (in float32, 1 / 127 too),
+ * c+ and c- its positive and its negative columns: to the roundings of q_g and of the bounds a bound of
  * q_g . k over the page (so scale > 0 in the attention that follows).  NaN counts
  * as the largest of numbers; of equal pages the first ones are taken.  The first
  * `first` pages of a table and the `last` newest ones of a row are taken before

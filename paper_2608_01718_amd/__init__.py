@@ -546,7 +546,8 @@ def _capturing(index: int, stream) -> bool:
 
 
 def _given(t: torch.Tensor, shape, dtype, index: int, name: str) -> torch.Tensor:
-    if t.dtype != dtype or t.get_device() != index or t.shape != torch.Size(shape) or not t.is_contiguous():
+    if t.dtype != dtype or t.get_device() != index or t.shape != (shape if type(shape) is torch.Size else torch.Size(shape)) or \
+            not t.is_contiguous():
         raise ValueError(f"{name}: expected a contiguous {list(shape)} {dtype} tensor on cuda:{index}")
     return t
 
@@ -1025,13 +1026,16 @@ def lacache_verify_workspace(V: int, B: int, k: int) -> int:
     return n
 
 
-def _logits(t, rows: int, V: int, like, name: str):
+def _logits(t, shape, dtype, index: int, name: str):
     """The strides of [B, rows, V] logits whose rows are each contiguous."""
-    if t.dtype != like.dtype or t.device != like.device or tuple(t.shape) != (like.shape[0], rows, V) or \
-            (V > 1 and t.numel() and t.stride(2) != 1):
-        raise ValueError(f"{name}: expected [{like.shape[0]}, {rows}, {V}] {like.dtype} on {like.device} with contiguous "
-                         f"rows, got {tuple(t.shape)} {t.dtype} on {t.device} with strides {t.stride()}")
-    return t.stride(0), t.stride(1)
+    stride = t.stride()
+    if t.dtype != dtype or t.get_device() != index or t.shape != shape or (shape[2] > 1 and t.numel() and stride[2] != 1):
+        raise ValueError(f"{name}: expected {list(shape)} {dtype} on cuda:{index} with contiguous rows, got {tuple(t.shape)} "
+                         f"{t.dtype} on {t.device} with strides {stride}")
+    return stride[0], stride[1]
+
+
+_verify_need = {}  # bytes of scratch by (V, B, k)
 
 
 def lacache_verify(logits, draft_logits, draft_tokens, u_accept, u_next, temperature=None, n_draft=None, out=None,
@@ -1040,38 +1044,46 @@ def lacache_verify(logits, draft_logits, draft_tokens, u_accept, u_next, tempera
     the draft model (float32 or bfloat16, rows contiguous), draft_tokens [B, k] int32, u_accept [B, k] and u_next [B]
     float32 random numbers from [0, 1), temperature [B] float32 (1 where it is not given; 0 is greedy), n_draft [B] int32
     (k where it is not given).  Returns (accept_len [B] int32, next_token [B] int32, p_target [B, k], p_draft [B, k])."""
-    kind = _ROW_DTYPES.get(logits.dtype)
-    if logits.dim() != 3 or logits.device.type != "cuda" or kind is None or logits.shape[1] < 1:
+    dtype, shape, index = logits.dtype, logits.shape, logits.get_device()
+    kind = _ROW_DTYPES.get(dtype)
+    if len(shape) != 3 or index < 0 or kind is None or shape[1] < 1:
         raise ValueError("logits: expected a float32 or bfloat16 [B, k + 1, V] tensor on a GPU")
-    B, k, V, index = logits.shape[0], logits.shape[1] - 1, logits.shape[2], logits.get_device()
-    t_seq, t_row = _logits(logits, k + 1, V, logits, "logits")
-    d_seq, d_row = _logits(draft_logits, k, V, logits, "draft_logits")
-    _given(draft_tokens, (B, k), torch.int32, index, "draft_tokens")
-    _given(u_accept, (B, k), torch.float32, index, "u_accept")
-    _given(u_next, (B,), torch.float32, index, "u_next")
+    B, k, V = shape[0], shape[1] - 1, shape[2]
+    per_draft, per_seq = torch.Size((B, k)), torch.Size((B,))
+    t_seq, t_row = _logits(logits, shape, dtype, index, "logits")
+    d_seq, d_row = _logits(draft_logits, torch.Size((B, k, V)), dtype, index, "draft_logits")
+    _given(draft_tokens, per_draft, torch.int32, index, "draft_tokens")
+    _given(u_accept, per_draft, torch.float32, index, "u_accept")
+    _given(u_next, per_seq, torch.float32, index, "u_next")
     if temperature is not None:
-        _given(temperature, (B,), torch.float32, index, "temperature")
+        _given(temperature, per_seq, torch.float32, index, "temperature")
     if n_draft is not None:
-        _given(n_draft, (B,), torch.int32, index, "n_draft")
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in
-                                       (logits, draft_logits, u_accept, u_next, temperature, *(out or ()))):
-        raise _no_gradient("lacache_verify")
-    shapes = (((B,), torch.int32, "accept_len"), ((B,), torch.int32, "next_token"), ((B, k), torch.float32, "p_target"),
-              ((B, k), torch.float32, "p_draft"))
+        _given(n_draft, per_seq, torch.int32, index, "n_draft")
     given = out is not None
+    if torch.is_grad_enabled() and (logits.requires_grad or draft_logits.requires_grad or u_accept.requires_grad or
+                                    u_next.requires_grad or (temperature is not None and temperature.requires_grad) or
+                                    (given and any(t.requires_grad for t in out))):
+        raise _no_gradient("lacache_verify")
     if given:
-        for t, (shape, dtype, name) in zip(out, shapes, strict=True):
-            _given(t, shape, dtype, index, name)
-    else:
-        out = tuple(_made(logits, shape, dtype, stream) for shape, dtype, _ in shapes)
-    space = _made(logits, (lacache_verify_workspace(V, B, k),), torch.uint8, stream)
+        for t, s, kind_of, name in zip(out, (per_seq, per_seq, per_draft, per_draft),
+                                       (torch.int32, torch.int32, torch.float32, torch.float32),
+                                       ("accept_len", "next_token", "p_target", "p_draft"), strict=True):
+            _given(t, s, kind_of, index, name)
+        out = tuple(out)
+    else:  # (two allocations, not four)
+        out = _made(logits, (2, B), torch.int32, stream).unbind(0) + _made(logits, (2, B, k), torch.float32, stream).unbind(0)
+    need = _verify_need.get((V, B, k))
+    if need is None:
+        need = _verify_need[V, B, k] = lacache_verify_workspace(V, B, k)
+    space = _made(logits, (need,), torch.uint8, stream)
     _check(_on(index, stream, _lib.lacache_verify, logits.data_ptr(), draft_logits.data_ptr(), kind, V, t_seq, t_row, d_seq,
                d_row, draft_tokens.data_ptr(), u_accept.data_ptr(), u_next.data_ptr(),
                None if temperature is None else temperature.data_ptr(), None if n_draft is None else n_draft.data_ptr(), B, k,
-               *(t.data_ptr() for t in out), space.data_ptr(), space.numel()), "lacache_verify")
+               out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), out[3].data_ptr(), space.data_ptr(), need),
+           "lacache_verify")
     if given:
         _written(out)
-    return tuple(out)
+    return out
 
 
 def raw_library() -> ctypes.CDLL:

@@ -302,7 +302,7 @@ int lacache_verify(const void* logits, const void* draft_logits, lacache_dtype d
                    int32_t* accept_len, int32_t* next_token, float* p_target, float* p_draft, void* workspace,
                    int64_t workspace_bytes, void* stream) {
     if (!is_dtype(dtype) || V < 1 || B < 0 || B > 65535 || k < 0 || k > 4096 || t_seq < 0 || t_row < 0 || d_seq < 0 ||
-        d_row < 0 || workspace_bytes < 0)
+        d_row < 0 || workspace_bytes < 0 || (int64_t)B * (V / 2048 + 1) >= 1 << 24)
         return LACACHE_EINVAL;
     if (B == 0) return LACACHE_OK;
     const uintptr_t esz = dtype == LACACHE_F32 ? 4 : 2;

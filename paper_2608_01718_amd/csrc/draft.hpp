@@ -24,12 +24,11 @@ struct DraftArgs {
     // the workspace
     float2* stats;    // [B (2 k + 1)][chunks] maxima and sums
     int chunks;
-    int64_t wide;     // logits of a chunk of the row that follows
-    int wides;
-    double2* sums;    // [B][wides] of both models
-    double* rest;     // [B][wides] of r
+    int pieces;       // of the row that follows
+    double2* sums;    // [B][pieces] of both models
+    double* rest;     // [B][pieces] of r
     DraftRow* rows;   // [B]
-    uint32_t* done;   // [B] workgroups of k_draft_pick that are through
+    uint32_t* done;   // [B] workgroups of k_draft_rest that are through, where they find the token
 };
 
 int64_t draft_workspace(int V, int B, int k);

@@ -4,12 +4,14 @@
 //   next token is the first v with r(0) + .. + r(v) > u sum r, r = max(0, p - q) of row n (p itself behind the last draft)
 //
 // How many drafts are taken and which token comes next are whole numbers, so both are what 64 bits give:
-//   1. k_draft_stats reads all rows once: a workgroup takes a chunk of a row into registers and writes its maximum and its
-//      sum of exponentials in float32.  This is the launch that the memory bounds.
-//   2. k_draft_sums takes the drafts.  With numerators in 64 bits the relative error of p and q is that of the sums alone
+//   1. k_draft_stats reads all rows once: a wave takes a chunk of a row into registers and writes its maximum and its sum of
+//      exponentials in float32.  This is the launch that the memory bounds.
+//   2. k_draft_accept takes the drafts.  With numerators in 64 bits the relative error of p and q is that of the sums alone
 //      (kSumError), so a comparison that is closer than that is done again with sums in 64 bits; about one in 50,000 is.
-//      Then it adds up row n of both models in 64 bits.
-//   3. k_draft_pick adds up r by chunks, and the last workgroup of a sequence finds the chunk and in it the token.
+//   3. k_draft_sums adds up row n of both models in 64 bits, a wave a piece, k_draft_rest r.  Exponentials bound them.
+//   4. k_draft_pick finds a sequence's piece and in it the token.
+// Where there are few pieces launches are most of the time: then every workgroup of k_draft_sums finds out by itself how many
+// drafts are taken, and the last workgroup of a sequence in k_draft_rest finds the token (TOGETHER; TIMED).
 #include "common.hpp"
 #include "draft.hpp"
 #include "launch.hpp"
@@ -19,12 +21,13 @@ namespace lacache {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kAccept = 512;    // threads of k_draft_accept
 constexpr int kPositions = 64;  // looked at together
 
 // Relative error of a chunked float32 sum S = sum 2^t, t = (x - m) c <= 0.  An exponent's three roundings (c, the
-// difference, the product) move 2^t by 3 |t| 2^-24 ln 2, the exponential is within 2^-22, adding up 32 of a thread in
-// pairs and 256 threads in a tree are 13 roundings.  The mean of |t| under the weights is below log2 V + 2 (their entropy
-// and the maximum's share), 33 for 2^31 logits: 33 * 1.24e-7 + 2.4e-7 + 13 * 6e-8 = 5.1e-6 for S, twice that for S_p / S_q.
+// difference, the product) move 2^t by 3 |t| 2^-24 ln 2, the exponential is within 2^-22, adding up 32 of a lane in
+// pairs and 64 lanes in a tree are 12 roundings.  The mean of |t| under the weights is below log2 V + 2 (their entropy
+// and the maximum's share), 33 for 2^31 logits: 33 * 1.24e-7 + 2.4e-7 + 12 * 6e-8 = 5.1e-6 for S, twice that for S_p / S_q.
 constexpr double kSumError = 0x1p-16;
 
 // 2^t for t <= 0: 2^n e^(f ln 2), |f| <= 1/2, by the exponential's series up to the 11th power (the 12th: 0.3466^12 / 12! =
@@ -48,6 +51,27 @@ __device__ __forceinline__ double exp2_64(double t) {
 }
 constexpr double kLog2e64 = 1.44269504088896340736;
 
+// 2^t for t <= 0 where many are needed: 2^f, |f| <= 1/2, by the polynomial of degree 9 that is exact at the zeros of the
+// Chebyshev polynomial of degree 10 (2e-14 of 2^f), times 2^n by adding to its exponent; adding 1.5 2^52 leaves n in the low
+// bits.  Below 2^-1021 it stays there: kNothing.  (Exponentials of 16.4M logits, both models of 64 sequences: k_draft_sums
+// TIMED with the series above.)
+__device__ __forceinline__ double exp2_many(double t) {
+    t = fmax(t, -1021.0);
+    const double z = t + 0x1.8p52, f = t - (z - 0x1.8p52);
+    double y = 1.0205905413765595e-07;
+    y = __builtin_fma(y, f, 1.325964524488711e-06);
+    y = __builtin_fma(y, f, 1.5252672924850737e-05);
+    y = __builtin_fma(y, f, 0.0001540343375125101);
+    y = __builtin_fma(y, f, 0.0013333558200794592);
+    y = __builtin_fma(y, f, 0.009618129193934313);
+    y = __builtin_fma(y, f, 0.05550410866465167);
+    y = __builtin_fma(y, f, 0.2402265069564034);
+    y = __builtin_fma(y, f, 0.6931471805599462);
+    y = __builtin_fma(y, f, 1.0000000000000135);
+    return __longlong_as_double(__double_as_longlong(y) + ((long long)(uint32_t)__double_as_longlong(z) << 52));
+}
+constexpr double kNothing = 0x1p-1000;  // weights up to this count as none
+
 // A sequence's temperature: log2 e / T, and whether it is greedy (T not in 2^-60 .. 2^60).
 struct Heat {
     double c;
@@ -63,30 +87,46 @@ __device__ __forceinline__ int drafts_of(const DraftArgs& a, int b) {
     return n < 0 ? 0 : n > a.k ? a.k : n;
 }
 
-// Logits v .. v + 7 of a row (rows begin at any element), -infinity from V on.
-__device__ __forceinline__ void logits8(const char* row, int dtype, int V, int64_t v, float (&x)[8]) {
+// NV times eight logits of a row (rows begin at any element), from v on and `step` apart, -infinity from V on.  ONCE: they are
+// not read again.  inside: all of the wave's are there (its loads are then issued together: 4096 rows of 32,000 bfloat16
+// logits TIMED).
+template <bool F32, int NV, bool ONCE>
+__device__ __forceinline__ void logits8(const char* row, int V, int64_t v, int64_t step, bool inside, float (&x)[NV][8]) {
     typedef u32x4 any2 __attribute__((aligned(2)));
     typedef f32x4 any4 __attribute__((aligned(4)));
-    if (v + 8 <= V) {
-        if (dtype == 0) {
-            const f32x4 p = __builtin_nontemporal_load((const any4*)(row + v * 4)),
-                        q = __builtin_nontemporal_load((const any4*)(row + v * 4 + 16));
+    auto eight = [&](int64_t at, float (&y)[8]) {
+        if constexpr (F32) {
+            const any4 *p = (const any4*)(row + at * 4), *q = (const any4*)(row + at * 4 + 16);
+            const f32x4 lo = ONCE ? __builtin_nontemporal_load(p) : *p, hi = ONCE ? __builtin_nontemporal_load(q) : *q;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = p[e], x[4 + e] = q[e];
+            for (int e = 0; e < 4; ++e) y[e] = lo[e], y[4 + e] = hi[e];
         } else {
-            const u32x4 w = __builtin_nontemporal_load((const any2*)(row + v * 2));
+            const any2* p = (const any2*)(row + at * 2);
+            const u32x4 w = ONCE ? __builtin_nontemporal_load(p) : *p;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                x[2 * e] = __uint_as_float(w[e] << 16);
-                x[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+                y[2 * e] = __uint_as_float(w[e] << 16);
+                y[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
             }
         }
-    } else {
+    };
+    if (inside) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            x[e] = v + e >= V     ? -__builtin_inff()
-                   : dtype == 0 ? ((const float*)row)[v + e]
-                                : bf16_to_f32(((const uint16_t*)row)[v + e]);
+        for (int i = 0; i < NV; ++i) eight(v + i * step, x[i]);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int64_t at = v + i * step;
+        if (at + 8 <= V) {
+            eight(at, x[i]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                x[i][e] = at + e >= V ? -__builtin_inff()
+                          : F32       ? ((const float*)row)[at + e]
+                                      : bf16_to_f32(((const uint16_t*)row)[at + e]);
+        }
     }
 }
 __device__ __forceinline__ float logit(const char* row, int dtype, int64_t v) {
@@ -101,15 +141,15 @@ __device__ __forceinline__ int64_t stat_row(const DraftArgs& a, int b, int j, bo
     return (int64_t)b * (2 * a.k + 1) + (draft ? a.k + 1 + j : j);
 }
 
-template <class T, class Op>
-__device__ __forceinline__ T all_threads(T x, T (&lds)[kThreads / 64], Op op) {
+template <int THREADS, class T, class Op>
+__device__ __forceinline__ T all_threads(T x, T (&lds)[THREADS / 64], Op op) {
     x = wave_reduce(x, op);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
     __syncthreads();
     x = lds[0];
 #pragma unroll
-    for (int w = 1; w < kThreads / 64; ++w) x = op(x, lds[w]);
+    for (int w = 1; w < THREADS / 64; ++w) x = op(x, lds[w]);
     return x;
 }
 
@@ -121,9 +161,10 @@ struct Stat {
 };
 __device__ __forceinline__ Stat join_chunks(const DraftArgs& a, int64_t row, double c) {
     const float2* part = a.stats + row * a.chunks;
+    auto max2 = [](float x, float y) { return fmaxf(x, y); };
+    auto add2 = [](double x, double y) { return x + y; };
     float m = -__builtin_inff();
     for (int i = threadIdx.x & 15; i < a.chunks; i += 16) m = fmaxf(m, part[i].x);
-    auto max2 = [](float x, float y) { return fmaxf(x, y); };
     m = xor_combine<1>(xor_combine<2>(xor_combine<4>(xor_combine<8>(m, max2), max2), max2), max2);
     double s = 0.0;
     const bool fine = m < __builtin_inff() && m > -__builtin_inff();
@@ -131,51 +172,45 @@ __device__ __forceinline__ Stat join_chunks(const DraftArgs& a, int64_t row, dou
         const float2 x = part[i];
         s += x.y * (fine && x.x > -__builtin_inff() ? exp2_64(((double)x.x - m) * c) : 1.0);
     }
-    auto add2 = [](double x, double y) { return x + y; };
     s = xor_combine<1>(xor_combine<2>(xor_combine<4>(xor_combine<8>(s, add2), add2), add2), add2);
     return {m, fine && s > 0.0 && s < __builtin_inf() ? s : 0.0};
 }
 
 }  // namespace
 
-// A workgroup a chunk of NV x 2048 logits of a row.
-template <int NV>
+// A wave a chunk of NV x 512 logits of a row.
+template <int NV, bool F32>
 __global__ __launch_bounds__(kThreads) void k_draft_stats(DraftArgs a) {
-    __shared__ float lds[kThreads / 64], lds2[kThreads / 64];
-    const int tid = threadIdx.x;
-    const int64_t rows = (int64_t)a.B * (2 * a.k + 1);
-    for (int64_t item = blockIdx.x; item < rows * a.chunks; item += gridDim.x) {
-        const int64_t row = item / a.chunks;
-        const int chunk = (int)(item - row * a.chunks);
-        const int b = (int)(row / (2 * a.k + 1)), i = (int)(row - (int64_t)b * (2 * a.k + 1));
+    const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t each = 2 * (uint32_t)a.k + 1;
+    const int64_t items = (int64_t)a.B * each * a.chunks;
+    for (int64_t item = (int64_t)blockIdx.x * (kThreads / 64) + wid; item < items; item += (int64_t)gridDim.x * (kThreads / 64)) {
+        int64_t row;
+        int chunk, b, i;
+        if (items <= UINT32_MAX) {  // (divisions in 32 bits where that is enough)
+            const uint32_t r = (uint32_t)item / (uint32_t)a.chunks;
+            chunk = (int)((uint32_t)item - r * (uint32_t)a.chunks);
+            b = (int)(r / each), i = (int)(r - (uint32_t)b * each), row = r;
+        } else {
+            row = item / a.chunks;
+            chunk = (int)(item - row * a.chunks);
+            b = (int)(row / each), i = (int)(row - (int64_t)b * each);
+        }
         const bool draft = i > a.k;
         const int j = draft ? i - a.k - 1 : i, n = drafts_of(a, b);
         const Heat heat = heat_of(a, b);
-        if (tid == 0 && chunk == 0 && i == 0) a.done[b] = 0;
+        if (chunk == 0 && i == 0 && lane == 0) a.done[b] = 0;
         if (draft ? (j >= n || heat.greedy) : j > n) continue;
         const char* at = row_of(a, b, j, draft);
-        const int64_t v0 = (int64_t)chunk * (NV * 8 * kThreads);
+        const int64_t v0 = (int64_t)chunk * (NV * 512);
         float x[NV][8];
-#pragma unroll
-        for (int u = 0; u < NV; ++u) {
-            const int64_t v = v0 + (u * kThreads + tid) * 8;
-            if (v < a.V) {
-                logits8(at, a.dtype, a.V, v, x[u]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[u][e] = -__builtin_inff();
-            }
-        }
+        logits8<F32, NV, true>(at, a.V, v0 + lane * 8, 512, v0 + NV * 512 <= a.V, x);
         float m = -__builtin_inff();
-        float nan = 0.0f;  // (the maximum leaves NaN out)
 #pragma unroll
         for (int u = 0; u < NV; ++u)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                m = fmaxf(m, x[u][e]);
-                nan = x[u][e] == x[u][e] ? nan : x[u][e];
-            }
-        m = all_threads(m, lds, [](float p, float q) { return fmaxf(p, q); });
+            for (int e = 0; e < 8; ++e) m = fmaxf(m, x[u][e]);  // (leaves NaN out: the sum has it)
+        m = wave_reduce(m, [](float p, float q) { return fmaxf(p, q); });
         const float base = m > -__builtin_inff() ? m : 0.0f, c = (float)heat.c;
         float s = 0.0f;
 #pragma unroll
@@ -185,61 +220,68 @@ __global__ __launch_bounds__(kThreads) void k_draft_stats(DraftArgs a) {
             for (int e = 0; e < 8; ++e) y[e] = __builtin_amdgcn_exp2f((x[u][e] - base) * c);
             s += ((y[0] + y[1]) + (y[2] + y[3])) + ((y[4] + y[5]) + (y[6] + y[7]));
         }
-        s = all_threads(s + nan, lds2, [](float p, float q) { return p + q; });
-        if (tid == 0) a.stats[row * a.chunks + chunk] = make_float2(m, s);
+        s = wave_sum_f32(s);
+        if (lane == 0) a.stats[row * a.chunks + chunk] = make_float2(m, s);
     }
 }
 
 namespace {
 
 // The sum of a whole row in 64 bits, by all threads.
-__device__ double row_sum(const DraftArgs& a, const char* row, float m, double c, double (&lds)[kThreads / 64]) {
+template <bool F32, int THREADS>
+__device__ double row_sum(const DraftArgs& a, const char* row, float m, double c, double (&lds)[THREADS / 64]) {
     double s = 0.0;
-    for (int64_t v = threadIdx.x * 8; v < a.V; v += kThreads * 8) {
-        float x[8];
-        logits8(row, a.dtype, a.V, v, x);
+    for (int64_t v = threadIdx.x * 8; v < a.V; v += THREADS * 8) {
+        float x[1][8];
+        logits8<F32, 1, false>(row, a.V, v, 0, false, x);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s += exp2_64(((double)x[e] - m) * c);
+        for (int e = 0; e < 8; ++e) s += exp2_64(((double)x[0][e] - m) * c);
     }
-    return all_threads(s, lds, [](double p, double q) { return p + q; });
+    return all_threads<THREADS>(s, lds, [](double p, double q) { return p + q; });
 }
 
-}  // namespace
-
-// Workgroup b wides + w: how many drafts of sequence b are taken (every workgroup of b finds out, the first writes it down), and the
-// w-th chunks of row n of both models in 64 bits.
-__global__ __launch_bounds__(kThreads) void k_draft_sums(DraftArgs a) {
-    __shared__ float max_of[2][kPositions];
-    __shared__ double sum_of[2][kPositions], lds[kThreads / 64];
+// How many drafts of sequence b are taken, by a workgroup; writes: whether it writes the results down.
+template <bool F32, int THREADS>
+__device__ __forceinline__ DraftRow accept(const DraftArgs& a, int b, const Heat& heat, bool writes) {
+    __shared__ float max_of[2][kPositions + 1];
+    __shared__ double sum_of[2][kPositions + 1], lds[THREADS / 64];
     __shared__ uint64_t flags[2];  // the positions that are not taken, and those that are too close
-    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
-    const int b = blockIdx.x / a.wides, w = blockIdx.x % a.wides, n = drafts_of(a, b);
-    const Heat heat = heat_of(a, b);
+    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, n = drafts_of(a, b);
     int taken = n;
-    for (int j0 = 0; j0 < n; j0 += kPositions) {
-        const int here = n - j0 < kPositions ? n - j0 : kPositions;
+    DraftRow row{};
+    // positions j0 .. j0 + here - 1, and row n too with the last of them
+    for (int j0 = 0; j0 <= n; j0 += kPositions) {
+        const int here = n - j0 < kPositions ? n - j0 : kPositions, rows = n - j0 < kPositions ? here + 1 : here;
+        // the drafts' own logits are on their way while the rows' sums are put together
+        const int j = j0 + lane;
+        int t = -1;
+        float u = 0.0f, xp = 0.0f, xq = 0.0f;
+        if (wid == 0 && lane < here) {
+            t = a.tokens[(int64_t)b * a.k + j];
+            u = a.u_accept[(int64_t)b * a.k + j];
+            if (t >= 0 && t < a.V) {
+                xp = logit(row_of(a, b, j, false), a.dtype, t);
+                if (!heat.greedy) xq = logit(row_of(a, b, j, true), a.dtype, t);
+            }
+        }
         __syncthreads();
-        for (int i = tid >> 4; i < 2 * here; i += kThreads / 16) {
-            const bool draft = i >= here;
-            const int j = draft ? i - here : i;
+        for (int i = tid >> 4; i < rows + here; i += THREADS / 16) {
+            const bool draft = i >= rows;
+            const int at = draft ? i - rows : i;
             Stat s{0.0f, 0.0};
-            if (!(draft && heat.greedy)) s = join_chunks(a, stat_row(a, b, j0 + j, draft), heat.c);
-            if ((tid & 15) == 0) max_of[draft][j] = s.m, sum_of[draft][j] = s.s;
+            if (!(draft && heat.greedy)) s = join_chunks(a, stat_row(a, b, j0 + at, draft), heat.c);
+            if ((tid & 15) == 0) max_of[draft][at] = s.m, sum_of[draft][at] = s.s;
         }
         __syncthreads();
         double pn = 0.0, qn = 0.0;  // numerators of p and q
-        float u = 0.0f;
         if (wid == 0) {
             bool no = false, close = false;
             if (lane < here) {
-                const int j = j0 + lane, t = a.tokens[(int64_t)b * a.k + j];
-                u = a.u_accept[(int64_t)b * a.k + j];
                 const bool there = t >= 0 && t < a.V;
                 const double sp = sum_of[0][lane], sq = sum_of[1][lane];
                 float p = 0.0f, q = 0.0f;
                 if (there && sp > 0.0) {
-                    const float x = logit(row_of(a, b, j, false), a.dtype, t);
-                    pn = heat.greedy ? (x == max_of[0][lane] ? 1.0 : 0.0) : exp2_64(((double)x - max_of[0][lane]) * heat.c);
+                    pn = heat.greedy ? (xp == max_of[0][lane] ? 1.0 : 0.0) : exp2_64(((double)xp - max_of[0][lane]) * heat.c);
                     p = (float)(heat.greedy ? pn : pn / sp);
                 }
                 if (heat.greedy) {
@@ -247,8 +289,7 @@ __global__ __launch_bounds__(kThreads) void k_draft_sums(DraftArgs a) {
                     no = pn == 0.0;
                 } else if (sp > 0.0 && sq > 0.0) {
                     if (there) {
-                        const float x = logit(row_of(a, b, j, true), a.dtype, t);
-                        qn = exp2_64(((double)x - max_of[1][lane]) * heat.c);
+                        qn = exp2_64(((double)xq - max_of[1][lane]) * heat.c);
                         q = (float)(qn / sq);
                     }
                     const double l = u * (qn / sq), r = pn / sp;
@@ -257,7 +298,7 @@ __global__ __launch_bounds__(kThreads) void k_draft_sums(DraftArgs a) {
                 } else {
                     no = true;
                 }
-                if (w == 0) {
+                if (writes) {
                     a.p_target[(int64_t)b * a.k + j] = p;
                     a.p_draft[(int64_t)b * a.k + j] = q;
                 }
@@ -266,13 +307,14 @@ __global__ __launch_bounds__(kThreads) void k_draft_sums(DraftArgs a) {
             if (lane == 0) flags[0] = n0, flags[1] = n1;
         }
         __syncthreads();
-        if (taken == n) {
+        const bool open = taken == n;
+        if (open) {
             uint64_t no = flags[0], close = flags[1];
             while (no | close) {
                 const int at = __ffsll((unsigned long long)(no | close)) - 1;
                 if (close >> at & 1) {
-                    const double sp = row_sum(a, row_of(a, b, j0 + at, false), max_of[0][at], heat.c, lds);
-                    const double sq = row_sum(a, row_of(a, b, j0 + at, true), max_of[1][at], heat.c, lds);
+                    const double sp = row_sum<F32, THREADS>(a, row_of(a, b, j0 + at, false), max_of[0][at], heat.c, lds);
+                    const double sq = row_sum<F32, THREADS>(a, row_of(a, b, j0 + at, true), max_of[1][at], heat.c, lds);
                     __syncthreads();
                     if (tid == at) flags[0] = u * (qn / sq) < pn / sp;  // (the lane that has this position's numerators)
                     __syncthreads();
@@ -285,251 +327,319 @@ __global__ __launch_bounds__(kThreads) void k_draft_sums(DraftArgs a) {
                 taken = j0 + at;
                 break;
             }
-        }
-        if (taken < n && w != 0) break;
-    }
-    if (w == 0) {
-        for (int j = n + tid; j < a.k; j += kThreads) a.p_target[(int64_t)b * a.k + j] = a.p_draft[(int64_t)b * a.k + j] = 0.0f;
-    }
-    // row `taken` of both
-    const Stat t = join_chunks(a, stat_row(a, b, taken, false), heat.c);
-    Stat d{0.0f, 0.0};
-    if (taken < n && !heat.greedy) d = join_chunks(a, stat_row(a, b, taken, true), heat.c);
-    if (w == 0 && tid == 0) {
-        a.accept_len[b] = taken;
-        a.rows[b] = DraftRow{taken, t.s > 0.0 ? 1 : 0, d.s > 0.0 ? 1 : 0, t.m, d.m};
-    }
-    if (heat.greedy) return;
-    double sp = 0.0, sq = 0.0;
-    const int64_t end = (int64_t)(w + 1) * a.wide < a.V ? (int64_t)(w + 1) * a.wide : a.V;
-    const char *rt = row_of(a, b, taken, false), *rd = d.s > 0.0 ? row_of(a, b, taken, true) : nullptr;
-    for (int64_t v = (int64_t)w * a.wide + tid * 8; v < end; v += kThreads * 8) {
-        float x[8], y[8];
-        logits8(rt, a.dtype, a.V, v, x);
-        if (rd) logits8(rd, a.dtype, a.V, v, y);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sp += exp2_64(((double)x[e] - t.m) * heat.c);
-        if (rd) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sq += exp2_64(((double)y[e] - d.m) * heat.c);
+            if (taken - j0 < rows) {
+                const int at = taken - j0;
+                const bool has_q = taken < n && !heat.greedy && sum_of[1][at] > 0.0;
+                row = DraftRow{taken, sum_of[0][at] > 0.0 ? 1 : 0, has_q ? 1 : 0, max_of[0][at], has_q ? max_of[1][at] : 0.0f};
+            }
         }
     }
-    auto add2 = [](double p, double q) { return p + q; };
-    sp = all_threads(sp, lds, add2);
-    sq = all_threads(sq, lds, add2);
-    if (tid == 0) a.sums[(int64_t)b * a.wides + w] = make_double2(sp, sq);
+    if (writes) {
+        for (int j = n + tid; j < a.k; j += THREADS) a.p_target[(int64_t)b * a.k + j] = a.p_draft[(int64_t)b * a.k + j] = 0.0f;
+        if (tid == 0) {
+            a.accept_len[b] = taken;
+            a.rows[b] = row;
+        }
+    }
+    return row;
+}
+
+struct Add64 {
+    __device__ double operator()(double p, double q) const { return p + q; }
+};
+
+}  // namespace
+
+// Workgroup b: how many drafts of sequence b are taken.
+template <bool F32>
+__global__ __launch_bounds__(kAccept) void k_draft_accept(DraftArgs a) {
+    accept<F32, kAccept>(a, blockIdx.x, heat_of(a, blockIdx.x), true);
 }
 
 namespace {
 
-// r of eight logits
-struct Rest {
-    const char *rt, *rd;  // rd null: nothing is taken off
-    double mt, md, ft, fd, c;
-    __device__ __forceinline__ void at(const DraftArgs& a, int64_t v, double (&r)[8]) const {
-        float x[8];
-        logits8(rt, a.dtype, a.V, v, x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) r[e] = exp2_64(((double)x[e] - mt) * c) * ft;
-        if (rd) {
-            logits8(rd, a.dtype, a.V, v, x);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) r[e] = fmax(0.0, r[e] - exp2_64(((double)x[e] - md) * c) * fd);
-        }
-    }
+// The wave's piece: NV times 512 logits of row n of a sequence's.
+struct Piece {
+    int b, w;
+    bool live;
 };
-
-__device__ __forceinline__ double scan_wave(double x, int lane) {
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-        const double y = __shfl_up(x, o, 64);
-        if (lane >= o) x += y;
-    }
-    return x;
+__device__ __forceinline__ Piece piece_of(const DraftArgs& a) {
+    const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int groups = (a.pieces + kThreads / 64 - 1) / (kThreads / 64), b = (int)(blockIdx.x / (unsigned)groups);
+    const int w = (int)(blockIdx.x - (unsigned)b * groups) * (kThreads / 64) + wid;
+    return {b, w, w < a.pieces};
 }
 
 }  // namespace
 
-// Workgroup b wides + w: the sum of r over the w-th chunk; the last workgroup of b finds the token.
-__global__ __launch_bounds__(kThreads) void k_draft_pick(DraftArgs a) {
-    __shared__ double lds[kThreads / 64], before[kThreads / 64 + 1];
-    __shared__ int found, last;
-    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
-    const int b = blockIdx.x / a.wides, w = blockIdx.x % a.wides;
-    const Heat heat = heat_of(a, b);
-    const DraftRow row = a.rows[b];
-    if (!row.has_p) {
-        if (w == 0 && tid == 0) a.next_token[b] = -1;
-        return;
-    }
-    auto add2 = [](double p, double q) { return p + q; };
-    const char* rt = row_of(a, b, row.n, false);
-    const int64_t begin = (int64_t)w * a.wide, end = begin + a.wide < a.V ? begin + a.wide : a.V;
-    // the parts of a sum over all chunks: device-wide, since workgroups of one launch write and read them
-    auto put = [&](double x) {
-        __hip_atomic_store((uint64_t*)(a.rest + (int64_t)b * a.wides + w), (uint64_t)__double_as_longlong(x), __ATOMIC_RELAXED,
-                           __HIP_MEMORY_SCOPE_AGENT);
-    };
-    auto get = [&](int i) {
-        return __longlong_as_double((long long)__hip_atomic_load((const uint64_t*)(a.rest + (int64_t)b * a.wides + i),
-                                                                 __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-    };
-    auto is_last = [&]() {
-        last_workgroup_wait();
-        __syncthreads();
-        if (tid == 0)
-            last = __hip_atomic_fetch_add(a.done + b, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)a.wides - 1;
-        __syncthreads();
-        return last;
-    };
-    if (heat.greedy) {  // the first of the largest
-        int first = INT32_MAX;
-        for (int64_t v = begin + tid * 8; v < end; v += kThreads * 8) {
-            float x[8];
-            logits8(rt, a.dtype, a.V, v, x);
-#pragma unroll
-            for (int e = 7; e >= 0; --e) first = x[e] == row.mt && v + e < first ? (int)(v + e) : first;
-        }
-        auto min2 = [](double p, double q) { return fmin(p, q); };
-        const double f = all_threads((double)first, lds, min2);
-        if (tid == 0) put(f);
-        if (!is_last()) return;
-        double x = INT32_MAX;
-        for (int i = tid; i < a.wides; i += kThreads) x = fmin(x, get(i));
-        x = all_threads(x, lds, min2);
-        if (tid == 0) a.next_token[b] = (int)x;
-        return;
-    }
+// The sums over a piece of row n of both models in 64 bits.
+template <int NV, bool F32, bool TOGETHER>
+__global__ __launch_bounds__(kThreads) void k_draft_sums(DraftArgs a) {
+    const int lane = threadIdx.x & 63;
+    const Piece p = piece_of(a);
+    const Heat heat = heat_of(a, p.b);
+    DraftRow row;
+    if constexpr (TOGETHER) row = accept<F32, kThreads>(a, p.b, heat, p.w < kThreads / 64);
+    if (!p.live) return;
+    if constexpr (!TOGETHER) row = a.rows[p.b];
+    if (heat.greedy || !row.has_p) return;
+    const int64_t v0 = (int64_t)p.w * (NV * 512);
+    const bool inside = v0 + NV * 512 <= a.V;
+    float x[NV][8], y[NV][8];
+    logits8<F32, NV, false>(row_of(a, p.b, row.n, false), a.V, v0 + lane * 8, 512, inside, x);
+    if (row.has_q) logits8<F32, NV, false>(row_of(a, p.b, row.n, true), a.V, v0 + lane * 8, 512, inside, y);
     double sp = 0.0, sq = 0.0;
-    for (int i = tid; i < a.wides; i += kThreads) {
-        const double2 s = a.sums[(int64_t)b * a.wides + i];
-        sp += s.x, sq += s.y;
-    }
-    sp = all_threads(sp, lds, add2);
-    sq = all_threads(sq, lds, add2);
-    Rest rest{rt, row.has_q ? row_of(a, b, row.n, true) : nullptr, row.mt, row.md, 1.0 / sp, row.has_q ? 1.0 / sq : 0.0, heat.c};
-    double s = 0.0;
-    for (int64_t v = begin + tid * 8; v < end; v += kThreads * 8) {
-        double r[8];
-        rest.at(a, v, r);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s += r[e];
-    }
-    s = all_threads(s, lds, add2);
-    if (tid == 0) put(s);
-    if (!is_last()) return;
-
-    double all = 0.0;
-    for (int i = tid; i < a.wides; i += kThreads) all += get(i);
-    all = all_threads(all, lds, add2);
-    const bool none = rest.rd && !(all > 0x1p-30);  // p and q are the same: the token is drawn from p
-    if (none) rest.rd = nullptr;
-    auto part = [&](int i) { return none ? a.sums[(int64_t)b * a.wides + i].x * rest.ft : get(i); };
-    // Finds the first of `count` ordered parts that takes the running sum past `goal` (the last one above 0 if none does): a
-    // thread `each` of them, from tid * each on.  What lies before it is taken off goal.
-    auto find = [&](auto part_at, int64_t count, int64_t each, double& goal, bool whole) -> int64_t {
-        double own = 0.0;
-        for (int64_t i = tid * each; i < (tid + 1) * each && i < count; ++i) own += part_at(i);
-        double upto = scan_wave(own, lane);
-        __syncthreads();
-        if (lane == 63) lds[wid] = upto;
-        if (tid == 0) found = -1;
-        __syncthreads();
-        double lead = 0.0, total = 0.0;
-        for (int i = 0; i < kThreads / 64; ++i) {
-            lead += i < wid ? lds[i] : 0.0;
-            total += lds[i];
-        }
-        upto += lead;
-        const double target = whole ? goal * total : goal;  // (a share of the sum, or a sum)
-        const uint64_t past = __ballot(upto > target && own > 0.0), some = __ballot(own > 0.0);
-        __shared__ int wave_past[kThreads / 64], wave_some[kThreads / 64];
-        __syncthreads();
-        if (lane == 0) {
-            wave_past[wid] = past ? wid * 64 + __ffsll((unsigned long long)past) - 1 : -1;
-            wave_some[wid] = some ? wid * 64 + 63 - __clzll((long long)some) : -1;
-        }
-        __syncthreads();
-        int who = -1;
-        for (int i = kThreads / 64 - 1; i >= 0; --i) who = wave_past[i] >= 0 ? wave_past[i] : who;
-        const bool passes = who >= 0;
-        if (!passes)
-            for (int i = 0; i < kThreads / 64; ++i) who = wave_some[i] >= 0 ? wave_some[i] : who;
-        if (tid == who) {
-            double sum = upto - own;
-            int64_t at = -1;
-            for (int64_t i = tid * each; i < (tid + 1) * each && i < count; ++i) {
-                const double x = part_at(i);
-                if (x > 0.0) {
-                    at = i;
-                    before[0] = sum;
-                    if (passes && sum + x > target) break;
-                }
-                sum += x;
-            }
-            found = (int)at;
-            before[1] = target;
-        }
-        __syncthreads();
-        goal = before[1] - before[0];
-        return found;
-    };
-    double goal = a.u_next[b];
-    const int64_t chunk = find(part, a.wides, (a.wides + kThreads - 1) / kThreads, goal, true);
-    if (chunk < 0) {  // (a sum that is NaN)
-        if (tid == 0) a.next_token[b] = -1;
-        return;
-    }
-    const int64_t v0 = chunk * a.wide, count = a.V - v0 < a.wide ? a.V - v0 : a.wide;
-    auto one = [&](int64_t eight) {
-        double r[8], x = 0.0;
-        rest.at(a, v0 + eight * 8, r);
+    for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x += r[e];
-        return x;
-    };
-    const int64_t eights = (count + 7) / 8;
-    const int64_t eight = find(one, eights, (eights + kThreads - 1) / kThreads, goal, false);
-    if (tid == 0) {
-        int64_t token = -1;
-        if (eight >= 0) {
-            double r[8], sum = 0.0;
-            rest.at(a, v0 + eight * 8, r);
-            bool past = false;
+        for (int e = 0; e < 8; ++e) sp += exp2_many(((double)x[i][e] - row.mt) * heat.c);
+    if (row.has_q) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if (!past && r[e] > 0.0) {
-                    token = v0 + eight * 8 + e;
-                    past = sum + r[e] > goal;
-                }
-                sum += r[e];
-            }
-        }
-        a.next_token[b] = (int)token;
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sq += exp2_many(((double)y[i][e] - row.md) * heat.c);
     }
+    sp = wave_reduce(sp, Add64{});
+    sq = wave_reduce(sq, Add64{});
+    if (lane == 0) a.sums[(int64_t)p.b * a.pieces + p.w] = make_double2(sp, sq);
 }
 
 namespace {
 
-constexpr int64_t kSmall = 2048, kLarge = 8192;  // logits of a chunk of k_draft_stats
+// The sums of a sequence's pieces, by all lanes of a wave: their reciprocals.
+struct Scales {
+    double p, q;
+};
+__device__ __forceinline__ Scales scales_of(const DraftArgs& a, int b, bool has_q, int lane) {
+    double sp = 0.0, sq = 0.0;
+    for (int i = lane; i < a.pieces; i += 64) {
+        const double2 s = a.sums[(int64_t)b * a.pieces + i];
+        sp += s.x, sq += s.y;
+    }
+    sp = wave_reduce(sp, Add64{});
+    sq = wave_reduce(sq, Add64{});
+    return {1.0 / sp, has_q ? 1.0 / sq : 0.0};
+}
+__device__ __forceinline__ double rest_of(float x, float y, const DraftRow& row, const Scales& f, double c, bool with_q) {
+    const double r = exp2_many(((double)x - row.mt) * c) * f.p;
+    return with_q ? fmax(0.0, r - exp2_many(((double)y - row.md) * c) * f.q) : r;
+}
 
-int64_t chunk_of(int V, int64_t rows) { return rows * ((V + kLarge - 1) / kLarge) >= 1024 ? kLarge : kSmall; }
+}  // namespace
+
+namespace {
+
+// The token of sequence b, by a workgroup.  WIDE: r's sums were written in this launch, and are read device-wide.
+template <int NV, bool F32, bool WIDE>
+__device__ __forceinline__ void pick(const DraftArgs& a, int b, const Heat& heat, const DraftRow& row) {
+    __shared__ double lds[kThreads / 64], lead[2];
+    __shared__ int found[kThreads / 64][2], chosen;
+    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+    auto rest = [&](int i) {
+        const double* at = a.rest + (int64_t)b * a.pieces + i;
+        if (!WIDE) return *at;
+        return __longlong_as_double((long long)__hip_atomic_load((const uint64_t*)at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+    };
+    const double2* sums = a.sums + (int64_t)b * a.pieces;
+    if (heat.greedy) {
+        double least = INT32_MAX;
+        for (int i = tid; i < a.pieces; i += kThreads) least = fmin(least, rest(i));
+        least = all_threads<kThreads>(least, lds, [](double p, double q) { return fmin(p, q); });
+        if (tid == 0) a.next_token[b] = (int)least;
+        return;
+    }
+    // Finds the thread whose share `own` (in the order of threads) takes the running sum past `goal` (the last one with a
+    // share if none does), or past goal times all of it: who it is, the sum before it, the goal (in lead[1]).
+    auto find = [&](double own, double goal, bool whole, double& before) {
+        double upto = own;
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) {
+            const double y = __shfl_up(upto, o, 64);
+            if (lane >= o) upto += y;
+        }
+        __syncthreads();
+        if (lane == 63) lds[wid] = upto;
+        __syncthreads();
+        double total = 0.0, ahead = 0.0;
+#pragma unroll
+        for (int i = 0; i < kThreads / 64; ++i) {
+            ahead += i < wid ? lds[i] : 0.0;
+            total += lds[i];
+        }
+        upto += ahead;
+        if (whole) goal *= total;
+        const uint64_t past = __ballot(upto > goal && own > kNothing), some = __ballot(own > kNothing);
+        if (lane == 0) {
+            found[wid][0] = past ? wid * 64 + __ffsll((unsigned long long)past) - 1 : -1;
+            found[wid][1] = some ? wid * 64 + 63 - __clzll((long long)some) : -1;
+        }
+        __syncthreads();
+        int who = -1;
+#pragma unroll
+        for (int i = kThreads / 64 - 1; i >= 0; --i) who = found[i][0] >= 0 ? found[i][0] : who;
+        if (who < 0) {
+#pragma unroll
+            for (int i = 0; i < kThreads / 64; ++i) who = found[i][1] >= 0 ? found[i][1] : who;
+            goal = __builtin_inf();  // (its last one)
+        }
+        before = upto - own;
+        if (tid == who) lead[1] = goal;
+        return who;
+    };
+    const Scales f = scales_of(a, b, row.has_q, lane);
+    const int each = (a.pieces + kThreads - 1) / kThreads, first = tid * each;
+    const int end = first + each < a.pieces ? first + each : a.pieces;
+    double all = 0.0;
+    for (int i = first; i < end; ++i) all += rest(i);
+    bool with_q = row.has_q;
+    if (with_q && !(all_threads<kThreads>(all, lds, Add64{}) > 0x1p-30)) {  // p and q are the same: the token is drawn from p
+        with_q = false;
+        all = 0.0;
+        for (int i = first; i < end; ++i) all += sums[i].x;
+    }
+    const bool shares = row.has_q && !with_q;  // sums are S_p's, not r's
+    double before;
+    int who = find(all, (double)a.u_next[b], true, before);
+    if (who < 0) {
+        if (tid == 0) a.next_token[b] = -1;
+        return;
+    }
+    if (tid == who) {  // the piece among its own
+        int piece = -1;
+        for (int i = first; i < end; ++i) {
+            const double p = shares ? sums[i].x : rest(i);
+            if (p > kNothing) {
+                piece = i;
+                lead[0] = before;
+                if (before + p > lead[1]) break;
+            }
+            before += p;
+        }
+        chosen = piece;
+        lead[1] = (lead[1] - lead[0]) * (shares ? f.p : 1.0);
+    }
+    __syncthreads();
+    const double goal = lead[1];
+    const int64_t v0 = (int64_t)chosen * (NV * 512), v = v0 + tid * 8;
+    const bool mine = tid < NV * 64;
+    float x[1][8], y[1][8];
+    double r[8], own = 0.0;
+    if (mine) {
+        logits8<F32, 1, false>(row_of(a, b, row.n, false), a.V, v, 0, false, x);
+        if (with_q) logits8<F32, 1, false>(row_of(a, b, row.n, true), a.V, v, 0, false, y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            r[e] = rest_of(x[0][e], y[0][e], row, f, heat.c, with_q);
+            own += r[e];
+        }
+    }
+    who = find(own, goal, false, before);
+    if (tid == who) {
+        int64_t token = -1;
+        bool past = false;
+        const double to = lead[1];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (!past && r[e] > kNothing) {
+                token = v + e;
+                past = before + r[e] > to;
+            }
+            before += r[e];
+        }
+        a.next_token[b] = (int)token;
+    }
+    if (who < 0 && tid == 0) a.next_token[b] = -1;
+}
+
+}  // namespace
+
+// The sum of r over a piece; of a greedy sequence the first of the largest in it.
+template <int NV, bool F32, bool TOGETHER>
+__global__ __launch_bounds__(kThreads) void k_draft_rest(DraftArgs a) {
+    const int lane = threadIdx.x & 63;
+    const Piece p = piece_of(a);
+    const Heat heat = heat_of(a, p.b);
+    const DraftRow row = a.rows[p.b];
+    if (!row.has_p) {
+        if (TOGETHER && p.w == 0 && lane == 0) a.next_token[p.b] = -1;
+        return;
+    }
+    if (p.live) {
+        const int64_t v0 = (int64_t)p.w * (NV * 512);
+        const bool inside = v0 + NV * 512 <= a.V;
+        float x[NV][8], y[NV][8];
+        logits8<F32, NV, false>(row_of(a, p.b, row.n, false), a.V, v0 + lane * 8, 512, inside, x);
+        if (row.has_q) logits8<F32, NV, false>(row_of(a, p.b, row.n, true), a.V, v0 + lane * 8, 512, inside, y);
+        double s;
+        if (heat.greedy) {
+            s = INT32_MAX;
+#pragma unroll
+            for (int i = NV - 1; i >= 0; --i)
+#pragma unroll
+                for (int e = 7; e >= 0; --e) s = x[i][e] == row.mt ? (double)(v0 + i * 512 + lane * 8 + e) : s;
+            s = wave_reduce(s, [](double p, double q) { return fmin(p, q); });
+        } else {
+            const Scales f = scales_of(a, p.b, row.has_q, lane);
+            s = 0.0;
+            if (row.has_q) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s += rest_of(x[i][e], y[i][e], row, f, heat.c, true);
+            } else {
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s += rest_of(x[i][e], 0.0f, row, f, heat.c, false);
+            }
+            s = wave_reduce(s, Add64{});
+        }
+        double* to = a.rest + (int64_t)p.b * a.pieces + p.w;
+        if (lane == 0) {
+            if (TOGETHER)
+                __hip_atomic_store((uint64_t*)to, (uint64_t)__double_as_longlong(s), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            else *to = s;
+        }
+    }
+    if constexpr (TOGETHER) {
+        __shared__ int last;
+        last_workgroup_wait();
+        __syncthreads();
+        if (threadIdx.x == 0)
+            last = __hip_atomic_fetch_add(a.done + p.b, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+                   (uint32_t)((a.pieces + kThreads / 64 - 1) / (kThreads / 64)) - 1;
+        __syncthreads();
+        if (last) pick<NV, F32, true>(a, p.b, heat, row);
+    }
+}
+
+// Workgroup b: the token of sequence b.
+template <int NV, bool F32>
+__global__ __launch_bounds__(kThreads) void k_draft_pick(DraftArgs a) {
+    const int b = blockIdx.x;
+    const DraftRow row = a.rows[b];
+    if (row.has_p) pick<NV, F32, false>(a, b, heat_of(a, b), row);
+    else if (threadIdx.x == 0) a.next_token[b] = -1;
+}
+
+namespace {
+
+// Whether the rows fill the chip with chunks of 2048 logits.
+bool many(int V, int64_t rows) { return rows * ((V + 8191) / 8192) >= 1024; }
 
 void shape(DraftArgs& a, char* space, int64_t* bytes) {
-    const int64_t rows = (int64_t)a.B * (2 * a.k + 1), chunk = chunk_of(a.V, rows);
-    a.chunks = (int)((a.V + chunk - 1) / chunk);
-    // about a thousand workgroups for the rows that 64 bits are needed for
-    const int64_t least = (a.V + kSmall - 1) / kSmall, want = a.B < 1024 ? (1023 + a.B) / a.B : 1, wides = want < least ? want : least;
-    a.wide = ((a.V + wides - 1) / wides + kSmall - 1) / kSmall * kSmall;
-    a.wides = (int)((a.V + a.wide - 1) / a.wide);
+    const int64_t rows = (int64_t)a.B * (2 * a.k + 1);
+    const int chunk = many(a.V, rows) ? 2048 : 512, piece = many(a.V, a.B) ? 2048 : 512;
+    a.chunks = (int)(((int64_t)a.V + chunk - 1) / chunk);
+    a.pieces = (int)(((int64_t)a.V + piece - 1) / piece);
     int64_t at = 0;
     auto take = [&](int64_t n) {
         char* p = space + at;
         at += (n + 15) & ~int64_t(15);
         return p;
     };
-    a.sums = (double2*)take(16 * (int64_t)a.B * a.wides);
-    a.rest = (double*)take(8 * (int64_t)a.B * a.wides);
+    a.sums = (double2*)take(16 * (int64_t)a.B * a.pieces);
+    a.rest = (double*)take(8 * (int64_t)a.B * a.pieces);
     a.stats = (float2*)take(8 * rows * a.chunks);
     a.rows = (DraftRow*)take((int64_t)sizeof(DraftRow) * a.B);
     a.done = (uint32_t*)take(4 * (int64_t)a.B);
@@ -550,11 +660,28 @@ hipError_t launch_verify_drafts(DraftArgs a, void* workspace, hipStream_t s) {
     int64_t bytes;
     shape(a, (char*)workspace, &bytes);
     const int64_t rows = (int64_t)a.B * (2 * a.k + 1);
-    const dim3 grid((unsigned)grid_blocks(rows * a.chunks)), block(kThreads);
-    if (chunk_of(a.V, rows) == kLarge) k_draft_stats<4><<<grid, block, 0, s>>>(a);
-    else k_draft_stats<1><<<grid, block, 0, s>>>(a);
-    k_draft_sums<<<dim3((unsigned)(a.wides * a.B)), block, 0, s>>>(a);
-    k_draft_pick<<<dim3((unsigned)(a.wides * a.B)), block, 0, s>>>(a);
+    const dim3 grid((unsigned)grid_blocks((rows * a.chunks + 3) / 4)), block(kThreads), pieces((unsigned)((int64_t)((a.pieces + 3) / 4) * a.B));
+    auto go = [&](auto f32) {
+        constexpr bool F32 = decltype(f32)::value;
+        if (many(a.V, rows)) k_draft_stats<4, F32><<<grid, block, 0, s>>>(a);
+        else k_draft_stats<1, F32><<<grid, block, 0, s>>>(a);
+        if (many(a.V, a.B)) {
+            k_draft_accept<F32><<<dim3((unsigned)a.B), dim3(kAccept), 0, s>>>(a);
+            k_draft_sums<4, F32, false><<<pieces, block, 0, s>>>(a);
+            k_draft_rest<4, F32, false><<<pieces, block, 0, s>>>(a);
+            k_draft_pick<4, F32><<<dim3((unsigned)a.B), block, 0, s>>>(a);
+        } else if ((int64_t)pieces.x > 1024) {
+            k_draft_accept<F32><<<dim3((unsigned)a.B), dim3(kAccept), 0, s>>>(a);
+            k_draft_sums<1, F32, false><<<pieces, block, 0, s>>>(a);
+            k_draft_rest<1, F32, false><<<pieces, block, 0, s>>>(a);
+            k_draft_pick<1, F32><<<dim3((unsigned)a.B), block, 0, s>>>(a);
+        } else {
+            k_draft_sums<1, F32, true><<<pieces, block, 0, s>>>(a);
+            k_draft_rest<1, F32, true><<<pieces, block, 0, s>>>(a);
+        }
+    };
+    if (a.dtype == 0) go(std::true_type{});
+    else go(std::false_type{});
     return hipGetLastError();
 }
 

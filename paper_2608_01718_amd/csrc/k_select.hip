@@ -201,7 +201,7 @@ __global__ __launch_bounds__(256) void k_kv_score(SelectArgs a) {
                 auto or2 = [](int p, int q) { return p | q; };
                 top = xor_combine<1>(xor_combine<2>(xor_combine<4>(xor_combine<8>(top, max2), max2), max2), max2);
                 odd = xor_combine<1>(xor_combine<2>(xor_combine<4>(xor_combine<8>(odd, or2), or2), or2), or2);
-                const float unit = odd ? __builtin_nanf("") : top / 127.0f;
+                const float unit = odd ? __builtin_nanf("") : top * (1.0f / 127.0f);
 #pragma unroll
                 for (int k = 0; k < (KS + 3) / 4; ++k) {
                     const int c = 8 * (i + 16 * k);

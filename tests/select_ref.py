@@ -21,7 +21,7 @@ def scores(q, code, scale):
     q = q.float()
     top = q.abs().amax(2)
     fine = torch.isfinite(q).all(2)
-    unit = torch.where(fine, top / 127, float("nan"))
+    unit = torch.where(fine, top * torch.tensor(1 / 127), float("nan"))
     c = torch.where((unit > 0)[..., None], (q / torch.where(unit > 0, unit, 1.0)[..., None]).round().clamp(-127, 127), 0.0).long()
     hi, lo = code[:, :, 0].long(), code[:, :, 1].long()                   # [P, H, d]
     dot = torch.einsum("hgd,phd->hgp", c.clamp(min=0), hi) + torch.einsum("hgd,phd->hgp", c.clamp(max=0), lo)

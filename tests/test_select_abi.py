@@ -107,7 +107,7 @@ def test_reference_bounds_hold():
     hi, lo = code.double() * scale.double()
     assert bool((keys <= hi + 1e-6).all()) and bool((keys >= lo - 1e-6).all())
     s = sel.scores(q, code[None, None], scale.view(1, 1))
-    unit = q.abs().amax(2) / 127
+    unit = q.abs().amax(2) * torch.tensor(1 / 127)
     rounded = (q / unit[..., None]).round() * unit[..., None]
     assert float((rounded.double() @ keys.T).max()) <= float(s) * (1 + 1e-5)
     assert ctypes.sizeof(ctypes.c_void_p) == 8

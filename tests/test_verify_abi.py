@@ -27,7 +27,7 @@ def call(lc, **kw):
     dict(accept_len=0), dict(next_token=0), dict(p=0), dict(q=0), dict(workspace=0), dict(workspace=FAKE + 8),
     dict(logits=FAKE + 1), dict(draft=FAKE + 1), dict(dtype=0, logits=FAKE + 2), dict(tokens=FAKE + 2), dict(u=FAKE + 1),
     dict(u_next=FAKE + 2), dict(temperature=FAKE + 2), dict(n_draft=FAKE + 1), dict(p=FAKE + 2), dict(q=FAKE + 2),
-    dict(accept_len=FAKE + 2), dict(next_token=FAKE + 2), dict(bytes=16)])
+    dict(accept_len=FAKE + 2), dict(next_token=FAKE + 2), dict(bytes=16), dict(B=65535, V=2 ** 20)])
 def test_refused(lc, bad):
     assert call(lc, **bad) == EINVAL
 
@@ -42,7 +42,7 @@ def test_workspace(lc):
             lc.lacache_verify_workspace(*bad)
     assert lc.lacache_verify_workspace(1000, 0, 5) == 0
     need = lc.lacache_verify_workspace(128_256, 64, 20)
-    assert 0 < need < 2 ** 20
+    assert 0 < need < 2 ** 22
     assert call(lc, V=128_256, B=64, k=20, bytes=need - 1) == EINVAL
 
 
