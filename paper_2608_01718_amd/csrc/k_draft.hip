@@ -24,10 +24,11 @@ constexpr int kThreads = 256;
 constexpr int kAccept = 512;    // threads of k_draft_accept
 constexpr int kPositions = 64;  // looked at together
 
-// Relative error of a chunked float32 sum S = sum 2^t, t = (x - m) c <= 0.  An exponent's three roundings (c, the
-// difference, the product) move 2^t by 3 |t| 2^-24 ln 2, the exponential is within 2^-22, adding up 32 of a lane in
-// pairs and 64 lanes in a tree are 12 roundings.  The mean of |t| under the weights is below log2 V + 2 (their entropy
-// and the maximum's share), 33 for 2^31 logits: 33 * 1.24e-7 + 2.4e-7 + 12 * 6e-8 = 5.1e-6 for S, twice that for S_p / S_q.
+// Relative error of a chunked float32 sum S = sum 2^t, t = (x - m) c <= 0.  The roundings of an exponent (log2 e, c, the
+// difference, the product) move 2^t by 4 |t| 2^-24 ln 2, whether it is taken in one step or in several; the exponentials (one,
+// and up to five as the maximum rises and lanes are joined) are within 2^-22 each, adding up takes 15 roundings.  The mean of
+// |t| under the weights is below log2 V + 2 (their entropy and the maximum's share), 19 for V = 128,256:
+// 19 * 1.65e-7 + 6 * 2.4e-7 + 15 * 6e-8 = 5.5e-6 for S, twice that for S_p / S_q (1.5e-5 at V = 2^24).
 constexpr double kSumError = 0x1p-16;
 
 // 2^t for t <= 0: 2^n e^(f ln 2), |f| <= 1/2, by the exponential's series up to the 11th power (the 12th: 0.3466^12 / 12! =
@@ -77,49 +78,58 @@ struct Heat {
     double c;
     bool greedy;
 };
+__device__ __forceinline__ bool is_greedy(float t) { return !(t >= 0x1p-60f && t <= 0x1p60f); }
 __device__ __forceinline__ Heat heat_of(const DraftArgs& a, int b) {
-    const double t = a.temperature ? (double)a.temperature[b] : 1.0;
-    const bool greedy = !(t >= 0x1p-60 && t <= 0x1p60);
-    return {greedy ? kLog2e64 : kLog2e64 / t, greedy};
+    const float t = a.temperature ? a.temperature[b] : 1.0f;
+    const bool greedy = is_greedy(t);
+    return {greedy ? kLog2e64 : kLog2e64 / (double)t, greedy};
 }
 __device__ __forceinline__ int drafts_of(const DraftArgs& a, int b) {
     const int n = a.n_draft ? a.n_draft[b] : a.k;
     return n < 0 ? 0 : n > a.k ? a.k : n;
 }
 
-// NV times eight logits of a row (rows begin at any element), from v on and `step` apart, -infinity from V on.  ONCE: they are
-// not read again.  inside: all of the wave's are there (its loads are then issued together: 4096 rows of 32,000 bfloat16
-// logits TIMED).
-template <bool F32, int NV, bool ONCE>
-__device__ __forceinline__ void logits8(const char* row, int V, int64_t v, int64_t step, bool inside, float (&x)[NV][8]) {
-    typedef u32x4 any2 __attribute__((aligned(2)));
-    typedef f32x4 any4 __attribute__((aligned(4)));
-    auto eight = [&](int64_t at, float (&y)[8]) {
-        if constexpr (F32) {
-            const any4 *p = (const any4*)(row + at * 4), *q = (const any4*)(row + at * 4 + 16);
-            const f32x4 lo = ONCE ? __builtin_nontemporal_load(p) : *p, hi = ONCE ? __builtin_nontemporal_load(q) : *q;
+// Eight logits of a row (which begins at any element) as they lie in memory.  ONCE: they are not read again.
+template <bool F32>
+struct Raw8 {
+    u32x4 w[F32 ? 2 : 1];
+    template <bool ONCE>
+    __device__ __forceinline__ void load(const char* row, int64_t v) {
+        typedef u32x4 any __attribute__((aligned(2)));
+        const any* p = (const any*)(row + v * (F32 ? 4 : 2));
+        w[0] = ONCE ? __builtin_nontemporal_load(p) : *p;
+        if constexpr (F32) w[1] = ONCE ? __builtin_nontemporal_load(p + 1) : p[1];
+    }
+    __device__ __forceinline__ void unpack(float (&x)[8]) const {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = lo[e], y[4 + e] = hi[e];
-        } else {
-            const any2* p = (const any2*)(row + at * 2);
-            const u32x4 w = ONCE ? __builtin_nontemporal_load(p) : *p;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                y[2 * e] = __uint_as_float(w[e] << 16);
-                y[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (F32) {
+                x[e] = __uint_as_float(w[0][e]), x[4 + e] = __uint_as_float(w[1][e]);
+            } else {
+                x[2 * e] = __uint_as_float(w[0][e] << 16);
+                x[2 * e + 1] = __uint_as_float(w[0][e] & 0xFFFF0000u);
             }
         }
-    };
+    }
+};
+// NV times eight logits, from v on and `step` apart, -infinity from V on.  inside: all of the wave's are there, and their loads
+// are issued together.
+template <bool F32, int NV, bool ONCE>
+__device__ __forceinline__ void logits8(const char* row, int V, int64_t v, int64_t step, bool inside, float (&x)[NV][8]) {
+    Raw8<F32> raw[NV];
     if (inside) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) eight(v + i * step, x[i]);
+        for (int i = 0; i < NV; ++i) raw[i].template load<ONCE>(row, v + i * step);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) raw[i].unpack(x[i]);
         return;
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int64_t at = v + i * step;
         if (at + 8 <= V) {
-            eight(at, x[i]);
+            raw[i].template load<ONCE>(row, at);
+            raw[i].unpack(x[i]);
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -178,9 +188,12 @@ __device__ __forceinline__ Stat join_chunks(const DraftArgs& a, int64_t row, dou
 
 }  // namespace
 
-// A wave a chunk of NV x 512 logits of a row.
-template <int NV, bool F32>
+// A wave a chunk of a row: STEPS times NV x 512 logits, the next of them on their way while one is worked with.  The vector
+// unit is busy for most of the time of the launch (32 logits a lane: 32 exponentials at a quarter of its rate), so what a wave
+// works out for itself is spread over 8192 logits where there are many.
+template <int NV, int STEPS, bool F32>
 __global__ __launch_bounds__(kThreads) void k_draft_stats(DraftArgs a) {
+    constexpr int64_t kStep = NV * 512, kChunk = kStep * STEPS;
     const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t each = 2 * (uint32_t)a.k + 1;
     const int64_t items = (int64_t)a.B * each * a.chunks;
@@ -198,30 +211,58 @@ __global__ __launch_bounds__(kThreads) void k_draft_stats(DraftArgs a) {
         }
         const bool draft = i > a.k;
         const int j = draft ? i - a.k - 1 : i, n = drafts_of(a, b);
-        const Heat heat = heat_of(a, b);
+        const float t = a.temperature ? a.temperature[b] : 1.0f;
+        const bool greedy = is_greedy(t);
         if (chunk == 0 && i == 0 && lane == 0) a.done[b] = 0;
-        if (draft ? (j >= n || heat.greedy) : j > n) continue;
+        if (draft ? (j >= n || greedy) : j > n) continue;
+        const float c = greedy ? (float)kLog2e64 : (float)kLog2e64 / t;
         const char* at = row_of(a, b, j, draft);
-        const int64_t v0 = (int64_t)chunk * (NV * 512);
-        float x[NV][8];
-        logits8<F32, NV, true>(at, a.V, v0 + lane * 8, 512, v0 + NV * 512 <= a.V, x);
-        float m = -__builtin_inff();
+        const int64_t v0 = (int64_t)chunk * kChunk;
+        float m = -__builtin_inff(), s = 0.0f;
+        auto add = [&](const float (&x)[NV][8]) {
+            float top = m;
 #pragma unroll
-        for (int u = 0; u < NV; ++u)
+            for (int u = 0; u < NV; ++u)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) m = fmaxf(m, x[u][e]);  // (leaves NaN out: the sum has it)
-        m = wave_reduce(m, [](float p, float q) { return fmaxf(p, q); });
-        const float base = m > -__builtin_inff() ? m : 0.0f, c = (float)heat.c;
-        float s = 0.0f;
+                for (int e = 0; e < 8; ++e) top = fmaxf(top, x[u][e]);  // (leaves NaN out: the sum has it)
+            const float base = top > -__builtin_inff() ? top : 0.0f;
+            if constexpr (STEPS > 1) s *= __builtin_amdgcn_exp2f((m - base) * c);
+            m = top;
 #pragma unroll
-        for (int u = 0; u < NV; ++u) {
-            float y[8];
+            for (int u = 0; u < NV; ++u) {
+                float y[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = __builtin_amdgcn_exp2f((x[u][e] - base) * c);
-            s += ((y[0] + y[1]) + (y[2] + y[3])) + ((y[4] + y[5]) + (y[6] + y[7]));
+                for (int e = 0; e < 8; ++e) y[e] = __builtin_amdgcn_exp2f((x[u][e] - base) * c);
+                s += ((y[0] + y[1]) + (y[2] + y[3])) + ((y[4] + y[5]) + (y[6] + y[7]));
+            }
+        };
+        if (STEPS > 1 && v0 + kChunk <= a.V) {
+            Raw8<F32> raw[2][NV];
+            auto fetch = [&](int step, Raw8<F32> (&to)[NV]) {
+#pragma unroll
+                for (int u = 0; u < NV; ++u) to[u].template load<true>(at, v0 + step * kStep + u * 512 + lane * 8);
+            };
+            fetch(0, raw[0]);
+#pragma unroll
+            for (int step = 0; step < STEPS; ++step) {
+                if (step + 1 < STEPS) fetch(step + 1, raw[(step + 1) & 1]);
+                __builtin_amdgcn_sched_barrier(0);
+                float x[NV][8];
+#pragma unroll
+                for (int u = 0; u < NV; ++u) raw[step & 1][u].unpack(x[u]);
+                add(x);
+            }
+        } else {
+            for (int64_t v = v0; v < v0 + kChunk && v < a.V; v += kStep) {
+                float x[NV][8];
+                logits8<F32, NV, true>(at, a.V, v + lane * 8, 512, v + kStep <= a.V, x);
+                add(x);
+            }
         }
+        const float M = wave_reduce(m, [](float p, float q) { return fmaxf(p, q); });
+        s *= __builtin_amdgcn_exp2f(M > -__builtin_inff() ? (m - M) * c : 0.0f);
         s = wave_sum_f32(s);
-        if (lane == 0) a.stats[row * a.chunks + chunk] = make_float2(m, s);
+        if (lane == 0) a.stats[row * a.chunks + chunk] = make_float2(M, s);
     }
 }
 
@@ -624,12 +665,16 @@ __global__ __launch_bounds__(kThreads) void k_draft_pick(DraftArgs a) {
 
 namespace {
 
-// Whether the rows fill the chip with chunks of 2048 logits.
-bool many(int V, int64_t rows) { return rows * ((V + 8191) / 8192) >= 1024; }
+// Logits of a chunk of k_draft_stats: the longest that leave eight waves on each SIMD, or two.
+int chunk_of(int V, int64_t rows) {
+    return rows * ((V + INT64_C(8191)) / 8192) >= 8192 ? 8192 : rows * ((V + INT64_C(2047)) / 2048) >= 2048 ? 2048 : 512;
+}
+// Logits of a piece of the row behind the drafts.
+int piece_of(int V, int64_t B) { return B * ((V + INT64_C(8191)) / 8192) >= 1024 ? 1024 : 512; }
 
 void shape(DraftArgs& a, char* space, int64_t* bytes) {
     const int64_t rows = (int64_t)a.B * (2 * a.k + 1);
-    const int chunk = many(a.V, rows) ? 2048 : 512, piece = many(a.V, a.B) ? 2048 : 512;
+    const int chunk = chunk_of(a.V, rows), piece = piece_of(a.V, a.B);
     a.chunks = (int)(((int64_t)a.V + chunk - 1) / chunk);
     a.pieces = (int)(((int64_t)a.V + piece - 1) / piece);
     int64_t at = 0;
@@ -663,13 +708,15 @@ hipError_t launch_verify_drafts(DraftArgs a, void* workspace, hipStream_t s) {
     const dim3 grid((unsigned)grid_blocks((rows * a.chunks + 3) / 4)), block(kThreads), pieces((unsigned)((int64_t)((a.pieces + 3) / 4) * a.B));
     auto go = [&](auto f32) {
         constexpr bool F32 = decltype(f32)::value;
-        if (many(a.V, rows)) k_draft_stats<4, F32><<<grid, block, 0, s>>>(a);
-        else k_draft_stats<1, F32><<<grid, block, 0, s>>>(a);
-        if (many(a.V, a.B)) {
+        const int chunk = chunk_of(a.V, rows);
+        if (chunk == 8192) k_draft_stats<4, 4, F32><<<grid, block, 0, s>>>(a);
+        else if (chunk == 2048) k_draft_stats<4, 1, F32><<<grid, block, 0, s>>>(a);
+        else k_draft_stats<1, 1, F32><<<grid, block, 0, s>>>(a);
+        if (piece_of(a.V, a.B) == 1024) {
             k_draft_accept<F32><<<dim3((unsigned)a.B), dim3(kAccept), 0, s>>>(a);
-            k_draft_sums<4, F32, false><<<pieces, block, 0, s>>>(a);
-            k_draft_rest<4, F32, false><<<pieces, block, 0, s>>>(a);
-            k_draft_pick<4, F32><<<dim3((unsigned)a.B), block, 0, s>>>(a);
+            k_draft_sums<2, F32, false><<<pieces, block, 0, s>>>(a);
+            k_draft_rest<2, F32, false><<<pieces, block, 0, s>>>(a);
+            k_draft_pick<2, F32><<<dim3((unsigned)a.B), block, 0, s>>>(a);
         } else if ((int64_t)pieces.x > 1024) {
             k_draft_accept<F32><<<dim3((unsigned)a.B), dim3(kAccept), 0, s>>>(a);
             k_draft_sums<1, F32, false><<<pieces, block, 0, s>>>(a);
