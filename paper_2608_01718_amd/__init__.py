@@ -965,9 +965,13 @@ def lacache_kv_select(b: KVBounds, q, seqs: Sequences, n_blocks: int, first: int
         raise ValueError("n_blocks: expected at least one")
     out = _given(out, (shape[0], c.heads, n_blocks), torch.int32, index, "out") if given else \
         _made(q, (shape[0], c.heads, n_blocks), torch.int32, stream)
-    space = _made(q, (lacache_kv_select_workspace(c, shape[0], seqs._c.max_pages),), torch.uint8, stream)
+    key = ("select", shape[0], seqs._c.max_pages)
+    need = c._need.get(key)
+    if need is None:
+        need = c._need[key] = lacache_kv_select_workspace(c, shape[0], seqs._c.max_pages)
+    space = _made(q, (need,), torch.uint8, stream)
     _check(_on(index, stream, _lib.lacache_kv_select, c._ref, b._ref, seqs._ref, q.data_ptr(), dtype, shape[0], shape[1], q_row,
-               n_blocks, first, last, max_new, out.data_ptr(), space.data_ptr(), space.numel()), "lacache_kv_select")
+               n_blocks, first, last, max_new, out.data_ptr(), space.data_ptr(), need), "lacache_kv_select")
     if given:
         _written(out)
     return out
