@@ -42,8 +42,16 @@ constexpr int attend_occupancy(int dp, bool bytes, int R, bool f32) {
 }
 
 // What an attention launch is: all of it; the part over the prefixes that groups of sequences share, whose "sequences" are
-// the groups; the part over each sequence's own tokens, which takes up the other's results.
+// the groups; the part over each sequence's own tokens.  The launch behind the two parts puts them together.
 enum AttendMode { kWhole = 0, kPrefix = 1, kOwn = 2 };
+
+// The sums of a part for every (row, query head): where they lie, as the number of workers that have parts of its row group
+// (0: all of it is in o and ml), the first of them, and the row's place in the group.
+struct AttendSums {
+    float* o;    // [rows q_heads][dp] sums of values
+    float2* ml;  // [rows q_heads] their maxima and sums of weights
+    int2* at;    // [rows q_heads] workers; first worker + 2^16 place
+};
 
 // The shared prefixes of a call, as k_attend_share has laid them out.
 struct AttendShare {
@@ -52,8 +60,8 @@ struct AttendShare {
     int32_t* first;    // [n_groups] the first tile that any row sees
     int32_t* held;     // [n_seq] tokens that a sequence shares (0: it is in no group)
     int32_t* row_pos;  // [rows] positions of rows (-1 before the first)
-    float* o;          // [rows q_heads][dp] sums of values over the prefix
-    float2* ml;        // [rows q_heads] their maxima and sums of weights
+    int32_t* row_held; // [rows] whether a row's sequence shares tokens; -1: it is in no sequence
+    AttendSums sums[2];  // kPrefix, kOwn
 };
 
 // What a launch works with besides the arguments: the shape of a row group, its workers, the workspace.
@@ -61,6 +69,7 @@ struct AttendPlan {
     int group_shift;   // rows of a row group, as a shift
     int workers, waves;  // workgroups of the launch, and the waves of each
     int chunk_shift;   // the work is dealt out in chunks of this many tiles (a shift), so that counts fit in 32 bits
+    int extra;         // chunks that a row group counts for besides its tiles' (kOwn)
     uint32_t group_magic, group_bits;  // row / group = row * magic >> bits
     int join_here;     // parts are joined by the workgroup that ends last; otherwise by the launch that follows
     uint32_t* done;    // [kMaxWorkers] parts that are there of the row group that begins with a worker; 0 between launches
@@ -77,8 +86,7 @@ struct alignas(16) AttendSplit {
     int seq_row0, head0;   // the sequence's first row, the first query head
     int row, n_rows;       // rows row .. row + n_rows - 1 of the sequence's (0: there is no such row group)
     int worker0, parts;    // the first of its workers, their number
-    int held;              // whether there is a part over a prefix (kOwn)
-    int unused;
+    int unused[2];
 };
 
 // What the work of a sequence is: its rows and their groups, its tiles.
@@ -87,11 +95,11 @@ struct AttendSpan {
     int rows, groups;    // new tokens x group; row groups
     int first, tiles;    // the first tile that any row sees, the number of tiles
     int cap;             // positions that exist
-    int chunks;          // the tiles in chunks
+    int chunks, stride;  // the tiles in chunks; the items of a row group: these, and what it counts for besides
     int table;           // the sequence whose page table holds them
     int held;            // positions that another launch sees to
     __device__ int64_t pos0() const { return (int64_t)len - n; }  // of the first row
-    __device__ int items(const AttendArgs& a) const { return groups * a.pool.heads * chunks; }
+    __device__ int items(const AttendArgs& a) const { return groups * a.pool.heads * stride; }
 };
 template <int MODE = kWhole>
 __device__ inline AttendSpan attend_span(const AttendArgs& a, const AttendPlan& p, int b) {
@@ -118,6 +126,7 @@ __device__ inline AttendSpan attend_span(const AttendArgs& a, const AttendPlan& 
     r.tiles = (int)(((int64_t)r.cap + 31) >> 5) - r.first;
     if (r.tiles < 1) r.tiles = 1;  // rows that see nothing are written too
     r.chunks = (r.tiles + (1 << p.chunk_shift) - 1) >> p.chunk_shift;
+    r.stride = r.chunks + (MODE == kOwn ? p.extra : 0);
     return r;
 }
 __device__ __forceinline__ int token_of(const AttendPlan& p, int row) {
@@ -136,12 +145,12 @@ __device__ __forceinline__ AttendEnds ends_of(const AttendPlan& p, const AttendS
         int least = INT32_MAX, most = -1;
         for (int i = i0 + lane; i <= i1; i += 64) {
             const int pos = p.share.row_pos[s.row0 + i];
-            least = min(least, pos);
+            least = pos < 0 ? least : min(least, pos);  // (rows that see nothing: nothing_seen)
             most = max(most, pos);
         }
         least = wave_reduce(least, [](int x, int y) { return min(x, y); });
         most = wave_reduce(most, [](int x, int y) { return max(x, y); });
-        return {__builtin_amdgcn_readfirstlane(least), __builtin_amdgcn_readfirstlane(most)};
+        return {__builtin_amdgcn_readfirstlane(most < 0 ? -1 : least), __builtin_amdgcn_readfirstlane(most)};
     } else {
         const int64_t p0 = s.pos0() + i0, p1 = s.pos0() + i1;
         return {p0 < 0 ? -1 : (int)p0, p1 < 0 ? -1 : (int)p1};
@@ -222,6 +231,25 @@ __device__ __forceinline__ AttendRange attend_range(const AttendArgs& a, const A
     return r;
 }
 
+// Moves on to the next chunk of a worker's range: past sequences that are through and those without rows, and past the items
+// behind a row group's chunks.  Whether there is one.
+template <int MODE>
+__device__ __forceinline__ bool attend_next(const AttendArgs& a, const AttendPlan& p, AttendRange& r, AttendSpan& s) {
+    while (r.at < r.end) {
+        const int items = s.items(a);
+        if (r.at - r.before >= items) {
+            r.before += items;
+            do s = attend_span<MODE>(a, p, ++r.b);
+            while (s.n == 0);
+        }
+        if (MODE != kOwn) return true;
+        const int rel = r.at - r.before, c0 = rel - (int)((uint32_t)rel / (uint32_t)s.stride) * s.stride;
+        if (c0 < s.chunks) return true;
+        r.at += s.stride - c0;
+    }
+    return false;
+}
+
 // 16 bytes a lane from a tile whose bytes past `size` (0: there is no tile) are not read and come as zeros.  With few rows
 // keys and values are read once (ONCE): non-temporal loads are 12 % faster (131,071 tokens 89 us, 102 without; 256 sequences of 512 to
 // 2048 tokens, 16 heads of 64 columns 191 us, 214).
@@ -294,6 +322,18 @@ struct Attend {
 #pragma unroll
             for (int j = 0; j < NJ; ++j) o[r][j] = f32x4{0, 0, 0, 0};
         }
+    }
+    // Rows of no position among others' (kPrefix): what they summed up is left out, so that the others' tiles need not be hidden
+    // from them.
+    __device__ __forceinline__ void nothing_seen() {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (hi[r] < 0) {
+                m[r] = -__builtin_inff();
+                l[r] = 0.0f;
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) o[r][j] = f32x4{0, 0, 0, 0};
+            }
     }
     // every lane's sum over the tokens of the four lane groups
     __device__ __forceinline__ void reduce() {
@@ -710,24 +750,22 @@ struct Joined {
     }
 };
 
-// Takes up the part over the prefix: of element `at` of the results, four columns from col on.
-template <int DP>
-__device__ __forceinline__ void add_prefix(const AttendPlan& p, Joined& x, int64_t at, int dp, int col) {
-    const float2 ml = p.share.ml[at];
-    x.add(ml.x, ml.y, *(const f32x4*)(p.share.o + at * (DP > 0 ? DP : dp) + col));
+// Four columns of element `at` of a part's sums, and where they lie.
+template <int MODE>
+__device__ __forceinline__ void store_sums(const AttendPlan& p, int64_t at, int dp, int col, f32x4 o, float m, float l) {
+    const AttendSums& x = p.share.sums[MODE - kPrefix];
+    *(f32x4*)(x.o + at * dp + col) = o;
+    if (col == 0) x.ml[at] = make_float2(m, l);
+}
+template <int MODE>
+__device__ __forceinline__ void store_place(const AttendPlan& p, int64_t at, int parts, int worker0, int place) {
+    p.share.sums[MODE - kPrefix].at[at] = make_int2(parts, worker0 | place << 16);
 }
 
-template <int MODE = kWhole>
 __device__ __forceinline__ void store_joined(const AttendArgs& a, const AttendPlan& p, const AttendSplit& s, int row,
-                                             int col, Joined x) {
+                                             int col, const Joined& x) {
     const int r = s.row + row, i = token_of(p, r);
     const int64_t at = ((int64_t)s.seq_row0 + i) * a.q_heads + s.head0 + (r - i * a.group);
-    if constexpr (MODE == kPrefix) {
-        *(f32x4*)(p.share.o + at * a.pool.dp + col) = x.o;
-        if (col == 0) p.share.ml[at] = make_float2(x.m, x.l);
-        return;
-    }
-    if (MODE == kOwn && s.held) add_prefix<0>(p, x, at, a.pool.dp, col);
     const f32x4 o = x.o * (x.l == 0.0f ? 0.0f : 1.0f / x.l);
     if (col < a.pool.d) {
         if (a.dtype == 0) store4<true>(a, at * a.pool.d + col, o);
@@ -739,7 +777,7 @@ __device__ __forceinline__ void store_joined(const AttendArgs& a, const AttendPl
 // Joins the parts of a row group: of_row groups (a power of two) of dp / 4 lanes on a row, four parts loaded together.  The workgroup takes rows first, first + 1, ... as many as it has lane groups for, and
 // again from `step` times as many on.  load(part's first row + row, column, ml, o) loads four columns.  scratch: THREADS f32x4 and
 // float2 of LDS.
-template <int THREADS, int MODE, class Load>
+template <int THREADS, class Load>
 __device__ __forceinline__ void join_rows(const AttendArgs& a, const AttendPlan& p, const AttendSplit& s, int dp, int of_row, int tid,
                                           int first, int step, f32x4* scratch, Load load) {
     const int lanes = dp / 4, groups = THREADS / lanes;
@@ -771,7 +809,7 @@ __device__ __forceinline__ void join_rows(const AttendArgs& a, const AttendPlan&
                     x.add(ml_of[tid + k * lanes].x, ml_of[tid + k * lanes].y, scratch[tid + k * lanes]);
             __syncthreads();
         }
-        if (live && sub == 0) store_joined<MODE>(a, p, s, row, col, x);
+        if (live && sub == 0) store_joined(a, p, s, row, col, x);
     }
 }
 
@@ -795,7 +833,7 @@ __device__ __forceinline__ void store_part_ml(const AttendPlan& p, int64_t part,
 
 // After a workgroup's part of a row group has been stored: counts it, and joins the parts if it is the last.  scratch:
 // THREADS f32x4 and float2 of LDS that nothing else uses meanwhile.
-template <int THREADS, int DP, int MODE>
+template <int THREADS, int DP>
 __device__ __forceinline__ void join_parts(const AttendArgs& a, const AttendPlan& p, const AttendSplit& s,
                                            f32x4* scratch) {
     __shared__ int last;
@@ -812,7 +850,7 @@ __device__ __forceinline__ void join_parts(const AttendArgs& a, const AttendPlan
     // (all rows at once where they are few; a choice by the parts too costs more than it gains here)
     int of_row = 1;
     while (2 * of_row * s.n_rows <= THREADS / (DP / 4)) of_row *= 2;
-    join_rows<THREADS, MODE>(a, p, s, DP, of_row, tid, 0, 1, scratch, [&](int64_t at, int col, float2& ml, f32x4& o) {
+    join_rows<THREADS>(a, p, s, DP, of_row, tid, 0, 1, scratch, [&](int64_t at, int col, float2& ml, f32x4& o) {
         auto load8 = [](const void* from) {
             const uint64_t w = __hip_atomic_load((const uint64_t*)from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             return make_float2(__uint_as_float((uint32_t)w), __uint_as_float((uint32_t)(w >> 32)));
@@ -823,20 +861,18 @@ __device__ __forceinline__ void join_parts(const AttendArgs& a, const AttendPlan
     });
 }
 
-// HERE: parts are joined within the launch (for sequences' own tokens with three workgroups on a compute unit at most: two
-// registers of the narrowest heads would be kept in memory with four).
-template <int DP, int CT, int R, bool F32, bool HERE, int MODE = kWhole>
-__global__ __launch_bounds__(256, (HERE && MODE == kOwn && Attend<DP, CT, R, F32>::OCC > 3 ? 3 : Attend<DP, CT, R, F32>::OCC)) void k_attend(AttendArgs a, AttendPlan p) {
+// A worker of four waves.  HERE: parts are joined within the launch.
+template <int DP, int CT, int R, bool F32, bool HERE, int MODE>
+__device__ __forceinline__ void attend_narrow(const AttendArgs& a, const AttendPlan& p, const int worker) {
     using A = Attend<DP, CT, R, F32>;
     constexpr int GR = 16 * R;  // rows of a row group
     __shared__ float2 sml[4][GR];
     __shared__ float so[4][16][A::CB + 4];
     const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int worker = blockIdx.x;
 
     AttendRange range = attend_range<4, MODE>(a, p, worker, 4 >> (p.chunk_shift < 2 ? p.chunk_shift : 2), 1);
     if (range.at >= range.end) {
-        if (!HERE && tid == 0) p.split[worker].n_rows = 0;
+        if (MODE == kWhole && !HERE && tid == 0) p.split[worker].n_rows = 0;
         return;
     }
     AttendSplit split{};
@@ -846,7 +882,7 @@ __global__ __launch_bounds__(256, (HERE && MODE == kOwn && Attend<DP, CT, R, F32
     // A segment: tiles tile0 .. tile1 - 1 of one row group
     struct Segment {
         int h, rg, tile0, tile1, row0, rows, n_rows;  // n_rows: rows in the group
-        int first, table, held, item0, items;         // the row group's first item, its items
+        int first, table, item0, items;               // the row group's first item, its items
         bool starts, ends;                            // whether it holds the first and the last tile
         int seen0, seen1, all0, all1;                 // positions that one of the rows, that every row sees
     };
@@ -883,19 +919,19 @@ __global__ __launch_bounds__(256, (HERE && MODE == kOwn && Attend<DP, CT, R, F32
     // the segment that begins at item `at`, its queries and its first tiles
     auto open = [&]() {
         const int rel = range.at - range.before;
-        const int unit = (int)((uint32_t)rel / (uint32_t)s.chunks), c0 = rel - unit * s.chunks;
+        const int unit = (int)((uint32_t)rel / (uint32_t)s.stride), c0 = rel - unit * s.stride;
         g.h = (int)((uint32_t)unit / (uint32_t)s.groups);
         g.rg = unit - g.h * s.groups;
         const int left = range.end - range.at, c1 = s.chunks - c0 <= left ? s.chunks : c0 + left;
         range.at += c1 - c0;
-        g.item0 = range.before + unit * s.chunks;
+        g.item0 = range.before + unit * s.stride;
         g.items = s.chunks;
         g.starts = c0 == 0;
         g.ends = c1 == s.chunks;
         g.tile0 = c0 << p.chunk_shift;
         g.tile1 = g.ends ? s.tiles : c1 << p.chunk_shift;
         const int r0 = g.rg << p.group_shift;
-        g.row0 = s.row0, g.rows = s.rows, g.first = s.first, g.table = s.table, g.held = s.held;
+        g.row0 = s.row0, g.rows = s.rows, g.first = s.first, g.table = s.table;
         g.n_rows = s.rows - r0 < GR ? s.rows - r0 : GR;
         const AttendEnds ends = ends_of<MODE>(p, s, r0, g.n_rows, lane);
         const int q0 = ends.least, q1 = ends.most;
@@ -914,6 +950,9 @@ __global__ __launch_bounds__(256, (HERE && MODE == kOwn && Attend<DP, CT, R, F32
         A::load_v(tile, a, pl, there, lane);
         __builtin_amdgcn_sched_barrier(0);
     };
+    if (MODE == kOwn && !attend_next<MODE>(a, p, range, s)) {
+        return;
+    }
     open();
     bool more = true;
     while (more) {
@@ -940,25 +979,25 @@ __global__ __launch_bounds__(256, (HERE && MODE == kOwn && Attend<DP, CT, R, F32
                     g.all0, g.all1, lane);
         // The next segment's loads are on their way while this one's results are joined and stored.
         const Segment old = g;
+        if (MODE == kPrefix) w.nothing_seen();
         w.reduce();
-        more = range.at < range.end;
-        if (more) {
-            const int items = s.items(a);
-            if (range.at - range.before >= items) {  // past this sequence, and those without rows
-                range.before += items;
-                do s = attend_span<MODE>(a, p, ++range.b);
-                while (s.n == 0);
-            }
-            open();
-        }
+        more = attend_next<MODE>(a, p, range, s);
+        if (more) open();
         const bool whole = old.starts && old.ends;
         const int64_t part = part_of(p, worker, !old.ends);
         AttendSplit u0{};
         if (!whole) {
             const int first = (int)((uint32_t)old.item0 / (uint32_t)range.per);
             const int end = (int)((uint32_t)(old.item0 + old.items - 1) / (uint32_t)range.per);
-            u0 = AttendSplit{old.row0, old.h * a.group, old.rg * GR, old.n_rows, first, end - first + 1, old.held, 0};
+            u0 = AttendSplit{old.row0, old.h * a.group, old.rg * GR, old.n_rows, first, end - first + 1, {}};
             if (old.ends) split = u0;
+        }
+        if constexpr (MODE != kWhole) {
+            if (old.ends && tid < old.n_rows) {
+                const int r = old.rg * GR + tid, i = token_of(p, r);
+                store_place<MODE>(p, ((int64_t)old.row0 + i) * a.q_heads + old.h * a.group + (r - i * a.group), whole ? 0 : u0.parts,
+                                  u0.worker0, tid);
+            }
         }
         // four columns of a row of the group; its maximum and sum with the first of them
         auto put = [&](int row, int col, f32x4 x, float m, float l) {
@@ -974,15 +1013,9 @@ __global__ __launch_bounds__(256, (HERE && MODE == kOwn && Attend<DP, CT, R, F32
             }
             const int r = old.rg * GR + row, i = token_of(p, r), head = old.h * a.group + (r - i * a.group);
             const int64_t at = ((int64_t)old.row0 + i) * a.q_heads + head;
-            if constexpr (MODE == kPrefix) {
-                *(f32x4*)(p.share.o + at * DP + col) = x;
-                if (col == 0) p.share.ml[at] = make_float2(m, l);
+            if constexpr (MODE != kWhole) {
+                store_sums<MODE>(p, at, DP, col, x, m, l);
                 return;
-            }
-            if (MODE == kOwn && old.held) {
-                Joined j{m, l, x};
-                add_prefix<DP>(p, j, at, DP, col);
-                m = j.m, l = j.l, x = j.o;
             }
             if (col < a.pool.d) store4<F32>(a, at * a.pool.d + col, x * (l == 0.0f ? 0.0f : 1.0f / l));
             if (col == 0 && a.lse) a.lse[at] = lse_of(m, l);
@@ -1024,10 +1057,15 @@ __global__ __launch_bounds__(256, (HERE && MODE == kOwn && Attend<DP, CT, R, F32
             }
         if constexpr (HERE) {
             static_assert(sizeof(so) >= 256 * 24, "the join's scratch");
-            if (!whole) join_parts<256, DP, MODE>(a, p, u0, (f32x4*)&so[0][0][0]);
+            if (!whole) join_parts<256, DP>(a, p, u0, (f32x4*)&so[0][0][0]);
         }
     }
-    if (!HERE && tid == 0) p.split[worker] = split;
+    if (MODE == kWhole && !HERE && tid == 0) p.split[worker] = split;
+}
+
+template <int DP, int CT, int R, bool F32, bool HERE, int MODE = kWhole>
+__global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(AttendArgs a, AttendPlan p) {
+    attend_narrow<DP, CT, R, F32, HERE, MODE>(a, p, blockIdx.x);
 }
 
 }  // namespace lacache

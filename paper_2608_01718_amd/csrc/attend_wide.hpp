@@ -35,9 +35,9 @@ struct Wide {
     static constexpr int OCC = R * DP * (F32 ? 2 : 1) <= 256 ? 2 : 1;
 };
 
-template <int DP, int CT, int WAVES, int R, bool F32, int MODE = kWhole>
-__global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) void k_attend_wide(AttendArgs a,
-                                                                                              AttendPlan p) {
+// The worker of workgroup `block` of a launch's.
+template <int DP, int CT, int WAVES, int R, bool F32, int MODE>
+__device__ __forceinline__ void attend_wide(const AttendArgs& a, const AttendPlan& p, const int block) {
     using W = Wide<DP, CT, WAVES, R, F32>;
     using A = Attend<DP, CT, R, F32>;
     __shared__ u32x4 keys[2][2 * W::KC * 64], vals[2][W::NJ * 64];  // operands of 1 KB each
@@ -47,14 +47,14 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
     const int n = lane & 15, u = lane >> 4;
     // Workgroups go to the eight XCDs in turn; each XCD takes an eighth of the work in one piece, so that the row groups of
     // a (sequence, kv head) share its L2.
-    const int eighth = (p.workers + 7) >> 3, worker = (blockIdx.x & 7) * eighth + (blockIdx.x >> 3);
+    const int eighth = (p.workers + 7) >> 3, worker = (block & 7) * eighth + (block >> 3);
     if (worker >= p.workers) return;
 
     // (two tiles or more: a part of 128 rows is four times the bytes of a tile to write, and again to read in the join; one
     // sequence of 4096 tokens, 16 new ones 40 us, 50 with one)
     AttendRange range = attend_range<WAVES, MODE>(a, p, worker, 1, 2);
     if (range.at >= range.end) {
-        if (tid == 0) p.split[worker].n_rows = 0;
+        if (MODE == kWhole && tid == 0) p.split[worker].n_rows = 0;
         return;
     }
     AttendSplit split{};
@@ -62,10 +62,10 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
     const int tile_shift = a.pool.page_shift - 5;
     AttendSpan s = attend_span<MODE>(a, p, range.b);
 
-    while (true) {
+    while (attend_next<MODE>(a, p, range, s)) {
         // the segment that begins at item range.at
         const int rel = range.at - range.before;
-        const int unit = (int)((uint32_t)rel / (uint32_t)s.chunks), c0 = rel - unit * s.chunks;
+        const int unit = (int)((uint32_t)rel / (uint32_t)s.stride), c0 = rel - unit * s.stride;
         const int h = (int)((uint32_t)unit / (uint32_t)s.groups), rg = unit - h * s.groups;
         const int left = range.end - range.at, c1 = s.chunks - c0 <= left ? s.chunks : c0 + left;
         range.at += c1 - c0;
@@ -228,13 +228,21 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
                 w.spoil(a, a.seqs.pages + (int64_t)s.table * a.seqs.max_pages, h, s.first, tile0, tile1, 1, seen0, seen1, all0, all1,
                         lane);
         }
+        if (MODE == kPrefix) w.nothing_seen();
         w.reduce();
 
         const bool whole = starts && ends;
         const int64_t slot = part_of(p, worker, !ends);
         if (ends && !starts) {
-            const int first = (int)((uint32_t)(range.before + unit * s.chunks) / (uint32_t)range.per);
-            split = AttendSplit{s.row0, h * a.group, r0, n_rows, first, worker - first + 1, s.held, 0};
+            const int first = (int)((uint32_t)(range.before + unit * s.stride) / (uint32_t)range.per);
+            split = AttendSplit{s.row0, h * a.group, r0, n_rows, first, worker - first + 1, {}};
+        }
+        if constexpr (MODE != kWhole) {
+            if (ends && tid < n_rows) {
+                const int i = token_of(p, r0 + tid);
+                store_place<MODE>(p, ((int64_t)s.row0 + i) * a.q_heads + h * a.group + (r0 + tid - i * a.group), starts ? 0 : split.parts,
+                                  split.worker0, tid);
+            }
         }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -248,21 +256,10 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
             } else {
                 const int i = token_of(p, r0 + row), head = h * a.group + (r0 + row - i * a.group);
                 const int64_t at = ((int64_t)s.row0 + i) * a.q_heads + head;
-                if constexpr (MODE == kPrefix) {
+                if constexpr (MODE != kWhole) {
 #pragma unroll
-                    for (int j = 0; j < W::NJ; ++j) *(f32x4*)(p.share.o + at * DP + 16 * j + 4 * u) = w.o[r][j];
-                    if (u == 0) p.share.ml[at] = make_float2(w.m[r], w.l[r]);
+                    for (int j = 0; j < W::NJ; ++j) store_sums<MODE>(p, at, DP, 16 * j + 4 * u, w.o[r][j], w.m[r], w.l[r]);
                     continue;
-                }
-                if (MODE == kOwn && s.held) {
-                    Joined x{w.m[r], w.l[r], {}};
-#pragma unroll
-                    for (int j = 0; j < W::NJ; ++j) {
-                        x = Joined{w.m[r], w.l[r], w.o[r][j]};
-                        add_prefix<DP>(p, x, at, DP, 16 * j + 4 * u);
-                        w.o[r][j] = x.o;
-                    }
-                    w.m[r] = x.m, w.l[r] = x.l;
                 }
                 const float f = w.l[r] == 0.0f ? 0.0f : 1.0f / w.l[r];
 #pragma unroll
@@ -271,23 +268,56 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
                 if (u == 0 && a.lse) a.lse[at] = lse_of(w.m[r], w.l[r]);
             }
         }
-        if (range.at >= range.end) break;
-        if (range.at - range.before >= s.items(a)) {  // past this sequence, and those without rows
-            range.before += s.items(a);
-            do s = attend_span<MODE>(a, p, ++range.b);
-            while (s.n == 0);
-        }
         lds_barrier();  // the buffers have been read
     }
-    if (tid == 0) p.split[worker] = split;
+    if (MODE == kWhole && tid == 0) p.split[worker] = split;
 }
+
+template <int DP, int CT, int WAVES, int R, bool F32, int MODE = kWhole>
+__global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) void k_attend_wide(AttendArgs a, AttendPlan p) {
+    attend_wide<DP, CT, WAVES, R, F32, MODE>(a, p, blockIdx.x);
+}
+
+// Both parts of a call in one launch: workgroups below `prefix` those over the prefixes, the others over the sequences' own
+// tokens.  WIDE: many rows over the prefixes, which the matrix cores and the softmax bound, while memory bounds the own tokens;
+// one of each on a compute unit.
+template <int DP, int CT, bool F32, bool WIDE>
+__global__ __launch_bounds__(256, 2) void k_attend_both(AttendArgs a, AttendPlan p, AttendPlan own, int prefix) {
+    if ((int)blockIdx.x >= prefix) attend_narrow<DP, CT, 1, F32, false, kOwn>(a, own, blockIdx.x - prefix);
+    else if constexpr (WIDE) attend_wide<DP, CT, 4, F32 ? 1 : 2, F32, kPrefix>(a, p, blockIdx.x);
+    else attend_narrow<DP, CT, 1, F32, false, kPrefix>(a, p, blockIdx.x);
+}
+
+template <int DP>
+hipError_t launch_attend_both(const AttendArgs& a, const AttendPlan& p, const AttendPlan& own, hipStream_t s) {
+    const bool wide = p.group_shift > 5;
+    const int prefix = wide ? (p.workers + 7) & ~7 : p.workers;
+    const dim3 grid((unsigned)(prefix + own.workers)), block(256);
+    auto go = [&](auto ct, auto f32) {
+        constexpr int CT = decltype(ct)::value;
+        constexpr bool F32 = decltype(f32)::value;
+        if (wide) k_attend_both<DP, CT, F32, true><<<grid, block, 0, s>>>(a, p, own, prefix);
+        else k_attend_both<DP, CT, F32, false><<<grid, block, 0, s>>>(a, p, own, prefix);
+    };
+    auto of = [&](auto ct) {
+        if (a.dtype == 0) go(ct, std::true_type{});
+        else go(ct, std::false_type{});
+    };
+    if (a.pool.type == kKvBf16) of(std::integral_constant<int, kKvBf16>{});
+    else if (a.pool.type == kKvFp8) of(std::integral_constant<int, kKvFp8>{});
+    else of(std::integral_constant<int, kKvInt8>{});
+    return hipGetLastError();
+}
+extern template hipError_t launch_attend_both<64>(const AttendArgs&, const AttendPlan&, const AttendPlan&, hipStream_t);
+extern template hipError_t launch_attend_both<96>(const AttendArgs&, const AttendPlan&, const AttendPlan&, hipStream_t);
+extern template hipError_t launch_attend_both<128>(const AttendArgs&, const AttendPlan&, const AttendPlan&, hipStream_t);
 
 template <int DP, int MODE>
 hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
     const dim3 grid((unsigned)(p.group_shift < 6 ? p.workers : (p.workers + 7) & ~7)), block(p.waves * 64);
     auto go = [&](auto ct) {
         constexpr int CT = decltype(ct)::value;
-        constexpr bool HERE = MODE != kPrefix;
+        constexpr bool HERE = MODE == kWhole;
         if (a.dtype == 0) {
             if (HERE && p.join_here) k_attend<DP, CT, 1, true, HERE, MODE><<<grid, block, 0, s>>>(a, p);
             else if (p.group_shift == 4) k_attend<DP, CT, 1, true, false, MODE><<<grid, block, 0, s>>>(a, p);

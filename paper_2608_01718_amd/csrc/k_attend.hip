@@ -8,7 +8,6 @@ constexpr int kJoinThreads = 256;
 constexpr int64_t kMostItems = INT32_MAX / 2;  // chunks of tiles of all row groups
 
 // Many row groups, of few parts each: a thread four columns of a row, part after part (four loaded together).
-template <int MODE>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, AttendPlan p) {
     const AttendSplit s = p.split[blockIdx.x];
     const int dp = a.pool.dp, lanes = dp / 4, rows = 256 / lanes;
@@ -30,14 +29,13 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, AttendPlan p)
             for (int u = 0; u < 4; ++u)
                 if (k0 + u < parts) x.add(ml[u].x, ml[u].y, o[u]);
         }
-        store_joined<MODE>(a, p, s, row, col, x);
+        store_joined(a, p, s, row, col, x);
     }
 }
 
 // Few row groups, often of many parts each: the workgroups (x, .) join those that ended with one of `of` workers, each a
 // share of the rows.  The j-th of these workers is number (x + j) mod gridDim.x of the j-th gridDim.x of all, so that
 // neighbours among the workers, and those in regular steps, go to different workgroups.
-template <int MODE>
 __global__ __launch_bounds__(kJoinThreads) void k_attend_join_few(AttendArgs a, AttendPlan p, int of) {
     __shared__ f32x4 scratch[kJoinThreads * 3 / 2];
     auto worker = [&](int j) { return j * (int)gridDim.x + (int)((blockIdx.x + j) % gridDim.x); };
@@ -49,7 +47,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_attend_join_few(AttendArgs a, 
         int of_row = 1;
         while (2 * of_row <= groups && (8 * of_row <= s.parts || (4 * of_row <= s.parts && 2 * of_row * s.n_rows <= groups)))
             of_row *= 2;
-        join_rows<kJoinThreads, MODE>(a, p, s, a.pool.dp, of_row, threadIdx.x, blockIdx.y, gridDim.y, scratch,
+        join_rows<kJoinThreads>(a, p, s, a.pool.dp, of_row, threadIdx.x, blockIdx.y, gridDim.y, scratch,
                                 [&](int64_t at, int col, float2& ml, f32x4& o) {
                                     ml = p.part_ml[at];
                                     o = *(const f32x4*)(p.part_o + at * a.pool.dp + col);
@@ -74,13 +72,13 @@ Shape shape_of(const KvPool& pool, bool f32, int64_t rows) {
 }
 
 // The plan of a launch whose workspace begins at `space`, and the bytes it takes.
-AttendPlan plan_of(const KvPool& pool, bool f32, int max_new, int group, int num_cu, char* space, int64_t* bytes) {
+AttendPlan plan_of(const KvPool& pool, bool f32, int max_new, int group, int num_cu, char* space, int64_t* bytes, int occupancy = 0) {
     AttendPlan p{};
     // (the rows of a (sequence, kv head), if no bound is known: plenty)
     const Shape sh = shape_of(pool, f32, (int64_t)(max_new > 0 ? max_new : 64) * group);
     p.group_shift = sh.group_shift;
     p.waves = sh.waves;
-    p.workers = num_cu * sh.occupancy;
+    p.workers = num_cu * (occupancy ? occupancy : sh.occupancy);
     p.workers = p.workers < kMaxWorkers ? p.workers : kMaxWorkers;
     // (the counters first: at the same place in every launch)
     const int64_t done = 4 * kMaxWorkers, split = (int64_t)sizeof(AttendSplit) * p.workers;
@@ -113,9 +111,10 @@ int64_t attend_workspace(const KvPool& pool, int dtype, int q_heads, int max_new
 
 namespace {
 
-// The launches of one mode.  n_seq: what the mode counts as sequences; max_new: a bound (kPrefix: an average) on the rows of each.
+// What a mode's launch works with besides its plan.  n_seq: what the mode counts as sequences; max_new: a bound (kPrefix: an
+// average) on the rows of each.
 template <int MODE>
-hipError_t launch_mode(const AttendArgs& a, AttendPlan p, int n_seq, int64_t max_new, hipStream_t s) {
+void prepare(const AttendArgs& a, AttendPlan& p, int n_seq, int64_t max_new) {
     // row / group for rows below 2^31: magic = ceil(2^(31 + bits) / group), bits = ceil(log2 group)
     int bits = 0;
     while ((1 << bits) < a.group) ++bits;
@@ -125,6 +124,11 @@ hipError_t launch_mode(const AttendArgs& a, AttendPlan p, int n_seq, int64_t max
     const int64_t tiles = ((int64_t)a.seqs.max_pages << (a.pool.page_shift - 5)) + 1;
     const int64_t units = row_groups(a.pool, a.seqs.rows, n_seq, a.group, p.group_shift);
     while (units * (((tiles - 1) >> p.chunk_shift) + 1) > kMostItems && p.chunk_shift < 30) ++p.chunk_shift;
+    // Behind a shared prefix many sequences have a few tiles of their own, and beginning and ending a row group takes as long
+    // as some tiles: it counts for as many more, so that workgroups get as much to do (64 sequences with 16 to 2048 tokens of
+    // their own, 8 heads: 47 us by tiles alone, 30, 27, 28 and 32 with 4, 8, 12 and 20 more).
+    constexpr int kExtra = 8;
+    if (MODE == kOwn && units * (tiles + kExtra) <= kMostItems) p.extra = kExtra;
     // Small calls join their parts in the launch: where each wave has a tile at most, by what the page tables (or the
     // window) can hold, and a row group has few parts.  One launch less is 2 us on the host and 1 us on the GPU (one sequence of
     // 777 tokens, 8 heads 11.5 us, 13.7 in two); with more parts to join, or parts of many rows, the launch is faster (131,071
@@ -132,13 +136,11 @@ hipError_t launch_mode(const AttendArgs& a, AttendPlan p, int n_seq, int64_t max
     // tokens, 260 parts 19, 53; of 1000 tokens 13.4, 10.5).
     const int64_t seen = a.window > 0 && a.window / 32 + 2 + max_new / 32 < tiles && max_new > 0
                              ? a.window / 32 + 2 + max_new / 32 : tiles;
-    p.join_here = MODE != kPrefix && p.group_shift == 4 && seen <= 64 && units * seen <= 4 * (int64_t)p.workers;
-    const hipError_t e = a.pool.dp == 64    ? launch_attend<64, MODE>(a, p, s)
-                         : a.pool.dp == 96  ? launch_attend<96, MODE>(a, p, s)
-                         : a.pool.dp == 128 ? launch_attend<128, MODE>(a, p, s)
-                         : a.pool.dp == 192 ? launch_attend<192, MODE>(a, p, s)
-                                            : launch_attend<256, MODE>(a, p, s);
-    if (e != hipSuccess || p.join_here) return e;
+    p.join_here = MODE == kWhole && p.group_shift == 4 && seen <= 64 && units * seen <= 4 * (int64_t)p.workers;
+}
+
+// The join of a whole attention's parts.
+hipError_t launch_join(const AttendArgs& a, const AttendPlan& p, int n_seq, int64_t max_new, hipStream_t s) {
     // rows of a row group, row groups
     int64_t rows = (max_new <= 0 ? 64 : max_new < a.seqs.rows ? max_new : a.seqs.rows) * a.group;
     const int64_t live = n_seq < a.seqs.rows ? n_seq : a.seqs.rows;
@@ -146,7 +148,7 @@ hipError_t launch_mode(const AttendArgs& a, AttendPlan p, int n_seq, int64_t max
     rows = rows < (1 << p.group_shift) ? rows : 1 << p.group_shift;
     const int64_t lane_groups = kJoinThreads / (a.pool.dp / 4);
     if (groups_most >= 64) {
-        k_attend_join<MODE><<<dim3((unsigned)p.workers, (unsigned)((rows + lane_groups - 1) / lane_groups)), dim3(kJoinThreads),
+        k_attend_join<<<dim3((unsigned)p.workers, (unsigned)((rows + lane_groups - 1) / lane_groups)), dim3(kJoinThreads),
                               0, s>>>(a, p);
     } else {
         // About one row group that was split for each workgroup in x, and one pass over its rows, but no more than 2048
@@ -161,9 +163,21 @@ hipError_t launch_mode(const AttendArgs& a, AttendPlan p, int n_seq, int64_t max
         for (int64_t of_row = 1; at_once > 1 && 8 * of_row <= parts; of_row *= 2) at_once /= 2;
         int64_t y = (rows + at_once - 1) / at_once;
         y = y < 2048 / x ? y : 2048 / x;
-        k_attend_join_few<MODE><<<dim3((unsigned)x, (unsigned)(y > 1 ? y : 1)), dim3(kJoinThreads), 0, s>>>(a, p, of);
+        k_attend_join_few<<<dim3((unsigned)x, (unsigned)(y > 1 ? y : 1)), dim3(kJoinThreads), 0, s>>>(a, p, of);
     }
     return hipGetLastError();
+}
+
+// The launches of one mode.
+template <int MODE>
+hipError_t launch_mode(const AttendArgs& a, AttendPlan p, int n_seq, int64_t max_new, hipStream_t s) {
+    prepare<MODE>(a, p, n_seq, max_new);
+    const hipError_t e = a.pool.dp == 64    ? launch_attend<64, MODE>(a, p, s)
+                         : a.pool.dp == 96  ? launch_attend<96, MODE>(a, p, s)
+                         : a.pool.dp == 128 ? launch_attend<128, MODE>(a, p, s)
+                         : a.pool.dp == 192 ? launch_attend<192, MODE>(a, p, s)
+                                            : launch_attend<256, MODE>(a, p, s);
+    return e != hipSuccess || p.join_here || MODE != kWhole ? e : launch_join(a, p, n_seq, max_new, s);
 }
 
 }  // namespace
@@ -199,9 +213,18 @@ __global__ __launch_bounds__(64) void k_attend_share(AttendArgs a, AttendShare x
         for (int i = 0; i < x.n_groups; i += 64) count += __popcll(__ballot(i + lane < x.n_groups && group[i + lane] <= b));
         int from = 0, to = 0;
         const int held = count > 0 ? group_of(count - 1, from, to) : 0;
-        if (lane == 0) x.held[b] = b >= from && b < to ? held : 0;
+        const int mine = b >= from && b < to ? held : 0;
+        if (lane == 0) x.held[b] = mine;
         const KvSpan s = span_of(a.seqs, b);
-        for (int i = lane; i < s.n; i += 64) x.row_pos[s.row0 + i] = s.pos0 + i < 0 ? -1 : (int)(s.pos0 + i);
+        for (int i = lane; i < s.n; i += 64) {
+            x.row_pos[s.row0 + i] = s.pos0 + i < 0 ? -1 : (int)(s.pos0 + i);
+            x.row_held[s.row0 + i] = mine > 0;
+        }
+        // rows of no sequence
+        if (b == 0)
+            for (int64_t i = lane; i < s.row0; i += 64) x.row_held[i] = -1;
+        if (b == n_seq - 1)
+            for (int64_t i = s.row0 + s.n + lane; i < a.seqs.rows; i += 64) x.row_held[i] = -1;
         return;
     }
     const int g = blockIdx.x - n_seq;
@@ -221,6 +244,57 @@ __global__ __launch_bounds__(64) void k_attend_share(AttendArgs a, AttendShare x
     }
 }
 
+// Puts the two parts of every (row, query head) together: dp / 4 lanes on four columns each, of_row lane groups (a power of two)
+// one after another on the parts that workers have of it.
+template <bool F32>
+__global__ __launch_bounds__(256) void k_attend_together(AttendArgs a, AttendPlan prefix, AttendPlan own, int of_row) {
+    __shared__ f32x4 sums[256];
+    __shared__ float2 ml_of[256];
+    const int dp = a.pool.dp, lanes = dp / 4, rows = 256 / lanes / of_row, g = threadIdx.x / lanes, sub = g % of_row;
+    const int col = threadIdx.x % lanes * 4;
+    const AttendShare& x = own.share;
+    const int64_t all = a.seqs.rows * a.q_heads;
+    for (int64_t at0 = (int64_t)blockIdx.x * rows; at0 < all; at0 += (int64_t)gridDim.x * rows) {
+        const int64_t at = at0 + g / of_row;
+        const int held = g < rows * of_row && at < all ? x.row_held[at / a.q_heads] : -1;
+        Joined j;
+        if (held >= 0) {
+            const int2 of_own = x.sums[kOwn - kPrefix].at[at], of_prefix = held ? x.sums[0].at[at] : make_int2(0, 0);
+            const int n_own = of_own.x ? of_own.x : 1, n = n_own + (!held ? 0 : of_prefix.x ? of_prefix.x : 1);
+            for (int k0 = sub; k0 < n; k0 += 4 * of_row) {
+                float2 ml[4];
+                f32x4 o[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int k = k0 + i * of_row < n ? k0 + i * of_row : n - 1;
+                    const bool mine = k < n_own;
+                    const AttendPlan& p = mine ? own : prefix;
+                    const AttendSums& whole = x.sums[mine ? kOwn - kPrefix : 0];
+                    const int2 w = mine ? of_own : of_prefix;
+                    const int part = mine ? k : k - n_own;
+                    const int64_t slot = part_of(p, (w.y & 0xFFFF) + part, part < w.x - 1) + (w.y >> 16);
+                    ml[i] = w.x ? p.part_ml[slot] : whole.ml[at];
+                    o[i] = *(const f32x4*)(w.x ? p.part_o + slot * dp + col : whole.o + at * dp + col);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (k0 + i * of_row < n) j.add(ml[i].x, ml[i].y, o[i]);
+            }
+        }
+        if (of_row > 1) {
+            __syncthreads();
+            sums[threadIdx.x] = j.o;
+            ml_of[threadIdx.x] = make_float2(j.m, j.l);
+            __syncthreads();
+        }
+        if (held < 0 || sub > 0) continue;
+        for (int k = 1; k < of_row; ++k)
+            j.add(ml_of[threadIdx.x + k * lanes].x, ml_of[threadIdx.x + k * lanes].y, sums[threadIdx.x + k * lanes]);
+        if (col < a.pool.d) store4<F32>(a, at * a.pool.d + col, j.o * (j.l == 0.0f ? 0.0f : 1.0f / j.l));
+        if (col == 0 && a.lse) a.lse[at] = lse_of(j.m, j.l);
+    }
+}
+
 namespace {
 
 int prefix_rows(int64_t rows, int n_groups) {  // of a group, on average
@@ -228,28 +302,44 @@ int prefix_rows(int64_t rows, int n_groups) {  // of a group, on average
     return each < 1 ? 1 : (int)each;
 }
 
-// The plans of both launches, which use the same memory one after the other, and what lies behind it.
+// Whether both parts are in one launch: few rows of own tokens, and many or few over the prefixes, with room for two workgroups
+// on a compute unit.
+bool both_at_once(const KvPool& pool, bool f32, const AttendPlan& prefix, const AttendPlan& own) {
+    return pool.dp <= 128 && own.group_shift == 4 && (prefix.group_shift == 4 || prefix.group_shift == (f32 ? 6 : 7)) &&
+           attend_occupancy(pool.dp, pool.type != kKvBf16, 1, f32) >= 2;
+}
+
+// The plans of both parts, and what lies behind their memory.
 int64_t shared_plan(const KvPool& pool, bool f32, int64_t rows, int n_seq, int n_groups, int q_heads, int max_new, int num_cu,
-                    char* space, AttendPlan* prefix, AttendPlan* own) {
+                    char* space, AttendPlan* prefix, AttendPlan* own, bool* both) {
     const int group = q_heads / pool.heads;
-    int64_t one, two;
-    *prefix = plan_of(pool, f32, prefix_rows(rows, n_groups), group, num_cu, space, &one);
-    *own = plan_of(pool, f32, max_new, group, num_cu, space, &two);
-    int64_t at = one > two ? one : two;
+    int64_t at, bytes;
     auto take = [&](int64_t n) {
         at = (at + 15) & ~int64_t(15);
         char* p = space + at;
         at += n;
         return p;
     };
+    auto plans = [&](int occupancy) {
+        *prefix = plan_of(pool, f32, prefix_rows(rows, n_groups), group, num_cu, space, &at, occupancy);
+        *own = plan_of(pool, f32, max_new, group, num_cu, take(0), &bytes, occupancy);
+        at += bytes;
+    };
+    plans(0);
+    *both = n_groups > 0 && both_at_once(pool, f32, *prefix, *own);
+    if (*both) plans(1);
     AttendShare x{};
     x.n_groups = n_groups;
     x.span = (int4*)take(16 * (int64_t)n_groups);
     x.first = (int32_t*)take(4 * (int64_t)n_groups);
     x.held = (int32_t*)take(4 * (int64_t)n_seq);
     x.row_pos = (int32_t*)take(4 * rows);
-    x.ml = (float2*)take(8 * rows * q_heads);
-    x.o = (float*)take(4 * rows * q_heads * pool.dp);
+    x.row_held = (int32_t*)take(4 * rows);
+    for (AttendSums& y : x.sums) {
+        y.ml = (float2*)take(8 * rows * q_heads);
+        y.at = (int2*)take(8 * rows * q_heads);
+        y.o = (float*)take(4 * rows * q_heads * pool.dp);
+    }
     prefix->share = own->share = x;
     return at;
 }
@@ -264,19 +354,42 @@ bool attend_shared_fits(const KvPool& pool, int dtype, int64_t rows, int n_group
 int64_t attend_shared_workspace(const KvPool& pool, int dtype, int64_t rows, int n_seq, int n_groups, int q_heads, int max_new,
                                 int num_cu) {
     AttendPlan p, o;
-    return shared_plan(pool, dtype == 0, rows, n_seq, n_groups, q_heads, max_new, num_cu, nullptr, &p, &o);
+    bool both;
+    return shared_plan(pool, dtype == 0, rows, n_seq, n_groups, q_heads, max_new, num_cu, nullptr, &p, &o, &both);
 }
 
 hipError_t launch_kv_attend_shared(const AttendArgs& a, const int32_t* group, const int32_t* len, int n_groups, int max_new,
                                    void* workspace, int num_cu, hipStream_t s) {
     if (a.seqs.rows <= 0 || a.seqs.n_seq <= 0) return hipSuccess;
     AttendPlan prefix, own;
-    shared_plan(a.pool, a.dtype == 0, a.seqs.rows, a.seqs.n_seq, n_groups, a.q_heads, max_new, num_cu, (char*)workspace, &prefix, &own);
+    bool both;
+    shared_plan(a.pool, a.dtype == 0, a.seqs.rows, a.seqs.n_seq, n_groups, a.q_heads, max_new, num_cu, (char*)workspace, &prefix, &own,
+                &both);
+    const int each = prefix_rows(a.seqs.rows, n_groups);
     k_attend_share<<<dim3((unsigned)(a.seqs.n_seq + n_groups)), dim3(64), 0, s>>>(a, prefix.share, group, len);
     hipError_t e = hipGetLastError();
-    if (e == hipSuccess && n_groups > 0) e = launch_mode<kPrefix>(a, prefix, n_groups, prefix_rows(a.seqs.rows, n_groups), s);
-    if (e == hipSuccess) e = launch_mode<kOwn>(a, own, a.seqs.n_seq, max_new, s);
-    return e;
+    if (both) {
+        prepare<kPrefix>(a, prefix, n_groups, each);
+        prepare<kOwn>(a, own, a.seqs.n_seq, max_new);
+        if (e == hipSuccess)
+            e = a.pool.dp == 64   ? launch_attend_both<64>(a, prefix, own, s)
+                : a.pool.dp == 96 ? launch_attend_both<96>(a, prefix, own, s)
+                                  : launch_attend_both<128>(a, prefix, own, s);
+    } else {
+        if (e == hipSuccess && n_groups > 0) e = launch_mode<kPrefix>(a, prefix, n_groups, each, s);
+        if (e == hipSuccess) e = launch_mode<kOwn>(a, own, a.seqs.n_seq, max_new, s);
+    }
+    if (e != hipSuccess) return e;
+    // the parts of a row, about: its row group's share of the workers over the prefixes, and a few of its own; four to a lane group
+    const int64_t groups_of = n_groups > 0 ? (((int64_t)each * a.group >> prefix.group_shift) + 1) * n_groups * a.pool.heads : 1;
+    const int64_t parts = (n_groups > 0 ? prefix.workers / groups_of : 0) + 2;
+    int of_row = 1;
+    while (4 * of_row < parts && 2 * of_row <= 256 / (a.pool.dp / 4)) of_row *= 2;
+    const int rows = 256 / (a.pool.dp / 4) / of_row;
+    const dim3 grid((unsigned)grid_blocks((a.seqs.rows * a.q_heads + rows - 1) / rows));
+    if (a.dtype == 0) k_attend_together<true><<<grid, dim3(256), 0, s>>>(a, prefix, own, of_row);
+    else k_attend_together<false><<<grid, dim3(256), 0, s>>>(a, prefix, own, of_row);
+    return hipGetLastError();
 }
 
 }  // namespace lacache
