@@ -929,7 +929,7 @@ def lacache_kv_bounds_read(b: KVBounds, pages, out=None, stream=None):
     shape = (n, c.heads, c.d)
     given = out is not None
     if not given:
-        out = (_made(c.k, shape, torch.float32, stream), _made(c.k, shape, torch.float32, stream))
+        out = _made(c.k, (2, *shape), torch.float32, stream).unbind(0)
     else:
         _given(out[0], shape, torch.float32, c.index, "most")
         _given(out[1], shape, torch.float32, c.index, "least")

@@ -22,38 +22,42 @@ __global__ __launch_bounds__(256, (Attend<DP, CT, 1, F32>::OCC)) void k_attend_b
     const int unit = (int)(blockIdx.x / (unsigned)x.splits), split = (int)(blockIdx.x - (unsigned)unit * x.splits);
     const int list = unit / row_tiles, g0 = (unit - list * row_tiles) * 16;
     const int row = list / a.pool.heads, h = list - row * a.pool.heads;
+    const int32_t* blocks = x.blocks + (int64_t)list * x.n_blocks;
+    const int64_t tiles = (int64_t)x.n_blocks << tile_shift;
+    const int64_t end64 = (int64_t)(split + 1) * x.per;
+    const int end = (int)(end64 < tiles ? end64 : tiles);
+    // the wave's tiles t0, t0 + 4, ... of the list, a lane each: the first lanes' pages are on their way while the sequence is looked for
+    int t0 = split * x.per + wid;
+    auto listed = [&]() {
+        const int t = t0 + lane * 4;
+        return t < end ? blocks[t >> tile_shift] : -1;
+    };
+    int block = listed();
     const int b = sequence_of(a.seqs, row, lane);
     if (b < 0) return;
     const KvSpan span = span_of(a.seqs, b);
     const int64_t pos64 = span.pos0 + (row - span.row0);
     const int pos = pos64 < 0 ? -1 : (int)pos64, n_rows = a.group - g0 < 16 ? a.group - g0 : 16;
-    const int32_t* blocks = x.blocks + (int64_t)list * x.n_blocks;
     const int32_t* pages = a.seqs.pages + (int64_t)b * a.seqs.max_pages;
-    const int64_t tiles = (int64_t)x.n_blocks << tile_shift;
-    const int64_t end64 = (int64_t)(split + 1) * x.per;
-    const int end = (int)(end64 < tiles ? end64 : tiles);
-
     A w;
     typename A::Tile tile;
     w.clear();
-    int t0 = split * x.per + wid, page = -1, index = 0, there = 0;
+    int page = -1, index = 0, there = 0;
     uint64_t todo = 0;
-    auto load_pages = [&]() {  // the wave's tiles t0, t0 + 4, ... of the list, a lane each
-        const int t = t0 + lane * 4;
+    auto load_pages = [&]() {
         page = -1;
-        if (t < end) {
-            const int block = blocks[t >> tile_shift];
-            if (block >= 0 && block < a.seqs.max_pages && (int64_t)block << a.pool.page_shift <= pos64) {
-                index = (block << tile_shift) + (t & ((1 << tile_shift) - 1));
-                if (32 * index <= pos) page = pages[block];
-            }
+        if (block >= 0 && block < a.seqs.max_pages && (int64_t)block << a.pool.page_shift <= pos64) {
+            index = (block << tile_shift) + ((t0 + lane * 4) & ((1 << tile_shift) - 1));
+            if (32 * index <= pos) page = pages[block];
         }
-        todo = __ballot(page >= 0 && page < a.pool.n_pages);
     };
+    auto look = [&]() { todo = __ballot(page >= 0 && page < a.pool.n_pages); };
     auto next = [&]() {
         while (!todo && t0 + 256 < end) {
             t0 += 256;
+            block = listed();
             load_pages();
+            look();
         }
         there = todo ? 1 : 0;
         const int k = there ? __ffsll((unsigned long long)todo) - 1 : 0;
@@ -67,8 +71,10 @@ __global__ __launch_bounds__(256, (Attend<DP, CT, 1, F32>::OCC)) void k_attend_b
     p.group_magic = x.magic, p.group_bits = x.bits, p.group_shift = 4;
     AttendSpan s{};
     s.row0 = row, s.n = 1, s.len = pos + 1, s.rows = a.group;
-    w.load_q(a, p, s, h, g0, 16, lane);
+    w.load_q(a, p, s, h, g0, 16, lane);  // while the page numbers are on their way
     const float scale2 = scale_of(a);
+    __builtin_amdgcn_sched_barrier(0);
+    look();
     {
         const int64_t place = next();
         A::load_k(tile, a, place, there, lane);
