@@ -473,7 +473,7 @@ namespace {
 
 // The token of sequence b, by a workgroup.  WIDE: r's sums were written in this launch, and are read device-wide.
 template <int NV, bool F32, bool WIDE>
-__device__ __forceinline__ void pick(const DraftArgs& a, int b, const Heat& heat, const DraftRow& row) {
+__device__ __forceinline__ void pick(const DraftArgs& a, int b, const Heat& heat, const DraftRow& row, const Scales& f) {
     __shared__ double lds[kThreads / 64], lead[2];
     __shared__ int found[kThreads / 64][2], chosen;
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
@@ -492,7 +492,7 @@ __device__ __forceinline__ void pick(const DraftArgs& a, int b, const Heat& heat
     }
     // Finds the thread whose share `own` (in the order of threads) takes the running sum past `goal` (the last one with a
     // share if none does), or past goal times all of it: who it is, the sum before it, the goal (in lead[1]).
-    auto find = [&](double own, double goal, bool whole, double& before) {
+    auto find = [&](double own, double goal, bool whole, double& before, double& total) {
         double upto = own;
 #pragma unroll
         for (int o = 1; o < 64; o *= 2) {
@@ -502,7 +502,8 @@ __device__ __forceinline__ void pick(const DraftArgs& a, int b, const Heat& heat
         __syncthreads();
         if (lane == 63) lds[wid] = upto;
         __syncthreads();
-        double total = 0.0, ahead = 0.0;
+        double ahead = 0.0;
+        total = 0.0;
 #pragma unroll
         for (int i = 0; i < kThreads / 64; ++i) {
             ahead += i < wid ? lds[i] : 0.0;
@@ -528,20 +529,21 @@ __device__ __forceinline__ void pick(const DraftArgs& a, int b, const Heat& heat
         if (tid == who) lead[1] = goal;
         return who;
     };
-    const Scales f = scales_of(a, b, row.has_q, lane);
     const int each = (a.pieces + kThreads - 1) / kThreads, first = tid * each;
     const int end = first + each < a.pieces ? first + each : a.pieces;
     double all = 0.0;
     for (int i = first; i < end; ++i) all += rest(i);
     bool with_q = row.has_q;
-    if (with_q && !(all_threads<kThreads>(all, lds, Add64{}) > 0x1p-30)) {  // p and q are the same: the token is drawn from p
+    double before, total;
+    int who = find(all, (double)a.u_next[b], true, before, total);
+    if (with_q && !(total > 0x1p-30)) {  // p and q are the same: the token is drawn from p
         with_q = false;
         all = 0.0;
         for (int i = first; i < end; ++i) all += sums[i].x;
+        __syncthreads();
+        who = find(all, (double)a.u_next[b], true, before, total);
     }
     const bool shares = row.has_q && !with_q;  // sums are S_p's, not r's
-    double before;
-    int who = find(all, (double)a.u_next[b], true, before);
     if (who < 0) {
         if (tid == 0) a.next_token[b] = -1;
         return;
@@ -575,7 +577,7 @@ __device__ __forceinline__ void pick(const DraftArgs& a, int b, const Heat& heat
             own += r[e];
         }
     }
-    who = find(own, goal, false, before);
+    who = find(own, goal, false, before, total);
     if (tid == who) {
         int64_t token = -1;
         bool past = false;
@@ -606,6 +608,7 @@ __global__ __launch_bounds__(kThreads) void k_draft_rest(DraftArgs a) {
         if (TOGETHER && p.w == 0 && lane == 0) a.next_token[p.b] = -1;
         return;
     }
+    Scales f{};
     if (p.live) {
         const int64_t v0 = (int64_t)p.w * (NV * 512);
         const bool inside = v0 + NV * 512 <= a.V;
@@ -621,7 +624,7 @@ __global__ __launch_bounds__(kThreads) void k_draft_rest(DraftArgs a) {
                 for (int e = 7; e >= 0; --e) s = x[i][e] == row.mt ? (double)(v0 + i * 512 + lane * 8 + e) : s;
             s = wave_reduce(s, [](double p, double q) { return fmin(p, q); });
         } else {
-            const Scales f = scales_of(a, p.b, row.has_q, lane);
+            f = scales_of(a, p.b, row.has_q, lane);
             s = 0.0;
             if (row.has_q) {
 #pragma unroll
@@ -644,6 +647,7 @@ __global__ __launch_bounds__(kThreads) void k_draft_rest(DraftArgs a) {
         }
     }
     if constexpr (TOGETHER) {
+        if (!p.live && !heat.greedy) f = scales_of(a, p.b, row.has_q, lane);
         __shared__ int last;
         last_workgroup_wait();
         __syncthreads();
@@ -651,7 +655,7 @@ __global__ __launch_bounds__(kThreads) void k_draft_rest(DraftArgs a) {
             last = __hip_atomic_fetch_add(a.done + p.b, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
                    (uint32_t)((a.pieces + kThreads / 64 - 1) / (kThreads / 64)) - 1;
         __syncthreads();
-        if (last) pick<NV, F32, true>(a, p.b, heat, row);
+        if (last) pick<NV, F32, true>(a, p.b, heat, row, f);
     }
 }
 
@@ -660,8 +664,14 @@ template <int NV, bool F32>
 __global__ __launch_bounds__(kThreads) void k_draft_pick(DraftArgs a) {
     const int b = blockIdx.x;
     const DraftRow row = a.rows[b];
-    if (row.has_p) pick<NV, F32, false>(a, b, heat_of(a, b), row);
-    else if (threadIdx.x == 0) a.next_token[b] = -1;
+    if (!row.has_p) {
+        if (threadIdx.x == 0) a.next_token[b] = -1;
+        return;
+    }
+    const Heat heat = heat_of(a, b);
+    Scales f{};
+    if (!heat.greedy) f = scales_of(a, b, row.has_q, threadIdx.x & 63);
+    pick<NV, F32, false>(a, b, heat, row, f);
 }
 
 namespace {
