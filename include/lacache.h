@@ -566,8 +566,10 @@ typedef struct {
  * results to rounding, the prefix of a group read once for all of its rows
  * (through the page table of its first sequence).  The other arguments are those
  * of lacache_kv_attend.
- *   workspace  lacache_kv_attend_shared_workspace bytes, under the rules of
- *              lacache_kv_attend's; the calls may share one.
+ *   workspace  lacache_kv_attend_shared_workspace bytes of device memory (about
+ *              8 rows q_heads D, for the sums of both parts), 16-byte aligned, in
+ *              any state, for one call at a time.  It may be lacache_kv_attend's:
+ *              that call's counters stay as they are.
  * n_groups is at most 2^20, n_seq too.
  */
 int64_t lacache_kv_attend_shared_workspace(const lacache_kv *kv, lacache_dtype dtype, int64_t rows, int32_t n_seq,

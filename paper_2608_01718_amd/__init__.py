@@ -901,12 +901,10 @@ def lacache_kv_attend_shared(c: KVCache, q, seqs: Sequences, prefixes: Prefixes,
     need = c._need.get(key)
     if need is None:
         need = c._need[key] = lacache_kv_attend_shared_workspace(c, *key[1:])
-    space = c._space
-    if space is None or space.numel() < need:
-        space = c._scratch(q, need, stream)
+    space = _made(q, (need,), torch.uint8, stream)  # (all rows' sums: too much to keep for the largest call)
     _check(_on(index, stream, _lib.lacache_kv_attend_shared, c._ref, seqs._ref, prefixes._ref, q.data_ptr(), dtype, rows, q_heads,
                q_row, max_new, c.d ** -0.5 if scale is None else scale, window, out[0].data_ptr(), out[1].data_ptr(),
-               space.data_ptr(), space.numel()), "lacache_kv_attend_shared")
+               space.data_ptr(), need), "lacache_kv_attend_shared")
     if given:
         _written(out)
     return out

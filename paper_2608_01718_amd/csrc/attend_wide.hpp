@@ -62,7 +62,8 @@ __device__ __forceinline__ void attend_wide(const AttendArgs& a, const AttendPla
     const int tile_shift = a.pool.page_shift - 5;
     AttendSpan s = attend_span<MODE>(a, p, range.b);
 
-    while (attend_next<MODE>(a, p, range, s)) {
+    bool more = MODE != kOwn || attend_next<MODE>(a, p, range, s);
+    while (more) {
         // the segment that begins at item range.at
         const int rel = range.at - range.before;
         const int unit = (int)((uint32_t)rel / (uint32_t)s.stride), c0 = rel - unit * s.stride;
@@ -268,7 +269,8 @@ __device__ __forceinline__ void attend_wide(const AttendArgs& a, const AttendPla
                 if (u == 0 && a.lse) a.lse[at] = lse_of(w.m[r], w.l[r]);
             }
         }
-        lds_barrier();  // the buffers have been read
+        more = attend_next<MODE>(a, p, range, s);
+        if (more) lds_barrier();  // the buffers have been read
     }
     if (MODE == kWhole && tid == 0) p.split[worker] = split;
 }
