@@ -174,14 +174,29 @@ __device__ __forceinline__ Stat join_chunks(const DraftArgs& a, int64_t row, dou
     const float2* part = a.stats + row * a.chunks;
     auto max2 = [](float x, float y) { return fmaxf(x, y); };
     auto add2 = [](double x, double y) { return x + y; };
+    // (four at a time on their way, kept for the sum where that is all)
+    float2 x[4];
+    auto load = [&](int i0) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int i = i0 + 16 * k + (threadIdx.x & 15);
+            x[k] = i < a.chunks ? part[i] : make_float2(-__builtin_inff(), 0.0f);
+        }
+    };
     float m = -__builtin_inff();
-    for (int i = threadIdx.x & 15; i < a.chunks; i += 16) m = fmaxf(m, part[i].x);
+    for (int i0 = 0; i0 < a.chunks; i0 += 64) {
+        load(i0);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) m = fmaxf(m, x[k].x);
+    }
     m = xor_combine<1>(xor_combine<2>(xor_combine<4>(xor_combine<8>(m, max2), max2), max2), max2);
     double s = 0.0;
     const bool fine = m < __builtin_inff() && m > -__builtin_inff();
-    for (int i = threadIdx.x & 15; i < a.chunks; i += 16) {
-        const float2 x = part[i];
-        s += x.y * (fine && x.x > -__builtin_inff() ? exp2_64(((double)x.x - m) * c) : 1.0);
+    for (int i0 = 0; i0 < a.chunks; i0 += 64) {
+        if (a.chunks > 64) load(i0);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            s += x[k].y * (fine && x[k].x > -__builtin_inff() ? exp2_64(((double)x[k].x - m) * c) : 1.0);
     }
     s = xor_combine<1>(xor_combine<2>(xor_combine<4>(xor_combine<8>(s, add2), add2), add2), add2);
     return {m, fine && s > 0.0 && s < __builtin_inf() ? s : 0.0};
