@@ -78,14 +78,27 @@ __device__ inline KvSpan span_of(const KvSeqs& s, int b) {
     return {a, (int)(e - a), (int64_t)s.lens[b] - (e - a)};
 }
 
+// The last of n ascending numbers that is at most x, by all lanes of a wave: -1 if there is none.  Each step looks at up to 128
+// of them, the same distance apart.
+__device__ __forceinline__ int last_up_to(const int32_t* of, int n, int64_t x, int lane) {
+    for (int from = 0; n > 0;) {
+        const int apart = (int)(((int64_t)n + 127) >> 7);
+        const int64_t i = (int64_t)lane * apart, k = i + (int64_t)64 * apart;
+        const int low = of[from + (i < n ? i : 0)], high = of[from + (k < n ? k : 0)];
+        const int count = __popcll(__ballot(i < n && low <= x)) + __popcll(__ballot(k < n && high <= x));
+        if (count == 0) return from - 1;  // (in the first step, or where they do not ascend)
+        from += (count - 1) * apart;
+        if (apart == 1) return from;
+        n -= (count - 1) * apart;
+        n = n < apart ? n : apart;
+    }
+    return -1;
+}
+
 // The sequence of a row, by all lanes of a wave: -1 if it is none's.
 __device__ __forceinline__ int sequence_of(const KvSeqs& s, int64_t row, int lane) {
-    int count = 0;
-    for (int i = 0; i <= s.n_seq; i += 64) {
-        const bool at = i + lane <= s.n_seq && s.start[i + lane] <= row;
-        count += __popcll(__ballot(at));
-    }
-    return count > s.n_seq ? -1 : count - 1;
+    const int b = last_up_to(s.start, s.n_seq + 1, row, lane);
+    return b < s.n_seq ? b : -1;
 }
 
 __device__ inline float kv_value(const char* pool, int64_t i, int type) {

@@ -330,6 +330,31 @@ def test_attend_blocks_of_odd_lists(lc, kind):
     assert bool(((o.double() - want[0]).abs() <= eo).all()) and bool(((lse.double() - want[1]).abs() <= el).all())
 
 
+@pytest.mark.parametrize("count", [127, 128, 300, 17_000])
+def test_many_sequences(lc, count):
+    """More sequences than are looked at together, slots without rows among them: each row finds its own."""
+    lens, news = [20 + i % 41 for i in range(count)], [(i % 5 != 3) + (i % 97 == 5) for i in range(count)]
+    news[-1] = 0
+    pg = Paged(lc, "bf16", 1, 64, 32, count, 2, seed=count)
+    whole = pg.seqs(lens, lens)
+    k, v = (normals((sum(lens), 1, 64), i) for i in range(2))
+    pg.cache.append(k, v, whole)
+    held = list(zip(*(x.double().split(lens) for x in pg.cache.read(whole, sum(lens), dtype=torch.float32))))
+    b = lc.KVBounds(pg.cache)
+    b.update(whole, sum(lens))
+    q = normals((sum(news), 2, 64), seed=6)
+    seqs = pg.seqs(news, lens)
+    lists = b.select(q, seqs, 2)
+    last = torch.tensor([(n - m + i) // 32 for n, m in zip(lens, news) for i in range(m)])
+    assert lists[:, 0, 0].cpu().eq(0).all() and lists[:, 0, 1].cpu().equal(torch.where(last > 0, last, -1).to(torch.int32))
+    out = pg.cache.attend_blocks(q, seqs, lists)
+    first = torch.tensor([0, *news]).cumsum(0)
+    for a in {0, count // 2, max(0, count - 100)}:
+        e = min(count, a + 100)
+        at = slice(int(first[a]), int(first[e]))
+        check_blocks(lc, pg, held[a:e], q[at], news[a:e], lens[a:e], lists[at], out=(out[0][at], out[1][at]))
+
+
 @pytest.mark.parametrize("kind", ["bf16", "fp8"])
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_attend_blocks_leaves_out_what_is_not_listed(lc, kind, dtype):

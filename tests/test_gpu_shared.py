@@ -131,6 +131,24 @@ def test_groups_of_every_kind(lc, new, Hq):
     check_attend(lc, pg, same, q[:2 * new], [new] * 2, [300, 299], out=out)
 
 
+@pytest.mark.parametrize("count,each", [(390, 3), (260, 2), (900, 1), (17_000, 100)])
+def test_many_groups(lc, count, each):
+    """More groups and sequences than are looked at together, empty groups and slots without rows among them."""
+    lens = [70 + i % 40 for i in range(count)]
+    news = [i % 5 != 3 for i in range(count)]
+    groups = [(i, min(i + each, count), 64) for i in range(0, count, each) if i % 7]
+    pg, held = shared(lc, "bf16", 1, 64, 32, lens, groups, seed=each)
+    q = normals((sum(news), 2, 64), seed=6, dtype=torch.bfloat16)
+    p = prefixes(lc, groups)
+    seqs = pg.seqs(news, lens)
+    out = pg.cache.attend_shared(q, seqs, p, max_new=1)
+    first = torch.tensor([0, *news]).cumsum(0)
+    for a in {0, count // 2, max(0, count - 200)}:          # 200 sequences at a time
+        b = min(count, a + 200)
+        at = slice(int(first[a]), int(first[b]))
+        check_attend(lc, pg, held[a:b], q[at], news[a:b], lens[a:b], out=(out[0][at], out[1][at]))
+
+
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("new,Hq", [(1, 4), (1, 32), (21, 16)])
 def test_shared_pages_that_are_not_there(lc, kind, new, Hq):
