@@ -279,7 +279,8 @@ int lacache_accept_length(const void *logits, lacache_dtype dtype, int32_t V, co
  * is the target's row n the next token is -1, if it is the draft model's r = p_n.
  *   workspace     lacache_verify_workspace bytes of device memory, 16-byte aligned,
  *                 in any state, for one call at a time
- * B == 0 is a no-op.  k == 0 draws a token from each target row.
+ * The outputs overlap neither one another nor an input.  B == 0 is a no-op.
+ * k == 0 draws a token from each target row.
  */
 int64_t lacache_verify_workspace(int32_t V, int32_t B, int32_t k);
 int lacache_verify(const void *logits, const void *draft_logits, lacache_dtype dtype, int32_t V, int64_t t_seq,

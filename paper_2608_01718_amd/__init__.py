@@ -869,6 +869,13 @@ def lacache_kv_attend(c: KVCache, q, seqs: Sequences, scale=None, window: int = 
     return out
 
 
+def _keep(sizes: dict, key, need: int) -> int:
+    if len(sizes) >= 4096:  # (calls of ever other sizes)
+        sizes.clear()
+    sizes[key] = need
+    return need
+
+
 def lacache_kv_attend_shared_workspace(c: KVCache, dtype: int, rows: int, n_seq: int, n_groups: int, q_heads: int,
                                        max_new: int = 0) -> int:
     """Bytes of scratch that lacache_kv_attend_shared needs (dtype: F32 or BF16)."""
@@ -900,7 +907,7 @@ def lacache_kv_attend_shared(c: KVCache, q, seqs: Sequences, prefixes: Prefixes,
     key = ("shared", dtype, rows, seqs._c.n_seq, prefixes._c.n_groups, q_heads, max_new)
     need = c._need.get(key)
     if need is None:
-        need = c._need[key] = lacache_kv_attend_shared_workspace(c, *key[1:])
+        need = _keep(c._need, key, lacache_kv_attend_shared_workspace(c, *key[1:]))
     space = _made(q, (need,), torch.uint8, stream)  # (all rows' sums: too much to keep for the largest call)
     _check(_on(index, stream, _lib.lacache_kv_attend_shared, c._ref, seqs._ref, prefixes._ref, q.data_ptr(), dtype, rows, q_heads,
                q_row, max_new, c.d ** -0.5 if scale is None else scale, window, out[0].data_ptr(), out[1].data_ptr(),
@@ -959,14 +966,14 @@ def lacache_kv_select(b: KVBounds, q, seqs: Sequences, n_blocks: int, first: int
         raise ValueError(f"q: expected float32 or bfloat16 [rows, q_heads, d], and sequences on cuda:{index}")
     q_row = _rows(q, shape[1], c.d, index, kind, "q")
     given = out is not None
-    if n_blocks < 1:
-        raise ValueError("n_blocks: expected at least one")
+    if n_blocks < 1 or first < 0 or last < 0 or first + last > n_blocks:
+        raise ValueError("expected n_blocks >= 1, first >= 0, last >= 0 and first + last <= n_blocks")
     out = _given(out, (shape[0], c.heads, n_blocks), torch.int32, index, "out") if given else \
         _made(q, (shape[0], c.heads, n_blocks), torch.int32, stream)
     key = ("select", shape[0], seqs._c.max_pages)
     need = c._need.get(key)
     if need is None:
-        need = c._need[key] = lacache_kv_select_workspace(c, shape[0], seqs._c.max_pages)
+        need = _keep(c._need, key, lacache_kv_select_workspace(c, shape[0], seqs._c.max_pages))
     space = _made(q, (need,), torch.uint8, stream)
     _check(_on(index, stream, _lib.lacache_kv_select, c._ref, b._ref, seqs._ref, q.data_ptr(), dtype, shape[0], shape[1], q_row,
                n_blocks, first, last, max_new, out.data_ptr(), space.data_ptr(), need), "lacache_kv_select")
@@ -1008,7 +1015,7 @@ def lacache_kv_attend_blocks(c: KVCache, q, seqs: Sequences, blocks, scale=None,
     key = ("blocks", rows, q_heads, n)
     need = c._need.get(key)
     if need is None:
-        need = c._need[key] = lacache_kv_attend_blocks_workspace(c, rows, q_heads, n)
+        need = _keep(c._need, key, lacache_kv_attend_blocks_workspace(c, rows, q_heads, n))
     space = c._space
     if need and (space is None or space.numel() < need):
         space = c._scratch(q, need, stream)
@@ -1076,7 +1083,7 @@ def lacache_verify(logits, draft_logits, draft_tokens, u_accept, u_next, tempera
         out = _made(logits, (2, B), torch.int32, stream).unbind(0) + _made(logits, (2, B, k), torch.float32, stream).unbind(0)
     need = _verify_need.get((V, B, k))
     if need is None:
-        need = _verify_need[V, B, k] = lacache_verify_workspace(V, B, k)
+        need = _keep(_verify_need, (V, B, k), lacache_verify_workspace(V, B, k))
     space = _made(logits, (need,), torch.uint8, stream)
     _check(_on(index, stream, _lib.lacache_verify, logits.data_ptr(), draft_logits.data_ptr(), kind, V, t_seq, t_row, d_seq,
                d_row, draft_tokens.data_ptr(), u_accept.data_ptr(), u_next.data_ptr(),

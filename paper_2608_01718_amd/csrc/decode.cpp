@@ -313,6 +313,17 @@ int lacache_verify(const void* logits, const void* draft_logits, lacache_dtype d
     if (k > 0 && (!draft_logits || !draft_tokens || !u_accept || !p_target || !p_draft || !aligned(draft_logits, esz) ||
                   !aligned(draft_tokens, 4) || !aligned(u_accept, 4) || !aligned(p_target, 4) || !aligned(p_draft, 4)))
         return LACACHE_EINVAL;
+    // (workgroups write a sequence's results while others still read what they are found from)
+    const struct {
+        const void* at;
+        int64_t n;
+    } used[] = {{accept_len, B}, {next_token, B}, {p_target, (int64_t)B * k}, {p_draft, (int64_t)B * k},  // written
+                {draft_tokens, (int64_t)B * k}, {u_accept, (int64_t)B * k}, {u_next, B}, {temperature, B}, {n_draft, B}};
+    for (int i = 0; i < 4; ++i)
+        for (int j = i + 1; j < 9; ++j) {
+            const uintptr_t x = (uintptr_t)used[i].at, y = (uintptr_t)used[j].at;
+            if (y && x < y + 4 * (uintptr_t)used[j].n && y < x + 4 * (uintptr_t)used[i].n) return LACACHE_EINVAL;
+        }
     DraftArgs a{};
     a.logits = (const char*)logits, a.draft_logits = (const char*)draft_logits;
     a.dtype = (int)dtype, a.V = V, a.B = B, a.k = k;

@@ -51,3 +51,13 @@ def test_binding_wants_gpu_tensors(lc):
     with pytest.raises(ValueError):
         lc.lacache_verify(x, x[:, :4], torch.zeros((2, 4), dtype=torch.int32), torch.zeros((2, 4)), torch.zeros(2))
     assert ctypes.sizeof(ctypes.c_void_p) == 8
+
+
+@pytest.mark.parametrize("out", ["accept_len", "next_token", "p", "q"])
+def test_outputs_that_overlap(lc, out):
+    at = {name: FAKE + 4096 * i for i, name in enumerate(
+        ("tokens", "u", "u_next", "temperature", "n_draft", "accept_len", "next_token", "p", "q"))}
+    for name in at:
+        if name != out:
+            for shift in (0, -4, 4):  # (two numbers or eight each)
+                assert call(lc, **{**at, out: at[name] + shift}) == EINVAL
