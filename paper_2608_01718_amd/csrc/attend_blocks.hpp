@@ -4,6 +4,9 @@
 // (row, kv head) has a list of its own, so that only its query heads share a tile: up to sixteen rows of an instruction.
 // Lists have the same room, known to the host: each is cut into `splits` equal ranges of tiles, a workgroup of four waves
 // each, and the workgroup that ends last joins their parts.
+//
+// Memory bounds it where there are many lists (64 rows of up to 48 pages of 64 tokens, 4 heads, fp8: 132 MB in 26 us, 5.0 TB/s;
+// 64 rows of 64 pages, 8 heads, bfloat16: 160 us, 6.7 TB/s), else the chain of list, table, tile and join (one row 9 us).
 #pragma once
 
 #include "attend.hpp"
