@@ -568,7 +568,8 @@ typedef struct {
  * (through the page table of its first sequence).  The other arguments are those
  * of lacache_kv_attend.
  *   workspace  lacache_kv_attend_shared_workspace bytes of device memory (about
- *              8 rows q_heads D, for the sums of both parts), 16-byte aligned, in
+ *              8 rows q_heads D for the sums of both parts, and up to 150 MB for
+ *              those of parts that several workgroups have), 16-byte aligned, in
  *              any state, for one call at a time.  It may be lacache_kv_attend's:
  *              that call's counters stay as they are.
  * n_groups is at most 2^20, n_seq too.

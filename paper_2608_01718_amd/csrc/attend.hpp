@@ -61,6 +61,7 @@ struct AttendShare {
     int32_t* held;     // [n_seq] tokens that a sequence shares (0: it is in no group)
     int32_t* row_pos;  // [rows] positions of rows (-1 before the first)
     int32_t* row_held; // [rows] whether a row's sequence shares tokens; -1: it is in no sequence
+    int32_t* deal;     // of a launch of both parts the workgroups that see to the prefixes
     AttendSums sums[2];  // kPrefix, kOwn
 };
 

@@ -280,12 +280,15 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
     attend_wide<DP, CT, WAVES, R, F32, MODE>(a, p, blockIdx.x);
 }
 
-// Both parts of a call in one launch: workgroups below `prefix` those over the prefixes, the others over the sequences' own
-// tokens.  WIDE: many rows over the prefixes, which the matrix cores and the softmax bound, while memory bounds the own tokens;
-// one of each on a compute unit (64 sequences, 8192 shared tokens and 16 to 2048 of their own: 149 MB in 35 us, the matrix cores
+// Both parts of a call in one launch: the first p.share.deal workgroups those over the prefixes, the others over the sequences'
+// own tokens.  WIDE: many rows over the prefixes, which the matrix cores and the softmax bound, while memory bounds the own tokens;
+// one of each on a compute unit, unless one part has much more to do (64 sequences, 8192 shared tokens and 16 to 2048 of their own: 149 MB in 35 us, the matrix cores
 // busy for 15 % of it, the vector unit 24 %).
 template <int DP, int CT, bool F32, bool WIDE>
-__global__ __launch_bounds__(256, 2) void k_attend_both(AttendArgs a, AttendPlan p, AttendPlan own, int prefix) {
+__global__ __launch_bounds__(256, 2) void k_attend_both(AttendArgs a, AttendPlan p, AttendPlan own) {
+    const int prefix = __builtin_amdgcn_readfirstlane(*p.share.deal);
+    own.workers -= prefix;
+    p.workers = prefix;
     if ((int)blockIdx.x >= prefix) attend_narrow<DP, CT, 1, F32, false, kOwn>(a, own, blockIdx.x - prefix);
     else if constexpr (WIDE) attend_wide<DP, CT, 4, F32 ? 1 : 2, F32, kPrefix>(a, p, blockIdx.x);
     else attend_narrow<DP, CT, 1, F32, false, kPrefix>(a, p, blockIdx.x);
@@ -294,13 +297,12 @@ __global__ __launch_bounds__(256, 2) void k_attend_both(AttendArgs a, AttendPlan
 template <int DP>
 hipError_t launch_attend_both(const AttendArgs& a, const AttendPlan& p, const AttendPlan& own, hipStream_t s) {
     const bool wide = p.group_shift > 5;
-    const int prefix = wide ? (p.workers + 7) & ~7 : p.workers;
-    const dim3 grid((unsigned)(prefix + own.workers)), block(256);
+    const dim3 grid((unsigned)own.workers), block(256);
     auto go = [&](auto ct, auto f32) {
         constexpr int CT = decltype(ct)::value;
         constexpr bool F32 = decltype(f32)::value;
-        if (wide) k_attend_both<DP, CT, F32, true><<<grid, block, 0, s>>>(a, p, own, prefix);
-        else k_attend_both<DP, CT, F32, false><<<grid, block, 0, s>>>(a, p, own, prefix);
+        if (wide) k_attend_both<DP, CT, F32, true><<<grid, block, 0, s>>>(a, p, own);
+        else k_attend_both<DP, CT, F32, false><<<grid, block, 0, s>>>(a, p, own);
     };
     auto of = [&](auto ct) {
         if (a.dtype == 0) go(ct, std::true_type{});

@@ -196,9 +196,34 @@ hipError_t launch_kv_attend(const AttendArgs& a, int max_new, void* workspace, i
 // and have 16 to 2048 of their own, 32 query heads on 8, d = 128: 45 us, of which 36 both parts; 256 by every sequence's table.)
 // ---------------------------------------------------------------------------
 
-// What the two launches need: workgroup b < n_seq the positions of sequence b's rows and what it shares, the others a group each.
+// How the workgroups of a launch of both parts are shared out.
+struct AttendDeal {
+    int workers;                       // 0: there is no such launch
+    int prefix_shift, own_shift, extra;  // rows of a row group, what one counts for besides its tiles
+    float weight;                      // a tile of the prefixes takes as long as so many of the sequences' own
+};
+
+// Half of them, or by the tiles of both, where that is much better: fewer workgroups begin row groups in more turns, more
+// leave more parts to join.  A multiple of eight (XCDs).  Tiles are counted roughly: the results are right with any number.
+// (64 sequences, 32 query heads on 8, d = 128: 65,536 shared tokens and 16 to 64 of their own 140 us, 174 by halves; 1024 and 1024
+// to 8192 198, 226; 4096 and 16 to 64 33, by tiles 40.)
+__device__ int deal_out(const AttendDeal& d, float prefix, float own, int lane) {
+    auto time = [&](int n) {  // of the longer of both, in tiles of the sequences' own
+        const int others = d.workers - n;
+        return others < 8 ? __builtin_inff() : fmaxf(d.weight * ceilf(prefix / (float)n), ceilf(own / (float)others));
+    };
+    const int half = d.workers / 2 & ~7, step = ((d.workers + 63) / 64 + 7) & ~7;
+    const float halves = time(half), mine = time(step * (lane + 1));
+    const float least = wave_reduce(mine, [](float s, float t) { return fminf(s, t); });
+    const int best = step * __ffsll((unsigned long long)__ballot(mine == least));
+    return least < 0.75f * halves && least < halves - 24.0f ? best : half;
+}
+
+// What the two launches need: workgroup b < n_seq the positions of sequence b's rows and what it shares, the others a group each, and one more
+// deals out the workgroups of a launch of both parts.
 // (64 sequences 4 us: lookups one after another.)
-__global__ __launch_bounds__(64) void k_attend_share(AttendArgs a, AttendShare x, const int32_t* group, const int32_t* len) {
+__global__ __launch_bounds__(64) void k_attend_share(AttendArgs a, AttendShare x, const int32_t* group, const int32_t* len,
+                                                     AttendDeal d) {
     const int lane = threadIdx.x, n_seq = a.seqs.n_seq;
     const int64_t known = (int64_t)a.seqs.max_pages << a.pool.page_shift;
     // sequences and tokens of group g (one sequence shares nothing)
@@ -226,6 +251,33 @@ __global__ __launch_bounds__(64) void k_attend_share(AttendArgs a, AttendShare x
             for (int64_t i = lane; i < s.row0; i += 64) x.row_held[i] = -1;
         if (b == n_seq - 1)
             for (int64_t i = s.row0 + s.n + lane; i < a.seqs.rows; i += 64) x.row_held[i] = -1;
+        return;
+    }
+    if ((int)blockIdx.x == n_seq + x.n_groups) {
+        // (all lengths are looked at one after another: a few thousand; with a window nearly all work is in a few tiles a row)
+        float prefix = 0.0f, own = 0.0f;
+        if (a.window == 0 && n_seq + x.n_groups <= 8192) {
+            for (int b = lane; b < n_seq; b += 64) {
+                const KvSpan s = span_of(a.seqs, b);
+                const int64_t end = s.pos0 + s.n, tiles = end < 0 ? 0 : (end < known ? end : known) >> 5;
+                own += (float)(((int64_t)s.n * a.group + (1 << d.own_shift) - 1) >> d.own_shift) * (float)(tiles + d.extra);
+            }
+            for (int g = lane; g < x.n_groups; g += 64) {
+                int from, to;
+                const int held = group_of(g, from, to) >> 5;
+                if (held == 0) continue;
+                const KvSpan s = span_of(a.seqs, to - 1);
+                const int64_t n = s.row0 + s.n - span_of(a.seqs, from).row0, rows = n < 0 ? 0 : n * a.group;
+                const int64_t live = to - from < n ? to - from : n, of_own = rows >> d.own_shift;
+                prefix += (float)((rows + (1 << d.prefix_shift) - 1) >> d.prefix_shift) * (float)held;
+                own -= (float)(live > of_own ? live : of_own) * (float)held;
+            }
+        }
+        auto add = [](float s, float t) { return s + t; };
+        prefix = wave_reduce(prefix, add) * (float)a.pool.heads;
+        own = fmaxf(wave_reduce(own, add), 0.0f) * (float)a.pool.heads;
+        const int n = deal_out(d, prefix, own, lane);
+        if (lane == 0) *x.deal = n;
         return;
     }
     const int g = blockIdx.x - n_seq;
@@ -309,7 +361,7 @@ int prefix_rows(int64_t rows, int n_groups) {  // of a group, on average
 // on a compute unit.
 bool both_at_once(const KvPool& pool, bool f32, const AttendPlan& prefix, const AttendPlan& own) {
     return pool.dp <= 128 && own.group_shift == 4 && (prefix.group_shift == 4 || prefix.group_shift == (f32 ? 6 : 7)) &&
-           attend_occupancy(pool.dp, pool.type != kKvBf16, 1, f32) >= 2;
+           attend_occupancy(pool.dp, pool.type != kKvBf16, 1, f32) >= 2 && prefix.workers >= 16;
 }
 
 // The plans of both parts, and what lies behind their memory.
@@ -330,7 +382,7 @@ int64_t shared_plan(const KvPool& pool, bool f32, int64_t rows, int n_seq, int n
     };
     plans(0);
     *both = n_groups > 0 && both_at_once(pool, f32, *prefix, *own);
-    if (*both) plans(1);
+    if (*both) plans(2);  // (as many workgroups as the launch has, for either)
     AttendShare x{};
     x.n_groups = n_groups;
     x.span = (int4*)take(16 * (int64_t)n_groups);
@@ -338,6 +390,7 @@ int64_t shared_plan(const KvPool& pool, bool f32, int64_t rows, int n_seq, int n
     x.held = (int32_t*)take(4 * (int64_t)n_seq);
     x.row_pos = (int32_t*)take(4 * rows);
     x.row_held = (int32_t*)take(4 * rows);
+    x.deal = (int32_t*)take(4);
     for (AttendSums& y : x.sums) {
         y.ml = (float2*)take(8 * rows * q_heads);
         y.at = (int2*)take(8 * rows * q_heads);
@@ -369,11 +422,16 @@ hipError_t launch_kv_attend_shared(const AttendArgs& a, const int32_t* group, co
     shared_plan(a.pool, a.dtype == 0, a.seqs.rows, a.seqs.n_seq, n_groups, a.q_heads, max_new, num_cu, (char*)workspace, &prefix, &own,
                 &both);
     const int each = prefix_rows(a.seqs.rows, n_groups);
-    k_attend_share<<<dim3((unsigned)(a.seqs.n_seq + n_groups)), dim3(64), 0, s>>>(a, prefix.share, group, len);
-    hipError_t e = hipGetLastError();
+    AttendDeal deal{};
     if (both) {
         prepare<kPrefix>(a, prefix, n_groups, each);
         prepare<kOwn>(a, own, a.seqs.n_seq, max_new);
+        // (64 sequences, 8 heads, bfloat16: a tile for 128 rows 1.7 us, one for up to 16 about 0.6)
+        deal = AttendDeal{own.workers, prefix.group_shift, own.group_shift, own.extra, prefix.group_shift > 4 ? 3.0f : 1.0f};
+    }
+    k_attend_share<<<dim3((unsigned)(a.seqs.n_seq + n_groups + both)), dim3(64), 0, s>>>(a, prefix.share, group, len, deal);
+    hipError_t e = hipGetLastError();
+    if (both) {
         if (e == hipSuccess)
             e = a.pool.dp == 64   ? launch_attend_both<64>(a, prefix, own, s)
                 : a.pool.dp == 96 ? launch_attend_both<96>(a, prefix, own, s)
@@ -385,7 +443,7 @@ hipError_t launch_kv_attend_shared(const AttendArgs& a, const int32_t* group, co
     if (e != hipSuccess) return e;
     // the parts of a row, about: its row group's share of the workers over the prefixes, and a few of its own; four to a lane group
     const int64_t groups_of = n_groups > 0 ? (((int64_t)each * a.group >> prefix.group_shift) + 1) * n_groups * a.pool.heads : 1;
-    const int64_t parts = (n_groups > 0 ? prefix.workers / groups_of : 0) + 2;
+    const int64_t parts = (n_groups > 0 ? prefix.workers / (both ? 2 : 1) / groups_of : 0) + 2;
     int of_row = 1;
     while (4 * of_row < parts && 2 * of_row <= 256 / (a.pool.dp / 4)) of_row *= 2;
     const int rows = 256 / (a.pool.dp / 4) / of_row;

@@ -131,6 +131,18 @@ def test_groups_of_every_kind(lc, new, Hq):
     check_attend(lc, pg, same, q[:2 * new], [new] * 2, [300, 299], out=out)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("count,prefix,own", [(64, 16_384, (3, 40)), (64, 1024, (1100, 1500)), (4, 65_536, (1, 30)), (4, 64, (9000, 9500)),
+                                              (40, 6400, (1, 3))])
+def test_parts_of_unequal_work(lc, dtype, count, prefix, own):
+    """Much more over the prefix than over the sequences' own tokens, or much less."""
+    lens = [prefix + own[0] + i * (own[1] - own[0]) // (count - 1) for i in range(count)]
+    pg, held = shared(lc, "fp8", 8, 64, 64, lens, [(0, count, prefix)], seed=count)
+    q = normals((count, 32, 64), seed=6, dtype=dtype)
+    check(lc, pg, held, q, [1] * count, lens, [(0, count, prefix)], max_new=1)
+    check(lc, pg, held, q, [1] * count, lens, [(0, count, prefix)], max_new=1, window=700)
+
+
 @pytest.mark.parametrize("count,each", [(390, 3), (260, 2), (900, 1), (17_000, 100)])
 def test_many_groups(lc, count, each):
     """More groups and sequences than are looked at together, empty groups and slots without rows among them."""
