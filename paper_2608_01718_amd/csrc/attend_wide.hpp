@@ -281,28 +281,32 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
 }
 
 // Both parts of a call in one launch: the first p.share.deal workgroups those over the prefixes, the others over the sequences'
-// own tokens.  WIDE: many rows over the prefixes, which the matrix cores and the softmax bound, while memory bounds the own tokens;
+// own tokens.  SHIFT: of the prefixes' row groups.  From 6 on: many rows over the prefixes, which the matrix cores and the softmax bound, while memory bounds the own tokens;
 // one of each on a compute unit, unless one part has much more to do (64 sequences, 8192 shared tokens and 16 to 2048 of their own: 149 MB in 35 us, the matrix cores
 // busy for 15 % of it, the vector unit 24 %).
-template <int DP, int CT, bool F32, bool WIDE>
+template <int DP, int CT, bool F32, int SHIFT>
 __global__ __launch_bounds__(256, 2) void k_attend_both(AttendArgs a, AttendPlan p, AttendPlan own) {
     const int prefix = __builtin_amdgcn_readfirstlane(*p.share.deal);
     own.workers -= prefix;
     p.workers = prefix;
     if ((int)blockIdx.x >= prefix) attend_narrow<DP, CT, 1, F32, false, kOwn>(a, own, blockIdx.x - prefix);
-    else if constexpr (WIDE) attend_wide<DP, CT, 4, F32 ? 1 : 2, F32, kPrefix>(a, p, blockIdx.x);
-    else attend_narrow<DP, CT, 1, F32, false, kPrefix>(a, p, blockIdx.x);
+    else if constexpr (SHIFT >= 6) attend_wide<DP, CT, 4, 1 << (SHIFT - 6), F32, kPrefix>(a, p, blockIdx.x);
+    else attend_narrow<DP, CT, 1 << (SHIFT - 4), F32, false, kPrefix>(a, p, blockIdx.x);
 }
 
 template <int DP>
 hipError_t launch_attend_both(const AttendArgs& a, const AttendPlan& p, const AttendPlan& own, hipStream_t s) {
-    const bool wide = p.group_shift > 5;
     const dim3 grid((unsigned)own.workers), block(256);
     auto go = [&](auto ct, auto f32) {
         constexpr int CT = decltype(ct)::value;
         constexpr bool F32 = decltype(f32)::value;
-        if (wide) k_attend_both<DP, CT, F32, true><<<grid, block, 0, s>>>(a, p, own);
-        else k_attend_both<DP, CT, F32, false><<<grid, block, 0, s>>>(a, p, own);
+        if (p.group_shift == 4) k_attend_both<DP, CT, F32, 4><<<grid, block, 0, s>>>(a, p, own);
+        else if (p.group_shift == 6) k_attend_both<DP, CT, F32, 6><<<grid, block, 0, s>>>(a, p, own);
+        else if constexpr (!F32) {
+            if (p.group_shift == 7) k_attend_both<DP, CT, F32, 7><<<grid, block, 0, s>>>(a, p, own);
+            else if constexpr (attend_occupancy(DP, CT != kKvBf16, 2, false) >= 2)
+                k_attend_both<DP, CT, F32, 5><<<grid, block, 0, s>>>(a, p, own);
+        }
     };
     auto of = [&](auto ct) {
         if (a.dtype == 0) go(ct, std::true_type{});

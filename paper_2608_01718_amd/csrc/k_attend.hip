@@ -357,11 +357,11 @@ int prefix_rows(int64_t rows, int n_groups) {  // of a group, on average
     return each < 1 ? 1 : (int)each;
 }
 
-// Whether both parts are in one launch: few rows of own tokens, and many or few over the prefixes, with room for two workgroups
-// on a compute unit.
+// Whether both parts are in one launch: few rows of own tokens, with room for two workgroups on a compute unit.  (16 sequences,
+// 32 query heads on 8, d = 128, 8192 shared tokens and 16 to 2048 of their own: 32 us, 42 in two launches; 1024 and 16 to 512: 20, 28.)
 bool both_at_once(const KvPool& pool, bool f32, const AttendPlan& prefix, const AttendPlan& own) {
-    return pool.dp <= 128 && own.group_shift == 4 && (prefix.group_shift == 4 || prefix.group_shift == (f32 ? 6 : 7)) &&
-           attend_occupancy(pool.dp, pool.type != kKvBf16, 1, f32) >= 2 && prefix.workers >= 16;
+    return pool.dp <= 128 && own.group_shift == 4 && prefix.workers >= 16 &&
+           attend_occupancy(pool.dp, pool.type != kKvBf16, prefix.group_shift == 5 ? 2 : 1, f32) >= 2;
 }
 
 // The plans of both parts, and what lies behind their memory.
@@ -427,7 +427,8 @@ hipError_t launch_kv_attend_shared(const AttendArgs& a, const int32_t* group, co
         prepare<kPrefix>(a, prefix, n_groups, each);
         prepare<kOwn>(a, own, a.seqs.n_seq, max_new);
         // (64 sequences, 8 heads, bfloat16: a tile for 128 rows 1.7 us, one for up to 16 about 0.6)
-        deal = AttendDeal{own.workers, prefix.group_shift, own.group_shift, own.extra, prefix.group_shift > 4 ? 3.0f : 1.0f};
+        const float weight = prefix.group_shift < 6 ? 1.0f : prefix.group_shift == 6 && a.dtype != 0 ? 2.0f : 3.0f;
+        deal = AttendDeal{own.workers, prefix.group_shift, own.group_shift, own.extra, weight};
     }
     k_attend_share<<<dim3((unsigned)(a.seqs.n_seq + n_groups + both)), dim3(64), 0, s>>>(a, prefix.share, group, len, deal);
     hipError_t e = hipGetLastError();
