@@ -281,16 +281,18 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
 }
 
 // Both parts of a call in one launch: the first p.share.deal workgroups those over the prefixes, the others over the sequences'
-// own tokens.  SHIFT: of the prefixes' row groups.  From 6 on: many rows over the prefixes, which the matrix cores and the softmax bound, while memory bounds the own tokens;
+// own tokens.  SHIFT, OWN: of their row groups (4, 5: attend_narrow).  From 6 on: many rows over the prefixes, which the matrix cores and the softmax bound, while memory bounds the own tokens;
 // one of each on a compute unit, unless one part has much more to do (64 sequences, 8192 shared tokens and 16 to 2048 of their own: 149 MB in 35 us, the matrix cores
 // busy for 15 % of it, the vector unit 24 %).
-template <int DP, int CT, bool F32, int SHIFT>
+template <int DP, int CT, bool F32, int SHIFT, int OWN>
 __global__ __launch_bounds__(256, 2) void k_attend_both(AttendArgs a, AttendPlan p, AttendPlan own) {
     const int prefix = __builtin_amdgcn_readfirstlane(*p.share.deal);
     own.workers -= prefix;
     p.workers = prefix;
-    if ((int)blockIdx.x >= prefix) attend_narrow<DP, CT, 1, F32, false, kOwn>(a, own, blockIdx.x - prefix);
-    else if constexpr (SHIFT >= 6) attend_wide<DP, CT, 4, 1 << (SHIFT - 6), F32, kPrefix>(a, p, blockIdx.x);
+    if ((int)blockIdx.x >= prefix) {
+        if constexpr (OWN >= 6) attend_wide<DP, CT, 4, 1 << (OWN - 6), F32, kOwn>(a, own, blockIdx.x - prefix);
+        else attend_narrow<DP, CT, 1, F32, false, kOwn>(a, own, blockIdx.x - prefix);
+    } else if constexpr (SHIFT >= 6) attend_wide<DP, CT, 4, 1 << (SHIFT - 6), F32, kPrefix>(a, p, blockIdx.x);
     else attend_narrow<DP, CT, 1 << (SHIFT - 4), F32, false, kPrefix>(a, p, blockIdx.x);
 }
 
@@ -300,12 +302,16 @@ hipError_t launch_attend_both(const AttendArgs& a, const AttendPlan& p, const At
     auto go = [&](auto ct, auto f32) {
         constexpr int CT = decltype(ct)::value;
         constexpr bool F32 = decltype(f32)::value;
-        if (p.group_shift == 4) k_attend_both<DP, CT, F32, 4><<<grid, block, 0, s>>>(a, p, own);
-        else if (p.group_shift == 6) k_attend_both<DP, CT, F32, 6><<<grid, block, 0, s>>>(a, p, own);
+        if (own.group_shift > 4) {
+            if constexpr (F32) k_attend_both<DP, CT, F32, 6, 6><<<grid, block, 0, s>>>(a, p, own);
+            else if (own.group_shift == 6) k_attend_both<DP, CT, F32, 7, 6><<<grid, block, 0, s>>>(a, p, own);
+            else k_attend_both<DP, CT, F32, 7, 7><<<grid, block, 0, s>>>(a, p, own);
+        } else if (p.group_shift == 4) k_attend_both<DP, CT, F32, 4, 4><<<grid, block, 0, s>>>(a, p, own);
+        else if (p.group_shift == 6) k_attend_both<DP, CT, F32, 6, 4><<<grid, block, 0, s>>>(a, p, own);
         else if constexpr (!F32) {
-            if (p.group_shift == 7) k_attend_both<DP, CT, F32, 7><<<grid, block, 0, s>>>(a, p, own);
+            if (p.group_shift == 7) k_attend_both<DP, CT, F32, 7, 4><<<grid, block, 0, s>>>(a, p, own);
             else if constexpr (attend_occupancy(DP, CT != kKvBf16, 2, false) >= 2)
-                k_attend_both<DP, CT, F32, 5><<<grid, block, 0, s>>>(a, p, own);
+                k_attend_both<DP, CT, F32, 5, 4><<<grid, block, 0, s>>>(a, p, own);
         }
     };
     auto of = [&](auto ct) {

@@ -219,8 +219,8 @@ __device__ int deal_out(const AttendDeal& d, float prefix, float own, int lane) 
     return least < 0.75f * halves && least < halves - 24.0f ? best : half;
 }
 
-// What the two launches need: workgroup b < n_seq the positions of sequence b's rows and what it shares, the others a group each, and one more
-// deals out the workgroups of a launch of both parts.
+// What both parts need: workgroup b < n_seq the positions of sequence b's rows and what it shares, the others a group each, and
+// one more deals out the workgroups of a launch of both.
 // (64 sequences 4 us: lookups one after another.)
 __global__ __launch_bounds__(64) void k_attend_share(AttendArgs a, AttendShare x, const int32_t* group, const int32_t* len,
                                                      AttendDeal d) {
@@ -300,7 +300,7 @@ __global__ __launch_bounds__(64) void k_attend_share(AttendArgs a, AttendShare x
 
 // Puts the two parts of every (row, query head) together: dp / 4 lanes on four columns each, of_row lane groups (a power of two)
 // one after another on the parts that workers have of it.  Reading the parts bounds it (64 rows of 32 heads, 17 MB of parts 8 us;
-// 945 rows of 12 heads, three groups 9 us).
+// 945 rows of 12 heads, three groups 7 us).
 template <bool F32>
 __global__ __launch_bounds__(256) void k_attend_together(AttendArgs a, AttendPlan prefix, AttendPlan own, int of_row) {
     __shared__ f32x4 sums[256];
@@ -357,11 +357,13 @@ int prefix_rows(int64_t rows, int n_groups) {  // of a group, on average
     return each < 1 ? 1 : (int)each;
 }
 
-// Whether both parts are in one launch: few rows of own tokens, with room for two workgroups on a compute unit.  (16 sequences,
-// 32 query heads on 8, d = 128, 8192 shared tokens and 16 to 2048 of their own: 32 us, 42 in two launches; 1024 and 16 to 512: 20, 28.)
+// Whether both parts are in one launch: few rows of own tokens, or many of both, with room for two workgroups on a compute
+// unit.  (16 sequences, 32 query heads on 8, d = 128, 8192 shared tokens and 16 to 2048 of their own: 32 us, 42 in two launches;
+// 1024 and 16 to 512: 20, 28; 16 new tokens, 2048 and 60 to 512: 42, 61.)
 bool both_at_once(const KvPool& pool, bool f32, const AttendPlan& prefix, const AttendPlan& own) {
-    return pool.dp <= 128 && own.group_shift == 4 && prefix.workers >= 16 &&
-           attend_occupancy(pool.dp, pool.type != kKvBf16, prefix.group_shift == 5 ? 2 : 1, f32) >= 2;
+    if (pool.dp > 128 || prefix.workers < 16) return false;
+    if (own.group_shift >= 6) return prefix.group_shift == (f32 ? 6 : 7);
+    return own.group_shift == 4 && attend_occupancy(pool.dp, pool.type != kKvBf16, prefix.group_shift == 5 ? 2 : 1, f32) >= 2;
 }
 
 // The plans of both parts, and what lies behind their memory.
@@ -382,7 +384,10 @@ int64_t shared_plan(const KvPool& pool, bool f32, int64_t rows, int n_seq, int n
     };
     plans(0);
     *both = n_groups > 0 && both_at_once(pool, f32, *prefix, *own);
-    if (*both) plans(2);  // (as many workgroups as the launch has, for either)
+    if (*both) {
+        plans(2);  // (as many workgroups as the launch has, for either)
+        prefix->workers = own->workers &= ~7;
+    }
     AttendShare x{};
     x.n_groups = n_groups;
     x.span = (int4*)take(16 * (int64_t)n_groups);
@@ -427,7 +432,9 @@ hipError_t launch_kv_attend_shared(const AttendArgs& a, const int32_t* group, co
         prepare<kPrefix>(a, prefix, n_groups, each);
         prepare<kOwn>(a, own, a.seqs.n_seq, max_new);
         // (64 sequences, 8 heads, bfloat16: a tile for 128 rows 1.7 us, one for up to 16 about 0.6)
-        const float weight = prefix.group_shift < 6 ? 1.0f : prefix.group_shift == 6 && a.dtype != 0 ? 2.0f : 3.0f;
+        const float weight = prefix.group_shift < 6 || prefix.group_shift == own.group_shift ? 1.0f
+                             : own.group_shift == 6                                          ? 1.5f
+                             : prefix.group_shift == 6 && a.dtype != 0                       ? 2.0f : 3.0f;
         deal = AttendDeal{own.workers, prefix.group_shift, own.group_shift, own.extra, weight};
     }
     k_attend_share<<<dim3((unsigned)(a.seqs.n_seq + n_groups + both)), dim3(64), 0, s>>>(a, prefix.share, group, len, deal);
