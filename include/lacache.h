@@ -553,8 +553,10 @@ int lacache_kv_attend(const lacache_kv *kv, const lacache_seqs *seqs, const void
  * Prefixes that sequences share (device arrays): sequences group[g] ..
  * group[g+1]-1 (non-decreasing; those outside all groups share nothing) hold the
  * same first len[g] tokens, rounded down to whole pages, in the same pages: the
- * first entries of their page tables are equal.  A group of one sequence shares
- * nothing.
+ * first entries of their page tables are equal.  That is asked of entries that a
+ * sequence's own tokens lie in: one that is shorter than the prefix has what it
+ * has of it, and a slot without tokens or without new rows may have any table.  A
+ * group of one sequence shares nothing.
  */
 typedef struct {
     const int32_t *group;  /* [n_groups + 1] */
@@ -565,8 +567,8 @@ typedef struct {
 /*
  * lacache_kv_attend of sequences of which groups share a prefix: the same
  * results to rounding, the prefix of a group read once for all of its rows
- * (through the page table of its first sequence).  The other arguments are those
- * of lacache_kv_attend.
+ * (through the page table of the longest of its sequences that have rows).  The
+ * other arguments are those of lacache_kv_attend.
  *   workspace  lacache_kv_attend_shared_workspace bytes of device memory (about
  *              8 rows q_heads D for the sums of both parts, and up to 150 MB for
  *              those of parts that several workgroups have), 16-byte aligned, in

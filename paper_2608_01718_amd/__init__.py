@@ -589,7 +589,8 @@ class Sequences:
 
 class Prefixes:
     """Tokens that sequences share: sequences group[g] .. group[g + 1] - 1 begin with the same len[g] tokens (whole pages of
-    them), and their page tables with the same pages.  group [n + 1] and len [n], int32 on one GPU."""
+    them), and their page tables with the same pages, as far as their own tokens reach (slots without tokens or new rows may
+    have any table).  group [n + 1] and len [n], int32 on one GPU."""
 
     def __init__(self, group: torch.Tensor, len: torch.Tensor):
         n, dev = len.shape[0], len.device

@@ -56,7 +56,7 @@ struct AttendSums {
 // The shared prefixes of a call, as k_attend_share has laid them out.
 struct AttendShare {
     int n_groups;
-    int4* span;        // [n_groups] first row, rows, shared tokens (whole pages), first sequence
+    int4* span;        // [n_groups] first row, rows, shared tokens (whole pages), the sequence whose page table is read
     int32_t* first;    // [n_groups] the first tile that any row sees
     int32_t* held;     // [n_seq] tokens that a sequence shares (0: it is in no group)
     int32_t* row_pos;  // [rows] positions of rows (-1 before the first)

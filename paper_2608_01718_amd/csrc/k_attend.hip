@@ -281,18 +281,25 @@ __global__ __launch_bounds__(64) void k_attend_share(AttendArgs a, AttendShare x
         return;
     }
     const int g = blockIdx.x - n_seq;
-    int from, to, least = INT32_MAX;
+    // The prefix is read through the page table of the longest of the sequences that have rows: all that any row sees of it is
+    // there, whatever the tables of idle slots, and of shorter sequences behind their own tokens, hold.
+    int from, to, least = INT32_MAX, longest = 0, table = INT32_MAX;
     const int held = group_of(g, from, to);
     for (int b = from + lane; b < to; b += 64) {
         const KvSpan s = span_of(a.seqs, b);
-        const int64_t first = s.pos0 < 0 ? 0 : s.pos0;
-        if (s.n > 0 && s.pos0 + s.n > 0) least = first < least ? (int)first : least;
+        const int64_t end = s.pos0 + s.n, first = s.pos0 < 0 ? 0 : s.pos0;
+        if (s.n <= 0 || end <= 0) continue;
+        least = first < least ? (int)first : least;
+        if (end > longest) longest = (int)end, table = b;
     }
-    least = wave_reduce(least, [](int p, int q) { return p < q ? p : q; });
+    auto min2 = [](int p, int q) { return p < q ? p : q; };
+    least = wave_reduce(least, min2);
+    const int most = wave_reduce(longest, [](int p, int q) { return p > q ? p : q; });
+    table = wave_reduce(longest == most ? table : INT32_MAX, min2);
     if (lane == 0) {
         const int64_t row0 = from < n_seq ? span_of(a.seqs, from).row0 : 0;
         const int64_t end = to > from ? span_of(a.seqs, to - 1).row0 + span_of(a.seqs, to - 1).n : row0;
-        x.span[g] = make_int4((int)row0, held > 0 && end > row0 ? (int)(end - row0) : 0, held, from);
+        x.span[g] = make_int4((int)row0, held > 0 && end > row0 ? (int)(end - row0) : 0, held, table < to ? table : from);
         const int64_t lo = a.window > 0 && least < INT32_MAX ? (int64_t)least - a.window + 1 : 0;
         x.first[g] = lo > 0 ? (int)(lo >> 5) : 0;
     }

@@ -307,3 +307,31 @@ def test_calls_that_are_refused(lc):
             f()
     with torch.no_grad():
         pg.cache.attend_shared(q.clone().requires_grad_(), seqs, p)
+
+
+IDLE = [  # new tokens, lengths, groups: slots without tokens or rows, and sequences shorter than the prefix, come first
+    ([1, 1, 1], [0, 290, 310], [(0, 3, 256)]),
+    ([1, 1, 1], [40, 290, 310], [(0, 3, 256)]),
+    ([1, 1, 1, 1], [0, 0, 70, 333], [(0, 4, 320)]),
+    ([0, 1, 1], [300, 290, 270], [(0, 3, 256)]),
+    ([1, 1], [40, 70], [(0, 2, 256)]),
+    ([1] * 8, [0, 260, 300, 33, 0, 257, 0, 129], [(0, 3, 256), (3, 6, 250), (6, 8, 128)]),
+    ([1, 1, 1], [300, 0, 290], [(0, 3, 256)]),
+]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("new,Hq,d", [(1, 4, 64), (1, 32, 64), (5, 16, 96), (30, 4, 64), (1, 4, 256), (9, 4, 256)])
+@pytest.mark.parametrize("news,lens,groups", IDLE)
+def test_any_sequence_of_a_group_may_be_idle(lc, dtype, new, Hq, d, news, lens, groups):
+    """Page tables have nothing behind their sequences' own tokens, and nothing at all where a slot has no rows: the others'
+    prefix is read all the same, through the table of one that holds it."""
+    say(f"[case] idle {dtype} {new} {Hq} {d} {news} {lens} {groups}")
+    pg, held = shared(lc, "bf16", 2, d, 32, lens, groups, seed=d + new)
+    table = pg.table.clone()
+    for i, (n, length) in enumerate(zip(news, lens)):
+        table[i, -(-length // 32) if n else 0:] = -1
+    news = [n * new for n in news]
+    q = normals((sum(news), Hq, d), seed=new, dtype=dtype, size=2)
+    for window in (0, 100):
+        check(lc, pg, held, q, news, lens, groups, window=window, max_new=new, table=table)
