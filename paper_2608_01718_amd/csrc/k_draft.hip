@@ -54,11 +54,10 @@ __device__ __forceinline__ double exp2_64(double t) {
 constexpr double kLog2e64 = 1.44269504088896340736;
 
 // 2^t for t <= 0 where many are needed: 2^f, |f| <= 1/2, by the polynomial of degree 9 that is exact at the zeros of the
-// Chebyshev polynomial of degree 10 (2e-14 of 2^f), times 2^n by adding to its exponent; adding 1.5 2^52 leaves n in the low
-// bits.  Below 2^-1021 it stays there: kNothing.  (Both models' rows of 64 sequences, 16.4M
-// logits: k_draft_sums 17 us, 27 with the series above.)
+// Chebyshev polynomial of degree 10 (2e-14 of 2^f), times 2^n; adding 1.5 2^52 leaves n in the low bits.  Below 2^-1074 it is 0.
+// (Both models' rows of 64 sequences, 16.4M logits: k_draft_sums 17 us, 27 with the series above.)
 __device__ __forceinline__ double exp2_many(double t) {
-    t = fmax(t, -1021.0);
+    t = fmax(t, -1100.0);
     const double z = t + 0x1.8p52, f = t - (z - 0x1.8p52);
     double y = 1.0205905413765595e-07;
     y = __builtin_fma(y, f, 1.325964524488711e-06);
@@ -70,9 +69,8 @@ __device__ __forceinline__ double exp2_many(double t) {
     y = __builtin_fma(y, f, 0.2402265069564034);
     y = __builtin_fma(y, f, 0.6931471805599462);
     y = __builtin_fma(y, f, 1.0000000000000135);
-    return __longlong_as_double(__double_as_longlong(y) + ((long long)(uint32_t)__double_as_longlong(z) << 52));
+    return __builtin_ldexp(y, (int)(uint32_t)__double_as_longlong(z));
 }
-constexpr double kNothing = 0x1p-1000;  // weights up to this count as none
 
 // A sequence's temperature: log2 e / T, and whether it is greedy (T not in 2^-60 .. 2^60).
 struct Heat {
@@ -480,9 +478,12 @@ __device__ __forceinline__ Scales scales_of(const DraftArgs& a, int b, bool has_
     sq = wave_reduce(sq, Add64{});
     return {1.0 / sp, has_q ? 1.0 / sq : 0.0};
 }
+// r of a token.  Pieces with a sum above 0 are searched for a token with r above 0: it has to come out the same in every kernel,
+// so which product is rounded is written down (a compiler may join either to the difference).
 __device__ __forceinline__ double rest_of(float x, float y, const DraftRow& row, const Scales& f, double c, bool with_q) {
-    const double r = exp2_many(((double)x - row.mt) * c) * f.p;
-    return with_q ? fmax(0.0, r - exp2_many(((double)y - row.md) * c) * f.q) : r;
+    const double p = exp2_many(((double)x - row.mt) * c);
+    if (!with_q) return p * f.p;
+    return fmax(0.0, __builtin_fma(p, f.p, -(exp2_many(((double)y - row.md) * c) * f.q)));
 }
 
 }  // namespace
@@ -529,7 +530,7 @@ __device__ __forceinline__ void pick(const DraftArgs& a, int b, const Heat& heat
         }
         upto += ahead;
         if (whole) goal *= total;
-        const uint64_t past = __ballot(upto > goal && own > kNothing), some = __ballot(own > kNothing);
+        const uint64_t past = __ballot(upto > goal && own > 0.0), some = __ballot(own > 0.0);
         if (lane == 0) {
             found[wid][0] = past ? wid * 64 + __ffsll((unsigned long long)past) - 1 : -1;
             found[wid][1] = some ? wid * 64 + 63 - __clzll((long long)some) : -1;
@@ -561,16 +562,17 @@ __device__ __forceinline__ void pick(const DraftArgs& a, int b, const Heat& heat
         __syncthreads();
         who = find(all, (double)a.u_next[b], true, before, total);
     }
-    const bool shares = row.has_q && !with_q;  // sums are S_p's, not r's
+    const bool shares = row.has_q && !with_q;  // sums are S_p's, not r's: weights are numerators
+    const Scales scales = shares ? Scales{1.0, 0.0} : f;
     if (who < 0) {
         if (tid == 0) a.next_token[b] = -1;
         return;
     }
-    if (tid == who) {  // the piece among its own
-        int piece = -1;
+    if (tid == who) {  // the piece among its own, of which one has a sum above 0
+        int piece = first;
         for (int i = first; i < end; ++i) {
             const double p = shares ? sums[i].x : rest(i);
-            if (p > kNothing) {
+            if (p > 0.0) {
                 piece = i;
                 lead[0] = before;
                 if (before + p > lead[1]) break;
@@ -578,7 +580,7 @@ __device__ __forceinline__ void pick(const DraftArgs& a, int b, const Heat& heat
             before += p;
         }
         chosen = piece;
-        lead[1] = (lead[1] - lead[0]) * (shares ? f.p : 1.0);
+        lead[1] -= lead[0];
     }
     __syncthreads();
     const double goal = lead[1];
@@ -591,7 +593,7 @@ __device__ __forceinline__ void pick(const DraftArgs& a, int b, const Heat& heat
         if (with_q) logits8<F32, 1, false>(row_of(a, b, row.n, true), a.V, v, 0, false, y);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            r[e] = rest_of(x[0][e], y[0][e], row, f, heat.c, with_q);
+            r[e] = rest_of(x[0][e], y[0][e], row, scales, heat.c, with_q);
             own += r[e];
         }
     }
@@ -602,7 +604,7 @@ __device__ __forceinline__ void pick(const DraftArgs& a, int b, const Heat& heat
         const double to = lead[1];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            if (!past && r[e] > kNothing) {
+            if (!past && r[e] > 0.0) {
                 token = v + e;
                 past = before + r[e] > to;
             }

@@ -225,3 +225,54 @@ def test_streams_outputs_and_graphs(lc):
             torch.cuda.synchronize()
             assert all(torch.equal(x, y) for x, y in zip(res, want[which]))
             assert all(torch.equal(x, y) for x, y in zip(eager, want[which]))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("B,V", [(2, 700), (2, 3000), (2, 150_001), (2, 262_144), (32, 262_147)])
+def test_smallest_weights(lc, B, V, dtype):
+    """A random number of 0 takes the first token with a weight, however small: weights between 2^-1000 and 2^-1050 (sums of
+    them on either side of 2^-1000), in front of all others or behind tokens without any, in pieces and threads of any number of
+    them.  What is below 2^-1074 has none."""
+    print(f"[case] {B} {V} {dtype}", flush=True)
+    u, tokens, drafts = torch.zeros((B, 0), device=DEV), torch.zeros((B, 0), dtype=torch.int32, device=DEV), (B, 0, V)
+    for size in (-693.0, -696.0, -700.0, -704.0, -728.0):
+        for first in (0, 5, V // 2 + 1):
+            logits = torch.full((B, 1, V), size, device=DEV)
+            logits[:, :, :first] = -math.inf
+            logits[1, :, :first] = -760.0                  # 2^-1096
+            logits[:, :, -1] = 0.0
+            got = lc.lacache_verify(logits.to(dtype), logits[:, :0].to(dtype), tokens, u, torch.zeros(B, device=DEV))
+            assert got[1].tolist() == [first] * B, (size, first)
+            assert got[0].tolist() == [0] * B and tuple(got[2].shape) == drafts[:2]
+
+
+@pytest.mark.parametrize("B,V", [(3, 900), (3, 140_003), (40, 262_145)])
+def test_smallest_weights_of_the_same_distribution(lc, B, V):
+    """Nothing is left of p - q, and the first token of p, for a random number of 0, is one of 2^-1004."""
+    logits = torch.full((B, 2, V), -math.inf, device=DEV)
+    logits[:, :, 7:7 + V // 2] = -696.0
+    logits[:, :, -2:] = 0.0
+    draft = logits[:, :1].clone()
+    u = torch.full((B, 1), 2.0, device=DEV)
+    got = lc.lacache_verify(logits, draft, torch.full((B, 1), V - 1, dtype=torch.int32, device=DEV), u, torch.zeros(B, device=DEV))
+    assert got[0].tolist() == [0] * B and got[1].tolist() == [7] * B
+
+
+@pytest.mark.parametrize("B,V", [(4, 5003), (3, 140_003), (70, 140_003)])
+def test_what_is_left_of_nearly_equal_models(lc, B, V):
+    """Rows that differ by two tokens that have changed places: r lies in one of them (at least 10 / (100 V) of 1), and in what
+    the roundings of 64 bits leave of the others' p - q (up to 2^-52 of p each, 2^-20 of r together at the most).  A token
+    is drawn, and for any random number but the smallest it is that one."""
+    g = torch.Generator(DEV).manual_seed(V)
+    draft = torch.randn((B, 1, V), generator=g, device=DEV) * 3
+    a, b = V // 3, 2 * V // 3
+    draft[:, :, a], draft[:, :, b] = 1.0, 3.0
+    logits = draft.expand(B, 2, V).clone()
+    logits[:, 0, a], logits[:, 0, b] = 3.0, 1.0
+    u = torch.full((B, 1), 100.0, device=DEV)
+    tokens = torch.full((B, 1), b, dtype=torch.int32, device=DEV)
+    for u_next in (0.5, 2.0 ** -18, 1 - 2.0 ** -18):
+        got = lc.lacache_verify(logits, draft, tokens, u, torch.full((B,), u_next, device=DEV))
+        assert got[0].tolist() == [0] * B and got[1].tolist() == [a] * B, u_next
+    got = lc.lacache_verify(logits, draft, tokens, u, torch.zeros(B, device=DEV))
+    assert bool((got[1] >= 0).all()) and bool((got[1] <= a).all())
