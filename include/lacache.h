@@ -270,7 +270,8 @@ int lacache_accept_length(const void *logits, lacache_dtype dtype, int32_t V, co
  *                 one) is greedy: a draft is taken if its logit is one of the
  *                 largest, the next token is the first of the largest; its rows of
  *                 draft_logits are not read
- *   1 <= V, 0 <= B <= 65535, 0 <= k <= 4096, B (V / 2048 + 1) below 2^24
+ *   1 <= V, 0 <= B <= 65535, 0 <= k <= 4096, B (V / 2048 + 1) below 2^24; a
+ *   stride that is used n times below 2^58 / n
  * Outputs: accept_len [B], next_token [B] int32, p_target and p_draft [B][k] the
  * p_j(x_j) and q_j(x_j) in float32 (a greedy sequence's: 1 or 0, and 1; those from
  * n_draft[b] on: 0).  accept_len and next_token are those of 64-bit arithmetic.
@@ -279,7 +280,9 @@ int lacache_accept_length(const void *logits, lacache_dtype dtype, int32_t V, co
  * is the target's row n the next token is -1, if it is the draft model's r = p_n.
  *   workspace     lacache_verify_workspace bytes of device memory, 16-byte aligned,
  *                 in any state, for one call at a time
- * The outputs overlap neither one another nor an input.  B == 0 is a no-op.
+ * The outputs and the workspace overlap neither one another nor an input (nor any
+ * of its rows, read or not; they may lie between rows): such calls are refused.
+ * B == 0 is a no-op.
  * k == 0 draws a token from each target row.
  */
 int64_t lacache_verify_workspace(int32_t V, int32_t B, int32_t k);

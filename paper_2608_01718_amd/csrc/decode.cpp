@@ -59,6 +59,24 @@ bool to_bounds(const lacache_bounds* b, KvBounds* out) {
     return true;
 }
 
+// Strides that keep n of them (0 or more) far from the ends of 64 bits.
+bool fits_far(int64_t stride, int64_t n) { return n < 2 || stride < (INT64_C(1) << 58) / n; }
+
+// Whether bytes lo .. hi - 1 meet one of the rows (n elements of esz bytes each, `rows` of them `row` elements apart in each of
+// `seqs` sequences, `seq` elements apart).  Where they lie between the first row's begin and the last one's end, sequence
+// after sequence: they may lie between rows.
+bool rows_meet(const void* base, int64_t esz, int64_t n, int64_t seq, int64_t seqs, int64_t row, int64_t rows, int64_t lo, int64_t hi) {
+    if (lo >= hi || seqs < 1 || rows < 1) return false;
+    lo -= (int64_t)base, hi -= (int64_t)base, n *= esz, seq *= seqs > 1 ? esz : 0, row *= rows > 1 ? esz : 0;
+    if (hi <= 0 || lo >= (seqs - 1) * seq + (rows - 1) * row + n) return false;
+    for (int64_t b = 0; b < seqs; ++b) {
+        const int64_t from = lo - b * seq - n, to = hi - b * seq;  // a row that begins between these
+        const int64_t j = from < 0 ? 0 : row > 0 ? from / row + 1 : rows;
+        if (j < rows && j * row < to) return true;
+    }
+    return false;
+}
+
 // Compute units of the current device; 0 on a HIP error.  (Asked once for each of the first 64 devices.)
 int compute_units() {
     static std::atomic<int> known[64];
@@ -313,17 +331,25 @@ int lacache_verify(const void* logits, const void* draft_logits, lacache_dtype d
     if (k > 0 && (!draft_logits || !draft_tokens || !u_accept || !p_target || !p_draft || !aligned(draft_logits, esz) ||
                   !aligned(draft_tokens, 4) || !aligned(u_accept, 4) || !aligned(p_target, 4) || !aligned(p_draft, 4)))
         return LACACHE_EINVAL;
+    if (!fits_far(t_seq, B) || !fits_far(d_seq, B) || !fits_far(t_row, k + 1) || !fits_far(d_row, k)) return LACACHE_EINVAL;
     // (workgroups write a sequence's results while others still read what they are found from)
     const struct {
         const void* at;
         int64_t n;
-    } used[] = {{accept_len, B}, {next_token, B}, {p_target, (int64_t)B * k}, {p_draft, (int64_t)B * k},  // written
-                {draft_tokens, (int64_t)B * k}, {u_accept, (int64_t)B * k}, {u_next, B}, {temperature, B}, {n_draft, B}};
-    for (int i = 0; i < 4; ++i)
-        for (int j = i + 1; j < 9; ++j) {
-            const uintptr_t x = (uintptr_t)used[i].at, y = (uintptr_t)used[j].at;
-            if (y && x < y + 4 * (uintptr_t)used[j].n && y < x + 4 * (uintptr_t)used[i].n) return LACACHE_EINVAL;
+    } used[] = {{workspace, draft_workspace(V, B, k)}, {accept_len, 4 * (int64_t)B}, {next_token, 4 * (int64_t)B},
+                {p_target, 4 * (int64_t)B * k}, {p_draft, 4 * (int64_t)B * k},  // written
+                {draft_tokens, 4 * (int64_t)B * k}, {u_accept, 4 * (int64_t)B * k}, {u_next, 4 * (int64_t)B},
+                {temperature, 4 * (int64_t)B}, {n_draft, 4 * (int64_t)B}};
+    for (int i = 0; i < 5; ++i) {
+        const int64_t x = (int64_t)used[i].at;
+        for (int j = i + 1; j < 10; ++j) {
+            const int64_t y = (int64_t)used[j].at;
+            if (y && x < y + used[j].n && y < x + used[i].n) return LACACHE_EINVAL;
         }
+        if (rows_meet(logits, (int64_t)esz, V, t_seq, B, t_row, k + 1, x, x + used[i].n) ||
+            rows_meet(draft_logits, (int64_t)esz, V, d_seq, B, d_row, k, x, x + used[i].n))
+            return LACACHE_EINVAL;
+    }
     DraftArgs a{};
     a.logits = (const char*)logits, a.draft_logits = (const char*)draft_logits;
     a.dtype = (int)dtype, a.V = V, a.B = B, a.k = k;

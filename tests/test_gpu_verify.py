@@ -276,3 +276,20 @@ def test_what_is_left_of_nearly_equal_models(lc, B, V):
         assert got[0].tolist() == [0] * B and got[1].tolist() == [a] * B, u_next
     got = lc.lacache_verify(logits, draft, tokens, u, torch.zeros(B, device=DEV))
     assert bool((got[1] >= 0).all()) and bool((got[1] <= a).all())
+
+
+def test_outputs_between_the_rows(lc):
+    """Results in the gaps of the logits' own buffer, next to rows."""
+    B, k, V = 3, 4, 1001
+    logits, draft, tokens, u, u_next = inputs(B, k, V, torch.float32)
+    want = check(lc, logits, draft, tokens, u, u_next)
+    wide = torch.full((B, k + 1, V + 40), 7.0, device=DEV)
+    wide[:, :, 20:20 + V] = logits
+    flat, stride = wide.view(-1), V + 40
+    gap = [flat[20 + V + i * stride:20 + V + i * stride + 12] for i in range(4)]       # (40 numbers each)
+    out = (gap[0][:B].view(torch.int32), gap[1][:B].view(torch.int32), gap[2].view(B, k), gap[3].view(B, k))
+    got = lc.lacache_verify(wide[:, :, 20:20 + V], draft, tokens, u, u_next, out=out)
+    assert all(torch.equal(x, y) for x, y in zip(want, got))
+    assert torch.equal(wide[:, :, 20:20 + V], logits) and bool((flat[:20] == 7).all())
+    with pytest.raises(lc.LaCacheError):
+        lc.lacache_verify(wide[:, :, 20:20 + V], draft, tokens, u, u_next, out=(*out[:3], flat[20 + V - 1:20 + V + 11].view(B, k)))

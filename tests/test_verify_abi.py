@@ -61,3 +61,40 @@ def test_outputs_that_overlap(lc, out):
         if name != out:
             for shift in (0, -4, 4):  # (two numbers or eight each)
                 assert call(lc, **{**at, out: at[name] + shift}) == EINVAL
+
+
+WRITTEN = ["accept_len", "next_token", "p", "q", "workspace"]
+
+
+@pytest.mark.parametrize("out", WRITTEN)
+@pytest.mark.parametrize("rows", ["logits", "draft"])
+def test_outputs_in_the_logits(lc, out, rows):
+    """Any byte of any row, first or last, of either model; rows and sequences apart, together, and in any order."""
+    far = {name: (1 << 40) + (1 << 24) * i for i, name in enumerate(("tokens", "u", "u_next", "temperature", "n_draft",
+                                                                      "logits", "draft", *WRITTEN))}
+    k = 4 if rows == "draft" else 5                        # rows of a sequence
+    at = 1 << 30
+    for t_seq, t_row in ((k * 100, 100), (100_000, 1000), (100, 5000), (0, 0), (0, 128), (1 << 12, 0), (1 << 40, 1 << 20)):
+        strides = dict(d_seq=t_seq, d_row=t_row) if rows == "draft" else dict(t_seq=t_seq, t_row=t_row)
+        for b in range(3):
+            for j in range(k):
+                row = at + 2 * (b * t_seq + j * t_row)
+                for x in (row, row + 96, row + 192):       # (200 bytes a row)
+                    assert call(lc, **{**far, rows: at, out: x, "B": 3, **strides}) == EINVAL
+
+
+@pytest.mark.parametrize("out", WRITTEN[:4])
+def test_outputs_in_the_workspace(lc, out):
+    far = {name: (1 << 40) + (1 << 24) * i for i, name in enumerate(("tokens", "u", "u_next", "temperature", "n_draft",
+                                                                      "logits", "draft", *WRITTEN))}
+    need = lc.lacache_verify_workspace(100, 2, 4)
+    for name in (out, "tokens", "u", "u_next", "temperature", "n_draft"):
+        for shift in (0, 16, need - 4):
+            assert call(lc, **{**far, name: far["workspace"] + shift}) == EINVAL
+
+
+def test_strides_beyond_64_bits(lc):
+    far = {name: (1 << 40) + (1 << 24) * i for i, name in enumerate(("tokens", "u", "u_next", "temperature", "n_draft",
+                                                                      "logits", "draft", *WRITTEN))}
+    for bad in ("t_seq", "t_row", "d_seq", "d_row"):
+        assert call(lc, **{**far, bad: 1 << 62}) == EINVAL
