@@ -25,12 +25,16 @@ constexpr int kThreads = 256;
 constexpr int kAccept = 512;    // threads of k_draft_accept
 constexpr int kPositions = 64;  // looked at together
 
-// Relative error of a chunked float32 sum S = sum 2^t, t = (x - m) c <= 0.  The roundings of an exponent (log2 e, c, the
-// difference, the product) move 2^t by 4 |t| 2^-24 ln 2, whether it is taken in one step or in several; the exponentials (one,
-// and up to five as the maximum rises and lanes are joined) are within 2^-22 each, adding up takes 15 roundings.  The mean of
-// |t| under the weights is below log2 V + 2 (their entropy and the maximum's share), 19 for V = 128,256:
-// 19 * 1.65e-7 + 6 * 2.4e-7 + 15 * 6e-8 = 5.5e-6 for S, twice that for S_p / S_q (1.5e-5 at V = 2^24).
-constexpr double kSumError = 0x1p-16;
+// Relative error of a chunked float32 sum S = sum 2^t, t = (x - m) c <= 0, of 2^log2_v logits.  Four roundings of an exponent (log2
+// e, c, the difference, the product) move 2^t by 4 |t| 2^-24 ln 2, whether it is taken in one step or in several; the mean of |t|
+// under the weights is below log2 V + 2 (their entropy and the maximum's share).  The exponentials (one, and up to five as the
+// maximum rises and lanes are joined) are within 2^-22 each.  A lane adds a chunk of four steps up in 3 + 4 x 4 roundings, four
+// more as the maximum rises, and a wave in 6.  (8.6e-6 for the longest rows, 6.3e-6 for 128,256 logits.)
+constexpr double sum_error(double log2_v) {
+    return (log2_v + 2) * 4 * 0x1p-24 * 0.6931472 + 6 * 0x1p-22 + (3 + 4 * 4 + 4 + 6) * 0x1p-24;
+}
+constexpr double kSumError = 0x1p-15;
+static_assert(2 * sum_error(31) < kSumError, "S_p / S_q of rows of any length");
 
 // 2^t for t <= 0: 2^n e^(f ln 2), |f| <= 1/2, by the exponential's series up to the 11th power (the 12th: 0.3466^12 / 12! =
 // 6e-15).  Below 2^-1074 it is 0.
