@@ -77,8 +77,14 @@ struct AttendPlan {
     struct AttendSplit* split;  // [workers]: the row group whose last part a worker had
     float* part_o;     // [2 workers][group rows][dp] partial sums of values
     float2* part_ml;   // [2 workers][group rows] their maxima and sums of weights
+};
+
+// That of a part's launch.
+struct AttendPartPlan : AttendPlan {
     AttendShare share;
 };
+template <int MODE>
+using PlanOf = std::conditional_t<MODE == kWhole, AttendPlan, AttendPartPlan>;
 
 constexpr int kMaxWorkers = 4096;
 
@@ -103,7 +109,7 @@ struct AttendSpan {
     __device__ int items(const AttendArgs& a) const { return groups * a.pool.heads * stride; }
 };
 template <int MODE = kWhole>
-__device__ inline AttendSpan attend_span(const AttendArgs& a, const AttendPlan& p, int b) {
+__device__ inline AttendSpan attend_span(const AttendArgs& a, const PlanOf<MODE>& p, int b) {
     AttendSpan r;
     if constexpr (MODE == kPrefix) {
         const int4 g = p.share.span[b];
@@ -119,7 +125,8 @@ __device__ inline AttendSpan attend_span(const AttendArgs& a, const AttendPlan& 
         const int64_t lo = a.window > 0 ? r.pos0() - a.window + 1 : 0;
         r.first = lo < 0 ? 0 : (int)(lo >> 5);
         r.table = b;
-        r.held = MODE == kOwn ? p.share.held[b] : 0;
+        r.held = 0;
+        if constexpr (MODE == kOwn) r.held = p.share.held[b];
         if (MODE == kOwn && r.first < r.held >> 5) r.first = r.held >> 5;  // (whole pages)
     }
     r.rows = r.n * a.group;
@@ -140,7 +147,7 @@ struct AttendEnds {
     int least, most;
 };
 template <int MODE>
-__device__ __forceinline__ AttendEnds ends_of(const AttendPlan& p, const AttendSpan& s, int r0, int n, int lane) {
+__device__ __forceinline__ AttendEnds ends_of(const PlanOf<MODE>& p, const AttendSpan& s, int r0, int n, int lane) {
     const int i0 = token_of(p, r0), i1 = token_of(p, r0 + n - 1);
     if constexpr (MODE == kPrefix) {
         int least = INT32_MAX, most = -1;
@@ -175,10 +182,12 @@ struct AttendRange {
     int b, before, at, end, per;
 };
 template <int WAVES, int MODE = kWhole>
-__device__ __forceinline__ AttendRange attend_range(const AttendArgs& a, const AttendPlan& p, int worker, int grain, int least) {
+__device__ __forceinline__ AttendRange attend_range(const AttendArgs& a, const PlanOf<MODE>& p, int worker, int grain, int least) {
     constexpr int THREADS = 64 * WAVES;
     __shared__ int total_of[WAVES], found[2], longest_of[WAVES];
-    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, n_seq = MODE == kPrefix ? p.share.n_groups : a.seqs.n_seq;
+    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+    int n_seq = a.seqs.n_seq;
+    if constexpr (MODE == kPrefix) n_seq = p.share.n_groups;
     int own = 0, sum = 0, all = 0, b = tid, longest = 1;
     // items up to sequence b within a round of THREADS (sum), and of the round (returned)
     auto scan = [&]() {
@@ -235,7 +244,7 @@ __device__ __forceinline__ AttendRange attend_range(const AttendArgs& a, const A
 // Moves on to the next chunk of a worker's range: past sequences that are through and those without rows, and past the items
 // behind a row group's chunks.  Whether there is one.
 template <int MODE>
-__device__ __forceinline__ bool attend_next(const AttendArgs& a, const AttendPlan& p, AttendRange& r, AttendSpan& s) {
+__device__ __forceinline__ bool attend_next(const AttendArgs& a, const PlanOf<MODE>& p, AttendRange& r, AttendSpan& s) {
     while (r.at < r.end) {
         const int items = s.items(a);
         if (r.at - r.before >= items) {
@@ -346,7 +355,7 @@ struct Attend {
     // 16 bytes of a row as KC operands: the three terms of a float32 sum back to it exactly, a bfloat16 is its own
     // Row tile r is rows row0 + step r .. + 15 of the sequence's (its last row in the place of those that it has not).
     template <int MODE = kWhole>
-    __device__ __forceinline__ void load_q(const AttendArgs& a, const AttendPlan& p, const AttendSpan& s, int h, int row0,
+    __device__ __forceinline__ void load_q(const AttendArgs& a, const PlanOf<MODE>& p, const AttendSpan& s, int h, int row0,
                                            int step, int lane) {
         const int u = lane >> 4;
 #pragma unroll
@@ -354,7 +363,9 @@ struct Attend {
             int row = row0 + step * r + (lane & 15);
             row = row < s.rows ? row : s.rows - 1;
             const int i = token_of(p, row), head = h * a.group + (row - i * a.group);
-            const int64_t pos = MODE == kPrefix ? p.share.row_pos[s.row0 + i] : s.pos0() + i;
+            int64_t pos;
+            if constexpr (MODE == kPrefix) pos = p.share.row_pos[s.row0 + i];
+            else pos = s.pos0() + i;
             hi[r] = pos < 0 ? -1 : (int)pos;
             lo[r] = a.window > 0 && hi[r] - a.window + 1 > 0 ? hi[r] - a.window + 1 : 0;
             if (MODE == kOwn) lo[r] = lo[r] > s.held ? lo[r] : s.held;
@@ -753,13 +764,13 @@ struct Joined {
 
 // Four columns of element `at` of a part's sums, and where they lie.
 template <int MODE>
-__device__ __forceinline__ void store_sums(const AttendPlan& p, int64_t at, int dp, int col, f32x4 o, float m, float l) {
+__device__ __forceinline__ void store_sums(const PlanOf<MODE>& p, int64_t at, int dp, int col, f32x4 o, float m, float l) {
     const AttendSums& x = p.share.sums[MODE - kPrefix];
     *(f32x4*)(x.o + at * dp + col) = o;
     if (col == 0) x.ml[at] = make_float2(m, l);
 }
 template <int MODE>
-__device__ __forceinline__ void store_place(const AttendPlan& p, int64_t at, int parts, int worker0, int place) {
+__device__ __forceinline__ void store_place(const PlanOf<MODE>& p, int64_t at, int parts, int worker0, int place) {
     p.share.sums[MODE - kPrefix].at[at] = make_int2(parts, worker0 | place << 16);
 }
 
@@ -864,7 +875,7 @@ __device__ __forceinline__ void join_parts(const AttendArgs& a, const AttendPlan
 
 // A worker of four waves.  HERE: parts are joined within the launch.
 template <int DP, int CT, int R, bool F32, bool HERE, int MODE>
-__device__ __forceinline__ void attend_narrow(const AttendArgs& a, const AttendPlan& p, const int worker) {
+__device__ __forceinline__ void attend_narrow(const AttendArgs& a, const PlanOf<MODE>& p, const int worker) {
     using A = Attend<DP, CT, R, F32>;
     constexpr int GR = 16 * R;  // rows of a row group
     __shared__ float2 sml[4][GR];
@@ -1065,7 +1076,7 @@ __device__ __forceinline__ void attend_narrow(const AttendArgs& a, const AttendP
 }
 
 template <int DP, int CT, int R, bool F32, bool HERE, int MODE = kWhole>
-__global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(AttendArgs a, AttendPlan p) {
+__global__ __launch_bounds__(256, (Attend<DP, CT, R, F32>::OCC)) void k_attend(AttendArgs a, PlanOf<MODE> p) {
     attend_narrow<DP, CT, R, F32, HERE, MODE>(a, p, blockIdx.x);
 }
 

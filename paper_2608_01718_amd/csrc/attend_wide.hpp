@@ -37,7 +37,7 @@ struct Wide {
 
 // The worker of workgroup `block` of a launch's.
 template <int DP, int CT, int WAVES, int R, bool F32, int MODE>
-__device__ __forceinline__ void attend_wide(const AttendArgs& a, const AttendPlan& p, const int block) {
+__device__ __forceinline__ void attend_wide(const AttendArgs& a, const PlanOf<MODE>& p, const int block) {
     using W = Wide<DP, CT, WAVES, R, F32>;
     using A = Attend<DP, CT, R, F32>;
     __shared__ u32x4 keys[2][2 * W::KC * 64], vals[2][W::NJ * 64];  // operands of 1 KB each
@@ -276,7 +276,7 @@ __device__ __forceinline__ void attend_wide(const AttendArgs& a, const AttendPla
 }
 
 template <int DP, int CT, int WAVES, int R, bool F32, int MODE = kWhole>
-__global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) void k_attend_wide(AttendArgs a, AttendPlan p) {
+__global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) void k_attend_wide(AttendArgs a, PlanOf<MODE> p) {
     attend_wide<DP, CT, WAVES, R, F32, MODE>(a, p, blockIdx.x);
 }
 
@@ -285,7 +285,7 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
 // one of each on a compute unit, unless one part has much more to do (64 sequences, 8192 shared tokens and 16 to 2048 of their own: 149 MB in 35 us, the matrix cores
 // busy for 15 % of it, the vector unit 24 %).
 template <int DP, int CT, bool F32, int SHIFT, int OWN>
-__global__ __launch_bounds__(256, 2) void k_attend_both(AttendArgs a, AttendPlan p, AttendPlan own) {
+__global__ __launch_bounds__(256, 2) void k_attend_both(AttendArgs a, AttendPartPlan p, AttendPartPlan own) {
     const int prefix = __builtin_amdgcn_readfirstlane(*p.share.deal);
     own.workers -= prefix;
     p.workers = prefix;
@@ -297,7 +297,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_both(AttendArgs a, AttendPlan
 }
 
 template <int DP>
-hipError_t launch_attend_both(const AttendArgs& a, const AttendPlan& p, const AttendPlan& own, hipStream_t s) {
+hipError_t launch_attend_both(const AttendArgs& a, const AttendPartPlan& p, const AttendPartPlan& own, hipStream_t s) {
     const dim3 grid((unsigned)own.workers), block(256);
     auto go = [&](auto ct, auto f32) {
         constexpr int CT = decltype(ct)::value;
@@ -323,12 +323,12 @@ hipError_t launch_attend_both(const AttendArgs& a, const AttendPlan& p, const At
     else of(std::integral_constant<int, kKvInt8>{});
     return hipGetLastError();
 }
-extern template hipError_t launch_attend_both<64>(const AttendArgs&, const AttendPlan&, const AttendPlan&, hipStream_t);
-extern template hipError_t launch_attend_both<96>(const AttendArgs&, const AttendPlan&, const AttendPlan&, hipStream_t);
-extern template hipError_t launch_attend_both<128>(const AttendArgs&, const AttendPlan&, const AttendPlan&, hipStream_t);
+extern template hipError_t launch_attend_both<64>(const AttendArgs&, const AttendPartPlan&, const AttendPartPlan&, hipStream_t);
+extern template hipError_t launch_attend_both<96>(const AttendArgs&, const AttendPartPlan&, const AttendPartPlan&, hipStream_t);
+extern template hipError_t launch_attend_both<128>(const AttendArgs&, const AttendPartPlan&, const AttendPartPlan&, hipStream_t);
 
 template <int DP, int MODE>
-hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
+hipError_t launch_attend(const AttendArgs& a, const PlanOf<MODE>& p, hipStream_t s) {
     const dim3 grid((unsigned)(p.group_shift < 6 ? p.workers : (p.workers + 7) & ~7)), block(p.waves * 64);
     auto go = [&](auto ct) {
         constexpr int CT = decltype(ct)::value;
@@ -370,15 +370,15 @@ extern template hipError_t launch_attend<96, kWhole>(const AttendArgs&, const At
 extern template hipError_t launch_attend<128, kWhole>(const AttendArgs&, const AttendPlan&, hipStream_t);
 extern template hipError_t launch_attend<192, kWhole>(const AttendArgs&, const AttendPlan&, hipStream_t);
 extern template hipError_t launch_attend<256, kWhole>(const AttendArgs&, const AttendPlan&, hipStream_t);
-extern template hipError_t launch_attend<64, kPrefix>(const AttendArgs&, const AttendPlan&, hipStream_t);
-extern template hipError_t launch_attend<96, kPrefix>(const AttendArgs&, const AttendPlan&, hipStream_t);
-extern template hipError_t launch_attend<128, kPrefix>(const AttendArgs&, const AttendPlan&, hipStream_t);
-extern template hipError_t launch_attend<192, kPrefix>(const AttendArgs&, const AttendPlan&, hipStream_t);
-extern template hipError_t launch_attend<256, kPrefix>(const AttendArgs&, const AttendPlan&, hipStream_t);
-extern template hipError_t launch_attend<64, kOwn>(const AttendArgs&, const AttendPlan&, hipStream_t);
-extern template hipError_t launch_attend<96, kOwn>(const AttendArgs&, const AttendPlan&, hipStream_t);
-extern template hipError_t launch_attend<128, kOwn>(const AttendArgs&, const AttendPlan&, hipStream_t);
-extern template hipError_t launch_attend<192, kOwn>(const AttendArgs&, const AttendPlan&, hipStream_t);
-extern template hipError_t launch_attend<256, kOwn>(const AttendArgs&, const AttendPlan&, hipStream_t);
+extern template hipError_t launch_attend<64, kPrefix>(const AttendArgs&, const AttendPartPlan&, hipStream_t);
+extern template hipError_t launch_attend<96, kPrefix>(const AttendArgs&, const AttendPartPlan&, hipStream_t);
+extern template hipError_t launch_attend<128, kPrefix>(const AttendArgs&, const AttendPartPlan&, hipStream_t);
+extern template hipError_t launch_attend<192, kPrefix>(const AttendArgs&, const AttendPartPlan&, hipStream_t);
+extern template hipError_t launch_attend<256, kPrefix>(const AttendArgs&, const AttendPartPlan&, hipStream_t);
+extern template hipError_t launch_attend<64, kOwn>(const AttendArgs&, const AttendPartPlan&, hipStream_t);
+extern template hipError_t launch_attend<96, kOwn>(const AttendArgs&, const AttendPartPlan&, hipStream_t);
+extern template hipError_t launch_attend<128, kOwn>(const AttendArgs&, const AttendPartPlan&, hipStream_t);
+extern template hipError_t launch_attend<192, kOwn>(const AttendArgs&, const AttendPartPlan&, hipStream_t);
+extern template hipError_t launch_attend<256, kOwn>(const AttendArgs&, const AttendPartPlan&, hipStream_t);
 
 }  // namespace lacache

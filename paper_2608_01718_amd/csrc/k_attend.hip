@@ -170,7 +170,7 @@ hipError_t launch_join(const AttendArgs& a, const AttendPlan& p, int n_seq, int6
 
 // The launches of one mode.
 template <int MODE>
-hipError_t launch_mode(const AttendArgs& a, AttendPlan p, int n_seq, int64_t max_new, hipStream_t s) {
+hipError_t launch_mode(const AttendArgs& a, PlanOf<MODE> p, int n_seq, int64_t max_new, hipStream_t s) {
     prepare<MODE>(a, p, n_seq, max_new);
     const hipError_t e = a.pool.dp == 64    ? launch_attend<64, MODE>(a, p, s)
                          : a.pool.dp == 96  ? launch_attend<96, MODE>(a, p, s)
@@ -309,7 +309,7 @@ __global__ __launch_bounds__(64) void k_attend_share(AttendArgs a, AttendShare x
 // one after another on the parts that workers have of it.  Reading the parts bounds it (64 rows of 32 heads, 17 MB of parts 8 us;
 // 945 rows of 12 heads, three groups 7 us).
 template <bool F32>
-__global__ __launch_bounds__(256) void k_attend_together(AttendArgs a, AttendPlan prefix, AttendPlan own, int of_row) {
+__global__ __launch_bounds__(256) void k_attend_together(AttendArgs a, AttendPartPlan prefix, AttendPartPlan own, int of_row) {
     __shared__ f32x4 sums[256];
     __shared__ float2 ml_of[256];
     const int dp = a.pool.dp, lanes = dp / 4, rows = 256 / lanes / of_row, g = threadIdx.x / lanes, sub = g % of_row;
@@ -330,7 +330,7 @@ __global__ __launch_bounds__(256) void k_attend_together(AttendArgs a, AttendPla
                 for (int i = 0; i < 4; ++i) {
                     const int k = k0 + i * of_row < n ? k0 + i * of_row : n - 1;
                     const bool mine = k < n_own;
-                    const AttendPlan& p = mine ? own : prefix;
+                    const AttendPartPlan& p = mine ? own : prefix;
                     const AttendSums& whole = x.sums[mine ? kOwn - kPrefix : 0];
                     const int2 w = mine ? of_own : of_prefix;
                     const int part = mine ? k : k - n_own;
@@ -375,7 +375,7 @@ bool both_at_once(const KvPool& pool, bool f32, const AttendPlan& prefix, const 
 
 // The plans of both parts, and what lies behind their memory.
 int64_t shared_plan(const KvPool& pool, bool f32, int64_t rows, int n_seq, int n_groups, int q_heads, int max_new, int num_cu,
-                    char* space, AttendPlan* prefix, AttendPlan* own, bool* both) {
+                    char* space, AttendPartPlan* prefix, AttendPartPlan* own, bool* both) {
     const int group = q_heads / pool.heads;
     int64_t at, bytes;
     auto take = [&](int64_t n) {
@@ -385,8 +385,8 @@ int64_t shared_plan(const KvPool& pool, bool f32, int64_t rows, int n_seq, int n
         return p;
     };
     auto plans = [&](int occupancy) {
-        *prefix = plan_of(pool, f32, prefix_rows(rows, n_groups), group, num_cu, space, &at, occupancy);
-        *own = plan_of(pool, f32, max_new, group, num_cu, take(0), &bytes, occupancy);
+        (AttendPlan&)*prefix = plan_of(pool, f32, prefix_rows(rows, n_groups), group, num_cu, space, &at, occupancy);
+        (AttendPlan&)*own = plan_of(pool, f32, max_new, group, num_cu, take(0), &bytes, occupancy);
         at += bytes;
     };
     plans(0);
@@ -421,7 +421,7 @@ bool attend_shared_fits(const KvPool& pool, int dtype, int64_t rows, int n_group
 
 int64_t attend_shared_workspace(const KvPool& pool, int dtype, int64_t rows, int n_seq, int n_groups, int q_heads, int max_new,
                                 int num_cu) {
-    AttendPlan p, o;
+    AttendPartPlan p, o;
     bool both;
     return shared_plan(pool, dtype == 0, rows, n_seq, n_groups, q_heads, max_new, num_cu, nullptr, &p, &o, &both);
 }
@@ -429,7 +429,7 @@ int64_t attend_shared_workspace(const KvPool& pool, int dtype, int64_t rows, int
 hipError_t launch_kv_attend_shared(const AttendArgs& a, const int32_t* group, const int32_t* len, int n_groups, int max_new,
                                    void* workspace, int num_cu, hipStream_t s) {
     if (a.seqs.rows <= 0 || a.seqs.n_seq <= 0) return hipSuccess;
-    AttendPlan prefix, own;
+    AttendPartPlan prefix, own;
     bool both;
     shared_plan(a.pool, a.dtype == 0, a.seqs.rows, a.seqs.n_seq, n_groups, a.q_heads, max_new, num_cu, (char*)workspace, &prefix, &own,
                 &both);

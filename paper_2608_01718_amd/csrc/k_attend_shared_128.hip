@@ -2,7 +2,7 @@
 #include "attend_wide.hpp"
 
 namespace lacache {
-template hipError_t launch_attend<128, kPrefix>(const AttendArgs&, const AttendPlan&, hipStream_t);
-template hipError_t launch_attend<128, kOwn>(const AttendArgs&, const AttendPlan&, hipStream_t);
-template hipError_t launch_attend_both<128>(const AttendArgs&, const AttendPlan&, const AttendPlan&, hipStream_t);
+template hipError_t launch_attend<128, kPrefix>(const AttendArgs&, const AttendPartPlan&, hipStream_t);
+template hipError_t launch_attend<128, kOwn>(const AttendArgs&, const AttendPartPlan&, hipStream_t);
+template hipError_t launch_attend_both<128>(const AttendArgs&, const AttendPartPlan&, const AttendPartPlan&, hipStream_t);
 }  // namespace lacache

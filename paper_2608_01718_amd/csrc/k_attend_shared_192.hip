@@ -2,6 +2,6 @@
 #include "attend_wide.hpp"
 
 namespace lacache {
-template hipError_t launch_attend<192, kPrefix>(const AttendArgs&, const AttendPlan&, hipStream_t);
-template hipError_t launch_attend<192, kOwn>(const AttendArgs&, const AttendPlan&, hipStream_t);
+template hipError_t launch_attend<192, kPrefix>(const AttendArgs&, const AttendPartPlan&, hipStream_t);
+template hipError_t launch_attend<192, kOwn>(const AttendArgs&, const AttendPartPlan&, hipStream_t);
 }  // namespace lacache

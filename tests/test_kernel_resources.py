@@ -77,3 +77,23 @@ def test_calibration_of_unaligned_rows_keeps_its_waves():
                  for k in _metadata(obj)["amdhsa.kernels"]}
     for name in ("k_pair_cosine<1, 0, 0>", "k_pair_cosine<2, 0, 0>"):
         assert registers[name] <= 64, (name, registers[name])
+
+
+def test_attention_takes_the_arguments_it_needs():
+    """What the parts over shared prefixes take (104 bytes more) is no argument of the whole attention's launches: the join of
+    its parts is 0.2 us longer with them."""
+    with open(LIB, "rb") as f:
+        blob = f.read()
+    whole = part = 0
+    for elf in _code_objects(blob):
+        for k in _metadata(elf)["amdhsa.kernels"]:
+            name, size = _name(k[".name"]) if "7lacache" in k[".name"] else "", k[".kernarg_segment_size"]
+            mode = 5 if name.startswith(("k_attend<", "k_attend_wide<")) else 0
+            args = name[name.find("<") + 1:-1].split(", ") if mode else []
+            if name.startswith("k_attend_join") or (mode and args[mode] == "0"):
+                whole += 1
+                assert size <= (488 if "join" in name else 232), (name, size)    # (256 more where gridDim is used)
+            elif mode:
+                part += 1
+                assert size >= 300, (name, size)
+    assert whole > 50 and part > 50
