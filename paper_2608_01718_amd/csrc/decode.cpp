@@ -59,6 +59,12 @@ bool to_bounds(const lacache_bounds* b, KvBounds* out) {
     return true;
 }
 
+// Bytes of the scores of all pages; LACACHE_EINVAL where they do not fit in 64 bits.
+int64_t select_space(const KvPool& p, int64_t rows, int max_pages) {
+    const int64_t lists = rows * p.heads, each = 4 * select_stride(max_pages);
+    return each == 0 || lists <= INT64_MAX / each ? lists * each : LACACHE_EINVAL;
+}
+
 // Strides that keep n of them (0 or more) far from the ends of 64 bits.
 bool fits_far(int64_t stride, int64_t n) { return n < 2 || stride < (INT64_C(1) << 58) / n; }
 
@@ -252,7 +258,7 @@ int64_t lacache_kv_select_workspace(const lacache_kv* kv, int64_t rows, int32_t 
     KvPool p;
     if (!to_pool(kv, false, &p) || rows < 0 || rows > INT32_MAX || max_pages < 0 || max_pages > kMostChosen)
         return LACACHE_EINVAL;
-    return 4 * rows * p.heads * select_stride(max_pages);
+    return select_space(p, rows, max_pages);
 }
 
 int lacache_kv_select(const lacache_kv* kv, const lacache_bounds* bounds, const lacache_seqs* seqs, const void* q,
@@ -266,8 +272,8 @@ int lacache_kv_select(const lacache_kv* kv, const lacache_bounds* bounds, const 
         (int64_t)first + last > n_blocks || workspace_bytes < 0)
         return LACACHE_EINVAL;
     if (rows == 0 || a.seqs.n_seq == 0) return LACACHE_OK;
-    const int64_t need = 4 * rows * a.pool.heads * select_stride(a.seqs.max_pages);
-    if (!q || !blocks || !aligned(q, dtype == LACACHE_F32 ? 4 : 2) || !aligned(blocks, 4) || workspace_bytes < need ||
+    const int64_t need = select_space(a.pool, rows, a.seqs.max_pages);
+    if (need < 0 || !q || !blocks || !aligned(q, dtype == LACACHE_F32 ? 4 : 2) || !aligned(blocks, 4) || workspace_bytes < need ||
         (need > 0 && (!workspace || !aligned(workspace, 16))) || (a.pool.n_pages > 0 && !to_bounds(bounds, &a.bounds)))
         return LACACHE_EINVAL;
     a.q = (const char*)q, a.dtype = (int)dtype, a.group = q_heads / kv->heads, a.q_row = q_row;

@@ -111,3 +111,14 @@ def test_reference_bounds_hold():
     rounded = (q / unit[..., None]).round() * unit[..., None]
     assert float((rounded.double() @ keys.T).max()) <= float(s) * (1 + 1e-5)
     assert ctypes.sizeof(ctypes.c_void_p) == 8
+
+
+def test_workspaces_beyond_64_bits(lc):
+    """2^31 rows of 65,535 heads have 2^67 scores of 2^20 pages: refused, not some number of bytes."""
+    f, c = lc.raw_library().lacache_kv_select_workspace, kv(lc, heads=65535)
+    for rows in ((1 << 31) - 1, 1 << 30, 1 << 29, 1 << 25):
+        want = 4 * rows * 65535 * (1 << 20)
+        assert f(ref(c), rows, 1 << 20) == (want if want < 1 << 63 else EINVAL), rows
+        if want >= 1 << 63:
+            assert select(lc, c, bounds(lc), seqs(lc, max_pages=1 << 20), rows=rows, q_heads=65535, bytes=(1 << 63) - 1) == EINVAL
+    assert f(ref(c), (1 << 31) - 1, 0) == 0
