@@ -335,3 +335,33 @@ def test_any_sequence_of_a_group_may_be_idle(lc, dtype, new, Hq, d, news, lens, 
     q = normals((sum(news), Hq, d), seed=new, dtype=dtype, size=2)
     for window in (0, 100):
         check(lc, pg, held, q, news, lens, groups, window=window, max_new=new, table=table)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("kind,heads,Hq,d,news,fronts,groups", [
+    ("bf16", 2, 8, 64, [600, 417, 33, 1030], [256, 256, 256, 256], [(0, 4, 256)]),
+    ("fp8", 1, 4, 128, [700, 1, 350], [640, 640, 0], [(0, 2, 640)]),
+    ("int8", 2, 4, 96, [301, 300, 290, 400], [96, 96, 320, 320], [(0, 2, 96), (2, 4, 320)]),
+    ("bf16", 1, 2, 256, [500, 450], [512, 512], [(0, 2, 512)])])
+def test_prompts_behind_a_prefix(lc, dtype, kind, heads, Hq, d, news, fronts, groups):
+    """All of the sequences' own tokens are new, as when instructions that prompts share have been cached before."""
+    say(f"[case] prompts {kind} {dtype} {heads} {Hq} {d} {news} {fronts}")
+    lens = [n + f for n, f in zip(news, fronts)]
+    pg, held = shared(lc, kind, heads, d, 32, lens, groups, seed=d)
+    q = normals((sum(news), Hq, d), seed=d, dtype=dtype, size=2)
+    check(lc, pg, held, q, news, lens, groups, max_new=max(news))
+    check(lc, pg, held, q, news, lens, groups, window=150)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("new,Hq,d", [(1, 8, 64), (21, 8, 64), (1, 4, 256)])
+def test_few_of_many_share(lc, dtype, new, Hq, d):
+    """Two small groups among sequences that share nothing, of other lengths."""
+    lens = [120 + (37 * i) % 500 for i in range(60)]
+    for i in (11, 12, 13, 40, 41):
+        lens[i] += 256
+    groups = [(11, 14, 256), (40, 42, 320)]
+    pg, held = shared(lc, "bf16", 2, d, 32, lens, groups, seed=3)
+    q = normals((60 * new, Hq, d), seed=5, dtype=dtype)
+    check(lc, pg, held, q, [new] * 60, lens, groups, max_new=new)
+    check(lc, pg, held, q, [new] * 60, lens, groups, window=90)
