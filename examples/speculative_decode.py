@@ -50,7 +50,7 @@ class Model:
 
     def logits(self, tokens, seqs, max_new, prefixes=None, decode=False):
         """tokens [rows]: the newest tokens of the sequences, packed.  Caches them and returns [rows, vocab].  prefixes: what
-        the sequences share."""
+        the sequences share, for a few new tokens of each (decode)."""
         x = self.embedding[tokens]
         for i, (cache, (w_in, w_out)) in enumerate(zip(self.caches, self.layers)):
             q, k, v = (y.unflatten(1, (-1, self.d)) for y in (_norm(x) @ w_in).split(self.sizes, 1))
@@ -60,7 +60,7 @@ class Model:
             if self.chosen and decode:
                 blocks = self.bounds[i].select(q, seqs, self.chosen, first=1, last=min(2, self.chosen - 1), max_new=max_new)
                 o, _ = cache.attend_blocks(q, seqs, blocks)
-            elif prefixes is not None:
+            elif prefixes is not None and decode:          # (prompts: sharing saves no products, which bound them)
                 o, _ = cache.attend_shared(q, seqs, prefixes, max_new=max_new)
             else:
                 o, _ = cache.attend(q, seqs, max_new=max_new)
@@ -97,8 +97,8 @@ class Requests:
             for model in (draft, target):
                 model.logits(prompts[0, :shared], front, shared)
         seqs, rest = r._newest(n - shared, r.cached), prompts[:, shared:].flatten()
-        draft.logits(rest, seqs, n - shared, r.prefixes)
-        r.tokens[:, n] = r.drawn(target.logits(rest, seqs, n - shared, r.prefixes).view(B, n - shared, -1)[:, -1])
+        draft.logits(rest, seqs, n - shared)
+        r.tokens[:, n] = r.drawn(target.logits(rest, seqs, n - shared).view(B, n - shared, -1)[:, -1])
         return r
 
     def some(self, which):
