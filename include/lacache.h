@@ -274,7 +274,9 @@ int lacache_accept_length(const void *logits, lacache_dtype dtype, int32_t V, co
  *   stride that is used n times below 2^58 / n
  * Outputs: accept_len [B], next_token [B] int32, p_target and p_draft [B][k] the
  * p_j(x_j) and q_j(x_j) in float32 (a greedy sequence's: 1 or 0, and 1; those from
- * n_draft[b] on: 0).  accept_len and next_token are those of 64-bit arithmetic.
+ * n_draft[b] on: 0).  accept_len and next_token are those of 64-bit arithmetic
+ * (exponentials of next_token within 2e-14); p_target and p_draft are numerators
+ * in 64 bits over sums in float32, at most 9e-6 of them off, about 1e-7 as a rule.
  * Logits of -infinity have probability 0.  A row without a finite logit, or with
  * +infinity or NaN, has no probabilities: its draft is not taken (p or q 0); if it
  * is the target's row n the next token is -1, if it is the draft model's r = p_n.
@@ -570,8 +572,10 @@ typedef struct {
 /*
  * lacache_kv_attend of sequences of which groups share a prefix: the same
  * results to rounding, the prefix of a group read once for all of its rows
- * (through the page table of the longest of its sequences that have rows).  The
- * other arguments are those of lacache_kv_attend.
+ * (through the page table of the longest of its sequences that have rows).  It
+ * pays for a few new tokens of each sequence behind some thousands of shared ones;
+ * prompts, which products bound, are faster in lacache_kv_attend.  The other
+ * arguments are those of that call.
  *   workspace  lacache_kv_attend_shared_workspace bytes of device memory (about
  *              8 rows q_heads D for the sums of both parts, and up to 150 MB for
  *              those of parts that several workgroups have), 16-byte aligned, in

@@ -113,7 +113,8 @@ EXPORTED = ("lacache_create", "lacache_create_ensemble", "lacache_models", "laca
             "lacache_profile", "lacache_profile_read", "lacache_replay_fallbacks", "lacache_strerror",
             "lacache_rope_table", "lacache_rope", "lacache_kv_append", "lacache_kv_read",
             "lacache_kv_attend_workspace", "lacache_kv_attend", "lacache_verify_workspace", "lacache_verify",
-            "lacache_kv_attend_shared_workspace", "lacache_kv_attend_shared", "lacache_kv_bound", "lacache_kv_bounds_read", "lacache_kv_select_workspace", "lacache_kv_select",
+            "lacache_kv_attend_shared_workspace", "lacache_kv_attend_shared", "lacache_kv_bound", "lacache_kv_bounds_read",
+            "lacache_kv_select_workspace", "lacache_kv_select",
             "lacache_kv_attend_blocks_workspace", "lacache_kv_attend_blocks")
 
 
@@ -890,7 +891,8 @@ def lacache_kv_attend_shared_workspace(c: KVCache, dtype: int, rows: int, n_seq:
 def lacache_kv_attend_shared(c: KVCache, q, seqs: Sequences, prefixes: Prefixes, scale=None, window: int = 0, max_new: int = 0,
                              out=None, stream=None):
     """lacache_kv_attend of sequences of which groups begin with the same pages, which are read once for all of a group's
-    rows.  Returns (out, lse) as that call."""
+    rows: for a few new tokens of each behind some thousands that they share (prompts are faster, and take less scratch, in
+    lacache_kv_attend).  Returns (out, lse) as that call."""
     index, kind, shape = c.index, q.dtype, q.shape
     dtype = _ROW_DTYPES.get(kind)
     if dtype is None or len(shape) != 3 or seqs.index != index or prefixes.index != index:
@@ -1045,7 +1047,7 @@ def _logits(t, shape, dtype, index: int, name: str):
     return stride[0], stride[1]
 
 
-_verify_need = {}  # bytes of scratch by (V, B, k)
+_verify_need = {}  # bytes of scratch by (V, B, k); a thread that empties it costs others a question again, no more
 
 
 def lacache_verify(logits, draft_logits, draft_tokens, u_accept, u_next, temperature=None, n_draft=None, out=None,

@@ -18,8 +18,8 @@ SOURCES = ["lacache.cpp", "k_store.hip", "k_stage1_stream.hip", "k_stage1_gemm.h
            "k_calibrate.hip", "k_accept.hip", "k_draft.hip", "k_lsh.hip", "decode.cpp", "k_rope.hip",
            "k_kv_store.hip", "k_attend.hip", "k_attend_64.hip", "k_attend_96.hip", "k_attend_128.hip", "k_attend_192.hip",
            "k_attend_256.hip", "k_attend_shared_64.hip", "k_attend_shared_96.hip", "k_attend_shared_128.hip",
-           "k_attend_shared_192.hip", "k_attend_shared_256.hip", "k_select.hip", "k_attend_blocks.hip", "k_attend_blocks_64.hip", "k_attend_blocks_96.hip",
-           "k_attend_blocks_128.hip", "k_attend_blocks_192.hip", "k_attend_blocks_256.hip"]
+           "k_attend_shared_192.hip", "k_attend_shared_256.hip", "k_select.hip", "k_attend_blocks.hip",
+           "k_attend_blocks_64.hip", "k_attend_blocks_96.hip", "k_attend_blocks_128.hip", "k_attend_blocks_192.hip", "k_attend_blocks_256.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 FLAGS = [

@@ -786,9 +786,9 @@ __device__ __forceinline__ void store_joined(const AttendArgs& a, const AttendPl
     if (col == 0 && a.lse) a.lse[at] = lse_of(x.m, x.l);
 }
 
-// Joins the parts of a row group: of_row groups (a power of two) of dp / 4 lanes on a row, four parts loaded together.  The workgroup takes rows first, first + 1, ... as many as it has lane groups for, and
-// again from `step` times as many on.  load(part's first row + row, column, ml, o) loads four columns.  scratch: THREADS f32x4 and
-// float2 of LDS.
+// Joins the parts of a row group: of_row groups (a power of two) of dp / 4 lanes on a row, four parts loaded together.  The
+// workgroup takes rows first, first + 1, ... as many as it has lane groups for, and again from `step` times as many on.
+// load(part's first row + row, column, ml, o) loads four columns.  scratch: THREADS f32x4 and float2 of LDS.
 template <int THREADS, class Load>
 __device__ __forceinline__ void join_rows(const AttendArgs& a, const AttendPlan& p, const AttendSplit& s, int dp, int of_row, int tid,
                                           int first, int step, f32x4* scratch, Load load) {

@@ -281,9 +281,10 @@ __global__ __launch_bounds__(64 * WAVES, (Wide<DP, CT, WAVES, R, F32>::OCC)) voi
 }
 
 // Both parts of a call in one launch: the first p.share.deal workgroups those over the prefixes, the others over the sequences'
-// own tokens.  SHIFT, OWN: of their row groups (4, 5: attend_narrow).  From 6 on: many rows over the prefixes, which the matrix cores and the softmax bound, while memory bounds the own tokens;
-// one of each on a compute unit, unless one part has much more to do (64 sequences, 8192 shared tokens and 16 to 2048 of their own: 149 MB in 35 us, the matrix cores
-// busy for 15 % of it, the vector unit 24 %).
+// own tokens.  SHIFT, OWN: of their row groups (4, 5: attend_narrow).  From 6 on: many rows over the prefixes, which the matrix
+// cores and the softmax bound, while memory bounds the own tokens; one of each on a compute unit, unless one part has much more
+// to do (64 sequences, 8192 shared tokens and 16 to 2048 of their own: 149 MB in 36 us, the matrix cores busy for 15 % of it, the
+// vector unit 24 %).
 template <int DP, int CT, bool F32, int SHIFT, int OWN>
 __global__ __launch_bounds__(256, 2) void k_attend_both(AttendArgs a, AttendPartPlan p, AttendPartPlan own) {
     const int prefix = __builtin_amdgcn_readfirstlane(*p.share.deal);
